@@ -162,14 +162,18 @@ def _inputs(case, seed):
     return s
 
 
+def _slots(lens, off, tbl, block):
+    """[request, token]: block * block size + offset; 0 past a request's end."""
+    pos = np.arange(max(lens))[None, :]
+    at = np.minimum(off[:-1, None] + pos // block, len(tbl) - 1)
+    slot = np.where(pos < np.asarray(lens)[:, None], tbl[at].astype(np.int64) * block + pos % block, 0)
+    return torch.from_numpy(slot).cuda()
+
+
 def prepare(case, seed):
     s = _inputs(case, seed)
     c, lens, p_lens, B = s["case"], s["lens"], s["prefix_lens"], case.get("block", _DEFAULTS["block"])
 
-    # where each token of each request lies, for the plain forms: a program without the operators keeps such an index
-    def slots(first, n, o, t, blk):
-        pos = np.arange(n)
-        return t[o[first] + pos // blk].astype(np.int64) * blk + pos % blk
     if own:
         from paper_2408_08147_b200.sequences import CacheSession, Sequences
         from paper_2408_08147_b200.workloads import Geometry
@@ -184,10 +188,14 @@ def prepare(case, seed):
         else:
             s["session"] = CacheSession(g, s["pool"], seqs, num_q_heads=c["heads"] * c["group"], q_tokens=c["q_tokens"], dtype=dt)
     else:
-        s["slots"] = [torch.from_numpy(slots(i, n, s["off"], s["tbl"], B)).cuda() for i, n in enumerate(lens)]
-        s["prefix_slots"] = [torch.from_numpy(slots(i, n, s["prefix_off"], s["prefix_tbl"], B)).cuda() for i, n in enumerate(p_lens)]
+        # where each token lies (padded to the longest request): what a program without the operators keeps
+        s["len_t"] = torch.tensor(lens, device="cuda")
+        s["slots"] = _slots(lens, s["off"], s["tbl"], B)
+        if p_lens:
+            s["prefix_len_t"] = torch.tensor(p_lens, device="cuda")
+            s["prefix_slots"] = _slots(p_lens, s["prefix_off"], s["prefix_tbl"], B)
         if c["op"] == "evict":
-            s["dst_slots"] = [torch.from_numpy(slots(i, min(n, c["budget"]), s["dst_off"], s["dst_tbl"], c["dst_block"])).cuda() for i, n in enumerate(lens)]
+            s["dst_slots"] = _slots([min(n, c["budget"]) for n in lens], s["dst_off"], s["dst_tbl"], c["dst_block"])
     return s
 
 
@@ -215,74 +223,78 @@ def _plane(pool, layout, layer, kv):
 
 
 def _rows(plane, slots, block):
-    """[head, token, dim] in 32 bits of the given slots."""
-    return plane[slots // block, slots % block].transpose(0, 1).float()
+    """[request, head, token, dim] in 32 bits of the given slots."""
+    return plane[slots // block, slots % block].transpose(1, 2).float()
 
 
 def _plain_attend(s):
     c = s["case"]
-    H, G, D, Q = c["heads"], c["group"], c["dim"], c["q_tokens"]
+    n, H, G, D, Q, P = c["n"], c["heads"], c["group"], c["dim"], c["q_tokens"], c["prefixes"]
     k_all, v_all = (_plane(s["pool"], c["layout"], s["layer"], kv) for kv in (0, 1))
-    scale = 1.0 / math.sqrt(D)
-    q = s["q"].float().view(c["n"], Q, H, G, D).permute(0, 2, 1, 3, 4).reshape(c["n"], H, Q * G, D)
-    shared = [(_rows(k_all, t, c["block"]), _rows(v_all, t, c["block"])) for t in s["prefix_slots"]]
-    outs, lses = [], []
-    if c["op"] == "weigh":
-        s["scores_out"].copy_(s["scores"])
-    first_hidden = torch.arange(Q, device="cuda").repeat_interleave(G) - (Q - 1)
-    for i, n in enumerate(s["lens"]):
-        k, v = _rows(k_all, s["slots"][i], c["block"]), _rows(v_all, s["slots"][i], c["block"])
-        logits = torch.matmul(q[i], k.transpose(1, 2)) * scale
-        if Q > 1:
-            seen = torch.arange(n, device="cuda")[None, :] < (n + first_hidden)[:, None]
-            logits = logits.masked_fill(~seen, -math.inf)
-        if s["member"][i] >= 0:
-            pk, pv = shared[s["member"][i]]
-            logits = torch.cat([torch.matmul(q[i], pk.transpose(1, 2)) * scale, logits], -1)
-        top = logits.amax(-1, keepdim=True)
-        p = torch.exp(logits - top)
-        total = p.sum(-1, keepdim=True)
-        if s["member"][i] >= 0:
-            o = torch.matmul(p[..., :-n], pv) + torch.matmul(p[..., -n:], v)
-        else:
-            o = torch.matmul(p, v)
-        outs.append(o / total)
-        lses.append((top + torch.log(total)).squeeze(-1))
-        if c["op"] == "weigh":
-            s["scores_out"][i, :, :n] += (p[..., -n:] / total).sum(1)
-    out = torch.stack(outs).view(c["n"], H, Q, G, D).permute(0, 2, 1, 3, 4).reshape(c["n"], Q, H * G, D).to(s["q"].dtype)
-    lse = torch.stack(lses).view(c["n"], H, Q, G).permute(0, 2, 1, 3).reshape(c["n"], Q, H * G).contiguous()
-    return {"out": out, "lse": lse, "scores": s["scores_out"]} if c["op"] == "weigh" else {"out": out, "lse": lse}
+    q = s["q"].float().view(n, Q, H, G, D).permute(0, 2, 1, 3, 4).reshape(n, H, Q * G, D) / math.sqrt(D)
+    W = s["slots"].shape[1]
+    logits = torch.matmul(q, _rows(k_all, s["slots"], c["block"]).transpose(2, 3))            # [request, head, row, token]
+    pos = torch.arange(W, device="cuda")
+    hidden = (Q - 1) - torch.arange(Q, device="cuda").repeat_interleave(G)                    # newest tokens a row does not see
+    seen = pos[None, None, :] < (s["len_t"][:, None] - hidden[None, :])[:, :, None]
+    logits.masked_fill_(~seen[:, None], -math.inf)
+    if P:
+        # requests of one prefix side by side, so that its keys are multiplied once; request i has prefix i % P
+        M = -(-n // P)
+        grouped = torch.zeros(M * P, H, Q * G, D, device="cuda")
+        grouped[:n] = q
+        grouped = grouped.view(M, P, H, Q * G, D).permute(1, 2, 0, 3, 4).reshape(P, H, M * Q * G, D)
+        over = torch.matmul(grouped, _rows(k_all, s["prefix_slots"], c["block"]).transpose(2, 3))
+        wide = over.shape[-1]
+        over.masked_fill_((torch.arange(wide, device="cuda")[None, :] >= s["prefix_len_t"][:, None])[:, None, None, :], -math.inf)
+        over = over.view(P, H, M, Q * G, wide).permute(2, 0, 1, 3, 4).reshape(M * P, H, Q * G, wide)[:n]
+        logits = torch.cat([logits, over], -1)
+    top = logits.amax(-1, keepdim=True)
+    p = torch.exp(logits - top)
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p[..., :W], _rows(v_all, s["slots"], c["block"]))
+    if P:
+        weights = torch.zeros(M * P, H, Q * G, wide, device="cuda")
+        weights[:n] = p[..., W:]
+        weights = weights.view(M, P, H, Q * G, wide).permute(1, 2, 0, 3, 4).reshape(P, H, M * Q * G, wide)
+        op = torch.matmul(weights, _rows(v_all, s["prefix_slots"], c["block"]))
+        o += op.view(P, H, M, Q * G, D).permute(2, 0, 1, 3, 4).reshape(M * P, H, Q * G, D)[:n]
+    lse = (top + torch.log(total)).view(n, H, Q, G).permute(0, 2, 1, 3).reshape(n, Q, H * G)
+    out = (o / total).view(n, H, Q, G, D).permute(0, 2, 1, 3, 4).reshape(n, Q, H * G, D).to(s["q"].dtype)
+    if c["op"] != "weigh":
+        return {"out": out, "lse": lse}
+    torch.add(s["scores"], (p[..., :W] / total).sum(2), out=s["scores_out"])
+    return {"out": out, "lse": lse, "scores": s["scores_out"]}
 
 
 def _plain_evict(s):
     c = s["case"]
-    L, H, K = c["layers"], c["heads"], c["budget"]
-    kept = torch.full((L, c["n"], H, K), -1, dtype=torch.int32, device="cuda")
-    kept_scores = torch.zeros(L, c["n"], H, K, device="cuda")
-    src = [[_plane(s["pool"], c["layout"], l, kv) for kv in (0, 1)] for l in range(L)]
-    dst = [[_plane(s["dst_pool"], c["dst_layout"], l, kv) for kv in (0, 1)] for l in range(L)]
-    head = torch.arange(H, device="cuda")
-    for i, n in enumerate(s["lens"]):
-        m = min(n, K)
-        if n <= K:
-            idx = torch.arange(n, device="cuda").expand(L, H, n)
+    L, H, K, n = c["layers"], c["heads"], c["budget"], c["n"]
+    W = s["slots"].shape[1]
+    pos, length = torch.arange(W, device="cuda"), s["len_t"][:, None]
+    weight = s["scores"].masked_fill((pos[None] >= length)[None, :, None], -math.inf)
+    always = (pos[None] < c["sink"]) | ((pos[None] >= length - c["recent"]) & (pos[None] < length))
+    weight = weight.masked_fill(always[None, :, None], math.inf)
+    idx = torch.sort(weight, dim=-1, descending=True, stable=True)[1][..., :K]
+    idx = torch.where(idx < length[None, :, None], idx, W).sort(-1)[0]                        # in order, W: nothing
+    wide = idx.shape[-1]
+    held = idx < W
+    kept = torch.full((L, n, H, K), -1, dtype=torch.int32, device="cuda")
+    kept[..., :wide] = torch.where(held, idx, -1)
+    kept_scores = torch.zeros(L, n, H, K, device="cuda")
+    kept_scores[..., :wide] = torch.gather(s["scores"], 3, idx.clamp(max=W - 1)).masked_fill(~held, 0.0)
+    l, r, h, j = held.nonzero(as_tuple=True)
+    at, to = s["slots"][r, idx[l, r, h, j]], s["dst_slots"][r, j]
+    for kv in (0, 1):
+        if c["layout"] == BLOCK_MAJOR:
+            rows = s["pool"][at // c["block"], l, kv, at % c["block"], h]
         else:
-            sink, recent = c["sink"], c["recent"]
-            mid = s["scores"][:, i, :, sink:n - recent]
-            best = torch.sort(mid, dim=-1, descending=True, stable=True)[1][..., :K - sink - recent] + sink
-            ends = [torch.arange(a, b, device="cuda").expand(L, H, b - a) for a, b in ((0, sink), (n - recent, n))]
-            idx = torch.cat([ends[0], best.sort(-1)[0], ends[1]], -1)
-        kept[:, i, :, :m] = idx.int()
-        kept_scores[:, i, :, :m] = torch.gather(s["scores"][:, i], 2, idx)
-        to = s["dst_slots"][i]
-        for l in range(L):
-            at = s["slots"][i][idx[l]]                                  # [head, kept]
-            for kv in (0, 1):
-                rows = src[l][kv][at // c["block"], at % c["block"], head[:, None]]
-                dst[l][kv][(to // c["dst_block"])[None], (to % c["dst_block"])[None], head[:, None]] = rows
-    lens = torch.tensor([min(n, K) for n in s["lens"]], dtype=torch.int32, device="cuda")
-    return {"kept": kept, "scores": kept_scores, "lens": lens, "pool": s["dst_pool"]}
+            rows = s["pool"][l, kv, at // c["block"], h, at % c["block"]]
+        if c["dst_layout"] == BLOCK_MAJOR:
+            s["dst_pool"][to // c["dst_block"], l, kv, to % c["dst_block"], h] = rows
+        else:
+            s["dst_pool"][l, kv, to // c["dst_block"], h, to % c["dst_block"]] = rows
+    return {"kept": kept, "scores": kept_scores, "lens": s["len_t"].clamp(max=K).int(), "pool": s["dst_pool"]}
 
 
 # ---------------------------------------------------------------------------
