@@ -68,6 +68,7 @@ extern "C" {
 typedef struct pdkv_pool pdkv_pool; /* opaque: geometry + borrowed device base */
 typedef struct pdkv_plan pdkv_plan; /* opaque: validated batch + device tile lists */
 typedef struct pdkv_queue pdkv_queue; /* opaque: receive slots for asynchronous retrieval */
+typedef struct pdkv_seqs pdkv_seqs; /* opaque: the cached sequences of a batch in one pool */
 
 enum pdkv_layout {
     PDKV_LAYOUT_BLOCK_MAJOR = 0,
@@ -373,6 +374,140 @@ int pdkv_sm_partition_create(int device, int transfer_sms, pdkv_sm_partition **o
 int pdkv_sm_partition_info(const pdkv_sm_partition *partition, int *transfer_sms, int *compute_sms);
 int pdkv_sm_partition_stream(const pdkv_sm_partition *partition, int which, void **stream);
 int pdkv_sm_partition_destroy(pdkv_sm_partition *partition);
+
+/* ---------------------------------------------------------------------------
+ * Operators on a filled pool: what the decode side does with the KV that was
+ * transferred (attention over it, in single-token or few-token steps) and what
+ * keeps it small (accumulated attention weights, eviction by them).  (The paper
+ * leaves both to the serving engine; Sec. 2.3's block-fixed pools and shared
+ * prefixes are what they work on.)
+ *
+ * pdkv_seqs describes the sequences of a batch inside one pool.  Sequence r owns
+ * `seq_len[r]` cached tokens in the blocks of its table.  A sequence may also sit
+ * behind a shared prefix (`seq_prefix[r]` = index of the prefix, or -1): the
+ * prefix' tokens come before its own, lie in the blocks of the prefix' table, and
+ * are read once for all sequences behind it.  A prefix ends anywhere in a block;
+ * the own tokens start in a block of their own.
+ *
+ * Like a plan, the handle is validated on the host and immutable afterwards, holds
+ * small device arrays (tables and work lists), and may be used from any thread and
+ * stream.  `seq_len` is the number of tokens the tables are good for: a call may be
+ * given shorter, current lengths in device memory, so that one handle (and one
+ * recorded CUDA graph) serves every step until a request needs another block. */
+enum pdkv_dtype {
+    PDKV_DTYPE_BF16 = 0,
+    PDKV_DTYPE_FP16 = 1
+};
+
+/* All arrays are host memory, read only during pdkv_seqs_create().  Tables are CSR
+ * as in pdkv_batch_desc.  The attention fields may all be zero in a handle that only
+ * evicts. */
+typedef struct {
+    int32_t n_seq;
+    const int32_t *seq_len;        /* [n_seq] own cached tokens (an upper bound when lengths come from the device) */
+    const int64_t *tbl_off;        /* [n_seq+1] */
+    const int32_t *tbl;            /* block ids */
+    int32_t n_prefix;              /* 0: no shared prefixes, the next four are ignored */
+    const int32_t *prefix_len;     /* [n_prefix] */
+    const int64_t *prefix_tbl_off; /* [n_prefix+1] */
+    const int32_t *prefix_tbl;
+    const int32_t *seq_prefix;     /* [n_seq] index of the prefix, -1: none */
+    int32_t num_q_heads;           /* a multiple of the pool's KV heads; 0: no attention through this handle */
+    int32_t q_tokens;              /* query tokens of every sequence in one call (1: plain decode) */
+    int32_t dtype;                 /* enum pdkv_dtype, of K, V, q and out */
+} pdkv_seqs_desc;
+
+/* `workspace` as in pdkv_plan_create_in(): NULL lets the handle allocate its device
+ * arrays, otherwise they are placed there and `needed_bytes` (optional) receives their
+ * size.  Attention takes pools of 2-byte elements whose head_dim is a multiple of 8
+ * and at most 256.  Copies of the lists are enqueued on `stream` and waited for.
+ * Errors: INVALID_ARG, GEOMETRY (pool or head counts the attention does not take),
+ * TABLE (ids out of range, tables too short), BUFFER_TOO_SMALL, CUDA, NOMEM. */
+int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *desc, void *workspace, size_t workspace_bytes,
+                     size_t *needed_bytes, void *stream, pdkv_seqs **out);
+/* Call it once the work enqueued with the handle has completed. */
+int pdkv_seqs_destroy(pdkv_seqs *seqs);
+
+/* Attention of one layer.  Query token i of sequence r is one of its newest: it attends
+ * to the whole prefix and to own tokens t < len_r - (q_tokens - 1 - i) (the token's own
+ * key is expected in the cache).  Query head h*G + g reads KV head h, G = num_q_heads /
+ * num_kv_heads.  Logits are scale * q.k; sums, maxima and weights are held in 32 bits,
+ * the weights are rounded to the pool's type for the product with V.  A row with
+ * nothing to attend to (or whose every logit is -infinity) gives zeros and lse =
+ * -infinity.  Cached rows past a sequence's length are never read into a result,
+ * whatever they hold. */
+typedef struct {
+    const void *q;                 /* device [n_seq][q_tokens][num_q_heads][head_dim] */
+    int64_t q_stride[3];           /* elements between sequences, query tokens, heads */
+    void *out;                     /* device, as q */
+    int64_t out_stride[3];
+    float *lse;                    /* device [n_seq][q_tokens][num_q_heads], natural logarithm, or NULL */
+    float scale;
+    const int32_t *seq_len;        /* device [n_seq] current own lengths, or NULL: those of the handle.
+                                      Values are clamped to [0, the handle's length] */
+    /* Accumulated attention weights of own tokens (prefix tokens are shared and have none):
+     * scores_out[r][h][t] = scores_in[r][h][t] + sum over q_tokens and the G query heads of the
+     * weight of token t; a token past len_r has no weight.  Rows hold as many tokens as the
+     * longest sequence of the handle; entries behind those are left as they are.  scores_out
+     * NULL: not wanted.  scores_in NULL: zeros.  scores_in may equal scores_out (same strides). */
+    const float *scores_in;
+    float *scores_out;
+    int64_t scores_in_stride[2];   /* floats between sequences, KV heads; tokens are adjacent */
+    int64_t scores_out_stride[2];
+} pdkv_attend_args;
+
+/* Scratch bytes one pdkv_attend() call needs.  The scratch is the caller's; calls that may
+ * run at the same time need one each.  Nothing in it outlives the call. */
+int pdkv_attend_scratch(const pdkv_seqs *seqs, int with_scores, size_t *bytes);
+/* Enqueues only (no allocation, copy or synchronisation): it can be recorded into a CUDA
+ * graph.  q and out are 16-byte aligned, their strides multiples of 8 elements; rows of out
+ * and of scores_out must not overlap; out must not overlap q, the pool or the scratch.
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL (scratch), CUDA. */
+int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, void *scratch, size_t scratch_bytes,
+                void *stream);
+
+/* Eviction by accumulated attention weight, per (layer, sequence, KV head), over layers
+ * [layer_begin, layer_end).  With len tokens and `budget`: len <= budget keeps all of them;
+ * otherwise the first `sink` tokens, the last `recent` ones and the budget - sink - recent
+ * heaviest of those between are kept (equal weights: the lower index first; a NaN weighs
+ * less than everything else).  The kept tokens' keys and values are written, in order, to
+ * token slots 0.. of the same sequence in `dst`; everything else in either pool stays as it
+ * is.  `dst` is the same handle (compaction in place: the freed blocks are the table's
+ * tail) or one over another pool of the same layers, KV heads, head_dim and element size
+ * that does not overlap this one; layout and block size may differ.  Its sequences must
+ * hold min(len, budget) tokens and its blocks must belong to one sequence each.  Elements
+ * are moved bit for bit, of any elem_bytes.  Prefixes are shared and stay. */
+typedef struct {
+    int32_t budget, sink, recent;  /* tokens; 0 <= sink, recent; sink + recent <= budget; budget >= 1 */
+    const int32_t *seq_len;        /* device [n_seq] current own lengths, or NULL (as for pdkv_attend) */
+    const float *scores;           /* device [layer][n_seq][num_kv_heads][token], layer counted from layer_begin */
+    int64_t scores_stride[3];      /* floats between layers, sequences, KV heads */
+    int32_t *kept;                 /* device [layer][n_seq][num_kv_heads][budget], dense: indices of the kept tokens,
+                                      ascending, -1 behind them; required */
+    float *kept_scores;            /* device: the scores of the kept tokens in order, then zeros up to
+                                      kept_scores_len; NULL: not wanted.  May equal `scores` (same strides) */
+    int64_t kept_scores_stride[3];
+    int32_t kept_scores_len;       /* entries of a row of kept_scores, >= min(budget, longest sequence) */
+    int32_t *new_len;              /* device [n_seq]: min(len, budget), or NULL.  May equal seq_len */
+} pdkv_evict_args;
+
+/* Enqueues only; no scratch.  Errors: INVALID_ARG, GEOMETRY (the pools disagree), TABLE
+ * (dst sequences too short, or a dst block used twice), CUDA. */
+int pdkv_evict(const pdkv_seqs *seqs, const pdkv_seqs *dst, int layer_begin, int layer_end, const pdkv_evict_args *args,
+               void *stream);
+
+/* One entry of a handle's attention work list, for inspection and host-side tests: rows
+ * [row_begin, row_end) of one KV head against tokens [tok_begin, tok_end) of a prefix
+ * (prefix >= 0) or of a sequence's own tokens (prefix -1, sequence `seq`).  Rows of a
+ * sequence are numbered query token * G + g; rows of a prefix run through its sequences in
+ * order.  Items are listed in the order the CTAs walk them. */
+typedef struct {
+    int32_t prefix, seq, head;
+    int32_t row_begin, row_end;
+    int32_t tok_begin, tok_end;
+    int32_t kernel, cta;
+} pdkv_attend_item;
+int pdkv_seqs_items(const pdkv_seqs *seqs, const pdkv_attend_item **items, int64_t *n_items);
 
 /* Number of GPU operations (kernel launches + memcpys) one call of `op`
  * enqueues; op = 3 asks about pdkv_transfer_blockwise. */

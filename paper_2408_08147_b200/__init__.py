@@ -2,6 +2,7 @@
 
 ``binding``   ctypes binding over ``libpdkv.so`` with the names of ``include/pdkv.h``
 ``session``   convenience holder of the C handles of one batch
+``sequences`` operators on a filled pool: attention (shared prefixes, accumulated weights), eviction
 ``workloads`` seeded synthetic inputs (no transfer arithmetic)
 ``build``     builds the shared library with nvcc
 ``p2d``       sender rank / receiver rank protocol over ``torch.distributed``
@@ -9,4 +10,4 @@
 Nothing here falls back to a CPU path: without the built library every call
 raises.
 """
-__all__ = ["binding", "session", "workloads", "build", "p2d"]
+__all__ = ["binding", "session", "sequences", "workloads", "build", "p2d"]

@@ -46,6 +46,7 @@ EXPORTS = (
     "pdkv_plan_autotune", "pdkv_plan_shape", "pdkv_plan_set_shape", "pdkv_plan_launch_shape", "pdkv_plan_option",
     "pdkv_sm_partition_create", "pdkv_sm_partition_info", "pdkv_sm_partition_stream", "pdkv_sm_partition_destroy",
     "pdkv_transfer_copies",
+    "pdkv_seqs_create", "pdkv_seqs_destroy", "pdkv_seqs_items", "pdkv_attend_scratch", "pdkv_attend", "pdkv_evict",
 )
 
 
@@ -72,6 +73,31 @@ class pdkv_launch_shape(C.Structure):
                                          "debug_bounds")]
 
 
+PDKV_DTYPE_BF16 = 0
+PDKV_DTYPE_FP16 = 1
+
+
+class pdkv_seqs_desc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("seq_len", C.c_void_p), ("tbl_off", C.c_void_p), ("tbl", C.c_void_p),
+                ("n_prefix", C.c_int32), ("prefix_len", C.c_void_p), ("prefix_tbl_off", C.c_void_p), ("prefix_tbl", C.c_void_p),
+                ("seq_prefix", C.c_void_p), ("num_q_heads", C.c_int32), ("q_tokens", C.c_int32), ("dtype", C.c_int32)]
+
+
+class pdkv_attend_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64 * 3), ("out", C.c_void_p), ("out_stride", C.c_int64 * 3),
+                ("lse", C.c_void_p), ("scale", C.c_float), ("seq_len", C.c_void_p), ("scores_in", C.c_void_p),
+                ("scores_out", C.c_void_p), ("scores_in_stride", C.c_int64 * 2), ("scores_out_stride", C.c_int64 * 2)]
+
+
+class pdkv_evict_args(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("sink", C.c_int32), ("recent", C.c_int32), ("seq_len", C.c_void_p),
+                ("scores", C.c_void_p), ("scores_stride", C.c_int64 * 3), ("kept", C.c_void_p),
+                ("kept_scores", C.c_void_p), ("kept_scores_stride", C.c_int64 * 3), ("kept_scores_len", C.c_int32),
+                ("new_len", C.c_void_p)]
+
+
+ITEM_DTYPE = np.dtype([(k, "<i4") for k in ("prefix", "seq", "head", "row_begin", "row_end", "tok_begin", "tok_end",
+                                            "kernel", "cta")])
 TILE_DTYPE = np.dtype([("src_off", "<i8"), ("dst_off", "<i8"), ("ntok", "<i4"), ("n_kept", "<i4")])
 
 
@@ -134,6 +160,12 @@ def lib() -> C.CDLL:
     L.pdkv_tune_get.argtypes = [C.c_char_p, C.POINTER(i64)]
     L.pdkv_strerror.restype = C.c_char_p
     L.pdkv_strerror.argtypes = [C.c_int]
+    L.pdkv_seqs_create.argtypes = [vp, C.POINTER(pdkv_seqs_desc), vp, C.c_size_t, C.POINTER(C.c_size_t), vp, C.POINTER(vp)]
+    L.pdkv_seqs_destroy.argtypes = [vp]
+    L.pdkv_seqs_items.argtypes = [vp, C.POINTER(vp), C.POINTER(i64)]
+    L.pdkv_attend_scratch.argtypes = [vp, C.c_int, C.POINTER(C.c_size_t)]
+    L.pdkv_attend.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), vp, C.c_size_t, vp]
+    L.pdkv_evict.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(pdkv_evict_args), vp]
     for name in EXPORTS:
         if name not in ("pdkv_pool_bytes", "pdkv_strerror"):
             getattr(L, name).restype = C.c_int
@@ -422,6 +454,58 @@ def pdkv_queue_stats(queue: int):
 
 def pdkv_queue_destroy(queue: int) -> None:
     _check(lib().pdkv_queue_destroy(C.c_void_p(queue)), "pdkv_queue_destroy")
+
+
+def pdkv_seqs_create(pool: int, seq_len, tbl_off, tbl, prefix_len=None, prefix_tbl_off=None, prefix_tbl=None,
+                     seq_prefix=None, num_q_heads: int = 0, q_tokens: int = 0, dtype: int = PDKV_DTYPE_BF16,
+                     workspace_ptr: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    """Returns (handle, needed_bytes); raises PdkvError with ``.needed_bytes`` set when the workspace is too small."""
+    def arr(a, dt):
+        return None if a is None else np.ascontiguousarray(a, dt)
+
+    a = [arr(seq_len, np.int32), arr(tbl_off, np.int64), arr(tbl, np.int32), arr(prefix_len, np.int32),
+         arr(prefix_tbl_off, np.int64), arr(prefix_tbl, np.int32), arr(seq_prefix, np.int32)]
+    p = [None if x is None else x.ctypes.data for x in a]
+    n = 0 if a[0] is None else int(a[0].shape[0])
+    n_prefix = 0 if a[3] is None else int(a[3].shape[0])
+    desc = pdkv_seqs_desc(n, p[0], p[1], p[2], n_prefix, p[3], p[4], p[5], p[6], num_q_heads, q_tokens, dtype)
+    out, need = C.c_void_p(), C.c_size_t()
+    rc = lib().pdkv_seqs_create(C.c_void_p(pool), C.byref(desc), C.c_void_p(workspace_ptr), workspace_bytes,
+                                C.byref(need), C.c_void_p(stream), C.byref(out))
+    if rc != PDKV_OK:
+        err = PdkvError(rc, "pdkv_seqs_create")
+        err.needed_bytes = int(need.value)
+        raise err
+    return out.value, int(need.value)
+
+
+def pdkv_seqs_destroy(seqs: int) -> None:
+    _check(lib().pdkv_seqs_destroy(C.c_void_p(seqs)), "pdkv_seqs_destroy")
+
+
+def pdkv_seqs_items(seqs: int) -> np.ndarray:
+    """Copy of the handle's attention work list as a structured numpy array."""
+    p, n = C.c_void_p(), C.c_int64()
+    _check(lib().pdkv_seqs_items(C.c_void_p(seqs), C.byref(p), C.byref(n)), "pdkv_seqs_items")
+    if n.value == 0:
+        return np.zeros(0, ITEM_DTYPE)
+    return np.frombuffer(C.string_at(p, n.value * ITEM_DTYPE.itemsize), ITEM_DTYPE).copy()
+
+
+def pdkv_attend_scratch(seqs: int, with_scores: bool) -> int:
+    n = C.c_size_t()
+    _check(lib().pdkv_attend_scratch(C.c_void_p(seqs), int(with_scores), C.byref(n)), "pdkv_attend_scratch")
+    return int(n.value)
+
+
+def pdkv_attend(seqs: int, layer: int, args: pdkv_attend_args, scratch_ptr: int, scratch_bytes: int, stream: int = 0) -> None:
+    _check(lib().pdkv_attend(C.c_void_p(seqs), layer, C.byref(args), C.c_void_p(scratch_ptr), scratch_bytes,
+                             C.c_void_p(stream)), "pdkv_attend")
+
+
+def pdkv_evict(seqs: int, dst: int, layer_begin: int, layer_end: int, args: pdkv_evict_args, stream: int = 0) -> None:
+    _check(lib().pdkv_evict(C.c_void_p(seqs), C.c_void_p(dst), layer_begin, layer_end, C.byref(args), C.c_void_p(stream)),
+           "pdkv_evict")
 
 
 def pdkv_tune(key: str, value: int) -> None:

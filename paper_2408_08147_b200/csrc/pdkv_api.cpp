@@ -14,13 +14,6 @@
 
 #include "pdkv_internal.h"
 
-struct pdkv_pool {
-    pdkv_pool_desc d;
-    char *base;
-    size_t bytes;
-    int device;
-};
-
 namespace {
 
 using pdkv::Tile;

@@ -9,6 +9,13 @@
 
 #include "pdkv.h"
 
+struct pdkv_pool {
+    pdkv_pool_desc d;
+    char *base;
+    size_t bytes;
+    int device;
+};
+
 namespace pdkv {
 
 // One unit of work along the token axis: `ntok` consecutive kept tokens of one

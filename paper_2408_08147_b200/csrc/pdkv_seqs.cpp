@@ -1,0 +1,580 @@
+// Handles of cached sequences and the entry points of the operators that work on them: the host
+// checks a batch's tables once, cuts its attention into work items of equal cost and uploads the
+// lists; the calls themselves only enqueue kernels.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <stdexcept>
+
+#include "pdkv_seqs.h"
+
+namespace pdkv {
+
+PoolView pool_view(const pdkv_pool &p)
+{
+    const int64_t row = (int64_t)p.d.head_dim * p.d.elem_bytes, hrow = row * p.d.num_kv_heads;
+    PoolView v;
+    v.base = p.base;
+    v.block_tokens = p.d.block_tokens;
+    if (p.d.layout == PDKV_LAYOUT_BLOCK_MAJOR) {
+        v.lc_stride = p.d.block_tokens * hrow;
+        v.block_stride = 2 * p.d.num_layers * v.lc_stride;
+        v.tok_stride = hrow;
+        v.head_stride = row;
+    } else {
+        v.block_stride = p.d.block_tokens * hrow;
+        v.lc_stride = p.d.num_blocks * v.block_stride;
+        v.tok_stride = row;
+        v.head_stride = p.d.block_tokens * row;
+    }
+    return v;
+}
+
+}  // namespace pdkv
+
+namespace {
+
+using pdkv::AttnItem;
+using pdkv::AttnSeg;
+using pdkv::AttnSeq;
+using pdkv::AttnUnit;
+
+constexpr int kMaxRowTile = 64;    // rows of one work item
+constexpr int64_t kQuantum = 64;   // tokens; work is cut along the tokens in multiples of this
+
+bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+    return a_bytes && b_bytes && a0 < b0 + b_bytes && b0 < a0 + a_bytes;
+}
+
+bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Do rows of `len` entries at i0*s0 + i1*s1 + i2*s2 lie apart from one another?  Axes of one entry do
+// not count; the others have to nest (each stride spans everything inside it).
+bool rows_apart(int64_t len, const int64_t *stride, const int64_t *n, int axes)
+{
+    std::vector<std::pair<int64_t, int64_t>> ax;
+    for (int i = 0; i < axes; ++i) {
+        if (n[i] > 1) ax.emplace_back(stride[i], n[i]);
+        if (stride[i] < 0) return false;
+    }
+    std::sort(ax.begin(), ax.end());
+    int64_t span = len;
+    for (const auto &a : ax) {
+        if (a.first < span) return false;
+        span += a.first * (a.second - 1);
+    }
+    return true;
+}
+
+// Bytes from the first to past the last element of such rows.
+int64_t rows_span(int64_t len, const int64_t *stride, const int64_t *n, int axes)
+{
+    int64_t span = len;
+    for (int i = 0; i < axes; ++i)
+        if (n[i] > 0) span += stride[i] * (n[i] - 1);
+    return span;
+}
+
+int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int32_t n, int64_t B, int64_t NB)
+{
+    if (!off || !len) return PDKV_ERR_INVALID_ARG;
+    if (off[0] < 0) return PDKV_ERR_TABLE;
+    for (int32_t r = 0; r < n; ++r) {
+        if (len[r] < 0) return PDKV_ERR_INVALID_ARG;
+        if (off[r + 1] < off[r]) return PDKV_ERR_TABLE;
+        const int64_t need = ((int64_t)len[r] + B - 1) / B;
+        if (off[r + 1] - off[r] < need) return PDKV_ERR_TABLE;
+        if (need && !tbl) return PDKV_ERR_INVALID_ARG;
+        for (int64_t j = 0; j < need; ++j)
+            if (tbl[off[r] + j] < 0 || tbl[off[r] + j] >= NB) return PDKV_ERR_TABLE;
+    }
+    return PDKV_OK;
+}
+
+int row_tile(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile; }
+
+// Work list.  Units (segment, row tile, head) lie behind one another on an axis of cost -- token quanta
+// plus a constant for the start and the end of a unit -- and the CTAs take equal stretches of it.
+void plan_items(pdkv_seqs &s, const std::vector<int32_t> &n_rows, int n_ctas_max)
+{
+    struct Work { int32_t seg, head, row0, rows; int64_t quanta; };
+    std::vector<Work> work;
+    const int32_t H = s.pool.d.num_kv_heads;
+    constexpr int64_t kOverhead = 1;
+    int64_t total = 0;
+    for (size_t g = 0; g < s.segs.size(); ++g) {
+        const AttnSeg &seg = s.segs[g];
+        if (seg.len == 0 || n_rows[g] == 0) continue;
+        const int tile = row_tile(n_rows[g]);
+        for (int32_t r0 = 0; r0 < n_rows[g]; r0 += tile)
+            for (int32_t h = 0; h < H; ++h) {
+                work.push_back({(int32_t)g, h, r0, std::min<int32_t>(tile, n_rows[g] - r0), (seg.len + kQuantum - 1) / kQuantum});
+                total += work.back().quanta + kOverhead;
+            }
+    }
+    s.units.resize(work.size());
+    s.cta_items.assign(1, 0);
+    if (work.empty()) return;
+    // a CTA gets at least four quanta, so that joining the parts stays cheap beside reading the tokens
+    const int64_t n_ctas = std::max<int64_t>(1, std::min<int64_t>(n_ctas_max, total / 4));
+    int64_t at = 0, cta = 0;
+    for (size_t u = 0; u < work.size(); ++u) {
+        const Work &w = work[u];
+        AttnUnit &unit = s.units[u];
+        unit.part_row = s.part_rows;
+        unit.rows = w.rows;
+        unit.n_parts = 0;
+        int64_t q = 0;
+        while (q < w.quanta) {
+            // `at` is where quantum q of this unit lies; this CTA's stretch ends at end
+            while (cta + 1 < n_ctas && at + kOverhead >= (cta + 1) * total / n_ctas) {
+                ++cta;
+                s.cta_items.push_back((int32_t)s.items.size());
+            }
+            int64_t n = w.quanta - q;
+            if (cta + 1 < n_ctas) n = std::min(n, (cta + 1) * total / n_ctas - at);
+            n = std::max<int64_t>(n, 1);
+            AttnItem it{};
+            it.part_row = s.part_rows;
+            it.seg = w.seg;
+            it.head = w.head;
+            it.row0 = w.row0;
+            it.rows = w.rows;
+            it.tok0 = (int32_t)(q * kQuantum);
+            it.tok1 = (int32_t)std::min<int64_t>(s.segs[w.seg].len, (q + n) * kQuantum);
+            s.items.push_back(it);
+            pdkv_attend_item li{};
+            li.prefix = w.seg >= s.n_seq ? w.seg - s.n_seq : -1;
+            li.seq = w.seg < s.n_seq ? w.seg : -1;
+            li.head = w.head;
+            li.row_begin = w.row0;
+            li.row_end = w.row0 + w.rows;
+            li.tok_begin = it.tok0;
+            li.tok_end = it.tok1;
+            li.kernel = 0;
+            li.cta = (int32_t)cta;
+            s.listing.push_back(li);
+            s.part_rows += w.rows;
+            ++unit.n_parts;
+            q += n;
+            at += n;
+        }
+        at += kOverhead;
+    }
+    while ((int64_t)s.cta_items.size() < n_ctas) s.cta_items.push_back((int32_t)s.items.size());
+    s.cta_items.push_back((int32_t)s.items.size());
+}
+
+}  // namespace
+
+extern "C" {
+
+int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *workspace, size_t workspace_bytes,
+                     size_t *needed_bytes, void *stream, pdkv_seqs **out)
+{
+    if (out) *out = nullptr;
+    if (needed_bytes) *needed_bytes = 0;
+    if (!out || !pool || !d) return PDKV_ERR_INVALID_ARG;
+    if (d->n_seq < 0 || d->n_prefix < 0 || d->num_q_heads < 0) return PDKV_ERR_INVALID_ARG;
+    if (workspace && !aligned(workspace, 16)) return PDKV_ERR_INVALID_ARG;
+    const pdkv_pool_desc &g = pool->d;
+    const bool attention = d->num_q_heads > 0;
+    if (attention) {
+        if (d->q_tokens < 1 || (d->dtype != PDKV_DTYPE_BF16 && d->dtype != PDKV_DTYPE_FP16)) return PDKV_ERR_INVALID_ARG;
+        if (d->num_q_heads % g.num_kv_heads || g.elem_bytes != 2 || g.head_dim % 8 || g.head_dim > 256) return PDKV_ERR_GEOMETRY;
+        // rows of one sequence and head, and rows behind one prefix, are counted in 32 bits
+        if ((int64_t)d->q_tokens * d->num_q_heads * std::max(1, d->n_seq) > (int64_t)1 << 30) return PDKV_ERR_INVALID_ARG;
+    }
+    const int64_t B = g.block_tokens;
+    try {
+        if (d->n_seq > 0) {
+            const int rc = check_lists(d->tbl_off, d->tbl, d->seq_len, d->n_seq, B, g.num_blocks);
+            if (rc != PDKV_OK) return rc;
+        }
+        if (d->n_prefix > 0) {
+            const int rc = check_lists(d->prefix_tbl_off, d->prefix_tbl, d->prefix_len, d->n_prefix, B, g.num_blocks);
+            if (rc != PDKV_OK) return rc;
+            if (!d->seq_prefix && d->n_seq > 0) return PDKV_ERR_INVALID_ARG;
+            for (int32_t r = 0; r < d->n_seq; ++r)
+                if (d->seq_prefix[r] < -1 || d->seq_prefix[r] >= d->n_prefix) return PDKV_ERR_INVALID_ARG;
+        }
+        pdkv_seqs *s = new pdkv_seqs;
+        struct Holder {
+            pdkv_seqs *s;
+            ~Holder() { if (s) pdkv_seqs_destroy(s); }
+        } hold{s};
+        s->pool = *pool;
+        s->device = pool->device;
+        s->n_seq = d->n_seq;
+        s->n_prefix = d->n_prefix;
+        s->len.assign(d->seq_len, d->seq_len + d->n_seq);
+        for (int32_t n : s->len) s->max_len = std::max(s->max_len, n);
+        s->Hq = d->num_q_heads;
+        s->G = attention ? d->num_q_heads / g.num_kv_heads : 0;
+        s->q_tokens = attention ? d->q_tokens : 0;
+        s->dtype = d->dtype;
+
+        if (!pdkv::tunables().dry_run) {
+            const cudaError_t e = cudaDeviceGetAttribute(&s->sm_count, cudaDevAttrMultiProcessorCount, s->device);
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaDeviceGetAttribute");
+        }
+
+        // tables, own tokens first, only the entries that hold tokens
+        std::vector<int32_t> tbl;
+        std::vector<uint8_t> seen((size_t)g.num_blocks, 0);
+        auto add = [&](const int64_t *off, const int32_t *ids, int32_t r, int32_t len, int32_t seq) {
+            AttnSeg seg{};
+            seg.tbl = (int64_t)tbl.size();
+            seg.len = len;
+            seg.seq = seq;
+            const int64_t need = ((int64_t)len + B - 1) / B;
+            for (int64_t j = 0; j < need; ++j) {
+                const int32_t id = ids[off[r] + j];
+                tbl.push_back(id);
+                if (seen[(size_t)id]) s->unique_blocks = false;
+                seen[(size_t)id] = 1;
+            }
+            s->segs.push_back(seg);
+        };
+        for (int32_t r = 0; r < d->n_seq; ++r) add(d->tbl_off, d->tbl, r, d->seq_len[r], r);
+        for (int32_t p = 0; p < d->n_prefix; ++p) add(d->prefix_tbl_off, d->prefix_tbl, p, d->prefix_len[p], -1);
+
+        std::vector<int32_t> members;
+        if (attention) {
+            const int64_t R = (int64_t)s->G * s->q_tokens;
+            std::vector<int32_t> n_rows(s->segs.size(), 0), row0((size_t)s->n_seq, 0);
+            for (int32_t r = 0; r < s->n_seq; ++r) n_rows[(size_t)r] = (int32_t)R;
+            for (int32_t p = 0; p < s->n_prefix; ++p) {
+                AttnSeg &seg = s->segs[(size_t)(s->n_seq + p)];
+                seg.member_begin = (int32_t)members.size();
+                for (int32_t r = 0; r < s->n_seq; ++r)
+                    if (d->seq_prefix[r] == p) {
+                        row0[(size_t)r] = n_rows[(size_t)(s->n_seq + p)];
+                        n_rows[(size_t)(s->n_seq + p)] += (int32_t)R;
+                        members.push_back(r);
+                    }
+            }
+            plan_items(*s, n_rows, 2 * s->sm_count);
+            // unit of (row tile 0, head 0) of every segment: units are in the order of the segments
+            std::vector<int32_t> unit0(s->segs.size(), -1);
+            for (size_t i = 0, u = 0; i < s->segs.size(); ++i) {
+                if (s->segs[i].len == 0 || n_rows[i] == 0) continue;
+                unit0[i] = (int32_t)u;
+                const int t = row_tile(n_rows[i]);
+                u += (size_t)((n_rows[i] + t - 1) / t) * (size_t)g.num_kv_heads;
+            }
+            s->seqs.resize((size_t)s->n_seq);
+            for (int32_t r = 0; r < s->n_seq; ++r) {
+                AttnSeq &q = s->seqs[(size_t)r];
+                q.len = s->len[(size_t)r];
+                q.own_unit = unit0[(size_t)r];
+                q.own_tile = row_tile(R);
+                const int32_t p = d->n_prefix > 0 ? d->seq_prefix[r] : -1;
+                q.prefix_unit = p >= 0 ? unit0[(size_t)(s->n_seq + p)] : -1;
+                q.prefix_tile = p >= 0 ? row_tile(n_rows[(size_t)(s->n_seq + p)]) : 1;
+                q.prefix_row0 = row0[(size_t)r];
+                q.logit_stride = (q.len + 3) / 4 * 4;
+                q.logits = s->logit_floats;
+                s->logit_floats += (int64_t)q.logit_stride * R * g.num_kv_heads;
+                q.direct = q.own_unit >= 0 && q.prefix_unit < 0;
+                if (q.direct) {   // every (row tile, head) in one part?
+                    const int64_t tiles = (R + q.own_tile - 1) / q.own_tile;
+                    for (int64_t u = 0; u < tiles * g.num_kv_heads; ++u)
+                        if (s->units[(size_t)(q.own_unit + u)].n_parts != 1) q.direct = 0;
+                }
+                if (!q.direct) s->join = true;
+            }
+            for (AttnItem &it : s->items) it.direct = it.seg < s->n_seq && s->seqs[(size_t)it.seg].direct;
+        }
+
+        // device arrays: one block, each list 16-byte aligned
+        size_t bytes = 0;
+        auto place = [&](size_t n) {
+            const size_t o = bytes;
+            bytes += (n + 15) / 16 * 16;
+            return o;
+        };
+        const size_t o_tbl = place(tbl.size() * 4), o_members = place(members.size() * 4), o_cta = place(s->cta_items.size() * 4),
+                     o_segs = place(s->segs.size() * sizeof(AttnSeg)), o_units = place(s->units.size() * sizeof(AttnUnit)),
+                     o_seqs = place(s->seqs.size() * sizeof(AttnSeq)), o_items = place(s->items.size() * sizeof(AttnItem));
+        bytes = std::max<size_t>(bytes, 16);
+        if (needed_bytes) *needed_bytes = bytes;
+        if (workspace && workspace_bytes < bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
+        if (!pdkv::tunables().dry_run) {
+            std::vector<char> image(bytes, 0);
+            auto put = [&](size_t o, const void *p, size_t n) { if (n) memcpy(image.data() + o, p, n); };
+            put(o_tbl, tbl.data(), tbl.size() * 4);
+            put(o_members, members.data(), members.size() * 4);
+            put(o_cta, s->cta_items.data(), s->cta_items.size() * 4);
+            put(o_segs, s->segs.data(), s->segs.size() * sizeof(AttnSeg));
+            put(o_units, s->units.data(), s->units.size() * sizeof(AttnUnit));
+            put(o_seqs, s->seqs.data(), s->seqs.size() * sizeof(AttnSeq));
+            put(o_items, s->items.data(), s->items.size() * sizeof(AttnItem));
+            pdkv::DeviceGuard guard(s->device);
+            if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
+            if (workspace) {
+                s->dev_mem = workspace;
+                s->owns_dev_mem = false;
+            } else {
+                cudaError_t e = cudaMalloc(&s->dev_mem, bytes);
+                if (e != cudaSuccess) {
+                    s->dev_mem = nullptr;
+                    return pdkv::report_cuda_error(e, "cudaMalloc");
+                }
+            }
+            cudaStream_t st = static_cast<cudaStream_t>(stream);
+            cudaError_t e = cudaMemcpyAsync(s->dev_mem, image.data(), bytes, cudaMemcpyHostToDevice, st);
+            if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaMemcpyAsync");
+            const char *b = static_cast<const char *>(s->dev_mem);
+            s->d_tbl = reinterpret_cast<const int32_t *>(b + o_tbl);
+            s->d_members = reinterpret_cast<const int32_t *>(b + o_members);
+            s->d_cta_items = reinterpret_cast<const int32_t *>(b + o_cta);
+            s->d_segs = reinterpret_cast<const AttnSeg *>(b + o_segs);
+            s->d_units = reinterpret_cast<const AttnUnit *>(b + o_units);
+            s->d_seqs = reinterpret_cast<const AttnSeq *>(b + o_seqs);
+            s->d_items = reinterpret_cast<const AttnItem *>(b + o_items);
+        }
+        hold.s = nullptr;
+        *out = s;
+        return PDKV_OK;
+    } catch (const std::bad_alloc &) {
+        return PDKV_ERR_NOMEM;
+    } catch (const std::length_error &) {
+        return PDKV_ERR_NOMEM;
+    }
+}
+
+int pdkv_seqs_destroy(pdkv_seqs *s)
+{
+    if (!s) return PDKV_OK;
+    int rc = PDKV_OK;
+    if (s->dev_mem && s->owns_dev_mem) {
+        pdkv::DeviceGuard guard(s->device);
+        cudaError_t e = cudaFree(s->dev_mem);
+        if (e != cudaSuccess) rc = pdkv::report_cuda_error(e, "cudaFree");
+    }
+    delete s;
+    return rc;
+}
+
+int pdkv_seqs_items(const pdkv_seqs *s, const pdkv_attend_item **items, int64_t *n_items)
+{
+    if (!s || !items || !n_items) return PDKV_ERR_INVALID_ARG;
+    *items = s->listing.data();
+    *n_items = (int64_t)s->listing.size();
+    return PDKV_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+struct ScratchLayout {
+    size_t o = 0, ml = 0, logits = 0, bytes = 0;
+};
+
+ScratchLayout scratch_layout(const pdkv_seqs *s, bool with_scores)
+{
+    ScratchLayout l;
+    auto place = [&](size_t n) {
+        const size_t o = l.bytes;
+        l.bytes += (n + 255) / 256 * 256;
+        return o;
+    };
+    l.o = place(s->join ? (size_t)s->part_rows * (size_t)s->pool.d.head_dim * 4 : 0);
+    l.ml = place((s->join || with_scores) ? (size_t)s->part_rows * 8 : 0);
+    l.logits = place(with_scores ? (size_t)s->logit_floats * 4 : 0);
+    return l;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pdkv_attend_scratch(const pdkv_seqs *s, int with_scores, size_t *bytes)
+{
+    if (!s || !bytes || s->Hq == 0) return PDKV_ERR_INVALID_ARG;
+    *bytes = scratch_layout(s, with_scores != 0).bytes;
+    return PDKV_OK;
+}
+
+int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *scratch, size_t scratch_bytes, void *stream)
+{
+    if (!s || !a || s->Hq == 0 || layer < 0 || layer >= s->pool.d.num_layers) return PDKV_ERR_INVALID_ARG;
+    if (!std::isfinite(a->scale)) return PDKV_ERR_INVALID_ARG;
+    try {
+        const int64_t rows[3] = {s->n_seq, s->q_tokens, s->Hq};
+        const int64_t D = s->pool.d.head_dim;
+        if (s->n_seq > 0) {
+            if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16)) return PDKV_ERR_INVALID_ARG;
+            for (int i = 0; i < 3; ++i)
+                if (rows[i] > 1 && (a->q_stride[i] % 8 || a->out_stride[i] % 8 || a->q_stride[i] < 0)) return PDKV_ERR_INVALID_ARG;
+            if (!rows_apart(D, a->out_stride, rows, 3)) return PDKV_ERR_INVALID_ARG;
+            const size_t out_span = 2 * (size_t)rows_span(D, a->out_stride, rows, 3);
+            const size_t q_span = 2 * (size_t)rows_span(D, a->q_stride, rows, 3);
+            if (ranges_overlap(a->out, out_span, s->pool.base, pdkv_pool_bytes(&s->pool.d)) || ranges_overlap(a->out, out_span, a->q, q_span) ||
+                ranges_overlap(a->out, out_span, scratch, scratch_bytes))
+                return PDKV_ERR_INVALID_ARG;
+        }
+        if (a->lse && !aligned(a->lse, 4)) return PDKV_ERR_INVALID_ARG;
+        if (a->seq_len && !aligned(a->seq_len, 4)) return PDKV_ERR_INVALID_ARG;
+        const bool scores = a->scores_out != nullptr;
+        if (!scores && a->scores_in) return PDKV_ERR_INVALID_ARG;
+        if (scores) {
+            if (!aligned(a->scores_out, 4) || !aligned(a->scores_in, 4)) return PDKV_ERR_INVALID_ARG;
+            const int64_t n[2] = {s->n_seq, s->pool.d.num_kv_heads};
+            if (!rows_apart(s->max_len, a->scores_out_stride, n, 2)) return PDKV_ERR_INVALID_ARG;
+            if (a->scores_in) {
+                const bool same = a->scores_in == a->scores_out;
+                for (int i = 0; i < 2; ++i)
+                    if (n[i] > 1 && (a->scores_in_stride[i] < 0 || (same && a->scores_in_stride[i] != a->scores_out_stride[i])))
+                        return PDKV_ERR_INVALID_ARG;
+                if (!same && ranges_overlap(a->scores_in, 4 * (size_t)rows_span(s->max_len, a->scores_in_stride, n, 2), a->scores_out,
+                                            4 * (size_t)rows_span(s->max_len, a->scores_out_stride, n, 2)))
+                    return PDKV_ERR_INVALID_ARG;
+            }
+        }
+        const ScratchLayout l = scratch_layout(s, scores);
+        if (l.bytes && (!scratch || !aligned(scratch, 16))) return PDKV_ERR_INVALID_ARG;
+        if (scratch_bytes < l.bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
+        if (!s->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
+        if (s->n_seq == 0) return PDKV_OK;
+
+        pdkv::AttnParams p{};
+        p.pool = pdkv::pool_view(s->pool);
+        p.tbl = s->d_tbl;
+        p.segs = s->d_segs;
+        p.units = s->d_units;
+        p.seqs = s->d_seqs;
+        p.members = s->d_members;
+        p.items = s->d_items;
+        p.cta_items = s->d_cta_items;
+        p.n_ctas = (int32_t)s->cta_items.size() - 1;
+        p.n_seq = s->n_seq;
+        p.H = s->pool.d.num_kv_heads;
+        p.G = s->G;
+        p.D = s->pool.d.head_dim;
+        p.q_tokens = s->q_tokens;
+        p.q = a->q;
+        p.out = a->out;
+        for (int i = 0; i < 3; ++i) {
+            p.q_stride[i] = rows[i] > 1 ? a->q_stride[i] : 0;
+            p.out_stride[i] = rows[i] > 1 ? a->out_stride[i] : 0;
+        }
+        p.lse = a->lse;
+        p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+        p.seq_len = a->seq_len;
+        char *w = static_cast<char *>(scratch);
+        p.part_o = reinterpret_cast<float *>(w + l.o);
+        p.part_ml = reinterpret_cast<float *>(w + l.ml);
+        if (scores) {
+            p.logits = reinterpret_cast<float *>(w + l.logits);
+            p.scores_in = a->scores_in;
+            p.scores_out = a->scores_out;
+            for (int i = 0; i < 2; ++i) {
+                p.scores_in_stride[i] = a->scores_in_stride[i];
+                p.scores_out_stride[i] = a->scores_out_stride[i];
+            }
+        }
+        p.max_len = s->max_len;
+        p.layer = layer;
+        pdkv::DeviceGuard guard(s->device);
+        if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
+        cudaStream_t st = static_cast<cudaStream_t>(stream);
+        if (p.n_ctas > 0) {
+            const cudaError_t e = pdkv::launch_attend(p, s->dtype, st);
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention kernel launch");
+        }
+        if (s->join || scores) {
+            const cudaError_t e = pdkv::launch_attend_join(p, s->dtype, st);
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "join kernel launch");
+        }
+        return PDKV_OK;
+    } catch (const std::bad_alloc &) {
+        return PDKV_ERR_NOMEM;
+    }
+}
+
+int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int layer_end, const pdkv_evict_args *a, void *stream)
+{
+    if (!s || !t || !a || layer_begin < 0 || layer_begin > layer_end || layer_end > s->pool.d.num_layers) return PDKV_ERR_INVALID_ARG;
+    if (a->sink < 0 || a->recent < 0 || a->budget < 1 || (int64_t)a->sink + a->recent > a->budget) return PDKV_ERR_INVALID_ARG;
+    if (s->n_seq != t->n_seq) return PDKV_ERR_INVALID_ARG;
+    const pdkv_pool_desc &x = s->pool.d, &y = t->pool.d;
+    if (x.num_layers != y.num_layers || x.num_kv_heads != y.num_kv_heads || x.head_dim != y.head_dim || x.elem_bytes != y.elem_bytes)
+        return PDKV_ERR_GEOMETRY;
+    if (s->device != t->device) return PDKV_ERR_INVALID_ARG;
+    if (!t->unique_blocks) return PDKV_ERR_TABLE;
+    if (s != t) {
+        if (ranges_overlap(s->pool.base, pdkv_pool_bytes(&x), t->pool.base, pdkv_pool_bytes(&y))) return PDKV_ERR_INVALID_ARG;
+        for (int32_t r = 0; r < s->n_seq; ++r)
+            if (t->len[(size_t)r] < std::min(s->len[(size_t)r], a->budget)) return PDKV_ERR_TABLE;
+    }
+    try {
+        const int64_t layers = layer_end - layer_begin;
+        const int64_t n[3] = {layers, s->n_seq, x.num_kv_heads};
+        const int64_t top = std::min(s->max_len, a->budget);
+        if (s->n_seq > 0 && layers > 0 && s->max_len > 0) {
+            if (!a->scores || !a->kept || !aligned(a->scores, 4) || !aligned(a->kept, 4)) return PDKV_ERR_INVALID_ARG;
+            for (int i = 0; i < 3; ++i)
+                if (n[i] > 1 && a->scores_stride[i] < 0) return PDKV_ERR_INVALID_ARG;
+            if (a->kept_scores) {
+                if (!aligned(a->kept_scores, 4) || a->kept_scores_len < top) return PDKV_ERR_INVALID_ARG;
+                if (!rows_apart(a->kept_scores_len, a->kept_scores_stride, n, 3)) return PDKV_ERR_INVALID_ARG;
+                const bool same = a->kept_scores == a->scores;
+                for (int i = 0; i < 3; ++i)
+                    if (same && n[i] > 1 && a->scores_stride[i] != a->kept_scores_stride[i]) return PDKV_ERR_INVALID_ARG;
+                if (!same && ranges_overlap(a->scores, 4 * (size_t)rows_span(s->max_len, a->scores_stride, n, 3), a->kept_scores,
+                                            4 * (size_t)rows_span(a->kept_scores_len, a->kept_scores_stride, n, 3)))
+                    return PDKV_ERR_INVALID_ARG;
+            }
+        }
+        if (!s->dev_mem || !t->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
+        if (s->n_seq == 0 || layers == 0) return PDKV_OK;
+        if (s->max_len > 0 || a->kept || a->new_len) {
+            if (!a->kept) return PDKV_ERR_INVALID_ARG;
+            pdkv::EvictParams p{};
+            p.src = pdkv::pool_view(s->pool);
+            p.dst = pdkv::pool_view(t->pool);
+            p.src_tbl = s->d_tbl;
+            p.dst_tbl = t->d_tbl;
+            p.src_segs = s->d_segs;
+            p.dst_segs = t->d_segs;
+            p.n_seq = s->n_seq;
+            p.H = x.num_kv_heads;
+            p.row_bytes = x.head_dim * x.elem_bytes;
+            p.layer_begin = layer_begin;
+            p.n_layers = (int32_t)layers;
+            p.in_place = s == t;
+            p.budget = a->budget;
+            p.sink = a->sink;
+            p.recent = a->recent;
+            p.seq_len = a->seq_len;
+            p.scores = a->scores;
+            p.kept = a->kept;
+            p.kept_scores = a->kept_scores;
+            p.kept_scores_len = a->kept_scores_len;
+            p.new_len = a->new_len;
+            for (int i = 0; i < 3; ++i) {
+                p.scores_stride[i] = n[i] > 1 ? a->scores_stride[i] : 0;
+                p.kept_scores_stride[i] = n[i] > 1 ? a->kept_scores_stride[i] : 0;
+            }
+            p.max_len = s->max_len;
+            p.vec_bytes = 16;
+            while (p.vec_bytes > 1 && p.row_bytes % p.vec_bytes) p.vec_bytes /= 2;
+            pdkv::DeviceGuard guard(s->device);
+            if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
+            const cudaError_t e = pdkv::launch_evict(p, s->sm_count, static_cast<cudaStream_t>(stream));
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "eviction kernel launch");
+        }
+        return PDKV_OK;
+    } catch (const std::bad_alloc &) {
+        return PDKV_ERR_NOMEM;
+    }
+}
+
+}  // extern "C"

@@ -1,0 +1,242 @@
+"""Operators on a filled pool: attention over cached sequences, and eviction.
+
+:class:`CacheSession` keeps the C handles of one batch of cached sequences together, as
+:class:`~paper_2408_08147_b200.session.TransferSession` does for a transfer.  It marshals
+arguments and allocates outputs and scratch with torch; every number is computed by the
+library's kernels.
+
+    seqs = Sequences(seq_len, tbl_off, tbl)                       # the decode side's tables
+    with CacheSession(geom, pool_t, seqs, num_q_heads=32) as s:
+        out, lse = s.attend(layer, q, scores_t=scores)            # scores accumulate in place
+        kept, _, new_len = s.evict(s, scores_all, budget=1024, sink=4, recent=256,
+                                   kept_scores_t=scores_all)      # compacts the pool in place
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Optional, Sequence, Tuple
+
+import numpy as np
+
+from . import binding as B
+
+
+@dataclass
+class Sequences:
+    """Cached sequences of a batch (see ``pdkv_seqs_desc``): own tokens in CSR block tables,
+    optionally behind shared prefixes (``seq_prefix[r]``: index of the prefix, -1 for none)."""
+
+    seq_len: Sequence[int]
+    tbl_off: np.ndarray
+    tbl: np.ndarray
+    prefix_len: Optional[Sequence[int]] = None
+    prefix_tbl_off: Optional[np.ndarray] = None
+    prefix_tbl: Optional[np.ndarray] = None
+    seq_prefix: Optional[Sequence[int]] = None
+
+    def __post_init__(self):
+        def arr(a, dt):
+            return None if a is None else np.ascontiguousarray(a, dt)
+
+        self.seq_len, self.tbl_off, self.tbl = arr(self.seq_len, np.int32), arr(self.tbl_off, np.int64), arr(self.tbl, np.int32)
+        self.prefix_len, self.seq_prefix = arr(self.prefix_len, np.int32), arr(self.seq_prefix, np.int32)
+        self.prefix_tbl_off, self.prefix_tbl = arr(self.prefix_tbl_off, np.int64), arr(self.prefix_tbl, np.int32)
+        n = int(self.seq_len.shape[0])
+        if self.tbl_off.shape != (n + 1,):
+            raise ValueError("tbl_off needs one entry more than seq_len")
+        if n and self.tbl_off[-1] > self.tbl.shape[0]:
+            raise ValueError("tbl is shorter than tbl_off says")
+        if self.prefix_len is not None and self.prefix_len.size:
+            if self.prefix_tbl_off is None or self.prefix_tbl is None or self.seq_prefix is None:
+                raise ValueError("prefixes need prefix_tbl_off, prefix_tbl and seq_prefix")
+            if self.prefix_tbl_off.shape != (self.prefix_len.shape[0] + 1,) or self.seq_prefix.shape != (n,):
+                raise ValueError("prefix_tbl_off / seq_prefix do not match the lengths")
+            if self.prefix_tbl_off[-1] > self.prefix_tbl.shape[0]:
+                raise ValueError("prefix_tbl is shorter than prefix_tbl_off says")
+
+    @property
+    def n_seq(self) -> int:
+        return int(self.seq_len.shape[0])
+
+    @property
+    def max_len(self) -> int:
+        return int(self.seq_len.max()) if self.n_seq else 0
+
+
+def _strides(t, axes):
+    return [int(t.stride(i)) if t.shape[i] > 1 else 0 for i in range(axes)]
+
+
+class CacheSession:
+    """Pool handle + sequence handle of one batch.
+
+    ``pool_t`` is the torch CUDA tensor that holds the pool described by ``geom``.  With
+    ``num_q_heads`` the session attends; ``dtype`` (torch.bfloat16 or torch.float16) is the type
+    of K, V, q and out and defaults to the pool's own.  Scratch is allocated once and kept: calls
+    of one session are meant for one stream at a time (pass ``scratch_t`` for others).
+    ``stream`` None means torch's current stream of the pool's device at each call.
+    """
+
+    def __init__(self, geom, pool_t, seqs: Sequences, *, num_q_heads: int = 0, q_tokens: int = 1, dtype=None,
+                 stream: Optional[int] = None, workspace_t=None):
+        import torch
+
+        self.geom, self.pool_t, self.seqs = geom, pool_t, seqs
+        self.num_q_heads, self.q_tokens, self.stream = num_q_heads, q_tokens, stream
+        self.pool = self.handle = None
+        self._scratch = None
+        if dtype is None:
+            dtype = pool_t.dtype if pool_t.dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("attention takes bfloat16 or float16")
+        if not pool_t.is_contiguous():
+            raise ValueError("the pool tensor has to be contiguous")
+        self.dtype = dtype
+        try:
+            self.pool = B.pdkv_pool_create(B.desc_of(geom), pool_t.data_ptr(), pool_t.numel() * pool_t.element_size(),
+                                           pool_t.device.index or 0)
+            self.handle, self.workspace_bytes = B.pdkv_seqs_create(
+                self.pool, seqs.seq_len, seqs.tbl_off, seqs.tbl, seqs.prefix_len, seqs.prefix_tbl_off, seqs.prefix_tbl,
+                seqs.seq_prefix, num_q_heads, q_tokens if num_q_heads else 0,
+                B.PDKV_DTYPE_BF16 if dtype == torch.bfloat16 else B.PDKV_DTYPE_FP16,
+                workspace_t.data_ptr() if workspace_t is not None else 0,
+                workspace_t.numel() * workspace_t.element_size() if workspace_t is not None else 0,
+                self._on(None))
+            self.workspace_t = workspace_t
+        except Exception:
+            self.close()
+            raise
+
+    def _on(self, stream: Optional[int]) -> int:
+        if stream is not None:
+            return stream
+        if self.stream is not None:
+            return self.stream
+        import torch
+
+        return torch.cuda.current_stream(self.pool_t.device).cuda_stream if self.pool_t.is_cuda else 0
+
+    def _check(self, name, t, dtype, shape):
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != self.pool_t.device:
+            raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {self.pool_t.device}, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def _lens(self, seq_len_t):
+        import torch
+
+        if seq_len_t is None:
+            return 0
+        self._check("seq_len_t", seq_len_t, torch.int32, (self.seqs.n_seq,))
+        if not seq_len_t.is_contiguous():
+            raise ValueError("seq_len_t has to be contiguous")
+        return seq_len_t.data_ptr()
+
+    def _rows(self, name, t, lead, least):
+        """fp32 rows over tokens: shape (*lead, width) with adjacent tokens."""
+        import torch
+
+        if t.dtype != torch.float32 or t.device != self.pool_t.device or tuple(t.shape[:-1]) != tuple(lead) or t.shape[-1] < least:
+            raise ValueError(f"{name}: expected float32 {tuple(lead)} x at least {least} tokens on {self.pool_t.device}, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: tokens have to be adjacent")
+
+    def scratch_bytes(self, with_scores: bool = False) -> int:
+        return B.pdkv_attend_scratch(self.handle, with_scores)
+
+    def attend(self, layer: int, q_t, *, scale: Optional[float] = None, out_t=None, lse_t=None, scores_t=None,
+               scores_in_t=None, seq_len_t=None, scratch_t=None, stream: Optional[int] = None):
+        """Attention of one layer; ``q_t`` is ``[n_seq, q_tokens, num_q_heads, head_dim]`` (any strides with
+        adjacent dims).  Returns ``(out, lse)``.  With ``scores_t`` (float32 ``[n_seq, num_kv_heads, >= longest]``)
+        the attention weights of the own tokens are added to it, or to ``scores_in_t`` and the sums
+        stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device)."""
+        import torch
+
+        shape = (self.seqs.n_seq, self.q_tokens, self.num_q_heads, self.geom.head_dim)
+        self._check("q_t", q_t, self.dtype, shape)
+        if out_t is None:
+            out_t = torch.empty(shape, dtype=self.dtype, device=q_t.device)
+        else:
+            self._check("out_t", out_t, self.dtype, shape)
+        if lse_t is None:
+            lse_t = torch.empty(shape[:3], dtype=torch.float32, device=q_t.device)
+        else:
+            self._check("lse_t", lse_t, torch.float32, shape[:3])
+            if not lse_t.is_contiguous():
+                raise ValueError("lse_t has to be contiguous")
+        for name, t in (("q_t", q_t), ("out_t", out_t)):
+            if t.shape[3] > 1 and t.stride(3) != 1:
+                raise ValueError(f"{name}: the dims of a head have to be adjacent")
+        a = B.pdkv_attend_args()
+        a.q, a.out, a.lse = q_t.data_ptr(), out_t.data_ptr(), lse_t.data_ptr()
+        a.q_stride[:], a.out_stride[:] = _strides(q_t, 3), _strides(out_t, 3)
+        a.scale = self.geom.head_dim ** -0.5 if scale is None else scale
+        a.seq_len = self._lens(seq_len_t)
+        if scores_t is not None:
+            lead = (self.seqs.n_seq, self.geom.num_kv_heads)
+            scores_in_t = scores_t if scores_in_t is None else scores_in_t
+            self._rows("scores_t", scores_t, lead, self.seqs.max_len)
+            self._rows("scores_in_t", scores_in_t, lead, self.seqs.max_len)
+            a.scores_in, a.scores_out = scores_in_t.data_ptr(), scores_t.data_ptr()
+            a.scores_in_stride[:], a.scores_out_stride[:] = _strides(scores_in_t, 2), _strides(scores_t, 2)
+        elif scores_in_t is not None:
+            raise ValueError("scores_in_t needs scores_t to receive the sums")
+        need = self.scratch_bytes(scores_t is not None)
+        if scratch_t is None:
+            if self._scratch is None or self._scratch.numel() < need:
+                self._scratch = torch.empty(max(need, 16), dtype=torch.uint8, device=q_t.device)
+            scratch_t = self._scratch
+        B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), scratch_t.numel() * scratch_t.element_size(),
+                      self._on(stream))
+        return out_t, lse_t
+
+    def evict(self, dst: "CacheSession", scores_t, budget: int, *, sink: int = 0, recent: int = 0,
+              layers: Optional[Tuple[int, int]] = None, kept_t=None, kept_scores_t=None, new_len_t=None, seq_len_t=None,
+              stream: Optional[int] = None):
+        """Keep the ``budget`` heaviest tokens per (layer, sequence, KV head) and move them, in order, to the
+        front of the same sequences in ``dst`` (this session itself: in place).  ``scores_t`` is float32
+        ``[layers, n_seq, num_kv_heads, >= longest]``.  Returns ``(kept, kept_scores, new_len)``."""
+        import torch
+
+        l0, l1 = (0, self.geom.num_layers) if layers is None else layers
+        lead = (l1 - l0, self.seqs.n_seq, self.geom.num_kv_heads)
+        self._rows("scores_t", scores_t, lead, self.seqs.max_len)
+        dev = self.pool_t.device
+        if kept_t is None:
+            kept_t = torch.empty(*lead, budget, dtype=torch.int32, device=dev)
+        else:
+            self._check("kept_t", kept_t, torch.int32, (*lead, budget))
+            if not kept_t.is_contiguous():
+                raise ValueError("kept_t has to be contiguous")
+        if kept_scores_t is None:
+            kept_scores_t = torch.empty(*lead, budget, dtype=torch.float32, device=dev)
+        else:
+            self._rows("kept_scores_t", kept_scores_t, lead, min(budget, self.seqs.max_len))
+        if new_len_t is None:
+            new_len_t = torch.empty(self.seqs.n_seq, dtype=torch.int32, device=dev)
+        a = B.pdkv_evict_args()
+        a.budget, a.sink, a.recent = budget, sink, recent
+        a.seq_len, a.new_len = self._lens(seq_len_t), self._lens(new_len_t)
+        a.scores, a.kept, a.kept_scores = scores_t.data_ptr(), kept_t.data_ptr(), kept_scores_t.data_ptr()
+        a.scores_stride[:], a.kept_scores_stride[:] = _strides(scores_t, 3), _strides(kept_scores_t, 3)
+        a.kept_scores_len = kept_scores_t.shape[-1]
+        B.pdkv_evict(self.handle, dst.handle, l0, l1, a, self._on(stream))
+        return kept_t, kept_scores_t, new_len_t
+
+    def items(self) -> np.ndarray:
+        """The attention work list (``pdkv_attend_item``)."""
+        return B.pdkv_seqs_items(self.handle)
+
+    def close(self) -> None:
+        if self.handle:
+            B.pdkv_seqs_destroy(self.handle)
+            self.handle = None
+        if self.pool:
+            B.pdkv_pool_destroy(self.pool)
+            self.pool = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
