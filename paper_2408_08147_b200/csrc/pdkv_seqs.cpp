@@ -257,7 +257,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                         members.push_back(r);
                     }
             }
-            plan_items(*s, n_rows, 2 * s->sm_count);
+            plan_items(*s, n_rows, pdkv::attend_ctas_per_sm(g.head_dim) * s->sm_count);
             // unit of (row tile 0, head 0) of every segment: units are in the order of the segments
             std::vector<int32_t> unit0(s->segs.size(), -1);
             for (size_t i = 0, u = 0; i < s->segs.size(); ++i) {
@@ -482,6 +482,9 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         }
         p.max_len = s->max_len;
         p.layer = layer;
+        p.block_shift = -1;
+        for (int b = 0; b < 31; ++b)
+            if (s->pool.d.block_tokens == 1 << b) p.block_shift = b;
         pdkv::DeviceGuard guard(s->device);
         if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
         cudaStream_t st = static_cast<cudaStream_t>(stream);

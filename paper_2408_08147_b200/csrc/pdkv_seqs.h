@@ -79,8 +79,10 @@ struct AttnParams {
     int64_t scores_in_stride[2], scores_out_stride[2];
     int32_t max_len;
     int32_t layer;
+    int32_t block_shift;        // log2 of block_tokens, -1: not a power of two
 };
 
+int attend_ctas_per_sm(int head_dim);
 cudaError_t launch_attend(const AttnParams &p, int dtype, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttnParams &p, int dtype, cudaStream_t stream);
 
