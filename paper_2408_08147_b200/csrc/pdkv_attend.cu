@@ -12,10 +12,6 @@ namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
-
 __device__ __forceinline__ int own_len(const AttnParams &p, int seq, int cap)
 {
     if (!p.seq_len) return cap;
@@ -366,6 +362,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const AttnParams p)
 {
     extern __shared__ __align__(128) char smem[];
+    asm volatile("griddepcontrol.launch_dependents;");
     const int end = p.cta_items[blockIdx.x + 1];
     for (int i = p.cta_items[blockIdx.x]; i < end; ++i) {
         const AttnItem it = p.items[i];
@@ -412,21 +409,22 @@ __device__ __forceinline__ int64_t part_at(const Parts &x, int i)
     return i < x.n[0] ? x.first[0] + i * x.step[0] : x.first[1] + (i - x.n[0]) * x.step[1];
 }
 
-// Maximum and sum of a row over all of its parts; whole warp, every lane gets both.
-__device__ __forceinline__ float2 joined_ml(const AttnParams &p, const Parts &x, int lane)
+// Maximum and sum of a row over all of its parts, by W neighbouring lanes; each of them gets both.
+template <int W> __device__ __forceinline__ float2 joined_ml(const AttnParams &p, const Parts &x, int lane)
 {
     const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml);
     float m = -INFINITY, l = 0.f;
-    for (int i = lane; i < x.n[0] + x.n[1]; i += 32) {
+    for (int i = lane % W; i < x.n[0] + x.n[1]; i += W) {
         const float2 v = ml[part_at(x, i)];
         const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
-        l = l * exp2f(m - base) + v.y * exp2f(v.x - base);
+        l = l * pow2(m - base) + v.y * pow2(v.x - base);
         m = top;
     }
-    for (int o = 16; o; o /= 2) {
+#pragma unroll
+    for (int o = W / 2; o; o /= 2) {
         const float m2 = __shfl_xor_sync(~0u, m, o), l2 = __shfl_xor_sync(~0u, l, o);
         const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
-        l = l * exp2f(m - base) + l2 * exp2f(m2 - base);
+        l = l * pow2(m - base) + l2 * pow2(m2 - base);
         m = top;
     }
     return make_float2(m, l);
@@ -437,81 +435,90 @@ constexpr int kScoreRows = 64;     // rows whose lse is held at a time
 
 }  // namespace
 
-// Blocks (sequence, head, 0) join the parts of the rows: m = max m_p, l = sum l_p 2^(m_p - m),
-// O = sum O_p 2^(m_p - m).  Blocks (sequence, head, 1 + c) turn the logits of token chunk c into
-// weights 2^(z - lse) and add them to the scores; they take the lse from the parts themselves, so
-// no block waits for another.
+// The first `row_blocks` blocks of a (sequence, head) join the parts of four rows each, a warp per row:
+// m = max m_p, l = sum l_p 2^(m_p - m), O = sum O_p 2^(m_p - m).  The others turn the logits of a chunk of
+// tokens into weights 2^(z - lse) and add them to the scores; they take the lse from the parts themselves
+// (eight lanes a row), so no block waits for another.
 template <typename T>
-__global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, const int chunks)
+__global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, const int row_blocks, const int chunks)
 {
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int x = blockIdx.x % (1 + chunks), head = blockIdx.x / (1 + chunks) % p.H, seq = blockIdx.x / (1 + chunks) / p.H;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, per = row_blocks + chunks;
+    const int x = blockIdx.x % per, head = blockIdx.x / per % p.H, seq = blockIdx.x / per / p.H;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts are written by the kernel before
     const AttnSeq s = p.seqs[seq];
     const int R = p.G * p.q_tokens;
-    if (x == 0) {
-        if (s.direct) return;
-        for (int row = warp; row < R; row += 4) {
-            const Parts parts = parts_of(p, s, head, row);
-            const float2 ml = joined_ml(p, parts, lane);
-            const float base = ml.x == -INFINITY ? 0.f : ml.x;
-            float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-            for (int i = 0; i < parts.n[0] + parts.n[1]; ++i) {
-                const int64_t at = part_at(parts, i);
-                const float m = p.part_ml[2 * at];
-                if (m == -INFINITY) continue;   // nothing was written for this part
-                const float w = exp2f(m - base);
-                const float4 *o = reinterpret_cast<const float4 *>(p.part_o + at * p.D);
+    if (x < row_blocks) {
+        const int row = 4 * x + warp;
+        if (s.direct || row >= R) return;
+        const Parts parts = parts_of(p, s, head, row);
+        const int n = parts.n[0] + parts.n[1];
+        const float2 ml = joined_ml<32>(p, parts, lane);
+        const float base = ml.x == -INFINITY ? 0.f : ml.x;
+        float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const float w = i0 + lane < n ? pow2(p.part_ml[2 * part_at(parts, i0 + lane)] - base) : 0.f;
+            const int top = min(32, n - i0);
+#pragma unroll 8
+            for (int i = 0; i < top; ++i) {
+                const float wi = __shfl_sync(~0u, w, i);
+                const float4 *o = reinterpret_cast<const float4 *>(p.part_o + part_at(parts, i0 + i) * p.D);
+#pragma unroll
                 for (int k = 0; k < 2; ++k)
                     if (4 * (lane + 32 * k) < p.D) {
                         const float4 v = o[lane + 32 * k];
-                        acc[k].x += w * v.x;
-                        acc[k].y += w * v.y;
-                        acc[k].z += w * v.z;
-                        acc[k].w += w * v.w;
+                        acc[k].x += wi * v.x;
+                        acc[k].y += wi * v.y;
+                        acc[k].z += wi * v.z;
+                        acc[k].w += wi * v.w;
                     }
             }
-            const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
-            const int token = row / p.G, h = head * p.G + row % p.G;
-            T *out = static_cast<T *>(p.out) + seq * p.out_stride[0] + token * p.out_stride[1] + h * p.out_stride[2];
-            for (int k = 0; k < 2; ++k)
-                if (4 * (lane + 32 * k) < p.D) {
-                    T v[4] = {from_float<T>(acc[k].x * inv), from_float<T>(acc[k].y * inv), from_float<T>(acc[k].z * inv),
-                              from_float<T>(acc[k].w * inv)};
-                    *reinterpret_cast<uint2 *>(out + 4 * (lane + 32 * k)) = *reinterpret_cast<uint2 *>(v);
-                }
-            if (p.lse && lane == 0) p.lse[((int64_t)seq * p.q_tokens + token) * p.G * p.H + h] = (ml.x + log2f(ml.y)) * kLn2;
         }
+        const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
+        const int token = row / p.G, h = head * p.G + row % p.G;
+        T *out = static_cast<T *>(p.out) + seq * p.out_stride[0] + token * p.out_stride[1] + h * p.out_stride[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (4 * (lane + 32 * k) < p.D)
+                *reinterpret_cast<uint2 *>(out + 4 * (lane + 32 * k)) =
+                    make_uint2(pack<T>(acc[k].x * inv, acc[k].y * inv), pack<T>(acc[k].z * inv, acc[k].w * inv));
+        if (p.lse && lane == 0) p.lse[((int64_t)seq * p.q_tokens + token) * p.G * p.H + h] = (ml.x + log2f(ml.y)) * kLn2;
         return;
     }
     __shared__ float lse[kScoreRows];
-    const int len = own_len(p, seq, s.len), t0 = (x - 1) * kScoreChunk + 4 * threadIdx.x;
+    const int chunk = x - row_blocks, len = own_len(p, seq, s.len), t0 = chunk * kScoreChunk + 4 * threadIdx.x;
     // past the sequence's end there is no weight: nothing to do in place, else the row is carried over
     const int width = p.scores_in == p.scores_out ? len : p.max_len;
-    if ((x - 1) * kScoreChunk >= width) return;
+    if (chunk * kScoreChunk >= width) return;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < R; r0 += kScoreRows) {
         const int n = min(kScoreRows, R - r0);
         __syncthreads();
-        for (int row = warp; row < n; row += 4) {
-            const float2 ml = joined_ml(p, parts_of(p, s, head, r0 + row), lane);
+        for (int r = warp * 4; r < n; r += 16) {
+            const int row = r + lane / 8;
+            const float2 ml = joined_ml<8>(p, parts_of(p, s, head, r0 + min(row, n - 1)), lane);
             // an empty row gives no weight to anything: 2^(z - inf) = 0
-            if (lane == 0) lse[row] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+            if (lane % 8 == 0 && row < n) lse[row] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
         }
         __syncthreads();
         const float *z = p.logits + s.logits + ((int64_t)head * R + r0) * s.logit_stride + t0;
-        if (t0 < len)
+        if (t0 < len) {
+#pragma unroll 4
             for (int row = 0; row < n; ++row) {
                 const float4 v = *reinterpret_cast<const float4 *>(z + (int64_t)row * s.logit_stride);
-                sum[0] += exp2f(v.x - lse[row]);
-                if (t0 + 1 < len) sum[1] += exp2f(v.y - lse[row]);
-                if (t0 + 2 < len) sum[2] += exp2f(v.z - lse[row]);
-                if (t0 + 3 < len) sum[3] += exp2f(v.w - lse[row]);
+                const float e = lse[row];
+                sum[0] += pow2(v.x - e);
+                sum[1] += pow2(v.y - e);
+                sum[2] += pow2(v.z - e);
+                sum[3] += pow2(v.w - e);
             }
+        }
     }
+#pragma unroll
     for (int k = 0; k < 4; ++k)
         if (t0 + k < width) {
             const float in = p.scores_in ? p.scores_in[seq * p.scores_in_stride[0] + head * p.scores_in_stride[1] + t0 + k] : 0.f;
-            p.scores_out[seq * p.scores_out_stride[0] + head * p.scores_out_stride[1] + t0 + k] = in + sum[k];
+            // (what lies in the scratch behind the last token is no logit)
+            p.scores_out[seq * p.scores_out_stride[0] + head * p.scores_out_stride[1] + t0 + k] = t0 + k < len ? in + sum[k] : in;
         }
 }
 
@@ -556,16 +563,25 @@ cudaError_t launch_attend(const AttnParams &p, int dtype, cudaStream_t stream)
     return dtype == PDKV_DTYPE_BF16 ? launch_type<__nv_bfloat16>(p, stream) : launch_type<__half>(p, stream);
 }
 
-cudaError_t launch_attend_join(const AttnParams &p, int dtype, cudaStream_t stream)
+cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream)
 {
+    const int row_blocks = join ? (p.G * p.q_tokens + 3) / 4 : 0;
     const int chunks = p.logits ? (p.max_len + kScoreChunk - 1) / kScoreChunk : 0;
-    const int64_t blocks = (int64_t)p.n_seq * p.H * (1 + chunks);
+    const int64_t blocks = (int64_t)p.n_seq * p.H * (row_blocks + chunks);
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-    if (dtype == PDKV_DTYPE_BF16)
-        attend_join_kernel<__nv_bfloat16><<<(unsigned)blocks, 128, 0, stream>>>(p, chunks);
-    else
-        attend_join_kernel<__half><<<(unsigned)blocks, 128, 0, stream>>>(p, chunks);
-    return cudaGetLastError();
+    if (blocks == 0) return cudaSuccess;
+    // May be launched before the kernel in front of it has finished; it waits on the device for its results.
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(128);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = p.n_ctas > 0 ? 1 : 0;
+    if (dtype == PDKV_DTYPE_BF16) return cudaLaunchKernelEx(&cfg, attend_join_kernel<__nv_bfloat16>, p, row_blocks, chunks);
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<__half>, p, row_blocks, chunks);
 }
 
 }  // namespace pdkv

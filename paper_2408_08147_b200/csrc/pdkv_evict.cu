@@ -1,4 +1,5 @@
 // Eviction: which tokens of a (layer, sequence, KV head) stay, and the move of their rows.
+#include <algorithm>
 #include <cmath>
 
 #include "pdkv_seqs.h"
@@ -25,133 +26,404 @@ __device__ __forceinline__ uint32_t order_key(float x)
 
 }  // namespace
 
-// One block per (layer, sequence, head): the key of the last token to keep is found bit by bit.
-__global__ void __launch_bounds__(256) evict_select_kernel(const EvictParams p)
-{
-    __shared__ int counts[8];
-    __shared__ int warp_keep[8], warp_tie[8];
-    const int head = blockIdx.x % p.H, seq = blockIdx.x / p.H % p.n_seq, layer = blockIdx.x / p.H / p.n_seq;
-    const int len = own_len(p, seq), lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    int32_t *kept = p.kept + (int64_t)blockIdx.x * p.budget;
-    for (int j = min(len, p.budget) + threadIdx.x; j < p.budget; j += 256) kept[j] = -1;
-    if (len <= p.budget) {
-        for (int j = threadIdx.x; j < len; j += 256) kept[j] = j;
-        return;
-    }
-    const float *row = p.scores + layer * p.scores_stride[0] + seq * p.scores_stride[1] + head * p.scores_stride[2];
-    const int lo = p.sink, hi = len - p.recent, want = p.budget - p.sink - p.recent;
-    auto count = [&](uint32_t at_least) {
-        int n = 0;
-        for (int t = lo + threadIdx.x; t < hi; t += 256) n += order_key(row[t]) >= at_least;
-        for (int o = 16; o; o /= 2) n += __shfl_xor_sync(~0u, n, o);
-        __syncthreads();
-        if (lane == 0) counts[warp] = n;
-        __syncthreads();
-        n = 0;
-        for (int w = 0; w < 8; ++w) n += counts[w];
-        return n;
-    };
-    uint32_t key = 0;   // largest key that at least `want` tokens reach
-    if (want > 0)
-        for (int b = 31; b >= 0; --b)
-            if (count(key | 1u << b) >= want) key |= 1u << b;
-    const int above = want > 0 && key != 0xffffffffu ? count(key + 1) : 0;
-    const int ties = want - above;   // of the tokens at the key itself, the first ones
-    int done = p.sink, tied = 0;
-    for (int j = threadIdx.x; j < p.sink; j += 256) kept[j] = j;
-    for (int t0 = lo; t0 < hi; t0 += 256) {
-        const int t = t0 + threadIdx.x;
-        const uint32_t k = t < hi ? order_key(row[t]) : 0u;
-        const bool over = want > 0 && t < hi && k > key, tie = want > 0 && t < hi && k == key;
-        const unsigned tie_mask = __ballot_sync(~0u, tie);
-        __syncthreads();
-        if (lane == 0) warp_tie[warp] = __popc(tie_mask);
-        __syncthreads();
-        int tie_rank = tied + __popc(tie_mask & ((1u << lane) - 1));
-        for (int w = 0; w < 8; ++w) {
-            if (w < warp) tie_rank += warp_tie[w];
-            tied += warp_tie[w];
-        }
-        const bool keep = over || (tie && tie_rank < ties);
-        const unsigned mask = __ballot_sync(~0u, keep);
-        if (lane == 0) warp_keep[warp] = __popc(mask);
-        __syncthreads();
-        int at = done + __popc(mask & ((1u << lane) - 1));
-        for (int w = 0; w < 8; ++w) {
-            if (w < warp) at += warp_keep[w];
-            done += warp_keep[w];
-        }
-        if (keep) kept[at] = t;
-    }
-    for (int j = threadIdx.x; j < p.recent; j += 256) kept[p.budget - p.recent + j] = hi + j;
-}
-
 namespace {
 
-__device__ __forceinline__ char *row_at(const PoolView &v, const int32_t *tbl, const AttnSeg &seg, int lc, int head, int t)
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectWarps = kSelectThreads / 32;
+constexpr int kMaxKeys = 16;   // keys a thread holds in registers
+
+__device__ __forceinline__ uint32_t cluster_rank()
 {
-    const int64_t blk = tbl[seg.tbl + t / v.block_tokens];
-    return v.base + blk * v.block_stride + lc * v.lc_stride + head * v.head_stride + (int64_t)(t % v.block_tokens) * v.tok_stride;
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// Barrier over the CTAs of the cluster (all of their threads); a cluster of one is the CTA.
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Word `p` of this CTA's shared memory, as CTA `rank` of the cluster holds it.
+__device__ __forceinline__ int peer_word(const int *p, uint32_t rank)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), far;
+    int v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(at), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(far) : "memory");
+    return v;
+}
+
+struct SelectShared {
+    int warp_count[2][kSelectWarps][4];
+    int cta_count[2][4];
+    int warp_over[kSelectWarps], warp_tie[kSelectWarps];
+    int totals[2];
+};
+
+// Token t of a row's middle part is one of the `want` heaviest: kept[at ..) receives them in order.
+// K keys a thread live in registers, read once; K = 0 reads them again in every round.
+template <int K>
+__device__ __forceinline__ void select_row(SelectShared &sh, const float *row, int lo, int hi, int per, int want, int32_t *kept,
+                                           uint32_t rank, uint32_t ranks)
+{
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    // tokens of this warp: a contiguous run of 32 * per, lane by lane
+    const int64_t first = lo + ((int64_t)rank * kSelectWarps + warp) * 32 * per + lane;
+    const int begin = (int)min(first, (int64_t)hi);
+    uint32_t keys[K > 0 ? K : 1];
+    if (K > 0) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) keys[i] = i < per && begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u;
+    }
+    uint32_t key = 0;   // largest value known to be reached by at least `want` keys
+    int reached = hi - lo;
+#pragma unroll 1
+    for (int round = 0; round < 16 && reached != want; ++round) {
+        const int shift = 30 - 2 * round, buf = round & 1;
+        const uint32_t p1 = key | 1u << shift, p2 = key | 2u << shift, p3 = key | 3u << shift;
+        int c1 = 0, c2 = 0, c3 = 0;
+        auto add = [&](uint32_t k) {   // (a missing key is 0 and reaches nothing)
+            c1 += k >= p1;
+            c2 += k >= p2;
+            c3 += k >= p3;
+        };
+        if (K > 0) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) add(keys[i]);
+        } else {
+            for (int i = 0; i < per; ++i) add(begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u);
+        }
+        c1 = __reduce_add_sync(~0u, c1);
+        c2 = __reduce_add_sync(~0u, c2);
+        c3 = __reduce_add_sync(~0u, c3);
+        if (lane == 0) *reinterpret_cast<int4 *>(sh.warp_count[buf][warp]) = make_int4(c1, c2, c3, 0);
+        __syncthreads();
+        const int4 v = *reinterpret_cast<const int4 *>(sh.warp_count[buf][lane]);   // kSelectWarps == 32: a lane each
+        c1 = __reduce_add_sync(~0u, v.x);
+        c2 = __reduce_add_sync(~0u, v.y);
+        c3 = __reduce_add_sync(~0u, v.z);
+        if (ranks > 1) {
+            if (threadIdx.x == 0) {
+                sh.cta_count[buf][0] = c1;
+                sh.cta_count[buf][1] = c2;
+                sh.cta_count[buf][2] = c3;
+            }
+            cluster_barrier();
+            // lane 4 r + i: count i of CTA r
+            const int n = lane % 4 < 3 && lane / 4 < ranks ? peer_word(&sh.cta_count[buf][lane % 4], lane / 4) : 0;
+            c1 = __reduce_add_sync(~0u, lane % 4 == 0 ? n : 0);
+            c2 = __reduce_add_sync(~0u, lane % 4 == 1 ? n : 0);
+            c3 = __reduce_add_sync(~0u, lane % 4 == 2 ? n : 0);
+        }
+        if (c3 >= want) {
+            key = p3;
+            reached = c3;
+        } else if (c2 >= want) {
+            key = p2;
+            reached = c2;
+        } else if (c1 >= want) {
+            key = p1;
+            reached = c1;
+        }
+    }
+    // Either exactly `want` keys reach `key`: all of them stay.  Or `key` is the want-th key itself: of the
+    // keys equal to it those of the lowest tokens stay, as many as are left.
+    const bool all = reached == want;
+    auto each = [&](auto &&f) {   // every lane of the warp takes part
+        if (K > 0) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) f(keys[i], begin + 32 * i, i < per);
+        } else {
+            for (int i = 0; i < per; ++i) f(begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u, begin + 32 * i, true);
+        }
+    };
+    int over = 0, tie = 0;
+    each([&](uint32_t k, int t, bool there) {
+        there = there && t < hi;
+        over += there && (all ? k >= key : k > key);
+        tie += there && !all && k == key;
+    });
+    over = __reduce_add_sync(~0u, over);
+    tie = __reduce_add_sync(~0u, tie);
+    if (lane == 0) {
+        sh.warp_over[warp] = over;
+        sh.warp_tie[warp] = tie;
+    }
+    __syncthreads();
+    {
+        const int o = sh.warp_over[lane], e = sh.warp_tie[lane];
+        over = __reduce_add_sync(~0u, lane < warp ? o : 0);   // from here on: counts before this warp
+        tie = __reduce_add_sync(~0u, lane < warp ? e : 0);
+        const int all_over = __reduce_add_sync(~0u, o), all_tie = __reduce_add_sync(~0u, e);
+        int left = want - all_over;   // of the ties
+        if (ranks > 1) {
+            if (threadIdx.x == 0) {
+                sh.totals[0] = all_over;
+                sh.totals[1] = all_tie;
+            }
+            cluster_barrier();
+            const int o_r = lane < ranks ? peer_word(&sh.totals[0], lane) : 0, e_r = lane < ranks ? peer_word(&sh.totals[1], lane) : 0;
+            over += __reduce_add_sync(~0u, lane < rank ? o_r : 0);
+            tie += __reduce_add_sync(~0u, lane < rank ? e_r : 0);
+            left = want - (int)__reduce_add_sync(~0u, o_r);
+            cluster_barrier();   // nobody leaves while its shared memory is being read
+        }
+        const unsigned below = (1u << lane) - 1;
+        each([&](uint32_t k, int t, bool there) {
+            there = there && t < hi;
+            const bool is_over = there && (all ? k >= key : k > key), is_tie = there && !all && k == key;
+            const unsigned over_mask = __ballot_sync(~0u, is_over), tie_mask = __ballot_sync(~0u, is_tie);
+            const int x = over + __popc(over_mask & below), e = tie + __popc(tie_mask & below);
+            if (is_over || (is_tie && e < left)) kept[x + min(e, left)] = t;
+            over += __popc(over_mask);
+            tie += __popc(tie_mask);
+        });
+    }
 }
 
 }  // namespace
 
-// One block per (layer, sequence, head, K/V) walks the kept tokens in order.  Token kept[j] >= j goes
-// to slot j, so slots written for chunk j hold sources of chunks <= j only: in place it is enough
-// that a chunk is read whole before it is written.
-template <typename V>
-__global__ void __launch_bounds__(256) evict_move_kernel(const EvictParams p)
+// One cluster per (layer, sequence, head): the lightest key that stays is found two bits a round by
+// counting the keys that reach three values, until exactly the wanted number does or all 32 bits are
+// known; then the indices are written in order.  Counting needs two instructions a key and value and
+// no atomics (a histogram in shared memory was 1.5 times slower: scores crowd into few bins);
+// warps add their counts by integer reductions, CTAs of a cluster over distributed shared memory.
+// Every warp owns a contiguous run of tokens, so the order of the indices follows from counts per
+// warp alone.  Bound by the latency of the rounds.
+__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p)
 {
-    const int c = blockIdx.x & 1, stream = blockIdx.x >> 1;
+    __shared__ __align__(16) SelectShared sh;
+    asm volatile("griddepcontrol.launch_dependents;");
+    const uint32_t rank = cluster_rank(), ranks = cluster_size();
+    const int row_id = blockIdx.x / ranks;
+    const int head = row_id % p.H, seq = row_id / p.H % p.n_seq, layer = row_id / p.H / p.n_seq;
+    const int len = own_len(p, seq);
+    int32_t *kept = p.kept + (int64_t)row_id * p.budget;
+    const int first = rank * kSelectThreads + threadIdx.x, step = ranks * kSelectThreads;
+    const int want = p.budget - p.sink - p.recent;
+    for (int j = min(len, p.budget) + first; j < p.budget; j += step) kept[j] = -1;
+    if (len <= p.budget || want == 0) {
+        const int n = min(len, p.budget), head_part = len <= p.budget ? n : p.sink;
+        for (int j = first; j < n; j += step) kept[j] = j < head_part ? j : len - n + j;
+        return;
+    }
+    const int lo = p.sink, hi = len - p.recent;
+    for (int j = first; j < p.sink; j += step) kept[j] = j;
+    for (int j = first; j < p.recent; j += step) kept[p.budget - p.recent + j] = hi + j;
+    const float *row = p.scores + layer * p.scores_stride[0] + seq * p.scores_stride[1] + head * p.scores_stride[2];
+    const int per = (hi - lo + step - 1) / step;
+    kept += p.sink;
+    if (per <= 2)
+        select_row<2>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else if (per <= 4)
+        select_row<4>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else if (per <= 8)
+        select_row<8>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else if (per <= kMaxKeys)
+        select_row<kMaxKeys>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else
+        select_row<0>(sh, row, lo, hi, per, want, kept, rank, ranks);
+}
+
+namespace {
+
+constexpr int kMoveThreads = 128, kMoveWarps = kMoveThreads / 32;
+constexpr int kMoveVecs = 8;      // vectors a lane has in flight
+
+// Vectors of 32 bytes are moved as eight words: one 256-bit access.
+struct Vec32 {
+    uint32_t w[8];
+};
+template <typename V> __device__ __forceinline__ V load_vec(const char *p) { return *reinterpret_cast<const V *>(p); }
+template <> __device__ __forceinline__ Vec32 load_vec<Vec32>(const char *p)
+{
+    Vec32 v;
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]), "=r"(v.w[6]), "=r"(v.w[7])
+                 : "l"(p) : "memory");
+    return v;
+}
+template <typename V> __device__ __forceinline__ void store_vec(char *p, const V &v) { *reinterpret_cast<V *>(p) = v; }
+template <> __device__ __forceinline__ void store_vec<Vec32>(char *p, const Vec32 &v)
+{
+    asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]), "r"(v.w[3]), "r"(v.w[4]),
+                 "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7]), "l"(p) : "memory");
+}
+
+// Kept tokens of a row of indices: they stand before the -1s.  32 probes a round.
+__device__ __forceinline__ int count_kept(const int32_t *kept, int most, int lane)
+{
+    int lo = 0, hi = most;   // kept[lo - 1] >= 0, kept[hi] < 0
+    while (lo < hi) {
+        const int step = (hi - lo + 31) / 32, at = lo + step * lane + step - 1;
+        const bool there = at < hi && kept[at] >= 0;
+        const int n = __popc(__ballot_sync(~0u, there));
+        const int new_lo = lo + n * step;
+        hi = min(hi, new_lo + step - 1);
+        lo = new_lo;
+    }
+    return lo;
+}
+
+}  // namespace
+
+// Moves the kept rows of one (layer, sequence, head, K/V); bound by memory.  A warp moves `rows`
+// consecutive kept rows at a time: lane i looks up where row i lies and goes, the vectors of the
+// rows are dealt to the lanes, all of a lane's loads are issued before its first store, and the next
+// rows are looked up meanwhile.  Nothing is shared between warps.
+//
+// Out of place the steps of a row list are dealt to `parts` blocks.  ORDERED (in place, or scores that
+// are compacted where they stand): token kept[j] >= j goes to slot j, so the slots that rows [a, b)
+// write hold sources of rows < b only.  It is enough that rows are written after all rows up to
+// them were read: the parts are the CTAs of one cluster, all of its warps load consecutive rows, and
+// a barrier stands between their loads and their stores.  Rows that stay where they are are not touched.
+template <typename V, bool ORDERED>
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictParams p, const int parts)
+{
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int part = blockIdx.x % parts, x = blockIdx.x / parts, c = x & 1, stream = x >> 1;
     const int head = stream % p.H, seq = stream / p.H % p.n_seq, layer = stream / p.H / p.n_seq;
     const int32_t *kept = p.kept + (int64_t)stream * p.budget;
     const AttnSeg from = p.src_segs[seq], to = p.dst_segs[seq];
-    const int lc = 2 * (p.layer_begin + layer) + c, vecs = p.row_bytes / (int)sizeof(V);
-    const int top = min(min(p.budget, from.len), to.len);
+    const int vecs = p.row_bytes / (int)sizeof(V);
+    const int most = min(p.budget, from.len);
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the indices are written by the kernel before
+    const int n_kept = p.seq_len ? count_kept(kept, most, lane) : most;
+    const char *src = p.src.base + (2 * (p.layer_begin + layer) + c) * p.src.lc_stride + head * p.src.head_stride;
+    char *dst = p.dst.base + (2 * (p.layer_begin + layer) + c) * p.dst.lc_stride + head * p.dst.head_stride;
     float *scores_to = c == 0 && p.kept_scores
                            ? p.kept_scores + layer * p.kept_scores_stride[0] + seq * p.kept_scores_stride[1] + head * p.kept_scores_stride[2]
                            : nullptr;
     const float *scores = p.scores + layer * p.scores_stride[0] + seq * p.scores_stride[1] + head * p.scores_stride[2];
-    int n_kept = 0;
-    for (int j0 = 0; j0 < top; j0 += 256) {   // scores and the count
-        const int j = j0 + threadIdx.x;
-        const int t = j < top ? kept[j] : -1;
-        float s = 0.f;
-        if (t >= 0 && scores_to) s = scores[t];
-        n_kept += __syncthreads_count(t >= 0);
-        if (t >= 0 && scores_to) scores_to[j] = s;
+    if (p.new_len && x == seq * p.H * 2 && part == 0 && threadIdx.x == 0) p.new_len[seq] = n_kept;
+
+    // rows of a step; a row of more vectors than a warp takes at once is moved in several pieces
+    constexpr int kWarpVecs = 32 * kMoveVecs;
+    const int rows = max(1, min(32, kWarpVecs / vecs)), pieces = (vecs + kWarpVecs - 1) / kWarpVecs;
+    const int64_t warps = (int64_t)parts * kMoveWarps, runs = (n_kept + rows - 1) / rows;
+    const int64_t steps = (runs + warps - 1) / warps * pieces;
+    int64_t next_from = -1, next_to = 0;
+    float next_score = 0.f;
+    int next_j = -1;
+    auto look_up = [&](int64_t step) {
+        const int64_t j = ((step / pieces * parts + part) * kMoveWarps + warp) * rows + lane;
+        next_from = -1;
+        next_j = -1;
+        if (step >= steps || lane >= rows || j >= n_kept) return;
+        const int t = kept[j];
+        const int sb = p.src_shift >= 0 ? t >> p.src_shift : t / p.src.block_tokens;
+        const int db = p.dst_shift >= 0 ? (int)j >> p.dst_shift : (int)j / p.dst.block_tokens;
+        next_to = p.dst_tbl[to.tbl + db] * p.dst.block_stride + ((int)j - db * p.dst.block_tokens) * p.dst.tok_stride;
+        if (!(p.in_place && t == j))
+            next_from = p.src_tbl[from.tbl + sb] * p.src.block_stride + (t - sb * p.src.block_tokens) * p.src.tok_stride;
+        if (scores_to && step % pieces == 0) {
+            next_score = scores[t];
+            next_j = (int)j;
+        }
+    };
+    look_up(0);
+    for (int64_t step = 0; step < steps; ++step) {
+        const int64_t from_at = next_from, to_at = next_to;
+        const float score = next_score;
+        const int score_j = next_j;
+        // vector k of the step: lane + 32 i; row k / vecs
+        const int first = (int)(step % pieces) * kWarpVecs + lane;
+        V v[kMoveVecs];
+        int row = pieces > 1 ? 0 : first / vecs, col = pieces > 1 ? first : first % vecs;
+#pragma unroll
+        for (int i = 0; i < kMoveVecs; ++i) {
+            const int64_t at = __shfl_sync(~0u, from_at, row & 31);
+            if (row < rows && col < vecs && at >= 0) v[i] = load_vec<V>(src + at + col * (int)sizeof(V));
+            col += 32;
+            if (pieces == 1)
+                while (col >= vecs) {
+                    col -= vecs;
+                    ++row;
+                }
+        }
+        look_up(step + 1);
+        if (ORDERED) cluster_barrier();
+        row = pieces > 1 ? 0 : first / vecs, col = pieces > 1 ? first : first % vecs;
+#pragma unroll
+        for (int i = 0; i < kMoveVecs; ++i) {
+            const int64_t at = __shfl_sync(~0u, from_at, row & 31), dat = __shfl_sync(~0u, to_at, row & 31);
+            if (row < rows && col < vecs && at >= 0) store_vec<V>(dst + dat + col * (int)sizeof(V), v[i]);
+            col += 32;
+            if (pieces == 1)
+                while (col >= vecs) {
+                    col -= vecs;
+                    ++row;
+                }
+        }
+        if (score_j >= 0) scores_to[score_j] = score;
     }
-    if (scores_to)
-        for (int j = n_kept + threadIdx.x; j < p.kept_scores_len; j += 256) scores_to[j] = 0.f;
-    if (p.new_len && c == 0 && layer == 0 && head == 0 && threadIdx.x == 0) p.new_len[seq] = n_kept;
-    const int64_t work = (int64_t)n_kept * vecs;
-    for (int64_t i0 = 0; i0 < work; i0 += 256) {
-        const int64_t i = i0 + threadIdx.x;
-        const int j = (int)(i / vecs), at = (int)(i % vecs);
-        V v{};
-        if (i < work) v = reinterpret_cast<const V *>(row_at(p.src, p.src_tbl, from, lc, head, kept[j]))[at];
-        __syncthreads();
-        if (i < work) reinterpret_cast<V *>(row_at(p.dst, p.dst_tbl, to, lc, head, j))[at] = v;
+    if (scores_to) {
+        if (ORDERED) cluster_barrier();
+        for (int j = n_kept + part * kMoveThreads + threadIdx.x; j < p.kept_scores_len; j += parts * kMoveThreads) scores_to[j] = 0.f;
     }
 }
 
+namespace {
+
+template <typename... P, typename... A>
+cudaError_t launch_clusters(void (*kernel)(P...), int64_t rows, int cluster, int threads, bool early, cudaStream_t stream, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * cluster));
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // `early`: the kernel waits for the one before it on the device
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = early ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <typename V> cudaError_t launch_move(const EvictParams &p, int sm_count, cudaStream_t stream)
+{
+    const int64_t streams = 2 * (int64_t)p.n_layers * p.n_seq * p.H;
+    const bool ordered = p.in_place || p.kept_scores == p.scores;
+    const int vecs = p.row_bytes / (int)sizeof(V), rows = std::max(1, std::min(32, 32 * kMoveVecs / vecs)) * kMoveWarps;
+    const int64_t steps = (std::min(p.budget, p.max_len) + rows - 1) / rows;
+    // four blocks for every SM if there are that many steps
+    int64_t parts = 1;
+    const int64_t most = ordered ? 8 : 1 << 16;
+    while (parts * 2 <= most && streams * parts < 4 * sm_count && steps >= 2 * parts) parts *= 2;
+    if (streams * parts > INT32_MAX) return cudaErrorInvalidConfiguration;
+    if (ordered) return launch_clusters(evict_move_kernel<V, true>, streams, (int)parts, kMoveThreads, true, stream, p, (int)parts);
+    return launch_clusters(evict_move_kernel<V, false>, streams * parts, 1, kMoveThreads, true, stream, p, (int)parts);
+}
+
+}  // namespace
+
 cudaError_t launch_evict(const EvictParams &p, int sm_count, cudaStream_t stream)
 {
-    (void)sm_count;
     const int64_t rows = (int64_t)p.n_layers * p.n_seq * p.H;
-    if (2 * rows > INT32_MAX) return cudaErrorInvalidConfiguration;
-    evict_select_kernel<<<(unsigned)rows, 256, 0, stream>>>(p);
-    cudaError_t e = cudaGetLastError();
+    // CTAs per row: one while its keys fit the registers and the rows alone fill the GPU
+    int cluster = 1;
+    while (cluster < 8 && (p.max_len > cluster * kSelectThreads * kMaxKeys || (rows * cluster < 2 * sm_count && p.max_len > cluster * 2048)))
+        cluster *= 2;
+    if (rows * cluster > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const cudaError_t e = launch_clusters(evict_select_kernel, rows, cluster, kSelectThreads, false, stream, p);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)(2 * rows);
     switch (p.vec_bytes) {
-    case 16: evict_move_kernel<uint4><<<grid, 256, 0, stream>>>(p); break;
-    case 8: evict_move_kernel<uint2><<<grid, 256, 0, stream>>>(p); break;
-    case 4: evict_move_kernel<uint32_t><<<grid, 256, 0, stream>>>(p); break;
-    case 2: evict_move_kernel<uint16_t><<<grid, 256, 0, stream>>>(p); break;
-    default: evict_move_kernel<uint8_t><<<grid, 256, 0, stream>>>(p); break;
+    case 32: return launch_move<Vec32>(p, sm_count, stream);
+    case 16: return launch_move<uint4>(p, sm_count, stream);
+    case 8: return launch_move<uint2>(p, sm_count, stream);
+    case 4: return launch_move<uint32_t>(p, sm_count, stream);
+    case 2: return launch_move<uint16_t>(p, sm_count, stream);
+    default: return launch_move<uint8_t>(p, sm_count, stream);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace pdkv

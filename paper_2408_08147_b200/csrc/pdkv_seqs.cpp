@@ -51,6 +51,13 @@ bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
 
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+int32_t log2_of(int32_t n)
+{
+    for (int b = 0; b < 31; ++b)
+        if (n == 1 << b) return b;
+    return -1;
+}
+
 // Do rows of `len` entries at i0*s0 + i1*s1 + i2*s2 lie apart from one another?  Axes of one entry do
 // not count; the others have to nest (each stride spans everything inside it).
 bool rows_apart(int64_t len, const int64_t *stride, const int64_t *n, int axes)
@@ -482,9 +489,7 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         }
         p.max_len = s->max_len;
         p.layer = layer;
-        p.block_shift = -1;
-        for (int b = 0; b < 31; ++b)
-            if (s->pool.d.block_tokens == 1 << b) p.block_shift = b;
+        p.block_shift = log2_of(s->pool.d.block_tokens);
         pdkv::DeviceGuard guard(s->device);
         if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
         cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -493,7 +498,7 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention kernel launch");
         }
         if (s->join || scores) {
-            const cudaError_t e = pdkv::launch_attend_join(p, s->dtype, st);
+            const cudaError_t e = pdkv::launch_attend_join(p, s->dtype, s->join, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "join kernel launch");
         }
         return PDKV_OK;
@@ -567,8 +572,10 @@ int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int laye
                 p.kept_scores_stride[i] = n[i] > 1 ? a->kept_scores_stride[i] : 0;
             }
             p.max_len = s->max_len;
-            p.vec_bytes = 16;
+            p.vec_bytes = aligned(p.src.base, 32) && aligned(p.dst.base, 32) ? 32 : 16;
             while (p.vec_bytes > 1 && p.row_bytes % p.vec_bytes) p.vec_bytes /= 2;
+            p.src_shift = log2_of(x.block_tokens);
+            p.dst_shift = log2_of(y.block_tokens);
             pdkv::DeviceGuard guard(s->device);
             if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
             const cudaError_t e = pdkv::launch_evict(p, s->sm_count, static_cast<cudaStream_t>(stream));

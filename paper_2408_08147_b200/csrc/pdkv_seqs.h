@@ -84,7 +84,7 @@ struct AttnParams {
 
 int attend_ctas_per_sm(int head_dim);
 cudaError_t launch_attend(const AttnParams &p, int dtype, cudaStream_t stream);
-cudaError_t launch_attend_join(const AttnParams &p, int dtype, cudaStream_t stream);
+cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream);
 
 struct EvictParams {
     PoolView src, dst;
@@ -104,6 +104,7 @@ struct EvictParams {
     int32_t *new_len;
     int32_t max_len;       // longest sequence of the handle
     int32_t vec_bytes;     // alignment every row of both pools has
+    int32_t src_shift, dst_shift;   // log2 of block_tokens, -1: not a power of two
 };
 cudaError_t launch_evict(const EvictParams &p, int sm_count, cudaStream_t stream);
 

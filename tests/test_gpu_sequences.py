@@ -352,6 +352,8 @@ EVICT = [
     dict(lens=[90, 33], budget=30, E=8, D=80, src=(BLOCK_MAJOR, 1), dst=(BLOCK_MAJOR, 16)),
     dict(lens=[90, 33], budget=30, E=2, D=128, H=5),
     dict(lens=[5000, 9000], budget=2049, recent=7, H=1, layers=1),
+    dict(lens=[140001], budget=70000, sink=1, recent=3, H=1, layers=1, D=4, src=(LAYER_MAJOR, 128), dst=(LAYER_MAJOR, 64)),
+    dict(lens=[20, 50], budget=40, H=1, layers=2, D=9000, E=2),
     dict(lens=[40001], budget=12345, sink=1, recent=3, H=1, layers=1, D=8, src=(LAYER_MAJOR, 128), dst=(LAYER_MAJOR, 64)),
 ]
 
