@@ -46,7 +46,7 @@ EXPORTS = (
     "pdkv_plan_autotune", "pdkv_plan_shape", "pdkv_plan_set_shape", "pdkv_plan_launch_shape", "pdkv_plan_option",
     "pdkv_sm_partition_create", "pdkv_sm_partition_info", "pdkv_sm_partition_stream", "pdkv_sm_partition_destroy",
     "pdkv_transfer_copies",
-    "pdkv_seqs_create", "pdkv_seqs_destroy", "pdkv_seqs_items", "pdkv_attend_scratch", "pdkv_attend", "pdkv_evict",
+    "pdkv_seqs_create", "pdkv_seqs_destroy", "pdkv_seqs_items", "pdkv_seqs_status", "pdkv_attend_scratch", "pdkv_attend", "pdkv_evict",
 )
 
 
@@ -163,6 +163,7 @@ def lib() -> C.CDLL:
     L.pdkv_seqs_create.argtypes = [vp, C.POINTER(pdkv_seqs_desc), vp, C.c_size_t, C.POINTER(C.c_size_t), vp, C.POINTER(vp)]
     L.pdkv_seqs_destroy.argtypes = [vp]
     L.pdkv_seqs_items.argtypes = [vp, C.POINTER(vp), C.POINTER(i64)]
+    L.pdkv_seqs_status.argtypes = [vp, vp]
     L.pdkv_attend_scratch.argtypes = [vp, C.c_int, C.POINTER(C.c_size_t)]
     L.pdkv_attend.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), vp, C.c_size_t, vp]
     L.pdkv_evict.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(pdkv_evict_args), vp]
@@ -492,6 +493,10 @@ def pdkv_seqs_items(seqs: int) -> np.ndarray:
     return np.frombuffer(C.string_at(p, n.value * ITEM_DTYPE.itemsize), ITEM_DTYPE).copy()
 
 
+def pdkv_seqs_status(seqs: int, stream: int = 0) -> None:
+    _check(lib().pdkv_seqs_status(seqs, stream), "pdkv_seqs_status")
+
+
 def pdkv_attend_scratch(seqs: int, with_scores: bool) -> int:
     n = C.c_size_t()
     _check(lib().pdkv_attend_scratch(C.c_void_p(seqs), int(with_scores), C.byref(n)), "pdkv_attend_scratch")
@@ -499,8 +504,7 @@ def pdkv_attend_scratch(seqs: int, with_scores: bool) -> int:
 
 
 def pdkv_attend(seqs: int, layer: int, args: pdkv_attend_args, scratch_ptr: int, scratch_bytes: int, stream: int = 0) -> None:
-    _check(lib().pdkv_attend(C.c_void_p(seqs), layer, C.byref(args), C.c_void_p(scratch_ptr), scratch_bytes,
-                             C.c_void_p(stream)), "pdkv_attend")
+    _check(lib().pdkv_attend(seqs, layer, C.byref(args), scratch_ptr, scratch_bytes, stream), "pdkv_attend")
 
 
 def pdkv_evict(seqs: int, dst: int, layer_begin: int, layer_end: int, args: pdkv_evict_args, stream: int = 0) -> None:

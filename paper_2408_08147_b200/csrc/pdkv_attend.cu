@@ -1,44 +1,9 @@
 // Attention of a batch's newest tokens over a paged pool, and the join of its parts.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <cmath>
 
-#include "pdkv_seqs.h"
+#include "pdkv_attend_device.cuh"
 
 namespace pdkv {
-
-namespace {
-
-constexpr float kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ int own_len(const AttnParams &p, int seq, int cap)
-{
-    if (!p.seq_len) return cap;
-    const int n = p.seq_len[seq];
-    return n < 0 ? 0 : (n < cap ? n : cap);
-}
-
-struct RowId {
-    int seq, token, g;
-};
-// Row `row` of a segment: which query token of which sequence, and which of the G heads.
-__device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnSeg &seg, int row)
-{
-    const int R = p.G * p.q_tokens;
-    RowId id;
-    if (seg.seq >= 0) {
-        id.seq = seg.seq;
-    } else {
-        id.seq = p.members[seg.member_begin + row / R];
-        row %= R;
-    }
-    id.token = row / p.G;
-    id.g = row % p.G;
-    return id;
-}
-
-}  // namespace
 
 namespace {
 
@@ -56,8 +21,6 @@ template <int DP> struct Ring {
     static constexpr int kBytes = kSlices * kSliceBytes;
     static constexpr int kCtas = DP <= 128 ? 2 : 1;
 };
-
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 // 16 bytes to shared memory; with `there` false zeros are written and nothing is read.
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool there)
@@ -90,26 +53,6 @@ __device__ __forceinline__ void multiply<__half>(float (&c)[4], const uint32_t (
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
-// 2^x, off by 2 units in the last place at most; 0 for -infinity.
-__device__ __forceinline__ float pow2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 template <int N> __device__ __forceinline__ void group_sync(int id)
 {
     if (N == 32)
@@ -524,18 +467,6 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
 
 namespace {
 
-// The opt-in to more than 48 KB of shared memory is per kernel and device.
-template <typename K> cudaError_t allow_shared(K kernel, int bytes, std::atomic<uint64_t> &devices)
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 64 && (devices.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess && dev < 64) devices.fetch_or(1ull << dev, std::memory_order_release);
-    return e;
-}
-
 template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
@@ -579,7 +510,7 @@ cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaSt
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = p.n_ctas > 0 ? 1 : 0;
+    cfg.numAttrs = p.n_ctas > 0 || p.n_tile_ctas > 0 ? 1 : 0;
     if (dtype == PDKV_DTYPE_BF16) return cudaLaunchKernelEx(&cfg, attend_join_kernel<__nv_bfloat16>, p, row_blocks, chunks);
     return cudaLaunchKernelEx(&cfg, attend_join_kernel<__half>, p, row_blocks, chunks);
 }

@@ -1,0 +1,76 @@
+// Device code shared by the attention kernels.
+#pragma once
+
+#include <atomic>
+#include <cmath>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pdkv_seqs.h"
+
+namespace pdkv {
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ int own_len(const AttnParams &p, int seq, int cap)
+{
+    if (!p.seq_len) return cap;
+    const int n = p.seq_len[seq];
+    return n < 0 ? 0 : (n < cap ? n : cap);
+}
+
+struct RowId {
+    int seq, token, g;
+};
+// Row `row` of a segment: which query token of which sequence, and which of the G heads.
+__device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnSeg &seg, int row)
+{
+    const int R = p.G * p.q_tokens;
+    RowId id;
+    if (seg.seq >= 0) {
+        id.seq = seg.seq;
+    } else {
+        id.seq = p.members[seg.member_begin + row / R];
+        row %= R;
+    }
+    id.token = row / p.G;
+    id.g = row % p.G;
+    return id;
+}
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// 2^x, off by 2 units in the last place at most; 0 for -infinity.
+__device__ __forceinline__ float pow2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The opt-in to more than 48 KB of shared memory is per kernel and device.
+template <typename K> inline cudaError_t allow_shared(K kernel, int bytes, std::atomic<uint64_t> &devices)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (devices.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) devices.fetch_or(1ull << dev, std::memory_order_release);
+    return e;
+}
+
+}  // namespace pdkv

@@ -1,0 +1,573 @@
+// Attention of many rows over one list of cached tokens -- the queries of all sequences behind a shared
+// prefix, or a window of query tokens over its own sequence -- on the fifth-generation tensor cores.
+//
+// A CTA holds up to 256 rows (two tiles of 128) of one KV head and runs over tiles of 128 tokens:
+//     S = Q K^T      tcgen05.mma, both operands in shared memory, S in tensor memory (128 columns a tile)
+//     P = 2^(S - m)  one thread a row, rounded to 16 bits and written over S
+//     O += P V       tcgen05.mma, P from tensor memory, O stays in tensor memory
+// Two row tiles take turns: while the threads of one turn S into P, the tensor cores work for the
+// other, and both use the same K and V, which halves what is read from L2.  Ten warps: four per row
+// tile for the softmax, one that issues the matrix instructions, one that issues the loads (TMA boxes of one
+// page, 64 dims and the 128-byte swizzle that the matrix instructions expect).
+//
+// O is rescaled only when a row's maximum grew by more than 2^8 since the last time: the weights stay below
+// 2^8, where 16-bit and 32-bit floating point lose nothing.  Maxima and sums are 32 bits, the sums taken
+// before the weights are rounded.
+#include <type_traits>
+
+#include <cuda.h>
+
+#include "pdkv_attend_device.cuh"
+
+namespace pdkv {
+
+namespace {
+
+constexpr int kTileRows = 128, kTileTokens = 128;
+constexpr int kSoftmaxThreads = 128;                          // of one row tile
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kTileThreads = 320;
+constexpr uint64_t kWaitNs = 1000000000;                     // a wait gives up after a second
+constexpr float kGrowth = 8.f;                                // log2 of how far a maximum may run ahead of its base
+
+// Tensor memory columns: S (and P over it) of tile t, O of tile t.
+constexpr uint32_t kColS = 0, kColO = 256, kColTile = 128, kColumns = 512;
+
+template <int DP> struct TileShape {
+    static constexpr int kSubs = DP / 64;                     // 64 dims: one swizzled row of 128 bytes
+    static constexpr uint32_t kSub = 128 * 128;               // bytes of 128 such rows
+    static constexpr uint32_t kOperand = kSubs * kSub;        // one tile of Q, K or V
+    static constexpr int kSlots = DP == 64 ? 8 : 4;           // K and V tiles in flight, in turns
+    static constexpr uint32_t kBytes = 2 * kOperand + kSlots * kOperand + 1024;
+};
+
+struct Barriers {
+    uint64_t full[8], empty[8];     // ring of K and V tiles
+    uint64_t q_ready[2];            // Q of a row tile is in shared memory
+    uint64_t s_full[2];             // S of a row tile is complete
+    uint64_t p_ready[2];            // P of a row tile is in tensor memory
+    uint64_t o_full[2];             // the last product of a row tile is complete
+    uint32_t tmem;
+};
+
+__device__ __forceinline__ void mbar_init(uint64_t *b, int count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t *b)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint64_t *b, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint64_t *b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t nanoseconds()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+// Bounded wait.  A thread that gives up records it and waits for nothing any more: every role then runs
+// through to the end of its list without touching memory for the results.
+__device__ __forceinline__ void mbar_wait(uint64_t *b, uint32_t parity, bool &dead, unsigned long long *status)
+{
+    if (dead || mbar_try(b, parity)) return;
+    const uint64_t start = nanoseconds();
+    while (!mbar_try(b, parity))
+        if (nanoseconds() - start > kWaitNs) {
+            dead = true;
+            atomicExch(status, 1ull);
+            return;
+        }
+}
+
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_load(float (&v)[32], uint32_t at)
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+        "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store32(uint32_t at, const float (&v)[32])
+{
+    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+        "%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
+        "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
+        "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory operand in the 128-byte swizzle: 8-row groups 1024 bytes apart.  K-major (Q, K: a row is 64
+// dims of one token): the leading offset is not used.  MN-major (V: a row is 64 dims, tokens run along
+// the product): the leading offset leads to the next 64 dims.
+__device__ __forceinline__ uint64_t operand(uint32_t smem, uint32_t leading)
+{
+    uint64_t d = (smem >> 4) & 0x3fff;
+    d |= (uint64_t)((leading >> 4) & 0x3fff) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= 1ull << 46;   // descriptor version of sm_100
+    d |= 2ull << 61;   // 128-byte swizzle
+    return d;
+}
+// Instruction word: 32-bit accumulator, A and B of one 16-bit type, M = 128.
+template <typename T> __device__ constexpr uint32_t instruction(int n, bool b_mn_major)
+{
+    const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return 1u << 4 | type << 7 | type << 10 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24;
+}
+__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t word, bool add)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(word), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t word, bool add)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b),
+                 "r"(word), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t *b)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5,%6}], [%7];" ::"r"(to),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_u32(bar)) : "memory");
+}
+
+// What every role has to know about an item.
+struct Work {
+    AttnItem it;
+    AttnSeg seg;
+    int len, limit, tiles, row_tiles;
+};
+__device__ __forceinline__ Work work_of(const AttnParams &p, int i)
+{
+    Work w;
+    w.it = p.tile_items[i];
+    w.seg = p.segs[w.it.seg];
+    w.len = w.seg.seq >= 0 ? own_len(p, w.seg.seq, w.seg.len) : w.seg.len;
+    w.limit = min(w.it.tok1, w.len);
+    w.tiles = w.limit > w.it.tok0 ? (w.limit - w.it.tok0 + kTileTokens - 1) / kTileTokens : 0;
+    w.row_tiles = w.it.rows > kTileRows ? 2 : 1;
+    return w;
+}
+
+}  // namespace
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p)
+{
+    using G = TileShape<DP>;
+    extern __shared__ char raw[];
+    __shared__ Barriers bar;
+    char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
+    const uint32_t q_at = smem_u32(smem), ring_at = q_at + 2 * G::kOperand;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < G::kSlots; ++i) {
+            mbar_init(&bar.full[i], 1);
+            mbar_init(&bar.empty[i], 1);
+        }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&bar.q_ready[t], kSoftmaxThreads);
+            mbar_init(&bar.s_full[t], 1);
+            mbar_init(&bar.p_ready[t], kSoftmaxThreads);
+            mbar_init(&bar.o_full[t], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    asm volatile("griddepcontrol.launch_dependents;");
+    const uint32_t tmem = bar.tmem;
+    const int first = p.cta_tile_items[blockIdx.x], end = p.cta_tile_items[blockIdx.x + 1];
+    bool dead = false;
+
+    if (warp == kLoadWarp) {
+        // K(0), V(0), K(1), V(1) ... into the ring; a lane loads a page (or its 128 tokens)
+        const int page_rows = min(p.pool.block_tokens, kTileTokens);
+        uint32_t n = 0;
+        for (int i = first; i < end; ++i) {
+            const Work w = work_of(p, i);
+            for (int j = 0; j < w.tiles; ++j) {
+                const int t0 = w.it.tok0 + j * kTileTokens, live = min(kTileTokens, w.limit - t0);
+                const int boxes = (live + page_rows - 1) / page_rows;   // pages past the end are not loaded
+                int block = 0, tt = 0;
+                if (lane < boxes) {
+                    const int t = t0 + lane * page_rows;
+                    block = p.tbl[w.seg.tbl + t / p.pool.block_tokens];
+                    tt = t % p.pool.block_tokens;
+                }
+                for (int kv = 0; kv < 2; ++kv, ++n) {
+                    const int slot = n % G::kSlots;
+                    mbar_wait(&bar.empty[slot], (n / G::kSlots & 1) ^ 1, dead, p.status);
+                    dead = __any_sync(~0u, dead);
+                    if (dead) continue;
+                    if (lane == 0) mbar_expect(&bar.full[slot], (uint32_t)boxes * page_rows * 128 * G::kSubs);
+                    __syncwarp();
+                    if (lane < boxes) {
+                        const uint32_t to = ring_at + slot * G::kOperand + lane * page_rows * 128;
+                        const int lc = 2 * p.layer + kv;
+#pragma unroll
+                        for (int s = 0; s < G::kSubs; ++s) {
+                            if (p.map_layer_major)
+                                load_box(to + s * G::kSub, &map, 64 * s, tt, w.it.head, block, lc, &bar.full[slot]);
+                            else
+                                load_box(to + s * G::kSub, &map, 64 * s, w.it.head, tt, lc, block, &bar.full[slot]);
+                        }
+                    }
+                }
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        if (lane == 0) {
+            constexpr uint32_t kWordS = instruction<T>(kTileTokens, false), kWordO = instruction<T>(DP, true);
+            uint32_t n = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+            auto product_s = [&](int t, uint32_t k_slot) {   // S(t) = Q(t) K^T
+                const uint32_t q = q_at + t * G::kOperand, k = ring_at + k_slot * G::kOperand;
+#pragma unroll
+                for (int s = 0; s < DP / 16; ++s) {
+                    const uint32_t o = s / 4 * G::kSub + s % 4 * 32;
+                    mma_shared(tmem + kColS + t * kColTile, operand(q + o, 16), operand(k + o, 16), kWordS, s > 0);
+                }
+            };
+            auto product_o = [&](int t, uint32_t v_slot, bool add) {   // O(t) += P(t) V
+                const uint32_t v = ring_at + v_slot * G::kOperand;
+#pragma unroll
+                for (int s = 0; s < kTileTokens / 16; ++s)
+                    mma_tensor(tmem + kColO + t * kColTile, tmem + kColS + t * kColTile + 8 * s, operand(v + s * 2048, G::kSub), kWordO, add || s > 0);
+            };
+            for (int i = first; i < end; ++i) {
+                const Work w = work_of(p, i);
+                if (w.tiles == 0) continue;
+                uint32_t k_slot = n % G::kSlots;
+                mbar_wait(&bar.full[k_slot], n / G::kSlots & 1, dead, p.status);
+                for (int t = 0; t < w.row_tiles; ++t) {
+                    mbar_wait(&bar.q_ready[t], q_phase[t], dead, p.status);
+                    q_phase[t] ^= 1;
+                    fence_after();
+                    if (!dead) product_s(t, k_slot);
+                    commit(&bar.s_full[t]);
+                }
+                commit(&bar.empty[k_slot]);
+                for (int j = 0; j < w.tiles; ++j, n += 2) {
+                    const uint32_t v_slot = (n + 1) % G::kSlots;
+                    const bool last = j + 1 == w.tiles;
+                    mbar_wait(&bar.full[v_slot], (n + 1) / G::kSlots & 1, dead, p.status);
+                    for (int t = 0; t < w.row_tiles; ++t) {
+                        mbar_wait(&bar.p_ready[t], p_phase[t], dead, p.status);
+                        p_phase[t] ^= 1;
+                        fence_after();
+                        if (!dead) product_o(t, v_slot, j > 0);
+                        if (last) {
+                            commit(&bar.o_full[t]);
+                        } else {
+                            if (t == 0) {
+                                k_slot = (n + 2) % G::kSlots;
+                                mbar_wait(&bar.full[k_slot], (n + 2) / G::kSlots & 1, dead, p.status);
+                                fence_after();
+                            }
+                            if (!dead) product_s(t, k_slot);
+                            commit(&bar.s_full[t]);
+                        }
+                    }
+                    commit(&bar.empty[v_slot]);
+                    if (!last) commit(&bar.empty[k_slot]);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // softmax of row tile t: one thread a row
+        const int t = warp / 4, r = threadIdx.x % kSoftmaxThreads;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const uint32_t s_at = tmem + lanes + kColS + t * kColTile, o_at = tmem + lanes + kColO + t * kColTile;
+        const float scale = fabsf(p.scale_log2);
+        const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
+        uint32_t s_phase = 0, o_phase = 0, n = 0;
+        int q_of = -1;
+        auto load_q = [&](const Work &w) {
+            const int row = t * kTileRows + r;
+            const bool live = row < w.it.rows;
+            const RowId id = row_id(p, w.seg, w.it.row0 + (live ? row : 0));
+            const T *q = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2];
+#pragma unroll
+            for (int c = 0; c < DP / 8; ++c) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (live && 8 * c < p.D) {
+                    v = *reinterpret_cast<const uint4 *>(q + 8 * c);
+                    v.x ^= flip;
+                    v.y ^= flip;
+                    v.z ^= flip;
+                    v.w ^= flip;
+                }
+                *reinterpret_cast<uint4 *>(smem + t * G::kOperand + c / 8 * G::kSub + r * 128 + ((c % 8) ^ (r % 8)) * 16) = v;
+            }
+            fence_async_smem();
+            mbar_arrive(&bar.q_ready[t]);
+        };
+        for (int i = first; i < end; ++i) {
+            const Work w = work_of(p, i);
+            const uint32_t n0 = n;
+            n += 2 * w.tiles;
+            if (t >= w.row_tiles) continue;
+            const int row = t * kTileRows + r;
+            const bool live = row < w.it.rows, own = w.seg.seq >= 0;
+            const RowId id = row_id(p, w.seg, w.it.row0 + (live ? row : 0));
+            float m = -INFINITY, l = 0.f;
+            if (w.tiles > 0) {
+                if (q_of != i) load_q(w);
+                const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;
+                const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
+                float *logits = nullptr;
+                if (p.logits && own && live) {
+                    const AttnSeq s = p.seqs[w.seg.seq];
+                    logits = p.logits + s.logits + ((int64_t)w.it.head * p.G * p.q_tokens + w.it.row0 + row) * s.logit_stride;
+                }
+                for (int j = 0; j < w.tiles; ++j) {
+                    const int t0 = w.it.tok0 + j * kTileTokens;
+                    const bool masked = t0 + kTileTokens > safe;
+                    mbar_wait(&bar.s_full[t], s_phase, dead, p.status);
+                    s_phase ^= 1;
+                    __syncwarp();
+                    fence_after();
+                    if (t == 0 && t0 + kTileTokens > w.limit) {
+                        // rows of V past the end may hold anything, and 0 * NaN is NaN: they become zero
+                        const uint32_t v = n0 + 2 * j + 1;
+                        mbar_wait(&bar.full[v % G::kSlots], v / G::kSlots & 1, dead, p.status);
+                        if (t0 + r >= w.limit) {
+                            char *zero = smem + 2 * G::kOperand + v % G::kSlots * G::kOperand + r * 128;
+#pragma unroll
+                            for (int s = 0; s < G::kSubs; ++s)
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4 *>(zero + s * G::kSub + c * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                    }
+                    float v[32], top = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_load(v, s_at + 32 * c);
+                        tmem_load_wait();
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (t0 + 32 * c + k < sees) top = fmaxf(top, v[k]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) top = fmaxf(top, v[k]);
+                        }
+                    }
+                    top = top == -INFINITY ? top : top * scale;
+                    if (__any_sync(~0u, top > m + kGrowth || (m == -INFINITY && top > m))) {
+                        const float new_m = fmaxf(m, top), f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
+                        l *= f;
+                        m = new_m;
+                        if (j > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < DP / 32; ++c) {
+                                tmem_load(v, o_at + 32 * c);
+                                tmem_load_wait();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) v[k] *= f;
+                                tmem_store32(o_at + 32 * c, v);
+                            }
+                            tmem_store_wait();
+                        }
+                    }
+                    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_load(v, s_at + 32 * c);
+                        tmem_load_wait();
+                        if (logits) {
+                            const int tc = t0 + 32 * c;
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4)
+                                if (tc + k < w.limit) {
+                                    float4 z;
+                                    z.x = tc + k < sees ? v[k] * scale : -INFINITY;
+                                    z.y = tc + k + 1 < sees ? v[k + 1] * scale : -INFINITY;
+                                    z.z = tc + k + 2 < sees ? v[k + 2] * scale : -INFINITY;
+                                    z.w = tc + k + 3 < sees ? v[k + 3] * scale : -INFINITY;
+                                    *reinterpret_cast<float4 *>(logits + tc + k) = z;
+                                }
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = pow2(fmaf(v[k], scale, -base));
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (t0 + 32 * c + k >= sees) v[k] = 0.f;
+                        }
+                        float sum = 0.f;
+                        uint32_t packed[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            sum += v[2 * k] + v[2 * k + 1];
+                            packed[k] = pack<T>(v[2 * k], v[2 * k + 1]);
+                        }
+                        l += sum;
+                        __syncwarp();
+                        tmem_store16(s_at + 16 * c, packed);
+                    }
+                    tmem_store_wait();
+                    fence_before();
+                    mbar_arrive(&bar.p_ready[t]);
+                }
+                // every product with Q is done: the next item's Q may take its place
+                if (i + 1 < end) {
+                    const Work next = work_of(p, i + 1);
+                    if (t < next.row_tiles && next.tiles > 0) {
+                        load_q(next);
+                        q_of = i + 1;
+                    }
+                }
+                mbar_wait(&bar.o_full[t], o_phase, dead, p.status);
+                o_phase ^= 1;
+                __syncwarp();
+                fence_after();
+            }
+            const int head = w.it.head * p.G + id.g;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            T *out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2];
+#pragma unroll 1
+            for (int c = 0; c < DP / 32; ++c) {
+                float v[32];
+                __syncwarp();
+                if (w.tiles > 0) {
+                    tmem_load(v, o_at + 32 * c);
+                    tmem_load_wait();
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = 0.f;
+                }
+                if (!live || dead) {
+                    // nothing to write
+                } else if (w.it.direct) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8)
+                        if (32 * c + k < p.D) {
+                            uint4 x;
+                            x.x = pack<T>(v[k] * inv, v[k + 1] * inv);
+                            x.y = pack<T>(v[k + 2] * inv, v[k + 3] * inv);
+                            x.z = pack<T>(v[k + 4] * inv, v[k + 5] * inv);
+                            x.w = pack<T>(v[k + 6] * inv, v[k + 7] * inv);
+                            *reinterpret_cast<uint4 *>(out + 32 * c + k) = x;
+                        }
+                } else {
+                    float *o = p.part_o + (w.it.part_row + row) * p.D + 32 * c;
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        if (32 * c + k < p.D) *reinterpret_cast<float4 *>(o + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                }
+            }
+            if (live && !dead) {
+                if (w.it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (m + log2f(l)) * kLn2;
+                if (!w.it.direct || p.logits) *reinterpret_cast<float2 *>(p.part_ml + 2 * (w.it.part_row + row)) = make_float2(m, l);
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns));
+    }
+}
+
+namespace {
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+{
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = allow_shared(attend_tile_kernel<T, DP>, (int)TileShape<DP>::kBytes, ready);
+    if (e != cudaSuccess) return e;
+    attend_tile_kernel<T, DP><<<p.n_tile_ctas, kTileThreads, TileShape<DP>::kBytes, stream>>>(map, p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+// Rows of 64 to 128 dims, and pages that whole tiles consist of or that consist of whole tiles.
+bool attend_tile_supported(const pdkv_pool_desc &d)
+{
+    const int B = d.block_tokens;
+    return d.elem_bytes == 2 && d.head_dim >= 64 && d.head_dim <= 128 && d.head_dim % 8 == 0 &&
+           (B >= kTileTokens ? B % kTileTokens == 0 : B >= 8 && kTileTokens % B == 0) && d.num_blocks <= 0x7fffffff;
+}
+
+bool make_attend_map(const pdkv_pool &pool, void *out)
+{
+    static_assert(sizeof(CUtensorMap) <= kMapBytes, "a handle's space for the map");
+    void *sym = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    const pdkv_pool_desc &d = pool.d;
+    const PoolView v = pool_view(pool);
+    const cuuint64_t H = d.num_kv_heads, B = d.block_tokens, D = d.head_dim, NB = d.num_blocks, LC = 2 * (cuuint64_t)d.num_layers;
+    const cuuint32_t rows = (cuuint32_t)(d.block_tokens < kTileTokens ? d.block_tokens : kTileTokens), ones[5] = {1, 1, 1, 1, 1};
+    const bool layer_major = d.layout == PDKV_LAYOUT_LAYER_MAJOR;
+    // block-major: (dim, head, token, layer and K/V, block); layer-major: (dim, token, head, block, layer and K/V)
+    const cuuint64_t dims_b[5] = {D, H, B, LC, NB}, dims_l[5] = {D, B, H, NB, LC};
+    const cuuint64_t strides_b[4] = {(cuuint64_t)v.head_stride, (cuuint64_t)v.tok_stride, (cuuint64_t)v.lc_stride, (cuuint64_t)v.block_stride};
+    const cuuint64_t strides_l[4] = {(cuuint64_t)v.tok_stride, (cuuint64_t)v.head_stride, (cuuint64_t)v.block_stride, (cuuint64_t)v.lc_stride};
+    const cuuint32_t box_b[5] = {64, 1, rows, 1, 1}, box_l[5] = {64, rows, 1, 1, 1};
+    const cuuint64_t *strides = layer_major ? strides_l : strides_b;
+    for (int i = 0; i < 4; ++i)
+        if (strides[i] >= 1ull << 40) return false;
+    return reinterpret_cast<EncodeTiled>(sym)(static_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, pool.base, layer_major ? dims_l : dims_b, strides,
+                                              layer_major ? box_l : box_b, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream)
+{
+    const CUtensorMap &m = *static_cast<const CUtensorMap *>(map);
+    if (dtype == PDKV_DTYPE_BF16)
+        return p.D <= 64 ? launch_dims<__nv_bfloat16, 64>(p, m, stream) : launch_dims<__nv_bfloat16, 128>(p, m, stream);
+    return p.D <= 64 ? launch_dims<__half, 64>(p, m, stream) : launch_dims<__half, 128>(p, m, stream);
+}
+
+}  // namespace pdkv

@@ -41,7 +41,7 @@ using pdkv::AttnSeq;
 using pdkv::AttnUnit;
 
 constexpr int kMaxRowTile = 64;    // rows of one work item
-constexpr int64_t kQuantum = 64;   // tokens; work is cut along the tokens in multiples of this
+constexpr int kTileMinRows = 48;   // rows from which the tile kernel takes a segment
 
 bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
 {
@@ -101,11 +101,22 @@ int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int3
     return PDKV_OK;
 }
 
-int row_tile(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile; }
+// Which kernel takes a segment, and how its rows are cut.  0, the warp kernel: 16 to 64 rows an item.
+// 1, the tile kernel: up to 256 rows an item.
+struct Shape {
+    int kernel, row_tile;
+    int64_t quantum;      // tokens; work is cut along the tokens in multiples of this
+};
+Shape shape_of(int64_t rows, bool tile_ok)
+{
+    if (tile_ok && rows >= kTileMinRows) return {1, 256, 128};
+    return {0, rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile, 64};
+}
 
-// Work list.  Units (segment, row tile, head) lie behind one another on an axis of cost -- token quanta
-// plus a constant for the start and the end of a unit -- and the CTAs take equal stretches of it.
-void plan_items(pdkv_seqs &s, const std::vector<int32_t> &n_rows, int n_ctas_max)
+// Work list of one kernel.  Units (segment, row tile, head) lie behind one another on an axis of cost -- token
+// quanta plus a constant for the start and the end of a unit -- and the CTAs take equal stretches of it.
+void plan_items(pdkv_seqs &s, int kernel, const std::vector<int32_t> &n_rows, const std::vector<Shape> &shape, std::vector<int32_t> &unit0,
+                int n_ctas_max)
 {
     struct Work { int32_t seg, head, row0, rows; int64_t quanta; };
     std::vector<Work> work;
@@ -114,32 +125,33 @@ void plan_items(pdkv_seqs &s, const std::vector<int32_t> &n_rows, int n_ctas_max
     int64_t total = 0;
     for (size_t g = 0; g < s.segs.size(); ++g) {
         const AttnSeg &seg = s.segs[g];
-        if (seg.len == 0 || n_rows[g] == 0) continue;
-        const int tile = row_tile(n_rows[g]);
-        for (int32_t r0 = 0; r0 < n_rows[g]; r0 += tile)
+        if (shape[g].kernel != kernel || seg.len == 0 || n_rows[g] == 0) continue;
+        unit0[g] = (int32_t)(s.units.size() + work.size());
+        for (int32_t r0 = 0; r0 < n_rows[g]; r0 += shape[g].row_tile)
             for (int32_t h = 0; h < H; ++h) {
-                work.push_back({(int32_t)g, h, r0, std::min<int32_t>(tile, n_rows[g] - r0), (seg.len + kQuantum - 1) / kQuantum});
+                work.push_back({(int32_t)g, h, r0, std::min<int32_t>(shape[g].row_tile, n_rows[g] - r0),
+                                (seg.len + shape[g].quantum - 1) / shape[g].quantum});
                 total += work.back().quanta + kOverhead;
             }
     }
-    s.units.resize(work.size());
-    s.cta_items.assign(1, 0);
+    std::vector<AttnItem> &items = s.items[kernel];
+    std::vector<int32_t> &cta_items = s.cta_items[kernel];
+    cta_items.assign(1, 0);
     if (work.empty()) return;
     // a CTA gets at least four quanta, so that joining the parts stays cheap beside reading the tokens
     const int64_t n_ctas = std::max<int64_t>(1, std::min<int64_t>(n_ctas_max, total / 4));
     int64_t at = 0, cta = 0;
-    for (size_t u = 0; u < work.size(); ++u) {
-        const Work &w = work[u];
-        AttnUnit &unit = s.units[u];
+    for (const Work &w : work) {
+        const int64_t quantum = shape[(size_t)w.seg].quantum;
+        AttnUnit unit{};
         unit.part_row = s.part_rows;
         unit.rows = w.rows;
-        unit.n_parts = 0;
         int64_t q = 0;
         while (q < w.quanta) {
-            // `at` is where quantum q of this unit lies; this CTA's stretch ends at end
+            // `at` is where quantum q of this unit lies; this CTA's stretch ends at (cta + 1) * total / n_ctas
             while (cta + 1 < n_ctas && at + kOverhead >= (cta + 1) * total / n_ctas) {
                 ++cta;
-                s.cta_items.push_back((int32_t)s.items.size());
+                cta_items.push_back((int32_t)items.size());
             }
             int64_t n = w.quanta - q;
             if (cta + 1 < n_ctas) n = std::min(n, (cta + 1) * total / n_ctas - at);
@@ -150,9 +162,9 @@ void plan_items(pdkv_seqs &s, const std::vector<int32_t> &n_rows, int n_ctas_max
             it.head = w.head;
             it.row0 = w.row0;
             it.rows = w.rows;
-            it.tok0 = (int32_t)(q * kQuantum);
-            it.tok1 = (int32_t)std::min<int64_t>(s.segs[w.seg].len, (q + n) * kQuantum);
-            s.items.push_back(it);
+            it.tok0 = (int32_t)(q * quantum);
+            it.tok1 = (int32_t)std::min<int64_t>(s.segs[(size_t)w.seg].len, (q + n) * quantum);
+            items.push_back(it);
             pdkv_attend_item li{};
             li.prefix = w.seg >= s.n_seq ? w.seg - s.n_seq : -1;
             li.seq = w.seg < s.n_seq ? w.seg : -1;
@@ -161,7 +173,7 @@ void plan_items(pdkv_seqs &s, const std::vector<int32_t> &n_rows, int n_ctas_max
             li.row_end = w.row0 + w.rows;
             li.tok_begin = it.tok0;
             li.tok_end = it.tok1;
-            li.kernel = 0;
+            li.kernel = kernel;
             li.cta = (int32_t)cta;
             s.listing.push_back(li);
             s.part_rows += w.rows;
@@ -169,10 +181,11 @@ void plan_items(pdkv_seqs &s, const std::vector<int32_t> &n_rows, int n_ctas_max
             q += n;
             at += n;
         }
+        s.units.push_back(unit);
         at += kOverhead;
     }
-    while ((int64_t)s.cta_items.size() < n_ctas) s.cta_items.push_back((int32_t)s.items.size());
-    s.cta_items.push_back((int32_t)s.items.size());
+    while ((int64_t)cta_items.size() < n_ctas) cta_items.push_back((int32_t)items.size());
+    cta_items.push_back((int32_t)items.size());
 }
 
 }  // namespace
@@ -264,24 +277,23 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                         members.push_back(r);
                     }
             }
-            plan_items(*s, n_rows, pdkv::attend_ctas_per_sm(g.head_dim) * s->sm_count);
-            // unit of (row tile 0, head 0) of every segment: units are in the order of the segments
+            bool tile_ok = pdkv::attend_tile_supported(g);
+            if (tile_ok && !pdkv::tunables().dry_run) tile_ok = pdkv::make_attend_map(*pool, s->map);
+            std::vector<Shape> shape;
+            for (int32_t n : n_rows) shape.push_back(shape_of(n, tile_ok));
+            // unit of (row tile 0, head 0) of every segment
             std::vector<int32_t> unit0(s->segs.size(), -1);
-            for (size_t i = 0, u = 0; i < s->segs.size(); ++i) {
-                if (s->segs[i].len == 0 || n_rows[i] == 0) continue;
-                unit0[i] = (int32_t)u;
-                const int t = row_tile(n_rows[i]);
-                u += (size_t)((n_rows[i] + t - 1) / t) * (size_t)g.num_kv_heads;
-            }
+            plan_items(*s, 1, n_rows, shape, unit0, s->sm_count);
+            plan_items(*s, 0, n_rows, shape, unit0, pdkv::attend_ctas_per_sm(g.head_dim) * s->sm_count);
             s->seqs.resize((size_t)s->n_seq);
             for (int32_t r = 0; r < s->n_seq; ++r) {
                 AttnSeq &q = s->seqs[(size_t)r];
                 q.len = s->len[(size_t)r];
                 q.own_unit = unit0[(size_t)r];
-                q.own_tile = row_tile(R);
+                q.own_tile = shape[(size_t)r].row_tile;
                 const int32_t p = d->n_prefix > 0 ? d->seq_prefix[r] : -1;
                 q.prefix_unit = p >= 0 ? unit0[(size_t)(s->n_seq + p)] : -1;
-                q.prefix_tile = p >= 0 ? row_tile(n_rows[(size_t)(s->n_seq + p)]) : 1;
+                q.prefix_tile = p >= 0 ? shape[(size_t)(s->n_seq + p)].row_tile : 1;
                 q.prefix_row0 = row0[(size_t)r];
                 q.logit_stride = (q.len + 3) / 4 * 4;
                 q.logits = s->logit_floats;
@@ -294,7 +306,8 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                 }
                 if (!q.direct) s->join = true;
             }
-            for (AttnItem &it : s->items) it.direct = it.seg < s->n_seq && s->seqs[(size_t)it.seg].direct;
+            for (std::vector<AttnItem> &list : s->items)
+                for (AttnItem &it : list) it.direct = it.seg < s->n_seq && s->seqs[(size_t)it.seg].direct;
         }
 
         // device arrays: one block, each list 16-byte aligned
@@ -304,10 +317,10 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             bytes += (n + 15) / 16 * 16;
             return o;
         };
-        const size_t o_tbl = place(tbl.size() * 4), o_members = place(members.size() * 4), o_cta = place(s->cta_items.size() * 4),
-                     o_segs = place(s->segs.size() * sizeof(AttnSeg)), o_units = place(s->units.size() * sizeof(AttnUnit)),
-                     o_seqs = place(s->seqs.size() * sizeof(AttnSeq)), o_items = place(s->items.size() * sizeof(AttnItem));
-        bytes = std::max<size_t>(bytes, 16);
+        const size_t o_status = place(16), o_tbl = place(tbl.size() * 4), o_members = place(members.size() * 4),
+                     o_cta[2] = {place(s->cta_items[0].size() * 4), place(s->cta_items[1].size() * 4)}, o_segs = place(s->segs.size() * sizeof(AttnSeg)), o_units = place(s->units.size() * sizeof(AttnUnit)),
+                     o_seqs = place(s->seqs.size() * sizeof(AttnSeq)),
+                     o_items[2] = {place(s->items[0].size() * sizeof(AttnItem)), place(s->items[1].size() * sizeof(AttnItem))};
         if (needed_bytes) *needed_bytes = bytes;
         if (workspace && workspace_bytes < bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
         if (!pdkv::tunables().dry_run) {
@@ -315,11 +328,13 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             auto put = [&](size_t o, const void *p, size_t n) { if (n) memcpy(image.data() + o, p, n); };
             put(o_tbl, tbl.data(), tbl.size() * 4);
             put(o_members, members.data(), members.size() * 4);
-            put(o_cta, s->cta_items.data(), s->cta_items.size() * 4);
+            for (int k = 0; k < 2; ++k) {
+                put(o_cta[k], s->cta_items[k].data(), s->cta_items[k].size() * 4);
+                put(o_items[k], s->items[k].data(), s->items[k].size() * sizeof(AttnItem));
+            }
             put(o_segs, s->segs.data(), s->segs.size() * sizeof(AttnSeg));
             put(o_units, s->units.data(), s->units.size() * sizeof(AttnUnit));
             put(o_seqs, s->seqs.data(), s->seqs.size() * sizeof(AttnSeq));
-            put(o_items, s->items.data(), s->items.size() * sizeof(AttnItem));
             pdkv::DeviceGuard guard(s->device);
             if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
             if (workspace) {
@@ -336,14 +351,17 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             cudaError_t e = cudaMemcpyAsync(s->dev_mem, image.data(), bytes, cudaMemcpyHostToDevice, st);
             if (e == cudaSuccess) e = cudaStreamSynchronize(st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaMemcpyAsync");
-            const char *b = static_cast<const char *>(s->dev_mem);
+            char *b = static_cast<char *>(s->dev_mem);
+            s->d_status = reinterpret_cast<unsigned long long *>(b + o_status);
             s->d_tbl = reinterpret_cast<const int32_t *>(b + o_tbl);
             s->d_members = reinterpret_cast<const int32_t *>(b + o_members);
-            s->d_cta_items = reinterpret_cast<const int32_t *>(b + o_cta);
+            for (int k = 0; k < 2; ++k) {
+                s->d_cta_items[k] = reinterpret_cast<const int32_t *>(b + o_cta[k]);
+                s->d_items[k] = reinterpret_cast<const AttnItem *>(b + o_items[k]);
+            }
             s->d_segs = reinterpret_cast<const AttnSeg *>(b + o_segs);
             s->d_units = reinterpret_cast<const AttnUnit *>(b + o_units);
             s->d_seqs = reinterpret_cast<const AttnSeq *>(b + o_seqs);
-            s->d_items = reinterpret_cast<const AttnItem *>(b + o_items);
         }
         hold.s = nullptr;
         *out = s;
@@ -366,6 +384,19 @@ int pdkv_seqs_destroy(pdkv_seqs *s)
     }
     delete s;
     return rc;
+}
+
+int pdkv_seqs_status(const pdkv_seqs *s, void *stream)
+{
+    if (!s || !s->dev_mem) return PDKV_ERR_INVALID_ARG;
+    pdkv::DeviceGuard guard(s->device);
+    if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
+    unsigned long long v = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaMemcpyAsync(&v, s->d_status, sizeof v, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaMemcpyAsync");
+    return v ? PDKV_ERR_DEVICE_BOUNDS : PDKV_OK;
 }
 
 int pdkv_seqs_items(const pdkv_seqs *s, const pdkv_attend_item **items, int64_t *n_items)
@@ -458,9 +489,14 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         p.units = s->d_units;
         p.seqs = s->d_seqs;
         p.members = s->d_members;
-        p.items = s->d_items;
-        p.cta_items = s->d_cta_items;
-        p.n_ctas = (int32_t)s->cta_items.size() - 1;
+        p.items = s->d_items[0];
+        p.cta_items = s->d_cta_items[0];
+        p.n_ctas = (int32_t)s->cta_items[0].size() - 1;
+        p.tile_items = s->d_items[1];
+        p.cta_tile_items = s->d_cta_items[1];
+        p.n_tile_ctas = (int32_t)s->cta_items[1].size() - 1;
+        p.map_layer_major = s->pool.d.layout == PDKV_LAYOUT_LAYER_MAJOR;
+        p.status = s->d_status;
         p.n_seq = s->n_seq;
         p.H = s->pool.d.num_kv_heads;
         p.G = s->G;
@@ -493,6 +529,10 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         pdkv::DeviceGuard guard(s->device);
         if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
         cudaStream_t st = static_cast<cudaStream_t>(stream);
+        if (p.n_tile_ctas > 0) {
+            const cudaError_t e = pdkv::launch_attend_tile(p, s->map, s->dtype, st);
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention tile kernel launch");
+        }
         if (p.n_ctas > 0) {
             const cudaError_t e = pdkv::launch_attend(p, s->dtype, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention kernel launch");

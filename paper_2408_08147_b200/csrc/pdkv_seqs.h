@@ -64,6 +64,11 @@ struct AttnParams {
     const AttnItem *items;
     const int32_t *cta_items;   // [n_ctas + 1] first item of each CTA
     int32_t n_ctas;
+    const AttnItem *tile_items;      // the same for the tile kernel
+    const int32_t *cta_tile_items;
+    int32_t n_tile_ctas;
+    int32_t map_layer_major;         // order of the coordinates of the pool's tensor map
+    unsigned long long *status;      // [0] != 0: a bounded wait gave up
     int32_t n_seq, H, G, D, q_tokens;
     const void *q;
     void *out;
@@ -84,6 +89,11 @@ struct AttnParams {
 
 int attend_ctas_per_sm(int head_dim);
 cudaError_t launch_attend(const AttnParams &p, int dtype, cudaStream_t stream);
+// The tile kernel (tcgen05): segments with many rows.  `map` is a CUtensorMap of the pool.
+constexpr int kMapBytes = 128;
+bool attend_tile_supported(const pdkv_pool_desc &d);
+bool make_attend_map(const pdkv_pool &pool, void *out);
+cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream);
 
 struct EvictParams {
@@ -123,17 +133,19 @@ struct pdkv_seqs {
     std::vector<pdkv::AttnSeg> segs;
     std::vector<pdkv::AttnUnit> units;
     std::vector<pdkv::AttnSeq> seqs;
-    std::vector<pdkv::AttnItem> items;
-    std::vector<int32_t> cta_items;
+    std::vector<pdkv::AttnItem> items[2];      // warp kernel, tile kernel
+    std::vector<int32_t> cta_items[2];
+    alignas(64) char map[pdkv::kMapBytes] = {};   // tensor map of the pool, for the tile kernel
     std::vector<pdkv_attend_item> listing;
     int64_t part_rows = 0, logit_floats = 0;
     bool join = false;           // some rows have several parts, or none
     // device arrays
     void *dev_mem = nullptr;
     bool owns_dev_mem = true;
-    const int32_t *d_tbl = nullptr, *d_members = nullptr, *d_cta_items = nullptr;
+    unsigned long long *d_status = nullptr;
+    const int32_t *d_tbl = nullptr, *d_members = nullptr, *d_cta_items[2] = {nullptr, nullptr};
     const pdkv::AttnSeg *d_segs = nullptr;
     const pdkv::AttnUnit *d_units = nullptr;
     const pdkv::AttnSeq *d_seqs = nullptr;
-    const pdkv::AttnItem *d_items = nullptr;
+    const pdkv::AttnItem *d_items[2] = {nullptr, nullptr};
 };

@@ -17,8 +17,11 @@ from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
+import torch
 
 from . import binding as B
+
+_DTYPES = {torch.bfloat16: B.PDKV_DTYPE_BF16, torch.float16: B.PDKV_DTYPE_FP16}
 
 
 @dataclass
@@ -63,10 +66,6 @@ class Sequences:
         return int(self.seq_len.max()) if self.n_seq else 0
 
 
-def _strides(t, axes):
-    return [int(t.stride(i)) if t.shape[i] > 1 else 0 for i in range(axes)]
-
-
 class CacheSession:
     """Pool handle + sequence handle of one batch.
 
@@ -79,15 +78,13 @@ class CacheSession:
 
     def __init__(self, geom, pool_t, seqs: Sequences, *, num_q_heads: int = 0, q_tokens: int = 1, dtype=None,
                  stream: Optional[int] = None, workspace_t=None):
-        import torch
-
         self.geom, self.pool_t, self.seqs = geom, pool_t, seqs
         self.num_q_heads, self.q_tokens, self.stream = num_q_heads, q_tokens, stream
         self.pool = self.handle = None
-        self._scratch = None
+        self._scratch = [None, None]   # without and with scores; never replaced, recorded graphs may hold them
         if dtype is None:
-            dtype = pool_t.dtype if pool_t.dtype in (torch.bfloat16, torch.float16) else torch.bfloat16
-        if dtype not in (torch.bfloat16, torch.float16):
+            dtype = pool_t.dtype if pool_t.dtype in _DTYPES else torch.bfloat16
+        if dtype not in _DTYPES:
             raise ValueError("attention takes bfloat16 or float16")
         if not pool_t.is_contiguous():
             raise ValueError("the pool tensor has to be contiguous")
@@ -98,11 +95,16 @@ class CacheSession:
             self.handle, self.workspace_bytes = B.pdkv_seqs_create(
                 self.pool, seqs.seq_len, seqs.tbl_off, seqs.tbl, seqs.prefix_len, seqs.prefix_tbl_off, seqs.prefix_tbl,
                 seqs.seq_prefix, num_q_heads, q_tokens if num_q_heads else 0,
-                B.PDKV_DTYPE_BF16 if dtype == torch.bfloat16 else B.PDKV_DTYPE_FP16,
+                _DTYPES[dtype],
                 workspace_t.data_ptr() if workspace_t is not None else 0,
                 workspace_t.numel() * workspace_t.element_size() if workspace_t is not None else 0,
                 self._on(None))
             self.workspace_t = workspace_t
+            self._need = [B.pdkv_attend_scratch(self.handle, w) if num_q_heads else 0 for w in (False, True)]
+            self._shape = (seqs.n_seq, q_tokens, num_q_heads, geom.head_dim)
+            self._max_len = seqs.max_len
+            self._scale = geom.head_dim ** -0.5
+            self._device = pool_t.device
         except Exception:
             self.close()
             raise
@@ -112,18 +114,14 @@ class CacheSession:
             return stream
         if self.stream is not None:
             return self.stream
-        import torch
-
         return torch.cuda.current_stream(self.pool_t.device).cuda_stream if self.pool_t.is_cuda else 0
 
     def _check(self, name, t, dtype, shape):
-        if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != self.pool_t.device:
-            raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {self.pool_t.device}, "
+        if t.dtype != dtype or t.shape != shape or t.device != self._device:
+            raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {self._device}, "
                              f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def _lens(self, seq_len_t):
-        import torch
-
         if seq_len_t is None:
             return 0
         self._check("seq_len_t", seq_len_t, torch.int32, (self.seqs.n_seq,))
@@ -133,8 +131,6 @@ class CacheSession:
 
     def _rows(self, name, t, lead, least):
         """fp32 rows over tokens: shape (*lead, width) with adjacent tokens."""
-        import torch
-
         if t.dtype != torch.float32 or t.device != self.pool_t.device or tuple(t.shape[:-1]) != tuple(lead) or t.shape[-1] < least:
             raise ValueError(f"{name}: expected float32 {tuple(lead)} x at least {least} tokens on {self.pool_t.device}, "
                              f"got {t.dtype} {tuple(t.shape)} on {t.device}")
@@ -142,7 +138,7 @@ class CacheSession:
             raise ValueError(f"{name}: tokens have to be adjacent")
 
     def scratch_bytes(self, with_scores: bool = False) -> int:
-        return B.pdkv_attend_scratch(self.handle, with_scores)
+        return self._need[bool(with_scores)]
 
     def attend(self, layer: int, q_t, *, scale: Optional[float] = None, out_t=None, lse_t=None, scores_t=None,
                scores_in_t=None, seq_len_t=None, scratch_t=None, stream: Optional[int] = None):
@@ -150,42 +146,39 @@ class CacheSession:
         adjacent dims).  Returns ``(out, lse)``.  With ``scores_t`` (float32 ``[n_seq, num_kv_heads, >= longest]``)
         the attention weights of the own tokens are added to it, or to ``scores_in_t`` and the sums
         stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device)."""
-        import torch
-
-        shape = (self.seqs.n_seq, self.q_tokens, self.num_q_heads, self.geom.head_dim)
+        shape = self._shape
         self._check("q_t", q_t, self.dtype, shape)
         if out_t is None:
-            out_t = torch.empty(shape, dtype=self.dtype, device=q_t.device)
+            out_t = torch.empty(shape, dtype=self.dtype, device=self._device)
         else:
             self._check("out_t", out_t, self.dtype, shape)
         if lse_t is None:
-            lse_t = torch.empty(shape[:3], dtype=torch.float32, device=q_t.device)
+            lse_t = torch.empty(shape[:3], dtype=torch.float32, device=self._device)
         else:
             self._check("lse_t", lse_t, torch.float32, shape[:3])
             if not lse_t.is_contiguous():
                 raise ValueError("lse_t has to be contiguous")
-        for name, t in (("q_t", q_t), ("out_t", out_t)):
-            if t.shape[3] > 1 and t.stride(3) != 1:
-                raise ValueError(f"{name}: the dims of a head have to be adjacent")
-        a = B.pdkv_attend_args()
-        a.q, a.out, a.lse = q_t.data_ptr(), out_t.data_ptr(), lse_t.data_ptr()
-        a.q_stride[:], a.out_stride[:] = _strides(q_t, 3), _strides(out_t, 3)
-        a.scale = self.geom.head_dim ** -0.5 if scale is None else scale
-        a.seq_len = self._lens(seq_len_t)
+        q_stride, out_stride = q_t.stride(), out_t.stride()
+        if shape[3] > 1 and (q_stride[3] != 1 or out_stride[3] != 1):
+            raise ValueError("q_t, out_t: the dims of a head have to be adjacent")
+        a = B.pdkv_attend_args(q=q_t.data_ptr(), q_stride=q_stride[:3], out=out_t.data_ptr(), out_stride=out_stride[:3],
+                               lse=lse_t.data_ptr(), scale=self._scale if scale is None else scale)
+        if seq_len_t is not None:
+            a.seq_len = self._lens(seq_len_t)
         if scores_t is not None:
-            lead = (self.seqs.n_seq, self.geom.num_kv_heads)
+            lead = (shape[0], self.geom.num_kv_heads)
             scores_in_t = scores_t if scores_in_t is None else scores_in_t
-            self._rows("scores_t", scores_t, lead, self.seqs.max_len)
-            self._rows("scores_in_t", scores_in_t, lead, self.seqs.max_len)
+            self._rows("scores_t", scores_t, lead, self._max_len)
+            self._rows("scores_in_t", scores_in_t, lead, self._max_len)
             a.scores_in, a.scores_out = scores_in_t.data_ptr(), scores_t.data_ptr()
-            a.scores_in_stride[:], a.scores_out_stride[:] = _strides(scores_in_t, 2), _strides(scores_t, 2)
+            a.scores_in_stride, a.scores_out_stride = scores_in_t.stride()[:2], scores_t.stride()[:2]
         elif scores_in_t is not None:
             raise ValueError("scores_in_t needs scores_t to receive the sums")
-        need = self.scratch_bytes(scores_t is not None)
         if scratch_t is None:
-            if self._scratch is None or self._scratch.numel() < need:
-                self._scratch = torch.empty(max(need, 16), dtype=torch.uint8, device=q_t.device)
-            scratch_t = self._scratch
+            which = scores_t is not None
+            scratch_t = self._scratch[which]
+            if scratch_t is None:
+                scratch_t = self._scratch[which] = torch.empty(max(self._need[which], 16), dtype=torch.uint8, device=self._device)
         B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), scratch_t.numel() * scratch_t.element_size(),
                       self._on(stream))
         return out_t, lse_t
@@ -196,12 +189,10 @@ class CacheSession:
         """Keep the ``budget`` heaviest tokens per (layer, sequence, KV head) and move them, in order, to the
         front of the same sequences in ``dst`` (this session itself: in place).  ``scores_t`` is float32
         ``[layers, n_seq, num_kv_heads, >= longest]``.  Returns ``(kept, kept_scores, new_len)``."""
-        import torch
-
         l0, l1 = (0, self.geom.num_layers) if layers is None else layers
         lead = (l1 - l0, self.seqs.n_seq, self.geom.num_kv_heads)
         self._rows("scores_t", scores_t, lead, self.seqs.max_len)
-        dev = self.pool_t.device
+        dev = self._device
         if kept_t is None:
             kept_t = torch.empty(*lead, budget, dtype=torch.int32, device=dev)
         else:
@@ -214,18 +205,20 @@ class CacheSession:
             self._rows("kept_scores_t", kept_scores_t, lead, min(budget, self.seqs.max_len))
         if new_len_t is None:
             new_len_t = torch.empty(self.seqs.n_seq, dtype=torch.int32, device=dev)
-        a = B.pdkv_evict_args()
-        a.budget, a.sink, a.recent = budget, sink, recent
-        a.seq_len, a.new_len = self._lens(seq_len_t), self._lens(new_len_t)
-        a.scores, a.kept, a.kept_scores = scores_t.data_ptr(), kept_t.data_ptr(), kept_scores_t.data_ptr()
-        a.scores_stride[:], a.kept_scores_stride[:] = _strides(scores_t, 3), _strides(kept_scores_t, 3)
-        a.kept_scores_len = kept_scores_t.shape[-1]
+        a = B.pdkv_evict_args(budget=budget, sink=sink, recent=recent, seq_len=self._lens(seq_len_t), scores=scores_t.data_ptr(),
+                              scores_stride=scores_t.stride()[:3], kept=kept_t.data_ptr(), kept_scores=kept_scores_t.data_ptr(),
+                              kept_scores_stride=kept_scores_t.stride()[:3], kept_scores_len=kept_scores_t.shape[-1],
+                              new_len=self._lens(new_len_t))
         B.pdkv_evict(self.handle, dst.handle, l0, l1, a, self._on(stream))
         return kept_t, kept_scores_t, new_len_t
 
     def items(self) -> np.ndarray:
         """The attention work list (``pdkv_attend_item``)."""
         return B.pdkv_seqs_items(self.handle)
+
+    def status(self, stream: Optional[int] = None) -> None:
+        """Wait for the session's stream and raise if a kernel reported an error."""
+        B.pdkv_seqs_status(self.handle, self._on(stream))
 
     def close(self) -> None:
         if self.handle:

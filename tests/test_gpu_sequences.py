@@ -123,6 +123,13 @@ CASES = [
     dict(lens=[5] * 17, prefix_len=[129, 64], member=[i % 2 for i in range(17)], H=1, G=8, D=64, block=32, layout=LAYER_MAJOR),
     dict(lens=[3] * 70, prefix_len=[515], member=[0] * 70, H=1, G=4, D=128, block=128, layout=LAYER_MAJOR),
     dict(lens=[0] * 9, prefix_len=[70], member=[0] * 9, H=2, G=8, D=128),
+    dict(lens=[2] * 20, prefix_len=[385, 1, 128], member=[i % 3 for i in range(20)], H=2, G=8, D=80, block=8),
+    dict(lens=[9] * 33, prefix_len=[700], member=[0] * 33, H=1, G=8, D=96, block=256, layout=LAYER_MAJOR, dtype="fp16"),
+    dict(lens=[9] * 33, prefix_len=[257], member=[0] * 33, H=3, G=2, D=72, block=64, q_scale=12.0),
+    dict(lens=[1, 500, 40, 0], H=2, G=6, Q=30, D=128, block=32),
+    dict(lens=[700], H=1, G=4, Q=64, D=64, block=128, layout=LAYER_MAJOR, dtype="fp16"),
+    dict(lens=[3000, 2990], H=1, G=8, Q=8, D=128, block=64, prefix_len=[1500], member=[0, 0]),
+    dict(lens=[40, 150], H=2, G=50, D=64, block=24),
 ]
 
 
@@ -131,6 +138,7 @@ def test_attention(kw):
     s = Setup(**kw)
     with s.session() as c:
         check(s, *c.attend(s.layer, s.q_t), s.expect())
+        c.status()
 
 
 @pytest.mark.parametrize("kw", CASES, ids=[str(i) for i in range(len(CASES))])
@@ -176,6 +184,14 @@ def test_strides_and_other_orders():
         check(s, view, lse, want)
         check_scores(s, np.zeros((n, s.H, 131)), sc.transpose(0, 1), want, s.lens)
     assert (out[..., :8] == 9).all() and (out[..., 8 + D:] == 9).all()
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1.5])
+@pytest.mark.parametrize("G", [2, 60])
+def test_scale(scale, G):
+    s = Setup([150, 40], G=G, D=64)
+    with s.session() as c:
+        check(s, *c.attend(s.layer, s.q_t, scale=scale), s.expect(scale=scale))
 
 
 def test_logits_of_minus_infinity_and_large_ones():

@@ -158,7 +158,8 @@ def test_refused_evictions():
 def cover(s, H, lens, prefix_len, seq_prefix, rows):
     """Every (head, row, token) of every segment lies in exactly one item; CTAs in order."""
     items = B.pdkv_seqs_items(s)
-    assert (np.diff(items["cta"]) >= 0).all()
+    for kernel in (0, 1):
+        assert (np.diff(items["cta"][items["kernel"] == kernel]) >= 0).all()
     todo = {("s", r): (n, rows) for r, n in enumerate(lens)}
     for p, n in enumerate(prefix_len):
         todo["p", p] = (n, rows * sum(x == p for x in seq_prefix))
