@@ -4,6 +4,7 @@
 #include <atomic>
 #include <cmath>
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -23,8 +24,8 @@ __device__ __forceinline__ int own_len(const AttnParams &p, int seq, int cap)
 struct RowId {
     int seq, token, g;
 };
-// Row `row` of a segment: which query token of which sequence, and which of the G heads.
-__device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnSeg &seg, int row)
+// Row `row` of an item's segment: which query token of which sequence, and which of the G heads.
+__device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnItem &seg, int row)
 {
     const int R = p.G * p.q_tokens;
     RowId id;
@@ -40,6 +41,48 @@ __device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnSeg &seg,
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+constexpr long long kWaitCycles = 2000000000;   // a wait gives up after a second
+
+__device__ __forceinline__ void mbar_init(uint64_t *b, int count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t *b)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint64_t *b, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint64_t *b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait.  A thread that gives up records it and waits for nothing any more: every role then runs
+// through to the end of its list without touching memory for the results.
+__device__ __forceinline__ void mbar_wait(uint64_t *b, uint32_t parity, bool &dead, unsigned long long *status)
+{
+    if (dead || mbar_try(b, parity)) return;
+    const long long start = clock64();
+    while (!mbar_try(b, parity))
+        if (clock64() - start > kWaitCycles) {
+            dead = true;
+            atomicExch(status, 1ull);
+            return;
+        }
+}
+
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5,%6}], [%7];" ::"r"(to),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_u32(bar)) : "memory");
+}
 
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi)

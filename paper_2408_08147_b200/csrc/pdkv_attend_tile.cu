@@ -26,7 +26,6 @@ namespace {
 constexpr int kTileRows = 128, kTileTokens = 128;
 constexpr int kSoftmaxThreads = 128;                          // of one row tile
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kTileThreads = 320;
-constexpr uint64_t kWaitNs = 1000000000;                     // a wait gives up after a second
 constexpr float kGrowth = 8.f;                                // log2 of how far a maximum may run ahead of its base
 
 // Tensor memory columns: S (and P over it) of tile t, O of tile t.
@@ -49,46 +48,6 @@ struct Barriers {
     uint32_t tmem;
 };
 
-__device__ __forceinline__ void mbar_init(uint64_t *b, int count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t *b)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
-}
-__device__ __forceinline__ void mbar_expect(uint64_t *b, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint64_t *b, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(smem_u32(b)), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ uint64_t nanoseconds()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-// Bounded wait.  A thread that gives up records it and waits for nothing any more: every role then runs
-// through to the end of its list without touching memory for the results.
-__device__ __forceinline__ void mbar_wait(uint64_t *b, uint32_t parity, bool &dead, unsigned long long *status)
-{
-    if (dead || mbar_try(b, parity)) return;
-    const uint64_t start = nanoseconds();
-    while (!mbar_try(b, parity))
-        if (nanoseconds() - start > kWaitNs) {
-            dead = true;
-            atomicExch(status, 1ull);
-            return;
-        }
-}
-
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
@@ -158,24 +117,16 @@ __device__ __forceinline__ void commit(uint64_t *b)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
-__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4, uint64_t *bar)
-{
-    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5,%6}], [%7];" ::"r"(to),
-                 "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_u32(bar)) : "memory");
-}
-
 // What every role has to know about an item.
 struct Work {
     AttnItem it;
-    AttnSeg seg;
     int len, limit, tiles, row_tiles;
 };
 __device__ __forceinline__ Work work_of(const AttnParams &p, int i)
 {
     Work w;
     w.it = p.tile_items[i];
-    w.seg = p.segs[w.it.seg];
-    w.len = w.seg.seq >= 0 ? own_len(p, w.seg.seq, w.seg.len) : w.seg.len;
+    w.len = w.it.seq >= 0 ? own_len(p, w.it.seq, w.it.len) : w.it.len;
     w.limit = min(w.it.tok1, w.len);
     w.tiles = w.limit > w.it.tok0 ? (w.limit - w.it.tok0 + kTileTokens - 1) / kTileTokens : 0;
     w.row_tiles = w.it.rows > kTileRows ? 2 : 1;
@@ -230,7 +181,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 int block = 0, tt = 0;
                 if (lane < boxes) {
                     const int t = t0 + lane * page_rows;
-                    block = p.tbl[w.seg.tbl + t / p.pool.block_tokens];
+                    block = p.tbl[w.it.tbl + t / p.pool.block_tokens];
                     tt = t % p.pool.block_tokens;
                 }
                 for (int kv = 0; kv < 2; ++kv, ++n) {
@@ -324,7 +275,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         auto load_q = [&](const Work &w) {
             const int row = t * kTileRows + r;
             const bool live = row < w.it.rows;
-            const RowId id = row_id(p, w.seg, w.it.row0 + (live ? row : 0));
+            const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             const T *q = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2];
 #pragma unroll
             for (int c = 0; c < DP / 8; ++c) {
@@ -347,8 +298,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             n += 2 * w.tiles;
             if (t >= w.row_tiles) continue;
             const int row = t * kTileRows + r;
-            const bool live = row < w.it.rows, own = w.seg.seq >= 0;
-            const RowId id = row_id(p, w.seg, w.it.row0 + (live ? row : 0));
+            const bool live = row < w.it.rows, own = w.it.seq >= 0;
+            const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             float m = -INFINITY, l = 0.f;
             if (w.tiles > 0) {
                 if (q_of != i) load_q(w);
@@ -356,7 +307,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
                 float *logits = nullptr;
                 if (p.logits && own && live) {
-                    const AttnSeq s = p.seqs[w.seg.seq];
+                    const AttnSeq s = p.seqs[w.it.seq];
                     logits = p.logits + s.logits + ((int64_t)w.it.head * p.G * p.q_tokens + w.it.row0 + row) * s.logit_stride;
                 }
                 for (int j = 0; j < w.tiles; ++j) {
@@ -535,7 +486,10 @@ bool attend_tile_supported(const pdkv_pool_desc &d)
            (B >= kTileTokens ? B % kTileTokens == 0 : B >= 8 && kTileTokens % B == 0) && d.num_blocks <= 0x7fffffff;
 }
 
-bool make_attend_map(const pdkv_pool &pool, void *out)
+int attend_tile_box(const pdkv_pool_desc &d) { return d.block_tokens < kTileTokens ? d.block_tokens : kTileTokens; }
+
+// A map of the pool whose boxes are 64 dims of `box_tokens` tokens of one head.
+bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out)
 {
     static_assert(sizeof(CUtensorMap) <= kMapBytes, "a handle's space for the map");
     void *sym = nullptr;
@@ -547,7 +501,7 @@ bool make_attend_map(const pdkv_pool &pool, void *out)
     const pdkv_pool_desc &d = pool.d;
     const PoolView v = pool_view(pool);
     const cuuint64_t H = d.num_kv_heads, B = d.block_tokens, D = d.head_dim, NB = d.num_blocks, LC = 2 * (cuuint64_t)d.num_layers;
-    const cuuint32_t rows = (cuuint32_t)(d.block_tokens < kTileTokens ? d.block_tokens : kTileTokens), ones[5] = {1, 1, 1, 1, 1};
+    const cuuint32_t rows = (cuuint32_t)box_tokens, ones[5] = {1, 1, 1, 1, 1};
     const bool layer_major = d.layout == PDKV_LAYOUT_LAYER_MAJOR;
     // block-major: (dim, head, token, layer and K/V, block); layer-major: (dim, token, head, block, layer and K/V)
     const cuuint64_t dims_b[5] = {D, H, B, LC, NB}, dims_l[5] = {D, B, H, NB, LC};

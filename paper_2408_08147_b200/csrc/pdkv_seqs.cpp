@@ -158,7 +158,10 @@ void plan_items(pdkv_seqs &s, int kernel, const std::vector<int32_t> &n_rows, co
             n = std::max<int64_t>(n, 1);
             AttnItem it{};
             it.part_row = s.part_rows;
-            it.seg = w.seg;
+            it.tbl = s.segs[(size_t)w.seg].tbl;
+            it.seq = s.segs[(size_t)w.seg].seq;
+            it.member_begin = s.segs[(size_t)w.seg].member_begin;
+            it.len = s.segs[(size_t)w.seg].len;
             it.head = w.head;
             it.row0 = w.row0;
             it.rows = w.rows;
@@ -278,7 +281,10 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                     }
             }
             bool tile_ok = pdkv::attend_tile_supported(g);
-            if (tile_ok && !pdkv::tunables().dry_run) tile_ok = pdkv::make_attend_map(*pool, s->map);
+            if (!pdkv::tunables().dry_run) {
+                tile_ok = tile_ok && pdkv::make_attend_map(*pool, pdkv::attend_tile_box(g), s->map[1]);
+                s->use_map = pdkv::attend_map_supported(g) && pdkv::make_attend_map(*pool, pdkv::attend_map_tokens(), s->map[0]);
+            }
             std::vector<Shape> shape;
             for (int32_t n : n_rows) shape.push_back(shape_of(n, tile_ok));
             // unit of (row tile 0, head 0) of every segment
@@ -307,7 +313,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                 if (!q.direct) s->join = true;
             }
             for (std::vector<AttnItem> &list : s->items)
-                for (AttnItem &it : list) it.direct = it.seg < s->n_seq && s->seqs[(size_t)it.seg].direct;
+                for (AttnItem &it : list) it.direct = it.seq >= 0 && s->seqs[(size_t)it.seq].direct;
         }
 
         // device arrays: one block, each list 16-byte aligned
@@ -495,6 +501,7 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         p.tile_items = s->d_items[1];
         p.cta_tile_items = s->d_cta_items[1];
         p.n_tile_ctas = (int32_t)s->cta_items[1].size() - 1;
+        p.use_map = s->use_map;
         p.map_layer_major = s->pool.d.layout == PDKV_LAYOUT_LAYER_MAJOR;
         p.status = s->d_status;
         p.n_seq = s->n_seq;
@@ -530,11 +537,11 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
         cudaStream_t st = static_cast<cudaStream_t>(stream);
         if (p.n_tile_ctas > 0) {
-            const cudaError_t e = pdkv::launch_attend_tile(p, s->map, s->dtype, st);
+            const cudaError_t e = pdkv::launch_attend_tile(p, s->map[1], s->dtype, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention tile kernel launch");
         }
         if (p.n_ctas > 0) {
-            const cudaError_t e = pdkv::launch_attend(p, s->dtype, st);
+            const cudaError_t e = pdkv::launch_attend(p, s->map[0], s->dtype, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention kernel launch");
         }
         if (s->join || scores) {

@@ -31,14 +31,17 @@ struct AttnUnit {
     int32_t rows;
 };
 
-// What one CTA does in one go: rows [row0, row0 + rows) of one head against tokens [tok0, tok1) of a segment.
-struct AttnItem {
+// What one CTA does in one go: rows [row0, row0 + rows) of one head against tokens [tok0, tok1) of a
+// segment.  Carries what it needs of the segment, so that a kernel starts on it after one load.
+struct alignas(16) AttnItem {
     int64_t part_row;
-    int32_t seg, head;
+    int64_t tbl;
+    int32_t seq, member_begin, len;   // of the segment
+    int32_t head;
     int32_t row0, rows;
     int32_t tok0, tok1;
     int32_t direct;     // 1: the only part of its rows, the item writes the result itself
-    int32_t pad;
+    int32_t pad[3];
 };
 
 // What the joining kernel has to know about a sequence.
@@ -67,6 +70,7 @@ struct AttnParams {
     const AttnItem *tile_items;      // the same for the tile kernel
     const int32_t *cta_tile_items;
     int32_t n_tile_ctas;
+    int32_t use_map;                 // the warp kernel loads through the tensor map
     int32_t map_layer_major;         // order of the coordinates of the pool's tensor map
     unsigned long long *status;      // [0] != 0: a bounded wait gave up
     int32_t n_seq, H, G, D, q_tokens;
@@ -88,11 +92,14 @@ struct AttnParams {
 };
 
 int attend_ctas_per_sm(int head_dim);
-cudaError_t launch_attend(const AttnParams &p, int dtype, cudaStream_t stream);
+bool attend_map_supported(const pdkv_pool_desc &d);
+int attend_map_tokens();
+cudaError_t launch_attend(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 // The tile kernel (tcgen05): segments with many rows.  `map` is a CUtensorMap of the pool.
 constexpr int kMapBytes = 128;
 bool attend_tile_supported(const pdkv_pool_desc &d);
-bool make_attend_map(const pdkv_pool &pool, void *out);
+int attend_tile_box(const pdkv_pool_desc &d);
+bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out);
 cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream);
 
@@ -135,7 +142,8 @@ struct pdkv_seqs {
     std::vector<pdkv::AttnSeq> seqs;
     std::vector<pdkv::AttnItem> items[2];      // warp kernel, tile kernel
     std::vector<int32_t> cta_items[2];
-    alignas(64) char map[pdkv::kMapBytes] = {};   // tensor map of the pool, for the tile kernel
+    alignas(64) char map[2][pdkv::kMapBytes] = {};   // tensor maps of the pool, for the two kernels
+    bool use_map = false;        // the warp kernel loads through its map
     std::vector<pdkv_attend_item> listing;
     int64_t part_rows = 0, logit_floats = 0;
     bool join = false;           // some rows have several parts, or none
