@@ -1,6 +1,8 @@
 // Attention of a batch's newest tokens over a paged pool, and the join of its parts.
 #include <cmath>
 
+#include <numeric>
+
 #include "pdkv_attend_device.cuh"
 
 namespace pdkv {
@@ -8,28 +10,27 @@ namespace pdkv {
 namespace {
 
 constexpr int kConsumers = 128, kThreads = 160;   // four warps that compute, one that loads
-constexpr int kSlice = 16;   // tokens of one ring slot: the depth of one matrix instruction in the product with V
+constexpr int kSlice = 32;                        // tokens of one ring slot, the work of a warp between two waits
 
-// Shared memory of a CTA: a ring of slices, each 16 rows of K and 16 of V, in pieces of 64 dims whose 16-byte
+// Shared memory of a CTA: a ring of slices, each 32 rows of K and 32 of V, in pieces of 64 dims whose 16-byte
 // chunks are swizzled (chunk c of row r lies at c ^ (r mod 8): the TMA unit's 128-byte swizzle, and the eight
 // rows of a matrix load lie in different banks); behind it the space through which warps join their
-// results.  About 100 KB and two CTAs per SM up to 128 dims, 210 KB and one CTA above: 130 to 150 KB of
-// loads in flight on each SM, twice what 6.5 TB/s at a microsecond of latency need.
+// results.  80 to 96 KB of slices per CTA and two CTAs per SM up to 128 dims, 160 to 168 KB and one CTA above:
+// twice the bytes in flight that 6.5 TB/s at a microsecond of latency need.
 template <int DP> struct Ring {
     static constexpr int kSubs = DP / 64;
     static constexpr int kSubBytes = kSlice * 128;
     static constexpr int kHalf = kSubs * kSubBytes;            // K or V of a slice
     static constexpr int kSliceBytes = 2 * kHalf;
-    static constexpr int kSlots = DP == 64 ? 24 : DP == 192 ? 16 : 12;
-    static constexpr int kQuarter = DP / 4;                    // dims that one warp of four joins
-    static constexpr int kXchRow = kQuarter + 4;               // floats
-    static constexpr int kXch = 4 * 16 * kXchRow * 4;
+    static constexpr int kSlots = DP == 64 ? 12 : DP == 128 ? 5 : DP == 192 ? 7 : 5;
+    static constexpr int kXchRow = DP + 4;                     // floats; 4 mod 16, so that a warp's stores do not collide
+    static constexpr int kXch = 4 * 8 * kXchRow * 4;
     static constexpr int kBytes = kSlots * kSliceBytes + kXch + 1024;
     static constexpr int kCtas = DP <= 128 ? 2 : 1;
 };
 
 struct RingBarriers {
-    uint64_t full[24], empty[24];
+    uint64_t full[12], empty[12];
 };
 
 // 16 bytes to shared memory; with `there` false zeros are written and nothing is read.
@@ -70,6 +71,13 @@ __device__ __forceinline__ void multiply<__half>(float (&c)[4], const uint32_t (
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Transposes an 8 x 8 tile of 16-bit numbers between the lanes of a warp.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 __device__ __forceinline__ int slices_of(const AttnParams &p, const AttnItem &it, int *len, int *limit)
@@ -79,10 +87,10 @@ __device__ __forceinline__ int slices_of(const AttnParams &p, const AttnItem &it
     return *limit > it.tok0 ? (*limit - it.tok0 + kSlice - 1) / kSlice : 0;
 }
 
-// The loading warp: slices of all items in order, into the ring.  Where a slice lies within one block
-// (block sizes that are multiples of 16) it is fetched by the TMA unit, a box of 64 dims per instruction; else
-// by 16-byte asynchronous copies, each row looked up by its own lane.  It runs ahead of the computing warps
-// across items, so memory stays busy while they join their results.
+// The loading warp: slices of all items in order, into the ring.  Where pages and slices divide one another
+// they are fetched by the TMA unit, a box of 64 dims per instruction; else by 16-byte asynchronous copies,
+// each row looked up by its own lane.  It runs ahead of the computing warps across items, so memory stays
+// busy while they join their results.
 template <int DP>
 __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorMap *map, uint32_t ring, RingBarriers &bar, int first, int end)
 {
@@ -96,27 +104,30 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
         int len, limit;
         const int count = slices_of(p, it, &len, &limit);
         if (p.use_map) {
-            int block = 0;
+            // lane: page, then piece of 64 dims of K or V
+            const int box = p.map_box, page = lane / (2 * R::kSubs), kv = lane / R::kSubs % 2, sub = lane % R::kSubs;
+            auto block_of = [&](int s) {
+                const int t = it.tok0 + s * kSlice + page * box;
+                return page * box < kSlice && t < limit ? p.tbl[it.tbl + (p.block_shift >= 0 ? t >> p.block_shift : t / p.pool.block_tokens)] : -1;
+            };
+            int next = block_of(0);
             for (int s = 0; s < count; ++s) {
-                const int t = it.tok0 + s * kSlice;
-                if (s % 32 == 0) {   // blocks of the next 32 slices
-                    const int tl = t + lane * kSlice;
-                    if (tl < limit) block = p.tbl[it.tbl + (p.block_shift >= 0 ? tl >> p.block_shift : tl / p.pool.block_tokens)];
-                }
-                const int b = __shfl_sync(~0u, block, s % 32);
+                const int block = next, t = it.tok0 + s * kSlice + page * box;
+                next = block_of(s + 1);
                 const int tt = p.block_shift >= 0 ? t & (p.pool.block_tokens - 1) : t % p.pool.block_tokens;
+                const int boxes = __popc(__ballot_sync(~0u, block >= 0));   // pages past the end are not loaded
                 mbar_wait(&bar.empty[slot], parity, dead, p.status);
                 dead = __any_sync(~0u, dead);
                 if (!dead) {
-                    if (lane == 0) mbar_expect(&bar.full[slot], R::kSliceBytes);
+                    if (lane == 0) mbar_expect(&bar.full[slot], boxes * box * 128);
                     __syncwarp();
-                    if (lane < 2 * R::kSubs) {
-                        const int kv = lane / R::kSubs, sub = lane % R::kSubs, lc = 2 * p.layer + kv;
-                        const uint32_t to = ring + slot * R::kSliceBytes + lane * R::kSubBytes;
+                    if (block >= 0) {
+                        const uint32_t to = ring + slot * R::kSliceBytes + kv * R::kHalf + sub * R::kSubBytes + page * box * 128;
+                        const int lc = 2 * p.layer + kv;
                         if (p.map_layer_major)
-                            load_box(to, map, 64 * sub, tt, it.head, b, lc, &bar.full[slot]);
+                            load_box(to, map, 64 * sub, tt, it.head, block, lc, &bar.full[slot]);
                         else
-                            load_box(to, map, 64 * sub, it.head, tt, lc, b, &bar.full[slot]);
+                            load_box(to, map, 64 * sub, it.head, tt, lc, block, &bar.full[slot]);
                     }
                 }
                 if (++slot == R::kSlots) {
@@ -129,7 +140,7 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
         const char *base = p.pool.base + 2 * (int64_t)p.layer * p.pool.lc_stride + it.head * p.pool.head_stride;
         // byte offset of token `lane` of a slice from `base`, -1: past the end
         auto offset_of = [&](int s) -> int64_t {
-            const int t = it.tok0 + s * kSlice + lane % kSlice;
+            const int t = it.tok0 + s * kSlice + lane;
             if (t >= limit) return -1;
             const int b = p.block_shift >= 0 ? t >> p.block_shift : t / p.pool.block_tokens;
             return p.tbl[it.tbl + b] * p.pool.block_stride + (int64_t)(t - b * p.pool.block_tokens) * p.pool.tok_stride;
@@ -142,8 +153,8 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
             dead = __any_sync(~0u, dead);
             const uint32_t to = ring + slot * R::kSliceBytes;
             if (!dead) {
-#pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {   // 16 rows x DP / 8 pieces, 32 lanes
+#pragma unroll 8
+                for (int k = 0; k < kSlice * DP / 8 / 32; ++k) {   // 32 rows x DP / 8 pieces, 32 lanes
                     constexpr int kCols = DP / 8;
                     const int x = lane + 32 * k, row = x / kCols, col = x % kCols;
                     const int64_t o = __shfl_sync(~0u, offset, row);
@@ -166,14 +177,20 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// One work item with WM warps along the rows (16 each) and 4 / WM groups of warps along the tokens: group g
+// One work item with WM warps along the rows (8 NT each) and 4 / WM groups of warps along the tokens: group g
 // takes slices g, g + groups, ...  `n` is the number of slices that went through the ring before.
 //
-// S = Q K^T and O += P V go through m16n8k16 matrix instructions with the rows (heads of one KV head,
-// query tokens, sequences behind one prefix) as M; the maximum and sum of each row are kept per slice in 32
-// bits, and O is only rescaled when a maximum moved.  The weights are rounded to 16 bits for the product
-// with V (the matrix instruction takes no wider operand beside a 16-bit V); their sum is taken before that.
-template <typename T, int DP, int WM>
+// The products are turned round, so that the rows (heads of one KV head, query tokens, sequences behind one
+// prefix), of which there are few, are the short side of the m16n8k16 matrix instructions:
+//     S^T [token][row] = K Q^T       O^T [dim][row] += V^T P^T
+// K and V are the 16-row operands, read from shared memory as they lie (V transposed by the matrix load), and
+// eight rows cost half the instructions and registers that they would cost as one side of sixteen.  P^T
+// changes from accumulator to operand layout by transposing its 8 x 8 tiles between lanes.
+// Maximum and sum of each row are kept in 32 bits; O is rescaled only when a maximum outgrew its base by
+// 2^8 (weights up to 2^8 lose nothing in 16-bit floating point).  The weights are rounded to 16 bits for
+// the product with V (the matrix instruction takes no wider operand beside a 16-bit V); their sum is
+// taken before that.  FULL: the head has exactly DP dims.
+template <typename T, int DP, bool FULL, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
                                             float (*sml)[16][2], RingBarriers &bar, uint32_t n, bool &dead)
 {
@@ -182,51 +199,77 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, wm = warp % WM, group = warp / WM;
     const bool own = it.seq >= 0;
     const uint32_t ring = smem_u32(smem);
+    const float scale = fabsf(p.scale_log2);
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
 
-    // this lane's two rows: lane / 4 and lane / 4 + 8 of the warp's sixteen
-    uint32_t q[DP / 16][4];
-    int sees[2];
+    // operand Q^T: row lane / 4 of each tile of eight, dims 2 (lane % 4) and 8 further of each sixteen
+    uint32_t q[DP / 16][NT][2];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int r = wm * 16 + lane / 4 + 8 * half;
+    for (int t = 0; t < NT; ++t) {
+        const int r = (wm * NT + t) * 8 + lane / 4;
         const bool live = r < it.rows;
         const RowId id = row_id(p, it, it.row0 + (live ? r : 0));
-        sees[half] = own ? min(limit, len - (p.q_tokens - 1 - id.token)) : limit;
         const T *row = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (it.head * p.G + id.g) * p.q_stride[2];
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int d = 16 * k + 8 * j + 2 * (lane % 4);
-                q[k][half + 2 * j] = live && d < p.D ? *reinterpret_cast<const uint32_t *>(row + d) : 0u;
+                q[k][t][j] = live && (FULL || d < p.D) ? *reinterpret_cast<const uint32_t *>(row + d) ^ flip : 0u;
             }
     }
+    // accumulators: rows 2 (lane % 4) and the next of each tile of eight
+    int sees[NT][2];
+    float *logits[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = (wm * NT + t) * 8 + 2 * (lane % 4) + j;
+            const bool live = r < it.rows;
+            sees[t][j] = limit;
+            logits[t][j] = nullptr;
+            if (own) {
+                sees[t][j] = min(limit, len - (p.q_tokens - 1 - (it.row0 + (live ? r : 0)) / p.G));
+                if (p.logits && live) {
+                    const AttnSeq s = p.seqs[it.seq];
+                    logits[t][j] = p.logits + s.logits + ((int64_t)it.head * p.G * p.q_tokens + it.row0 + r) * s.logit_stride;
+                }
+            }
+        }
     const int safe = own ? min(limit, len - (p.q_tokens - 1)) : limit;   // tokens before this one are seen by every row
-    float *logits = nullptr;
-    int64_t logit_row8 = 0;
-    bool store[2] = {false, false};
-    if (p.logits && own) {
-        const AttnSeq s = p.seqs[it.seq];
-        logits = p.logits + s.logits + ((int64_t)it.head * p.G * p.q_tokens + it.row0 + wm * 16 + lane / 4) * s.logit_stride;
-        logit_row8 = 8 * (int64_t)s.logit_stride;
-        store[0] = wm * 16 + lane / 4 < it.rows;
-        store[1] = wm * 16 + lane / 4 + 8 < it.rows;
-    }
+    const bool with_logits = p.logits && own;
 
-    float o[DP / 8][4];
+    float o[DP / 16][NT][4];
 #pragma unroll
-    for (int k = 0; k < DP / 8; ++k)
+    for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[k][j] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    // matrix loads: this lane's row of a slice, and which of the two 16-byte pieces of a step of 16 dims
-    const uint32_t k_row = (lane / 16) * 8 + lane % 8, k_piece = lane / 8 % 2;
-    const uint32_t v_row = (lane / 8 % 2) * 8 + lane % 8, v_piece = lane / 16;
-    const uint32_t k_at = k_row * 128, v_at = R::kHalf + v_row * 128, turn = lane % 8;   // (row mod 8 is lane mod 8 for both)
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[k][t][j] = 0.f;
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m[t][0] = m[t][1] = -INFINITY;
+        l[t][0] = l[t][1] = 0.f;
+    }
+    // matrix loads.  K: lanes 0-7 rows 0-7, 8-15 rows 8-15, then the same 8 dims further.  V (transposed): lanes
+    // 0-7 tokens 0-7, 8-15 the same 8 dims further, then tokens 8-15.  Row mod 8 is lane mod 8 for both.
+    const uint32_t k_at = (lane % 16) * 128, v_at = R::kHalf + ((lane / 16) * 8 + lane % 8) * 128;
+    uint32_t k_chunk[4], v_chunk[4];   // swizzled place of step s of 16 dims within a piece of 64
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        k_chunk[s] = ((2 * s + lane / 16) ^ (lane % 8)) * 16;
+        v_chunk[s] = ((2 * s + lane / 8 % 2) ^ (lane % 8)) * 16;
+    }
 
     uint32_t slot = (n + group) % R::kSlots, parity = (n + group) / R::kSlots & 1;
 #pragma unroll 1
     for (int s = group; s < n_slices; s += kGroups) {
+        // The parity of a barrier tells a phase from the next one only.  When the slots are not dealt to the groups
+        // evenly, another group had this slot before and may not even have received its slice yet (copies
+        // can land out of order): wait until it gave the slot back, then at most one phase is open.
+        if (R::kSlots % 4 && n + s >= R::kSlots) mbar_wait(&bar.empty[slot], parity ^ 1, dead, p.status);
         mbar_wait(&bar.full[slot], parity, dead, p.status);
         __syncwarp();
         const uint32_t slice = ring + slot * R::kSliceBytes;
@@ -241,74 +284,92 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             fence_async_smem();
             __syncwarp();
         }
-        float z[2][4] = {};
+        float z[2][NT][4] = {};   // [16 tokens][8 rows]: tokens lane / 4 and 8 further
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
-            if (16 * k < p.D) {
-                uint32_t b[4];
-                load_matrices(b, slice + k_at + k / 4 * R::kSubBytes + ((((k % 4) * 2 + k_piece) ^ turn) * 16));
-                multiply<T>(z[0], q[k], b[0], b[1]);
-                multiply<T>(z[1], q[k], b[2], b[3]);
+            if (FULL || 16 * k < p.D) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t a[4];
+                    load_matrices(a, slice + k_at + h * 2048 + k / 4 * R::kSubBytes + k_chunk[k % 4]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) multiply<T>(z[h][t], a, q[k][t][0], q[k][t][1]);
+                }
             }
+        const bool masked = t0 + kSlice > safe;
+        if (masked)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) z[i][j] *= p.scale_log2;
-        if (t0 + kSlice > safe)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                    for (int j = 0; j < 4; ++j)
+                        if (t0 + 16 * h + lane / 4 + 8 * (j >> 1) >= sees[t][j & 1]) z[h][t][j] = -INFINITY;
+        if (with_logits)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (t0 + 8 * i + 2 * (lane % 4) + (j & 1) >= sees[j >> 1]) z[i][j] = -INFINITY;
-        if (logits)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int t = t0 + 8 * i + 2 * (lane % 4);
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    if (store[half] && t < limit)
-                        *reinterpret_cast<float2 *>(logits + half * logit_row8 + t) = make_float2(z[i][2 * half], z[i][2 * half + 1]);
+                    for (int j = 0; j < 4; ++j) {
+                        const int tok = t0 + 16 * h + lane / 4 + 8 * (j >> 1);
+                        if (logits[t][j & 1] && tok < limit) logits[t][j & 1][tok] = z[h][t][j] == -INFINITY ? -INFINITY : z[h][t][j] * scale;
+                    }
+        float top[NT][2];
+        bool grew = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float x = fmaxf(fmaxf(z[0][t][j], z[0][t][j + 2]), fmaxf(z[1][t][j], z[1][t][j + 2]));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
+                top[t][j] = x == -INFINITY ? x : x * scale;
+                grew = grew || top[t][j] > m[t][j] + kGrowth || (m[t][j] == -INFINITY && top[t][j] > m[t][j]);
             }
-        float top[2], base[2];
+        if (__any_sync(~0u, grew)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float x = fmaxf(fmaxf(z[0][2 * half], z[0][2 * half + 1]), fmaxf(z[1][2 * half], z[1][2 * half + 1]));
-            x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
-            x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
-            top[half] = fmaxf(m[half], x);
-            base[half] = top[half] == -INFINITY ? 0.f : top[half];
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float new_m = fmaxf(m[t][j], top[t][j]), f = new_m == -INFINITY ? 1.f : pow2(m[t][j] - new_m);
+                    m[t][j] = new_m;
+                    l[t][j] *= f;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        o[k][t][j] *= f;
+                        o[k][t][j + 2] *= f;
+                    }
+                }
         }
-        if (__any_sync(~0u, top[0] > m[0] || top[1] > m[1])) {
-            const float f0 = pow2(m[0] - base[0]), f1 = pow2(m[1] - base[1]);
-            l[0] *= f0;
-            l[1] *= f1;
+        uint32_t w[2][NT][2];   // operand P^T
 #pragma unroll
-            for (int k = 0; k < DP / 8; ++k) {
-                o[k][0] *= f0;
-                o[k][1] *= f0;
-                o[k][2] *= f1;
-                o[k][3] *= f1;
-            }
-            m[0] = top[0];
-            m[1] = top[1];
-        }
-        uint32_t w[4];
+        for (int t = 0; t < NT; ++t) {
+            const float b0 = m[t][0] == -INFINITY ? 0.f : m[t][0], b1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float a = pow2(z[i][2 * half] - base[half]), b = pow2(z[i][2 * half + 1] - base[half]);
-                l[half] += a + b;
-                w[2 * i + half] = pack<T>(a, b);
+                for (int j = 0; j < 4; ++j) {
+                    float x = pow2(fmaf(z[h][t][j], scale, j & 1 ? -b1 : -b0));
+                    if (masked && t0 + 16 * h + lane / 4 + 8 * (j >> 1) >= sees[t][j & 1]) x = 0.f;
+                    l[t][j & 1] += x;
+                    z[h][t][j] = x;
+                }
+                w[h][t][0] = transpose8(pack<T>(z[h][t][0], z[h][t][1]));
+                w[h][t][1] = transpose8(pack<T>(z[h][t][2], z[h][t][3]));
             }
         }
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k)
-            if (16 * k < p.D) {
-                uint32_t b[4];
-                load_matrices_trans(b, slice + v_at + k / 4 * R::kSubBytes + ((((k % 4) * 2 + v_piece) ^ turn) * 16));
-                multiply<T>(o[2 * k], w, b[0], b[1]);
-                multiply<T>(o[2 * k + 1], w, b[2], b[3]);
+            if (FULL || 16 * k < p.D) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t a[4];
+                    load_matrices_trans(a, slice + v_at + h * 2048 + k / 4 * R::kSubBytes + v_chunk[k % 4]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) multiply<T>(o[k][t], a, w[h][t][0], w[h][t][1]);
+                }
             }
         __syncwarp();
         if (lane == 0) mbar_arrive_many(&bar.empty[slot], kGroups);   // a slot is free after four arrivals
@@ -319,97 +380,67 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
         }
     }
 
+    // Join the groups: every warp writes its maxima and sums and, eight rows at a time, its O; a warp per row
+    // adds them up and writes the result.
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        l[half] += __shfl_xor_sync(~0u, l[half], 1);
-        l[half] += __shfl_xor_sync(~0u, l[half], 2);
-    }
-    // Join the groups: all take the largest maximum, then each warp collects its share of the dims -- a quarter
-    // with four groups, two with two -- from the others, one quarter a round.
-    constexpr int kTiles = R::kQuarter / 8;   // accumulator tiles of a quarter
-    if (kGroups > 1) {
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-            if (lane % 4 == 0) *reinterpret_cast<float2 *>(sml[warp][lane / 4 + 8 * half]) = make_float2(m[half], l[half]);
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) l[t][j] += __shfl_xor_sync(~0u, l[t][j], x);
+            if (lane < 4) *reinterpret_cast<float2 *>(sml[warp][t * 8 + 2 * lane + j]) = make_float2(m[t][j], l[t][j]);
+        }
+    float *xch = reinterpret_cast<float *>(smem + R::kSlots * R::kSliceBytes);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float *mine = xch + (warp * 8 + 2 * (lane % 4)) * R::kXchRow + lane / 4;
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine[(j & 1) * R::kXchRow + 16 * k + 8 * (j >> 1)] = o[k][t][j];
         consumer_sync();
+#pragma unroll 1
+        for (int x = warp; x < WM * 8; x += 4) {
+            const int w = x / 8, r = (w * NT + t) * 8 + x % 8;   // row of the item: warp w of each group has it
+            if (r >= it.rows) continue;
+            float mt = -INFINITY, lt = 0.f, f[kGroups];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float mt = -INFINITY, lt = 0.f;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) mt = fmaxf(mt, sml[g * WM + wm][lane / 4 + 8 * half][0]);
+            for (int g = 0; g < kGroups; ++g) mt = fmaxf(mt, sml[g * WM + w][t * 8 + x % 8][0]);
             const float b = mt == -INFINITY ? 0.f : mt;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
-                const float *x = sml[g * WM + wm][lane / 4 + 8 * half];
-                lt += pow2(x[0] - b) * x[1];
+                f[g] = pow2(sml[g * WM + w][t * 8 + x % 8][0] - b);
+                lt += f[g] * sml[g * WM + w][t * 8 + x % 8][1];
             }
-            const float f = pow2(m[half] - b);
-            m[half] = mt;
-            l[half] = lt;
+            if (dead) continue;
+            const RowId id = row_id(p, it, it.row0 + r);
+            const int head = it.head * p.G + id.g;
+            const float inv = lt == 0.f ? 0.f : 1.f / lt;
+            T *out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2];
 #pragma unroll
-            for (int k = 0; k < DP / 8; ++k) {
-                o[k][2 * half] *= f;
-                o[k][2 * half + 1] *= f;
-            }
-        }
-        float *xch = reinterpret_cast<float *>(smem + R::kSlots * R::kSliceBytes);
-        float *mine = xch + (warp * 16 + lane / 4) * R::kXchRow + 2 * (lane % 4);
-        constexpr int kRounds = kGroups == 4 ? 3 : 2;
-#pragma unroll 1
-        for (int round = 0; round < kRounds; ++round) {
-            // the quarter that is given away, the one that is received, and from which warp
-            const int away = kGroups == 4 ? (group + 1 + round) % 4 : 2 * (1 - group) + round;
-            const int here = kGroups == 4 ? group : 2 * group + round;
-            const int peer = kGroups == 4 ? (group + 3 - round) % 4 : (1 - group) * WM + wm;
+            for (int d0 = 0; d0 < DP; d0 += 128) {
+                const int d = d0 + 4 * lane;
+                if (d >= p.D) continue;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int quarter = 0; quarter < 4; ++quarter)
-                if (quarter == away)
-#pragma unroll
-                    for (int k = 0; k < kTiles; ++k)
-#pragma unroll
-                        for (int half = 0; half < 2; ++half)
-                            *reinterpret_cast<float2 *>(mine + 8 * half * R::kXchRow + 8 * k) =
-                                make_float2(o[quarter * kTiles + k][2 * half], o[quarter * kTiles + k][2 * half + 1]);
-            consumer_sync();
-            const float *theirs = xch + (peer * 16 + lane / 4) * R::kXchRow + 2 * (lane % 4);
-#pragma unroll
-            for (int quarter = 0; quarter < 4; ++quarter)
-                if (quarter == here)
-#pragma unroll
-                    for (int k = 0; k < kTiles; ++k)
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const float2 x = *reinterpret_cast<const float2 *>(theirs + 8 * half * R::kXchRow + 8 * k);
-                            o[quarter * kTiles + k][2 * half] += x.x;
-                            o[quarter * kTiles + k][2 * half + 1] += x.y;
-                        }
-            consumer_sync();
-        }
-    }
-    if (dead) return;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int r = wm * 16 + lane / 4 + 8 * half;
-        if (r >= it.rows) continue;
-        const RowId id = row_id(p, it, it.row0 + r);
-        const int head = it.head * p.G + id.g;
-        const float inv = l[half] == 0.f ? 0.f : 1.f / l[half];
-        T *out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2] + 2 * (lane % 4);
-        float *part = p.part_o + (it.part_row + r) * p.D + 2 * (lane % 4);
-#pragma unroll
-        for (int k = 0; k < DP / 8; ++k) {
-            const int quarter = k / kTiles;
-            if ((kGroups == 1 || quarter / (4 / kGroups) == group) && 8 * k < p.D) {
+                for (int g = 0; g < kGroups; ++g) {
+                    const float4 y = *reinterpret_cast<const float4 *>(xch + ((g * WM + w) * 8 + x % 8) * R::kXchRow + d);
+                    v.x += f[g] * y.x;
+                    v.y += f[g] * y.y;
+                    v.z += f[g] * y.z;
+                    v.w += f[g] * y.w;
+                }
                 if (it.direct)
-                    *reinterpret_cast<uint32_t *>(out + 8 * k) = pack<T>(o[k][2 * half] * inv, o[k][2 * half + 1] * inv);
+                    *reinterpret_cast<uint2 *>(out + d) = make_uint2(pack<T>(v.x * inv, v.y * inv), pack<T>(v.z * inv, v.w * inv));
                 else
-                    *reinterpret_cast<float2 *>(part + 8 * k) = make_float2(o[k][2 * half], o[k][2 * half + 1]);
+                    *reinterpret_cast<float4 *>(p.part_o + (it.part_row + r) * p.D + d) = v;
+            }
+            if (lane == 0) {
+                if (it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (mt + log2f(lt)) * kLn2;
+                if (!it.direct || p.logits) *reinterpret_cast<float2 *>(p.part_ml + 2 * (it.part_row + r)) = make_float2(mt, lt);
             }
         }
-        if (lane % 4 == 0 && group == 0) {
-            if (it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (m[half] + log2f(l[half])) * kLn2;
-            if (!it.direct || p.logits) *reinterpret_cast<float2 *>(p.part_ml + 2 * (it.part_row + r)) = make_float2(m[half], l[half]);
-        }
+        consumer_sync();
     }
 }
 
@@ -417,7 +448,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 
 // Every CTA walks its stretch of the work list.  Warps are laid along the rows as far as there are rows,
 // the rest of them along the tokens.
-template <typename T, int DP>
+template <typename T, int DP, bool FULL>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p)
 {
     using R = Ring<DP>;
@@ -443,12 +474,14 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
         const AttnItem it = p.items[i];
         int len, limit;
         const int slices = slices_of(p, it, &len, &limit);
-        if (it.rows <= 16)
-            attend_item<T, DP, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+        if (it.rows <= 8)
+            attend_item<T, DP, FULL, 1, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+        else if (it.rows <= 16)
+            attend_item<T, DP, FULL, 2, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
         else if (it.rows <= 32)
-            attend_item<T, DP, 2>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+            attend_item<T, DP, FULL, 2, 2>(p, it, slices, len, limit, smem, sml, bar, n, dead);
         else
-            attend_item<T, DP, 4>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+            attend_item<T, DP, FULL, 2, 4>(p, it, slices, len, limit, smem, sml, bar, n, dead);
         n += slices;
     }
 }
@@ -602,34 +635,37 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
 
 namespace {
 
-template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, bool FULL> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(attend_items_kernel<T, DP>, Ring<DP>::kBytes, ready);
+    const cudaError_t e = allow_shared(attend_items_kernel<T, DP, FULL>, Ring<DP>::kBytes, ready);
     if (e != cudaSuccess) return e;
-    attend_items_kernel<T, DP><<<p.n_ctas, kThreads, Ring<DP>::kBytes, stream>>>(map, p);
+    attend_items_kernel<T, DP, FULL><<<p.n_ctas, kThreads, Ring<DP>::kBytes, stream>>>(map, p);
     return cudaGetLastError();
 }
 
 template <typename T> cudaError_t launch_type(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
-    if (p.D <= 64) return launch_dims<T, 64>(p, map, stream);
-    if (p.D <= 128) return launch_dims<T, 128>(p, map, stream);
-    if (p.D <= 192) return launch_dims<T, 192>(p, map, stream);
-    return launch_dims<T, 256>(p, map, stream);
+    // heads of exactly 64 and 128 dims without the checks for where a head ends
+    if (p.D == 64) return launch_dims<T, 64, true>(p, map, stream);
+    if (p.D == 128) return launch_dims<T, 128, true>(p, map, stream);
+    if (p.D <= 64) return launch_dims<T, 64, false>(p, map, stream);
+    if (p.D <= 128) return launch_dims<T, 128, false>(p, map, stream);
+    if (p.D <= 192) return launch_dims<T, 192, false>(p, map, stream);
+    return launch_dims<T, 256, false>(p, map, stream);
 }
 
 }  // namespace
 
 int attend_ctas_per_sm(int head_dim) { return head_dim <= 128 ? 2 : 1; }
 
-// Slices that lie within a block, rows that fill at least a box of 64 dims.
+// Blocks of a multiple of 8 tokens, rows that fill at least a box of 64 dims.  A box holds as many tokens as
+// divide both a block and a slice (8 at least: the period of the swizzle), so it lies within one block.
 bool attend_map_supported(const pdkv_pool_desc &d)
 {
-    return d.elem_bytes == 2 && d.head_dim >= 64 && d.head_dim <= 256 && d.head_dim % 8 == 0 && d.block_tokens % kSlice == 0 &&
-           d.num_blocks <= 0x7fffffff;
+    return d.elem_bytes == 2 && d.head_dim >= 64 && d.head_dim <= 256 && d.head_dim % 8 == 0 && d.num_blocks <= 0x7fffffff && d.block_tokens % 8 == 0;
 }
-int attend_map_tokens() { return kSlice; }
+int attend_map_box(const pdkv_pool_desc &d) { return std::gcd(d.block_tokens, kSlice); }
 
 cudaError_t launch_attend(const AttnParams &p, const void *map, int dtype, cudaStream_t stream)
 {

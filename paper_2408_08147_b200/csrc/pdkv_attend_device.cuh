@@ -42,6 +42,7 @@ __device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnItem &seg
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+constexpr float kGrowth = 8.f;                    // log2 of how far a maximum may run ahead of its base
 constexpr long long kWaitCycles = 2000000000;   // a wait gives up after a second
 
 __device__ __forceinline__ void mbar_init(uint64_t *b, int count)

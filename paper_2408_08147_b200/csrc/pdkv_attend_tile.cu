@@ -13,6 +13,7 @@
 // O is rescaled only when a row's maximum grew by more than 2^8 since the last time: the weights stay below
 // 2^8, where 16-bit and 32-bit floating point lose nothing.  Maxima and sums are 32 bits, the sums taken
 // before the weights are rounded.
+#include <numeric>
 #include <type_traits>
 
 #include <cuda.h>
@@ -26,7 +27,6 @@ namespace {
 constexpr int kTileRows = 128, kTileTokens = 128;
 constexpr int kSoftmaxThreads = 128;                          // of one row tile
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kTileThreads = 320;
-constexpr float kGrowth = 8.f;                                // log2 of how far a maximum may run ahead of its base
 
 // Tensor memory columns: S (and P over it) of tile t, O of tile t.
 constexpr uint32_t kColS = 0, kColO = 256, kColTile = 128, kColumns = 512;
@@ -170,8 +170,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     bool dead = false;
 
     if (warp == kLoadWarp) {
-        // K(0), V(0), K(1), V(1) ... into the ring; a lane loads a page (or its 128 tokens)
-        const int page_rows = min(p.pool.block_tokens, kTileTokens);
+        // K(0), V(0), K(1), V(1) ... into the ring; a lane loads a box of tokens within one block
+        const int page_rows = p.tile_box;
         uint32_t n = 0;
         for (int i = first; i < end; ++i) {
             const Work w = work_of(p, i);
@@ -478,15 +478,12 @@ template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const
 
 }  // namespace
 
-// Rows of 64 to 128 dims, and pages that whole tiles consist of or that consist of whole tiles.
+// Rows of 64 to 128 dims, blocks of a multiple of 8 tokens (the period of the swizzle).
 bool attend_tile_supported(const pdkv_pool_desc &d)
 {
-    const int B = d.block_tokens;
-    return d.elem_bytes == 2 && d.head_dim >= 64 && d.head_dim <= 128 && d.head_dim % 8 == 0 &&
-           (B >= kTileTokens ? B % kTileTokens == 0 : B >= 8 && kTileTokens % B == 0) && d.num_blocks <= 0x7fffffff;
+    return d.elem_bytes == 2 && d.head_dim >= 64 && d.head_dim <= 128 && d.head_dim % 8 == 0 && d.block_tokens % 8 == 0 && d.num_blocks <= 0x7fffffff;
 }
-
-int attend_tile_box(const pdkv_pool_desc &d) { return d.block_tokens < kTileTokens ? d.block_tokens : kTileTokens; }
+int attend_tile_box(const pdkv_pool_desc &d) { return std::gcd(d.block_tokens, kTileTokens); }
 
 // A map of the pool whose boxes are 64 dims of `box_tokens` tokens of one head.
 bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out)

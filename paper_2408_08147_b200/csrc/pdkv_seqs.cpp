@@ -283,7 +283,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             bool tile_ok = pdkv::attend_tile_supported(g);
             if (!pdkv::tunables().dry_run) {
                 tile_ok = tile_ok && pdkv::make_attend_map(*pool, pdkv::attend_tile_box(g), s->map[1]);
-                s->use_map = pdkv::attend_map_supported(g) && pdkv::make_attend_map(*pool, pdkv::attend_map_tokens(), s->map[0]);
+                s->use_map = pdkv::attend_map_supported(g) && pdkv::make_attend_map(*pool, pdkv::attend_map_box(g), s->map[0]);
             }
             std::vector<Shape> shape;
             for (int32_t n : n_rows) shape.push_back(shape_of(n, tile_ok));
@@ -502,6 +502,8 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         p.cta_tile_items = s->d_cta_items[1];
         p.n_tile_ctas = (int32_t)s->cta_items[1].size() - 1;
         p.use_map = s->use_map;
+        p.map_box = pdkv::attend_map_box(s->pool.d);
+        p.tile_box = pdkv::attend_tile_box(s->pool.d);
         p.map_layer_major = s->pool.d.layout == PDKV_LAYOUT_LAYER_MAJOR;
         p.status = s->d_status;
         p.n_seq = s->n_seq;

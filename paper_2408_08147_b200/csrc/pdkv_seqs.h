@@ -71,6 +71,7 @@ struct AttnParams {
     const int32_t *cta_tile_items;
     int32_t n_tile_ctas;
     int32_t use_map;                 // the warp kernel loads through the tensor map
+    int32_t map_box, tile_box;       // tokens of a box of the two maps
     int32_t map_layer_major;         // order of the coordinates of the pool's tensor map
     unsigned long long *status;      // [0] != 0: a bounded wait gave up
     int32_t n_seq, H, G, D, q_tokens;
@@ -93,7 +94,7 @@ struct AttnParams {
 
 int attend_ctas_per_sm(int head_dim);
 bool attend_map_supported(const pdkv_pool_desc &d);
-int attend_map_tokens();
+int attend_map_box(const pdkv_pool_desc &d);
 cudaError_t launch_attend(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 // The tile kernel (tcgen05): segments with many rows.  `map` is a CUtensorMap of the pool.
 constexpr int kMapBytes = 128;
