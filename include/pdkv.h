@@ -460,7 +460,7 @@ typedef struct {
     int64_t scores_out_stride[2];
 } pdkv_attend_args;
 
-/* Scratch bytes one pdkv_attend() call needs.  The scratch is the caller's; calls that may
+/* Scratch bytes one pdkv_attend() call needs (device, 32-byte aligned).  The scratch is the caller's; calls that may
  * run at the same time need one each.  Nothing in it outlives the call. */
 int pdkv_attend_scratch(const pdkv_seqs *seqs, int with_scores, size_t *bytes);
 /* Enqueues only (no allocation, copy or synchronisation): it can be recorded into a CUDA

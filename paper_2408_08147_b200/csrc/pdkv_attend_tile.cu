@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kTileRows = 128, kTileTokens = 128;
 constexpr int kSoftmaxThreads = 128;                          // of one row tile
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kTileThreads = 320;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kTileThreads = 384;   // (warps 10 and 11 only give up their registers)
 
 // Tensor memory columns: S (and P over it) of tile t, O of tile t.
 constexpr uint32_t kColS = 0, kColO = 256, kColTile = 128, kColumns = 512;
@@ -63,18 +63,15 @@ __device__ __forceinline__ void tmem_load(float (&v)[32], uint32_t at)
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(at));
 }
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_store32(uint32_t at, const float (&v)[32])
+__device__ __forceinline__ void tmem_load16(float (&v)[16], uint32_t at)
 {
-    const uint32_t *r = reinterpret_cast<const uint32_t *>(v);
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
-        "%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
-        "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
-        "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at));
 }
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16])
 {
     asm volatile(
@@ -84,6 +81,27 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
         : "memory");
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two 32-bit numbers at a time.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)),
+        "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return d;
+}
+// 32 bytes: a whole sector per lane.
+__device__ __forceinline__ void store8(float *to, const float *v)
+{
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]),
+                 "f"(v[6]), "f"(v[7]) : "memory");
+}
 
 // Shared-memory operand in the 128-byte swizzle: 8-row groups 1024 bytes apart.  K-major (Q, K: a row is 64
 // dims of one token): the leading offset is not used.  MN-major (V: a row is 64 dims, tokens run along
@@ -169,6 +187,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     const int first = p.cta_tile_items[blockIdx.x], end = p.cta_tile_items[blockIdx.x + 1];
     bool dead = false;
 
+    // 168 registers a thread at launch: the softmax threads, which hold a row of S, take 216, the others keep 72
+    // (256 x 216 + 128 x 72 = 384 x 168).
+    if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == kLoadWarp) {
         // K(0), V(0), K(1), V(1) ... into the ring; a lane loads a box of tokens within one block
         const int page_rows = p.tile_box;
@@ -263,7 +285,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             }
         }
         __syncwarp();
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // softmax of row tile t: one thread a row
         const int t = warp / 4, r = threadIdx.x % kSoftmaxThreads;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
@@ -272,22 +296,28 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
         uint32_t s_phase = 0, o_phase = 0, n = 0;
         int q_of = -1;
-        auto load_q = [&](const Work &w) {
-            const int row = t * kTileRows + r;
-            const bool live = row < w.it.rows;
-            const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
-            const T *q = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2];
+        auto load_q = [&](const Work &w) {   // a warp loads its 32 rows, DP / 8 neighbouring lanes a row
+            constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
+            const int mine = t * kTileRows + r;
+            const bool live = mine < w.it.rows;
+            const RowId id = row_id(p, w.it, w.it.row0 + (live ? mine : 0));
+            const int64_t at = live ? id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2] : -1;
+            const int c = lane % kLanes;
+            uint4 v[32 / kRows];
 #pragma unroll
-            for (int c = 0; c < DP / 8; ++c) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (live && 8 * c < p.D) {
-                    v = *reinterpret_cast<const uint4 *>(q + 8 * c);
-                    v.x ^= flip;
-                    v.y ^= flip;
-                    v.z ^= flip;
-                    v.w ^= flip;
-                }
-                *reinterpret_cast<uint4 *>(smem + t * G::kOperand + c / 8 * G::kSub + r * 128 + ((c % 8) ^ (r % 8)) * 16) = v;
+            for (int k = 0; k < 32 / kRows; ++k) {
+                const int64_t from = __shfl_sync(~0u, at, k * kRows + lane / kLanes);
+                v[k] = make_uint4(0, 0, 0, 0);
+                if (from >= 0 && 8 * c < p.D) v[k] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + from + 8 * c);
+            }
+#pragma unroll
+            for (int k = 0; k < 32 / kRows; ++k) {
+                const int row = warp % 4 * 32 + k * kRows + lane / kLanes;
+                v[k].x ^= flip;
+                v[k].y ^= flip;
+                v[k].z ^= flip;
+                v[k].w ^= flip;
+                *reinterpret_cast<uint4 *>(smem + t * G::kOperand + c / 8 * G::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16) = v[k];
             }
             fence_async_smem();
             mbar_arrive(&bar.q_ready[t]);
@@ -330,20 +360,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         }
                         fence_async_smem();
                     }
-                    float v[32], top = -INFINITY;
+                    float v[kTileTokens];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        tmem_load(v, s_at + 32 * c);
-                        tmem_load_wait();
-                        if (masked) {
+                    for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
+                    tmem_load_wait();
+                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    if (masked) {
 #pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (t0 + 32 * c + k < sees) top = fmaxf(top, v[k]);
-                        } else {
+                        for (int k = 0; k < kTileTokens; ++k)
+                            if (t0 + k < sees) tops[k % 4] = fmaxf(tops[k % 4], v[k]);
+                    } else {
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) top = fmaxf(top, v[k]);
-                        }
+                        for (int k = 0; k < kTileTokens; ++k) tops[k % 4] = fmaxf(tops[k % 4], v[k]);
                     }
+                    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     top = top == -INFINITY ? top : top * scale;
                     if (__any_sync(~0u, top > m + kGrowth || (m == -INFINITY && top > m))) {
                         const float new_m = fmaxf(m, top), f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
@@ -351,52 +381,52 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         m = new_m;
                         if (j > 0) {
 #pragma unroll 1
-                            for (int c = 0; c < DP / 32; ++c) {
-                                tmem_load(v, o_at + 32 * c);
+                            for (int c = 0; c < DP / 16; ++c) {
+                                float x[16];
+                                tmem_load16(x, o_at + 16 * c);
                                 tmem_load_wait();
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) v[k] *= f;
-                                tmem_store32(o_at + 32 * c, v);
+                                for (int k = 0; k < 16; ++k) x[k] *= f;
+                                tmem_store16(o_at + 16 * c, reinterpret_cast<uint32_t(&)[16]>(x));
                             }
                             tmem_store_wait();
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
+                    if (logits) {
+#pragma unroll
+                        for (int k = 0; k < kTileTokens; k += 4)
+                            if (t0 + k < w.limit) {
+                                float4 z;
+                                z.x = t0 + k < sees ? v[k] * scale : -INFINITY;
+                                z.y = t0 + k + 1 < sees ? v[k + 1] * scale : -INFINITY;
+                                z.z = t0 + k + 2 < sees ? v[k + 2] * scale : -INFINITY;
+                                z.w = t0 + k + 3 < sees ? v[k + 3] * scale : -INFINITY;
+                                *reinterpret_cast<float4 *>(logits + t0 + k) = z;
+                            }
+                    }
+                    __syncwarp();
+                    float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    const float2 scale2 = make_float2(scale, scale), base2 = make_float2(-base, -base);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        tmem_load(v, s_at + 32 * c);
-                        tmem_load_wait();
-                        if (logits) {
-                            const int tc = t0 + 32 * c;
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4)
-                                if (tc + k < w.limit) {
-                                    float4 z;
-                                    z.x = tc + k < sees ? v[k] * scale : -INFINITY;
-                                    z.y = tc + k + 1 < sees ? v[k + 1] * scale : -INFINITY;
-                                    z.z = tc + k + 2 < sees ? v[k + 2] * scale : -INFINITY;
-                                    z.w = tc + k + 3 < sees ? v[k + 3] * scale : -INFINITY;
-                                    *reinterpret_cast<float4 *>(logits + tc + k) = z;
-                                }
-                        }
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) v[k] = pow2(fmaf(v[k], scale, -base));
-                        if (masked) {
-#pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (t0 + 32 * c + k >= sees) v[k] = 0.f;
-                        }
-                        float sum = 0.f;
                         uint32_t packed[16];
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
-                            sum += v[2 * k] + v[2 * k + 1];
-                            packed[k] = pack<T>(v[2 * k], v[2 * k + 1]);
+                            const int i0 = 32 * c + 2 * k;
+                            float2 x = fma2(make_float2(v[i0], v[i0 + 1]), scale2, base2);
+                            x.x = pow2(x.x);
+                            x.y = pow2(x.y);
+                            if (masked) {
+                                if (t0 + i0 >= sees) x.x = 0.f;
+                                if (t0 + i0 + 1 >= sees) x.y = 0.f;
+                            }
+                            sums[k % 2] = add2(sums[k % 2], x);
+                            packed[k] = pack<T>(x.x, x.y);
                         }
-                        l += sum;
-                        __syncwarp();
                         tmem_store16(s_at + 16 * c, packed);
                     }
+                    l += sums[0].x + sums[0].y + (sums[1].x + sums[1].y);
                     tmem_store_wait();
                     fence_before();
                     mbar_arrive(&bar.p_ready[t]);
@@ -444,8 +474,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 } else {
                     float *o = p.part_o + (w.it.part_row + row) * p.D + 32 * c;
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4)
-                        if (32 * c + k < p.D) *reinterpret_cast<float4 *>(o + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+                    for (int k = 0; k < 32; k += 8)
+                        if (32 * c + k < p.D) store8(o + k, v + k);
                 }
             }
             if (live && !dead) {

@@ -483,7 +483,7 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
             }
         }
         const ScratchLayout l = scratch_layout(s, scores);
-        if (l.bytes && (!scratch || !aligned(scratch, 16))) return PDKV_ERR_INVALID_ARG;
+        if (l.bytes && (!scratch || !aligned(scratch, 32))) return PDKV_ERR_INVALID_ARG;
         if (scratch_bytes < l.bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
         if (!s->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0) return PDKV_OK;
