@@ -33,11 +33,6 @@ struct RingBarriers {
     uint64_t full[12], empty[12];
 };
 
-// 16 bytes to shared memory; with `there` false zeros are written and nothing is read.
-__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool there)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
-}
 // This thread's arrival, once its copies so far have landed.
 __device__ __forceinline__ void copy_arrive(uint64_t *b)
 {
@@ -92,15 +87,16 @@ __device__ __forceinline__ int slices_of(const AttnParams &p, const AttnItem &it
 // each row looked up by its own lane.  It runs ahead of the computing warps across items, so memory stays
 // busy while they join their results.
 template <int DP>
-__device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorMap *map, uint32_t ring, RingBarriers &bar, int first, int end)
+__device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorMap *map, uint32_t ring, RingBarriers &bar, AttnItem it)
 {
     using R = Ring<DP>;
     const int lane = threadIdx.x % 32;
     const int cols = (p.D + 15) / 16 * 2;   // 16-byte pieces of a row; one past the row's end is filled with zeros
     bool dead = false;
     uint32_t slot = 0, parity = 1;
-    for (int i = first; i < end; ++i) {
-        const AttnItem it = p.items[i];
+    for (bool more = true; more;) {
+        const AttnItem next_it = fetch_item(p.items, max(it.next, 0));   // in flight while this one is worked on
+        more = it.next >= 0;
         int len, limit;
         const int count = slices_of(p, it, &len, &limit);
         if (p.use_map) {
@@ -135,6 +131,7 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
                     parity ^= 1;
                 }
             }
+            it = next_it;
             continue;
         }
         const char *base = p.pool.base + 2 * (int64_t)p.layer * p.pool.lc_stride + it.head * p.pool.head_stride;
@@ -173,6 +170,7 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
                 parity ^= 1;
             }
         }
+        it = next_it;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
@@ -456,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
     __shared__ RingBarriers bar;
     __shared__ __align__(16) float sml[4][16][2];
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
-    const int first = p.cta_items[blockIdx.x], end = p.cta_items[blockIdx.x + 1];
+    AttnItem it = fetch_item(p.items, blockIdx.x);
     asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x < R::kSlots) {
         mbar_init(&bar.full[threadIdx.x], p.use_map ? 1 : 32);
@@ -465,25 +463,30 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
     }
     __syncthreads();
     if (threadIdx.x >= kConsumers) {
-        load_slices<DP>(p, &map, smem_u32(smem), bar, first, end);
-        return;
+        load_slices<DP>(p, &map, smem_u32(smem), bar, it);
+    } else {
+        bool dead = false;
+        uint32_t n = 0;
+        for (bool more = true; more;) {
+            const AttnItem next_it = fetch_item(p.items, max(it.next, 0));
+            more = it.next >= 0;
+            int len, limit;
+            const int slices = slices_of(p, it, &len, &limit);
+            if (it.rows <= 8)
+                attend_item<T, DP, FULL, 1, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+            else if (it.rows <= 16)
+                attend_item<T, DP, FULL, 2, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+            else if (it.rows <= 32)
+                attend_item<T, DP, FULL, 2, 2>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+            else
+                attend_item<T, DP, FULL, 2, 4>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+            n += slices;
+            it = next_it;
+        }
     }
-    bool dead = false;
-    uint32_t n = 0;
-    for (int i = first; i < end; ++i) {
-        const AttnItem it = p.items[i];
-        int len, limit;
-        const int slices = slices_of(p, it, &len, &limit);
-        if (it.rows <= 8)
-            attend_item<T, DP, FULL, 1, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
-        else if (it.rows <= 16)
-            attend_item<T, DP, FULL, 2, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
-        else if (it.rows <= 32)
-            attend_item<T, DP, FULL, 2, 2>(p, it, slices, len, limit, smem, sml, bar, n, dead);
-        else
-            attend_item<T, DP, FULL, 2, 4>(p, it, slices, len, limit, smem, sml, bar, n, dead);
-        n += slices;
-    }
+    // This kernel may run beside the tile kernel launched before it, which it does not depend on; whoever waits for
+    // this one has to find both complete.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 namespace {
@@ -541,15 +544,15 @@ template <int W> __device__ __forceinline__ float2 joined_ml(const AttnParams &p
     return make_float2(m, l);
 }
 
-constexpr int kScoreChunk = 512;   // tokens of one block of the score part
+constexpr int kScoreChunk = 128;   // tokens of one block of the score part
 constexpr int kScoreRows = 64;     // rows whose lse is held at a time
 
 }  // namespace
 
 // The first `row_blocks` blocks of a (sequence, head) join the parts of four rows each, a warp per row:
 // m = max m_p, l = sum l_p 2^(m_p - m), O = sum O_p 2^(m_p - m).  The others turn the logits of a chunk of
-// tokens into weights 2^(z - lse) and add them to the scores; they take the lse from the parts themselves
-// (eight lanes a row), so no block waits for another.
+// tokens into weights 2^(z - lse) and add them to the scores, a warp every fourth row; they take the lse from
+// the parts themselves, so no block waits for another.
 template <typename T>
 __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, const int row_blocks, const int chunks)
 {
@@ -596,41 +599,46 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
         return;
     }
     __shared__ float lse[kScoreRows];
-    const int chunk = x - row_blocks, len = own_len(p, seq, s.len), t0 = chunk * kScoreChunk + 4 * threadIdx.x;
+    __shared__ float4 sums[4][32];
+    const int chunk = x - row_blocks, len = own_len(p, seq, s.len), t0 = chunk * kScoreChunk + 4 * lane;
     // past the sequence's end there is no weight: nothing to do in place, else the row is carried over
     const int width = p.scores_in == p.scores_out ? len : p.max_len;
     if (chunk * kScoreChunk >= width) return;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int r0 = 0; r0 < R; r0 += kScoreRows) {
         const int n = min(kScoreRows, R - r0);
         __syncthreads();
-        for (int r = warp * 4; r < n; r += 16) {
-            const int row = r + lane / 8;
-            const float2 ml = joined_ml<8>(p, parts_of(p, s, head, r0 + min(row, n - 1)), lane);
+        for (int r = warp * 8; r < n; r += 32) {
+            const int row = r + lane / 4;
+            const float2 ml = joined_ml<4>(p, parts_of(p, s, head, r0 + min(row, n - 1)), lane);
             // an empty row gives no weight to anything: 2^(z - inf) = 0
-            if (lane % 8 == 0 && row < n) lse[row] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+            if (lane % 4 == 0 && row < n) lse[row] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
         }
         __syncthreads();
         const float *z = p.logits + s.logits + ((int64_t)head * R + r0) * s.logit_stride + t0;
-        if (t0 < len) {
-#pragma unroll 4
-            for (int row = 0; row < n; ++row) {
+        if (t0 < len) {   // a warp takes every fourth row
+#pragma unroll 8
+            for (int row = warp; row < n; row += 4) {
                 const float4 v = *reinterpret_cast<const float4 *>(z + (int64_t)row * s.logit_stride);
                 const float e = lse[row];
-                sum[0] += pow2(v.x - e);
-                sum[1] += pow2(v.y - e);
-                sum[2] += pow2(v.z - e);
-                sum[3] += pow2(v.w - e);
+                sum.x += pow2(v.x - e);
+                sum.y += pow2(v.y - e);
+                sum.z += pow2(v.z - e);
+                sum.w += pow2(v.w - e);
             }
         }
     }
+    sums[warp][lane] = sum;
+    __syncthreads();
+    const int t = chunk * kScoreChunk + threadIdx.x;
+    if (t < width) {
+        const float in = p.scores_in ? p.scores_in[seq * p.scores_in_stride[0] + head * p.scores_in_stride[1] + t] : 0.f;
+        float add = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (t0 + k < width) {
-            const float in = p.scores_in ? p.scores_in[seq * p.scores_in_stride[0] + head * p.scores_in_stride[1] + t0 + k] : 0.f;
-            // (what lies in the scratch behind the last token is no logit)
-            p.scores_out[seq * p.scores_out_stride[0] + head * p.scores_out_stride[1] + t0 + k] = t0 + k < len ? in + sum[k] : in;
-        }
+        for (int w = 0; w < 4; ++w) add += reinterpret_cast<const float *>(sums[w])[threadIdx.x];
+        // (what lies in the scratch behind the last token is no logit)
+        p.scores_out[seq * p.scores_out_stride[0] + head * p.scores_out_stride[1] + t] = t < len ? in + add : in;
+    }
 }
 
 namespace {
@@ -640,8 +648,17 @@ template <typename T, int DP, bool FULL> cudaError_t launch_dims(const AttnParam
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_shared(attend_items_kernel<T, DP, FULL>, Ring<DP>::kBytes, ready);
     if (e != cudaSuccess) return e;
-    attend_items_kernel<T, DP, FULL><<<p.n_ctas, kThreads, Ring<DP>::kBytes, stream>>>(map, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.n_ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Ring<DP>::kBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // beside the tile kernel, if there is one
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = p.n_tile_ctas > 0 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, attend_items_kernel<T, DP, FULL>, map, p);
 }
 
 template <typename T> cudaError_t launch_type(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)

@@ -21,6 +21,16 @@ __device__ __forceinline__ int own_len(const AttnParams &p, int seq, int cap)
     return n < 0 ? 0 : (n < cap ? n : cap);
 }
 
+__device__ __forceinline__ AttnItem fetch_item(const AttnItem *items, int i)
+{
+    AttnItem it;
+    const uint4 *from = reinterpret_cast<const uint4 *>(items + i);
+    uint4 *to = reinterpret_cast<uint4 *>(&it);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) to[k] = __ldg(from + k);
+    return it;
+}
+
 struct RowId {
     int seq, token, g;
 };
@@ -85,6 +95,11 @@ __device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap *map, in
                  "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_u32(bar)) : "memory");
 }
 
+// 16 bytes to shared memory; with `there` false zeros are written and nothing is read.
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi)
 {

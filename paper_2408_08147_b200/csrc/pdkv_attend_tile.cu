@@ -36,7 +36,8 @@ template <int DP> struct TileShape {
     static constexpr uint32_t kSub = 128 * 128;               // bytes of 128 such rows
     static constexpr uint32_t kOperand = kSubs * kSub;        // one tile of Q, K or V
     static constexpr int kSlots = DP == 64 ? 8 : 4;           // K and V tiles in flight, in turns
-    static constexpr uint32_t kBytes = 2 * kOperand + kSlots * kOperand + 1024;
+    static constexpr uint32_t kStage = 8 * 4096;              // a warp's way out: 32 rows of 32 dims
+    static constexpr uint32_t kBytes = 2 * kOperand + kSlots * kOperand + kStage + 1024;
 };
 
 struct Barriers {
@@ -96,13 +97,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
     return d;
 }
-// 32 bytes: a whole sector per lane.
-__device__ __forceinline__ void store8(float *to, const float *v)
-{
-    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]),
-                 "f"(v[6]), "f"(v[7]) : "memory");
-}
-
 // Shared-memory operand in the 128-byte swizzle: 8-row groups 1024 bytes apart.  K-major (Q, K: a row is 64
 // dims of one token): the leading offset is not used.  MN-major (V: a row is 64 dims, tokens run along
 // the product): the leading offset leads to the next 64 dims.
@@ -140,14 +134,14 @@ struct Work {
     AttnItem it;
     int len, limit, tiles, row_tiles;
 };
-__device__ __forceinline__ Work work_of(const AttnParams &p, int i)
+__device__ __forceinline__ Work work_of(const AttnParams &p, const AttnItem &it)
 {
     Work w;
-    w.it = p.tile_items[i];
-    w.len = w.it.seq >= 0 ? own_len(p, w.it.seq, w.it.len) : w.it.len;
-    w.limit = min(w.it.tok1, w.len);
-    w.tiles = w.limit > w.it.tok0 ? (w.limit - w.it.tok0 + kTileTokens - 1) / kTileTokens : 0;
-    w.row_tiles = w.it.rows > kTileRows ? 2 : 1;
+    w.it = it;
+    w.len = it.seq >= 0 ? own_len(p, it.seq, it.len) : it.len;
+    w.limit = min(it.tok1, w.len);
+    w.tiles = w.limit > it.tok0 ? (w.limit - it.tok0 + kTileTokens - 1) / kTileTokens : 0;
+    w.row_tiles = it.rows > kTileRows ? 2 : 1;
     return w;
 }
 
@@ -162,6 +156,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
     const uint32_t q_at = smem_u32(smem), ring_at = q_at + 2 * G::kOperand;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const AttnItem first = fetch_item(p.tile_items, blockIdx.x);
     if (threadIdx.x == 0) {
         for (int i = 0; i < G::kSlots; ++i) {
             mbar_init(&bar.full[i], 1);
@@ -184,7 +179,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     fence_after();
     asm volatile("griddepcontrol.launch_dependents;");
     const uint32_t tmem = bar.tmem;
-    const int first = p.cta_tile_items[blockIdx.x], end = p.cta_tile_items[blockIdx.x + 1];
     bool dead = false;
 
     // 168 registers a thread at launch: the softmax threads, which hold a row of S, take 216, the others keep 72
@@ -195,8 +189,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         // K(0), V(0), K(1), V(1) ... into the ring; a lane loads a box of tokens within one block
         const int page_rows = p.tile_box;
         uint32_t n = 0;
-        for (int i = first; i < end; ++i) {
-            const Work w = work_of(p, i);
+        AttnItem it = first;
+        for (bool more = true; more;) {
+            const AttnItem next_it = fetch_item(p.tile_items, max(it.next, 0));
+            more = it.next >= 0;
+            const Work w = work_of(p, it);
+            it = next_it;
             for (int j = 0; j < w.tiles; ++j) {
                 const int t0 = w.it.tok0 + j * kTileTokens, live = min(kTileTokens, w.limit - t0);
                 const int boxes = (live + page_rows - 1) / page_rows;   // pages past the end are not loaded
@@ -245,8 +243,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 for (int s = 0; s < kTileTokens / 16; ++s)
                     mma_tensor(tmem + kColO + t * kColTile, tmem + kColS + t * kColTile + 8 * s, operand(v + s * 2048, G::kSub), kWordO, add || s > 0);
             };
-            for (int i = first; i < end; ++i) {
-                const Work w = work_of(p, i);
+            AttnItem it = first;
+            for (bool more = true; more;) {
+                const AttnItem next_it = fetch_item(p.tile_items, max(it.next, 0));
+                more = it.next >= 0;
+                const Work w = work_of(p, it);
+                it = next_it;
                 if (w.tiles == 0) continue;
                 uint32_t k_slot = n % G::kSlots;
                 mbar_wait(&bar.full[k_slot], n / G::kSlots & 1, dead, p.status);
@@ -295,7 +297,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         const float scale = fabsf(p.scale_log2);
         const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
         uint32_t s_phase = 0, o_phase = 0, n = 0;
-        int q_of = -1;
+        bool q_there = false;
+        // A warp's 32 rows of 32 numbers leave by way of shared memory: a lane has a row, but eight neighbouring lanes
+        // store 128 bytes of one row (lanes storing their own rows touched 32 sectors an instruction: 8000 cycles
+        // for a tile of O).  f(row of the warp, number of the first of four columns, the four numbers).
+        char *stage = smem + (2 + G::kSlots) * G::kOperand + warp * 4096;
+        auto by_rows = [&](const float *v, auto &&f) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                *reinterpret_cast<float4 *>(stage + lane * 128 + ((k ^ (lane % 8)) * 16)) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r4 = 4 * k + lane / 8;
+                f(r4, 4 * (lane % 8), *reinterpret_cast<const float4 *>(stage + r4 * 128 + (((lane % 8) ^ (r4 % 8)) * 16)));
+            }
+            __syncwarp();
+        };
         auto load_q = [&](const Work &w) {   // a warp loads its 32 rows, DP / 8 neighbouring lanes a row
             constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
             const int mine = t * kTileRows + r;
@@ -303,27 +321,33 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const RowId id = row_id(p, w.it, w.it.row0 + (live ? mine : 0));
             const int64_t at = live ? id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2] : -1;
             const int c = lane % kLanes;
-            uint4 v[32 / kRows];
-#pragma unroll
-            for (int k = 0; k < 32 / kRows; ++k) {
-                const int64_t from = __shfl_sync(~0u, at, k * kRows + lane / kLanes);
-                v[k] = make_uint4(0, 0, 0, 0);
-                if (from >= 0 && 8 * c < p.D) v[k] = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + from + 8 * c);
-            }
-#pragma unroll
+            // 16 bytes a lane, zeros for rows that are not there; all copies of the warp are in flight together
+#pragma unroll 4
             for (int k = 0; k < 32 / kRows; ++k) {
                 const int row = warp % 4 * 32 + k * kRows + lane / kLanes;
-                v[k].x ^= flip;
-                v[k].y ^= flip;
-                v[k].z ^= flip;
-                v[k].w ^= flip;
-                *reinterpret_cast<uint4 *>(smem + t * G::kOperand + c / 8 * G::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16) = v[k];
+                const int64_t from = __shfl_sync(~0u, at, k * kRows + lane / kLanes);
+                const bool there = from >= 0 && 8 * c < p.D;
+                copy_async(smem_u32(smem + t * G::kOperand + c / 8 * G::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16),
+                           static_cast<const T *>(p.q) + (there ? from + 8 * c : 0), there);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (flip) {   // (a lane turns the signs of what it brought itself)
+#pragma unroll 1
+                for (int k = 0; k < 32 / kRows; ++k) {
+                    const int row = warp % 4 * 32 + k * kRows + lane / kLanes;
+                    uint4 *x = reinterpret_cast<uint4 *>(smem + t * G::kOperand + c / 8 * G::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16);
+                    *x = make_uint4(x->x ^ flip, x->y ^ flip, x->z ^ flip, x->w ^ flip);
+                }
             }
             fence_async_smem();
             mbar_arrive(&bar.q_ready[t]);
         };
-        for (int i = first; i < end; ++i) {
-            const Work w = work_of(p, i);
+        AttnItem it = first;
+        for (bool more = true; more;) {
+            const AttnItem next_it = fetch_item(p.tile_items, max(it.next, 0));
+            more = it.next >= 0;
+            const Work w = work_of(p, it);
+            it = next_it;
             const uint32_t n0 = n;
             n += 2 * w.tiles;
             if (t >= w.row_tiles) continue;
@@ -332,13 +356,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             float m = -INFINITY, l = 0.f;
             if (w.tiles > 0) {
-                if (q_of != i) load_q(w);
+                if (!q_there) load_q(w);
+                q_there = false;
                 const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;
                 const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
-                float *logits = nullptr;
-                if (p.logits && own && live) {
+                const bool with_logits = p.logits && own;
+                int64_t logit_row = -1;   // where this row's logits go
+                if (with_logits && live) {
                     const AttnSeq s = p.seqs[w.it.seq];
-                    logits = p.logits + s.logits + ((int64_t)w.it.head * p.G * p.q_tokens + w.it.row0 + row) * s.logit_stride;
+                    logit_row = s.logits + ((int64_t)w.it.head * p.G * p.q_tokens + w.it.row0 + row) * s.logit_stride;
                 }
                 for (int j = 0; j < w.tiles; ++j) {
                     const int t0 = w.it.tok0 + j * kTileTokens;
@@ -393,17 +419,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
-                    if (logits) {
+                    if (with_logits) {
 #pragma unroll
-                        for (int k = 0; k < kTileTokens; k += 4)
-                            if (t0 + k < w.limit) {
-                                float4 z;
-                                z.x = t0 + k < sees ? v[k] * scale : -INFINITY;
-                                z.y = t0 + k + 1 < sees ? v[k + 1] * scale : -INFINITY;
-                                z.z = t0 + k + 2 < sees ? v[k + 2] * scale : -INFINITY;
-                                z.w = t0 + k + 3 < sees ? v[k + 3] * scale : -INFINITY;
-                                *reinterpret_cast<float4 *>(logits + t0 + k) = z;
-                            }
+                        for (int c = 0; c < 4; ++c) {
+                            float z[32];
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) z[k] = t0 + 32 * c + k < sees ? v[32 * c + k] * scale : -INFINITY;
+                            by_rows(z, [&](int r4, int col, float4 x) {
+                                const int64_t at = __shfl_sync(~0u, logit_row, r4);
+                                const int tok = t0 + 32 * c + col;
+                                if (at >= 0 && tok < w.limit) *reinterpret_cast<float4 *>(p.logits + at + tok) = x;
+                            });
+                        }
                     }
                     __syncwarp();
                     float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -432,11 +459,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     mbar_arrive(&bar.p_ready[t]);
                 }
                 // every product with Q is done: the next item's Q may take its place
-                if (i + 1 < end) {
-                    const Work next = work_of(p, i + 1);
+                if (more) {
+                    const Work next = work_of(p, next_it);
                     if (t < next.row_tiles && next.tiles > 0) {
                         load_q(next);
-                        q_of = i + 1;
+                        q_there = true;
                     }
                 }
                 mbar_wait(&bar.o_full[t], o_phase, dead, p.status);
@@ -446,7 +473,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             }
             const int head = w.it.head * p.G + id.g;
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            T *out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2];
+            const int64_t to = !live || dead ? -1
+                               : w.it.direct ? id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2]
+                                             : (w.it.part_row + row) * p.D;
+            // (loops that run once an item stay rolled: fetching their instructions costs more than running them)
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 float v[32];
@@ -458,25 +488,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = 0.f;
                 }
-                if (!live || dead) {
-                    // nothing to write
-                } else if (w.it.direct) {
+                const float f = w.it.direct ? inv : 1.f;
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        if (32 * c + k < p.D) {
-                            uint4 x;
-                            x.x = pack<T>(v[k] * inv, v[k + 1] * inv);
-                            x.y = pack<T>(v[k + 2] * inv, v[k + 3] * inv);
-                            x.z = pack<T>(v[k + 4] * inv, v[k + 5] * inv);
-                            x.w = pack<T>(v[k + 6] * inv, v[k + 7] * inv);
-                            *reinterpret_cast<uint4 *>(out + 32 * c + k) = x;
-                        }
-                } else {
-                    float *o = p.part_o + (w.it.part_row + row) * p.D + 32 * c;
-#pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        if (32 * c + k < p.D) store8(o + k, v + k);
-                }
+                for (int k = 0; k < 32; ++k) v[k] *= f;
+                by_rows(v, [&](int r4, int col, float4 x) {
+                    const int64_t at = __shfl_sync(~0u, to, r4);
+                    const int d = 32 * c + col;
+                    if (at >= 0 && d < p.D) {
+                        if (w.it.direct)
+                            *reinterpret_cast<uint2 *>(static_cast<T *>(p.out) + at + d) = make_uint2(pack<T>(x.x, x.y), pack<T>(x.z, x.w));
+                        else
+                            *reinterpret_cast<float4 *>(p.part_o + at + d) = x;
+                    }
+                });
             }
             if (live && !dead) {
                 if (w.it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (m + log2f(l)) * kLn2;

@@ -113,82 +113,167 @@ Shape shape_of(int64_t rows, bool tile_ok)
     return {0, rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile, 64};
 }
 
-// Work list of one kernel.  Units (segment, row tile, head) lie behind one another on an axis of cost -- token
-// quanta plus a constant for the start and the end of a unit -- and the CTAs take equal stretches of it.
-void plan_items(pdkv_seqs &s, int kernel, const std::vector<int32_t> &n_rows, const std::vector<Shape> &shape, std::vector<int32_t> &unit0,
-                int n_ctas_max)
+// What starting and finishing an item costs, in quanta of its kernel.  Measured: about 10000 cycles against
+// 2100 a quantum in the tile kernel, 3 us against 1.5 us (a CTA's share of the memory rate) in the warp kernel.
+constexpr int64_t kItemCost[2] = {2, 5};
+
+struct Unit { int32_t seg, head, row0, rows; int64_t quanta; };
+struct Piece { size_t unit; int64_t from, n; int32_t cta; };
+
+// Deals units to CTAs in order, each CTA up to a load of `most` quanta; units are cut where a CTA is full.
+// Returns false when that takes more than `n_ctas` CTAs.
+bool deal(const std::vector<Unit> &units, int64_t cost, int64_t most, int64_t n_ctas, bool cut, std::vector<Piece> *out)
 {
-    struct Work { int32_t seg, head, row0, rows; int64_t quanta; };
-    std::vector<Work> work;
-    const int32_t H = s.pool.d.num_kv_heads;
-    constexpr int64_t kOverhead = 1;
-    int64_t total = 0;
+    int64_t cta = 0, load = 0;
+    for (size_t u = 0; u < units.size(); ++u) {
+        int64_t q = 0;
+        while (q < units[u].quanta) {
+            int64_t room = most - load - cost;
+            if (load > 0 && (room < 1 || (!cut && room < units[u].quanta))) {
+                ++cta;
+                load = 0;
+                room = most - cost;
+            }
+            const int64_t n = std::min(units[u].quanta - q, std::max<int64_t>(room, 1));
+            if (cta >= n_ctas || n > room || (!cut && n < units[u].quanta)) return false;
+            if (out) out->push_back({u, q, n, (int32_t)cta});
+            load += cost + n;
+            q += n;
+        }
+    }
+    return true;
+}
+
+// Smallest load per CTA with which the units fit.
+int64_t least_load(const std::vector<Unit> &units, int64_t cost, int64_t n_ctas, bool cut)
+{
+    int64_t total = 0, most = 0;
+    for (const Unit &u : units) {
+        total += u.quanta + cost;
+        most = std::max(most, u.quanta + cost);
+    }
+    int64_t lo = std::max((total + n_ctas - 1) / n_ctas, cut ? cost + 1 : most), hi = total;
+    while (lo < hi) {
+        const int64_t mid = lo + (hi - lo) / 2;
+        if (deal(units, cost, mid, n_ctas, cut, nullptr))
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    return lo;
+}
+
+std::vector<Unit> units_of(const pdkv_seqs &s, int kernel, const std::vector<int32_t> &n_rows, const std::vector<Shape> &shape)
+{
+    std::vector<Unit> units;
     for (size_t g = 0; g < s.segs.size(); ++g) {
         const AttnSeg &seg = s.segs[g];
         if (shape[g].kernel != kernel || seg.len == 0 || n_rows[g] == 0) continue;
-        unit0[g] = (int32_t)(s.units.size() + work.size());
         for (int32_t r0 = 0; r0 < n_rows[g]; r0 += shape[g].row_tile)
-            for (int32_t h = 0; h < H; ++h) {
-                work.push_back({(int32_t)g, h, r0, std::min<int32_t>(shape[g].row_tile, n_rows[g] - r0),
-                                (seg.len + shape[g].quantum - 1) / shape[g].quantum});
-                total += work.back().quanta + kOverhead;
-            }
+            for (int32_t h = 0; h < s.pool.d.num_kv_heads; ++h)
+                units.push_back({(int32_t)g, h, r0, std::min<int32_t>(shape[g].row_tile, n_rows[g] - r0),
+                                 (seg.len + shape[g].quantum - 1) / shape[g].quantum});
+    }
+    return units;
+}
+
+// SMs for the tile kernel when both kernels have work: they run at the same time, each on SMs of its own (a CTA of
+// the tile kernel leaves no shared memory for others), and the slower one should be as quick as possible.
+// Measured on B200: 1.1 us a quantum of the tile kernel and 4 us around it; the warp kernel reads at up to 6.3
+// TB/s in all and 75 GB/s per SM, 5 us around it.
+int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std::vector<Unit> &tile_units)
+{
+    if (warp_units.empty()) return s.sm_count;
+    if (tile_units.empty()) return 0;
+    double tile = 0, bytes = 0;
+    for (const Unit &u : tile_units) tile += (double)(u.quanta + kItemCost[1]);
+    for (const Unit &u : warp_units) bytes += 64.0 * (double)u.quanta * 4 * s.pool.d.head_dim;
+    int best = 1;
+    double best_us = 1e30;
+    for (int n = 1; n < s.sm_count; ++n) {
+        const double tile_us = 4 + 1.1 * std::max((tile + kItemCost[1] * (double)n) / n, (double)(1 + kItemCost[1]));
+        const double warp_us = 5 + std::max(bytes / 6.3e6, bytes / (75e3 * (s.sm_count - n)));
+        if (std::max(tile_us, warp_us) < best_us) {
+            best_us = std::max(tile_us, warp_us);
+            best = n;
+        }
+    }
+    return best;
+}
+
+// Work list of one kernel.  Whole units when that is as quick as cutting them (nothing is to be joined then,
+// which saves a kernel: about two quanta more); CTAs get at least four quanta, so that joining stays cheap.
+void plan_items(pdkv_seqs &s, int kernel, const std::vector<Unit> &units, const std::vector<Shape> &shape, std::vector<int32_t> &unit0,
+                int n_ctas_max)
+{
+    int64_t quanta = 0;
+    for (size_t u = 0; u < units.size(); ++u) {
+        quanta += units[u].quanta;
+        if (unit0[(size_t)units[u].seg] < 0) unit0[(size_t)units[u].seg] = (int32_t)(s.units.size() + u);
     }
     std::vector<AttnItem> &items = s.items[kernel];
-    std::vector<int32_t> &cta_items = s.cta_items[kernel];
-    cta_items.assign(1, 0);
-    if (work.empty()) return;
-    // a CTA gets at least four quanta, so that joining the parts stays cheap beside reading the tokens
-    const int64_t n_ctas = std::max<int64_t>(1, std::min<int64_t>(n_ctas_max, total / 4));
-    int64_t at = 0, cta = 0;
-    for (const Work &w : work) {
+    if (units.empty()) return;
+    const int64_t cost = kItemCost[kernel], n_ctas = std::max<int64_t>(1, std::min<int64_t>(n_ctas_max, std::max<int64_t>(units.size(), quanta / 4)));
+    std::vector<Piece> pieces;
+    const int64_t cut = least_load(units, cost, n_ctas, true), whole = least_load(units, cost, n_ctas, false);
+    const bool keep_whole = whole <= cut + 2;
+    deal(units, cost, keep_whole ? whole : cut, n_ctas, !keep_whole, &pieces);
+    const size_t first_unit = s.units.size();
+    s.units.resize(first_unit + units.size());
+    for (const Piece &x : pieces) {
+        const Unit &w = units[x.unit];
+        const AttnSeg &seg = s.segs[(size_t)w.seg];
         const int64_t quantum = shape[(size_t)w.seg].quantum;
-        AttnUnit unit{};
-        unit.part_row = s.part_rows;
-        unit.rows = w.rows;
-        int64_t q = 0;
-        while (q < w.quanta) {
-            // `at` is where quantum q of this unit lies; this CTA's stretch ends at (cta + 1) * total / n_ctas
-            while (cta + 1 < n_ctas && at + kOverhead >= (cta + 1) * total / n_ctas) {
-                ++cta;
-                cta_items.push_back((int32_t)items.size());
-            }
-            int64_t n = w.quanta - q;
-            if (cta + 1 < n_ctas) n = std::min(n, (cta + 1) * total / n_ctas - at);
-            n = std::max<int64_t>(n, 1);
-            AttnItem it{};
-            it.part_row = s.part_rows;
-            it.tbl = s.segs[(size_t)w.seg].tbl;
-            it.seq = s.segs[(size_t)w.seg].seq;
-            it.member_begin = s.segs[(size_t)w.seg].member_begin;
-            it.len = s.segs[(size_t)w.seg].len;
-            it.head = w.head;
-            it.row0 = w.row0;
-            it.rows = w.rows;
-            it.tok0 = (int32_t)(q * quantum);
-            it.tok1 = (int32_t)std::min<int64_t>(s.segs[(size_t)w.seg].len, (q + n) * quantum);
-            items.push_back(it);
-            pdkv_attend_item li{};
-            li.prefix = w.seg >= s.n_seq ? w.seg - s.n_seq : -1;
-            li.seq = w.seg < s.n_seq ? w.seg : -1;
-            li.head = w.head;
-            li.row_begin = w.row0;
-            li.row_end = w.row0 + w.rows;
-            li.tok_begin = it.tok0;
-            li.tok_end = it.tok1;
-            li.kernel = kernel;
-            li.cta = (int32_t)cta;
-            s.listing.push_back(li);
-            s.part_rows += w.rows;
-            ++unit.n_parts;
-            q += n;
-            at += n;
-        }
-        s.units.push_back(unit);
-        at += kOverhead;
+        AttnUnit &unit = s.units[first_unit + x.unit];
+        if (x.from == 0) unit = {s.part_rows, 0, w.rows};
+        ++unit.n_parts;
+        AttnItem it{};
+        it.part_row = s.part_rows;
+        it.tbl = seg.tbl;
+        it.seq = seg.seq;
+        it.member_begin = seg.member_begin;
+        it.len = seg.len;
+        it.head = w.head;
+        it.row0 = w.row0;
+        it.rows = w.rows;
+        it.tok0 = (int32_t)(x.from * quantum);
+        it.tok1 = (int32_t)std::min<int64_t>(seg.len, (x.from + x.n) * quantum);
+        s.part_rows += w.rows;
+        pdkv_attend_item li{};
+        li.prefix = w.seg >= s.n_seq ? w.seg - s.n_seq : -1;
+        li.seq = w.seg < s.n_seq ? w.seg : -1;
+        li.head = w.head;
+        li.row_begin = w.row0;
+        li.row_end = w.row0 + w.rows;
+        li.tok_begin = it.tok0;
+        li.tok_end = it.tok1;
+        li.kernel = kernel;
+        li.cta = x.cta;
+        s.listing.push_back(li);
+        items.push_back(it);
+        s.item_cta[kernel].push_back(x.cta);
     }
-    while ((int64_t)cta_items.size() < n_ctas) cta_items.push_back((int32_t)items.size());
-    cta_items.push_back((int32_t)items.size());
+    s.n_ctas[kernel] = pieces.back().cta + 1;
+}
+
+// The list as the kernels read it: the first item of CTA c at place c, the CTA's further ones behind all
+// first ones, each item leading to the next.  A CTA starts on its first item after one load.
+std::vector<AttnItem> chain_items(const std::vector<AttnItem> &items, const std::vector<int32_t> &cta, int32_t n_ctas)
+{
+    std::vector<AttnItem> out((size_t)n_ctas);
+    size_t last = 0;
+    for (size_t i = 0; i < items.size(); ++i) {
+        size_t at = (size_t)cta[i];
+        if (i > 0 && cta[i] == cta[i - 1]) {
+            at = out.size();
+            out.push_back(AttnItem{});
+            out[last].next = (int32_t)at;
+        }
+        out[at] = items[i];
+        out[at].next = -1;
+        last = at;
+    }
+    return out;
 }
 
 }  // namespace
@@ -289,8 +374,10 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             for (int32_t n : n_rows) shape.push_back(shape_of(n, tile_ok));
             // unit of (row tile 0, head 0) of every segment
             std::vector<int32_t> unit0(s->segs.size(), -1);
-            plan_items(*s, 1, n_rows, shape, unit0, s->sm_count);
-            plan_items(*s, 0, n_rows, shape, unit0, pdkv::attend_ctas_per_sm(g.head_dim) * s->sm_count);
+            const std::vector<Unit> warp_units = units_of(*s, 0, n_rows, shape), tile_units = units_of(*s, 1, n_rows, shape);
+            const int sms = tile_sms(*s, warp_units, tile_units);
+            plan_items(*s, 1, tile_units, shape, unit0, sms);
+            plan_items(*s, 0, warp_units, shape, unit0, pdkv::attend_ctas_per_sm(g.head_dim) * std::max(1, s->sm_count - s->n_ctas[1]));
             s->seqs.resize((size_t)s->n_seq);
             for (int32_t r = 0; r < s->n_seq; ++r) {
                 AttnSeq &q = s->seqs[(size_t)r];
@@ -324,9 +411,10 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             return o;
         };
         const size_t o_status = place(16), o_tbl = place(tbl.size() * 4), o_members = place(members.size() * 4),
-                     o_cta[2] = {place(s->cta_items[0].size() * 4), place(s->cta_items[1].size() * 4)}, o_segs = place(s->segs.size() * sizeof(AttnSeg)), o_units = place(s->units.size() * sizeof(AttnUnit)),
+                     o_segs = place(s->segs.size() * sizeof(AttnSeg)), o_units = place(s->units.size() * sizeof(AttnUnit)),
                      o_seqs = place(s->seqs.size() * sizeof(AttnSeq)),
                      o_items[2] = {place(s->items[0].size() * sizeof(AttnItem)), place(s->items[1].size() * sizeof(AttnItem))};
+        static_assert(sizeof(AttnItem) == 64, "an item is fetched as four vectors");
         if (needed_bytes) *needed_bytes = bytes;
         if (workspace && workspace_bytes < bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
         if (!pdkv::tunables().dry_run) {
@@ -335,8 +423,8 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             put(o_tbl, tbl.data(), tbl.size() * 4);
             put(o_members, members.data(), members.size() * 4);
             for (int k = 0; k < 2; ++k) {
-                put(o_cta[k], s->cta_items[k].data(), s->cta_items[k].size() * 4);
-                put(o_items[k], s->items[k].data(), s->items[k].size() * sizeof(AttnItem));
+                const std::vector<AttnItem> list = chain_items(s->items[k], s->item_cta[k], s->n_ctas[k]);
+                put(o_items[k], list.data(), list.size() * sizeof(AttnItem));
             }
             put(o_segs, s->segs.data(), s->segs.size() * sizeof(AttnSeg));
             put(o_units, s->units.data(), s->units.size() * sizeof(AttnUnit));
@@ -361,10 +449,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             s->d_status = reinterpret_cast<unsigned long long *>(b + o_status);
             s->d_tbl = reinterpret_cast<const int32_t *>(b + o_tbl);
             s->d_members = reinterpret_cast<const int32_t *>(b + o_members);
-            for (int k = 0; k < 2; ++k) {
-                s->d_cta_items[k] = reinterpret_cast<const int32_t *>(b + o_cta[k]);
-                s->d_items[k] = reinterpret_cast<const AttnItem *>(b + o_items[k]);
-            }
+            for (int k = 0; k < 2; ++k) s->d_items[k] = reinterpret_cast<const AttnItem *>(b + o_items[k]);
             s->d_segs = reinterpret_cast<const AttnSeg *>(b + o_segs);
             s->d_units = reinterpret_cast<const AttnUnit *>(b + o_units);
             s->d_seqs = reinterpret_cast<const AttnSeq *>(b + o_seqs);
@@ -496,11 +581,9 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         p.seqs = s->d_seqs;
         p.members = s->d_members;
         p.items = s->d_items[0];
-        p.cta_items = s->d_cta_items[0];
-        p.n_ctas = (int32_t)s->cta_items[0].size() - 1;
+        p.n_ctas = s->n_ctas[0];
         p.tile_items = s->d_items[1];
-        p.cta_tile_items = s->d_cta_items[1];
-        p.n_tile_ctas = (int32_t)s->cta_items[1].size() - 1;
+        p.n_tile_ctas = s->n_ctas[1];
         p.use_map = s->use_map;
         p.map_box = pdkv::attend_map_box(s->pool.d);
         p.tile_box = pdkv::attend_tile_box(s->pool.d);

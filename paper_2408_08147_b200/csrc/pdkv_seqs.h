@@ -41,7 +41,8 @@ struct alignas(16) AttnItem {
     int32_t row0, rows;
     int32_t tok0, tok1;
     int32_t direct;     // 1: the only part of its rows, the item writes the result itself
-    int32_t pad[3];
+    int32_t next;       // the CTA's next item, -1: none
+    int32_t pad[2];
 };
 
 // What the joining kernel has to know about a sequence.
@@ -64,11 +65,9 @@ struct AttnParams {
     const AttnUnit *units;
     const AttnSeq *seqs;
     const int32_t *members;
-    const AttnItem *items;
-    const int32_t *cta_items;   // [n_ctas + 1] first item of each CTA
+    const AttnItem *items;           // CTA c starts with item c
     int32_t n_ctas;
     const AttnItem *tile_items;      // the same for the tile kernel
-    const int32_t *cta_tile_items;
     int32_t n_tile_ctas;
     int32_t use_map;                 // the warp kernel loads through the tensor map
     int32_t map_box, tile_box;       // tokens of a box of the two maps
@@ -142,7 +141,8 @@ struct pdkv_seqs {
     std::vector<pdkv::AttnUnit> units;
     std::vector<pdkv::AttnSeq> seqs;
     std::vector<pdkv::AttnItem> items[2];      // warp kernel, tile kernel
-    std::vector<int32_t> cta_items[2];
+    std::vector<int32_t> item_cta[2];
+    int32_t n_ctas[2] = {0, 0};
     alignas(64) char map[2][pdkv::kMapBytes] = {};   // tensor maps of the pool, for the two kernels
     bool use_map = false;        // the warp kernel loads through its map
     std::vector<pdkv_attend_item> listing;
@@ -152,7 +152,7 @@ struct pdkv_seqs {
     void *dev_mem = nullptr;
     bool owns_dev_mem = true;
     unsigned long long *d_status = nullptr;
-    const int32_t *d_tbl = nullptr, *d_members = nullptr, *d_cta_items[2] = {nullptr, nullptr};
+    const int32_t *d_tbl = nullptr, *d_members = nullptr;
     const pdkv::AttnSeg *d_segs = nullptr;
     const pdkv::AttnUnit *d_units = nullptr;
     const pdkv::AttnSeq *d_seqs = nullptr;
