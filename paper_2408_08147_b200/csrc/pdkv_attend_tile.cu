@@ -44,7 +44,7 @@ struct Barriers {
     uint64_t full[8], empty[8];     // ring of K and V tiles
     uint64_t q_ready[2];            // Q of a row tile is in shared memory
     uint64_t s_full[2];             // S of a row tile is complete
-    uint64_t p_ready[2];            // P of a row tile is in tensor memory
+    uint64_t p_half[2], p_ready[2]; // P of a row tile is in tensor memory: its first 64 tokens, all of it
     uint64_t o_full[2];             // the last product of a row tile is complete
     uint32_t tmem;
 };
@@ -97,6 +97,39 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
     return d;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x for x <= 128 by arithmetic, beside the special function unit, which alone would need as long for the weights
+// as the tensor cores for both products.  x = n + f with |f| <= 1/2: adding 1.5 2^23 + 127 rounds x to n and
+// leaves n + 127 in the low bits; 2^f is a polynomial of degree 5 (minimax over [-1/2, 1/2] in the relative
+// error, fitted by iteratively reweighted least squares: 2.2e-7, 2^-22).  Under 2^-126: 0.  NaN stays NaN.
+__device__ __forceinline__ float2 pow2_arithmetic(float2 x)
+{
+    constexpr float kMagic = 12582912.f + 127.f;
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.x));   // -127
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.y));
+    const float2 t = add2(x, make_float2(kMagic, kMagic));
+    const float2 n = add2(t, make_float2(-kMagic, -kMagic));
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 y = make_float2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f);
+    y = fma2(y, f, make_float2(0x1.3d0c6p-7f, 0x1.3d0c6p-7f));
+    y = fma2(y, f, make_float2(0x1.c6b6e6p-5f, 0x1.c6b6e6p-5f));
+    y = fma2(y, f, make_float2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
+    y = fma2(y, f, make_float2(0x1.62e428p-1f, 0x1.62e428p-1f));
+    y = fma2(y, f, make_float2(0x1.000002p+0f, 0x1.000002p+0f));
+    return mul2(y, make_float2(__int_as_float(__float_as_int(t.x) << 23), __int_as_float(__float_as_int(t.y) << 23)));
+}
+
 // Shared-memory operand in the 128-byte swizzle: 8-row groups 1024 bytes apart.  K-major (Q, K: a row is 64
 // dims of one token): the leading offset is not used.  MN-major (V: a row is 64 dims, tokens run along
 // the product): the leading offset leads to the next 64 dims.
@@ -145,6 +178,29 @@ __device__ __forceinline__ Work work_of(const AttnParams &p, const AttnItem &it)
     return w;
 }
 
+// Q of a row tile: a warp brings its 32 rows, DP / 8 neighbouring lanes a row, 16 bytes each.  Place of the
+// lane's k-th piece in shared memory, in the swizzle that the matrix instructions read.
+template <int DP> __device__ __forceinline__ uint32_t q_place(int t, int k)
+{
+    constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
+    const int lane = threadIdx.x % 32, row = threadIdx.x / 32 % 4 * 32 + k * kRows + lane / kLanes, c = lane % kLanes;
+    return t * TileShape<DP>::kOperand + c / 8 * TileShape<DP>::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16;
+}
+template <typename T, int DP> __device__ __forceinline__ void fetch_q(const AttnParams &p, const Work &w, int t, uint32_t q_at)
+{
+    constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
+    const int lane = threadIdx.x % 32, mine = t * kTileRows + threadIdx.x % kSoftmaxThreads, d = 8 * (lane % kLanes);
+    const bool live = mine < w.it.rows;
+    const RowId id = row_id(p, w.it, w.it.row0 + (live ? mine : 0));
+    const int64_t at = live ? id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2] : -1;
+#pragma unroll 4
+    for (int k = 0; k < 32 / kRows; ++k) {
+        const int64_t from = __shfl_sync(~0u, at, k * kRows + lane / kLanes);
+        const bool there = from >= 0 && d < p.D;   // else zeros
+        copy_async(q_at + q_place<DP>(t, k), static_cast<const T *>(p.q) + (there ? from + d : 0), there);
+    }
+}
+
 }  // namespace
 
 template <typename T, int DP>
@@ -163,9 +219,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             mbar_init(&bar.empty[i], 1);
         }
         for (int t = 0; t < 2; ++t) {
-            mbar_init(&bar.q_ready[t], kSoftmaxThreads);
+            mbar_init(&bar.q_ready[t], kSoftmaxThreads / 32);   // a warp arrives once: arrivals of single threads queue up
             mbar_init(&bar.s_full[t], 1);
-            mbar_init(&bar.p_ready[t], kSoftmaxThreads);
+            mbar_init(&bar.p_half[t], kSoftmaxThreads / 32);
+            mbar_init(&bar.p_ready[t], kSoftmaxThreads / 32);
             mbar_init(&bar.o_full[t], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -173,6 +230,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    // the first item's Q comes while tensor memory is set up
+    bool q_early = false;
+    if (warp < kMmaWarp) {
+        const Work w = work_of(p, first);
+        q_early = w.tiles > 0 && warp / 4 < w.row_tiles;
+        if (q_early) fetch_q<T, DP>(p, w, warp / 4, q_at);
     }
     fence_before();
     __syncthreads();
@@ -237,11 +301,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     mma_shared(tmem + kColS + t * kColTile, operand(q + o, 16), operand(k + o, 16), kWordS, s > 0);
                 }
             };
-            auto product_o = [&](int t, uint32_t v_slot, bool add) {   // O(t) += P(t) V
+            auto product_o = [&](int t, uint32_t v_slot, int half, bool add) {   // O(t) += P(t) V, 64 tokens
                 const uint32_t v = ring_at + v_slot * G::kOperand;
 #pragma unroll
-                for (int s = 0; s < kTileTokens / 16; ++s)
-                    mma_tensor(tmem + kColO + t * kColTile, tmem + kColS + t * kColTile + 8 * s, operand(v + s * 2048, G::kSub), kWordO, add || s > 0);
+                for (int k = 0; k < kTileTokens / 32; ++k) {
+                    const int s = half * (kTileTokens / 32) + k;
+                    mma_tensor(tmem + kColO + t * kColTile, tmem + kColS + t * kColTile + 8 * s, operand(v + s * 2048, G::kSub), kWordO, add || k > 0);
+                }
             };
             AttnItem it = first;
             for (bool more = true; more;) {
@@ -265,10 +331,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     const bool last = j + 1 == w.tiles;
                     mbar_wait(&bar.full[v_slot], (n + 1) / G::kSlots & 1, dead, p.status);
                     for (int t = 0; t < w.row_tiles; ++t) {
+                        mbar_wait(&bar.p_half[t], p_phase[t], dead, p.status);
+                        fence_after();
+                        if (!dead) product_o(t, v_slot, 0, j > 0);
                         mbar_wait(&bar.p_ready[t], p_phase[t], dead, p.status);
                         p_phase[t] ^= 1;
                         fence_after();
-                        if (!dead) product_o(t, v_slot, j > 0);
+                        if (!dead) product_o(t, v_slot, 1, true);
                         if (last) {
                             commit(&bar.o_full[t]);
                         } else {
@@ -297,7 +366,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         const float scale = fabsf(p.scale_log2);
         const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
         uint32_t s_phase = 0, o_phase = 0, n = 0;
-        bool q_there = false;
+        bool q_there = q_early, q_done = false;   // the item's Q is on its way, has been handed over
         // A warp's 32 rows of 32 numbers leave by way of shared memory: a lane has a row, but eight neighbouring lanes
         // store 128 bytes of one row (lanes storing their own rows touched 32 sectors an instruction: 8000 cycles
         // for a tile of O).  f(row of the warp, number of the first of four columns, the four numbers).
@@ -314,33 +383,18 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             }
             __syncwarp();
         };
-        auto load_q = [&](const Work &w) {   // a warp loads its 32 rows, DP / 8 neighbouring lanes a row
-            constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
-            const int mine = t * kTileRows + r;
-            const bool live = mine < w.it.rows;
-            const RowId id = row_id(p, w.it, w.it.row0 + (live ? mine : 0));
-            const int64_t at = live ? id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2] : -1;
-            const int c = lane % kLanes;
-            // 16 bytes a lane, zeros for rows that are not there; all copies of the warp are in flight together
-#pragma unroll 4
-            for (int k = 0; k < 32 / kRows; ++k) {
-                const int row = warp % 4 * 32 + k * kRows + lane / kLanes;
-                const int64_t from = __shfl_sync(~0u, at, k * kRows + lane / kLanes);
-                const bool there = from >= 0 && 8 * c < p.D;
-                copy_async(smem_u32(smem + t * G::kOperand + c / 8 * G::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16),
-                           static_cast<const T *>(p.q) + (there ? from + 8 * c : 0), there);
-            }
+        auto finish_q = [&]() {
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (flip) {   // (a lane turns the signs of what it brought itself)
 #pragma unroll 1
-                for (int k = 0; k < 32 / kRows; ++k) {
-                    const int row = warp % 4 * 32 + k * kRows + lane / kLanes;
-                    uint4 *x = reinterpret_cast<uint4 *>(smem + t * G::kOperand + c / 8 * G::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16);
+                for (int k = 0; k < DP / 8; ++k) {
+                    uint4 *x = reinterpret_cast<uint4 *>(smem + q_place<DP>(t, k));
                     *x = make_uint4(x->x ^ flip, x->y ^ flip, x->z ^ flip, x->w ^ flip);
                 }
             }
             fence_async_smem();
-            mbar_arrive(&bar.q_ready[t]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.q_ready[t]);
         };
         AttnItem it = first;
         for (bool more = true; more;) {
@@ -356,8 +410,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             float m = -INFINITY, l = 0.f;
             if (w.tiles > 0) {
-                if (!q_there) load_q(w);
-                q_there = false;
+                if (!q_there) fetch_q<T, DP>(p, w, t, q_at);
+                if (!q_there || !q_done) finish_q();
+                q_there = q_done = false;
                 const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;
                 const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
                 const bool with_logits = p.logits && own;
@@ -390,16 +445,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
                     tmem_load_wait();
-                    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float top = -INFINITY;
                     if (masked) {
 #pragma unroll
                         for (int k = 0; k < kTileTokens; ++k)
-                            if (t0 + k < sees) tops[k % 4] = fmaxf(tops[k % 4], v[k]);
+                            if (t0 + k < sees) top = fmaxf(top, v[k]);
                     } else {
+                        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int k = 0; k < kTileTokens; ++k) tops[k % 4] = fmaxf(tops[k % 4], v[k]);
+                        for (int k = 0; k < kTileTokens / 2; ++k) tops[k % 4] = max3(tops[k % 4], v[2 * k], v[2 * k + 1]);
+                        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     }
-                    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     top = top == -INFINITY ? top : top * scale;
                     if (__any_sync(~0u, top > m + kGrowth || (m == -INFINITY && top > m))) {
                         const float new_m = fmaxf(m, top), f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
@@ -442,8 +498,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         for (int k = 0; k < 16; ++k) {
                             const int i0 = 32 * c + 2 * k;
                             float2 x = fma2(make_float2(v[i0], v[i0 + 1]), scale2, base2);
-                            x.x = pow2(x.x);
-                            x.y = pow2(x.y);
+                            if (k % 8 == 2 || k % 8 == 4 || k % 8 == 7) {   // three of eight: both units take about as long
+                                x = pow2_arithmetic(x);
+                            } else {
+                                x.x = pow2(x.x);
+                                x.y = pow2(x.y);
+                            }
                             if (masked) {
                                 if (t0 + i0 >= sees) x.x = 0.f;
                                 if (t0 + i0 + 1 >= sees) x.y = 0.f;
@@ -452,18 +512,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                             packed[k] = pack<T>(x.x, x.y);
                         }
                         tmem_store16(s_at + 16 * c, packed);
+                        if (c == 1) {
+                            tmem_store_wait();
+                            fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&bar.p_half[t]);
+                        }
                     }
                     l += sums[0].x + sums[0].y + (sums[1].x + sums[1].y);
                     tmem_store_wait();
                     fence_before();
-                    mbar_arrive(&bar.p_ready[t]);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar.p_ready[t]);
                 }
                 // every product with Q is done: the next item's Q may take its place
                 if (more) {
                     const Work next = work_of(p, next_it);
                     if (t < next.row_tiles && next.tiles > 0) {
-                        load_q(next);
-                        q_there = true;
+                        fetch_q<T, DP>(p, next, t, q_at);
+                        finish_q();
+                        q_there = q_done = true;
                     }
                 }
                 mbar_wait(&bar.o_full[t], o_phase, dead, p.status);
