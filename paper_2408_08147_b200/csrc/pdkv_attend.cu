@@ -294,8 +294,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                     for (int t = 0; t < NT; ++t) multiply<T>(z[h][t], a, q[k][t][0], q[k][t][1]);
                 }
             }
-        const bool masked = t0 + kSlice > safe;
-        if (masked)
+        if (t0 + kSlice > safe)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -349,8 +348,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float x = pow2(fmaf(z[h][t][j], scale, j & 1 ? -b1 : -b0));
-                    if (masked && t0 + 16 * h + lane / 4 + 8 * (j >> 1) >= sees[t][j & 1]) x = 0.f;
+                    const float x = pow2(fmaf(z[h][t][j], scale, j & 1 ? -b1 : -b0));
                     l[t][j & 1] += x;
                     z[h][t][j] = x;
                 }

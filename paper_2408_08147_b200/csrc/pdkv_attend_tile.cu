@@ -97,39 +97,12 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
     return d;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
-    return d;
-}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 2^x for x <= 128 by arithmetic, beside the special function unit, which alone would need as long for the weights
-// as the tensor cores for both products.  x = n + f with |f| <= 1/2: adding 1.5 2^23 + 127 rounds x to n and
-// leaves n + 127 in the low bits; 2^f is a polynomial of degree 5 (minimax over [-1/2, 1/2] in the relative
-// error, fitted by iteratively reweighted least squares: 2.2e-7, 2^-22).  Under 2^-126: 0.  NaN stays NaN.
-__device__ __forceinline__ float2 pow2_arithmetic(float2 x)
-{
-    constexpr float kMagic = 12582912.f + 127.f;
-    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.x));   // -127
-    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.y));
-    const float2 t = add2(x, make_float2(kMagic, kMagic));
-    const float2 n = add2(t, make_float2(-kMagic, -kMagic));
-    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 y = make_float2(0x1.5c08e6p-10f, 0x1.5c08e6p-10f);
-    y = fma2(y, f, make_float2(0x1.3d0c6p-7f, 0x1.3d0c6p-7f));
-    y = fma2(y, f, make_float2(0x1.c6b6e6p-5f, 0x1.c6b6e6p-5f));
-    y = fma2(y, f, make_float2(0x1.ebf918p-3f, 0x1.ebf918p-3f));
-    y = fma2(y, f, make_float2(0x1.62e428p-1f, 0x1.62e428p-1f));
-    y = fma2(y, f, make_float2(0x1.000002p+0f, 0x1.000002p+0f));
-    return mul2(y, make_float2(__int_as_float(__float_as_int(t.x) << 23), __int_as_float(__float_as_int(t.y) << 23)));
-}
-
 // Shared-memory operand in the 128-byte swizzle: 8-row groups 1024 bytes apart.  K-major (Q, K: a row is 64
 // dims of one token): the leading offset is not used.  MN-major (V: a row is 64 dims, tokens run along
 // the product): the leading offset leads to the next 64 dims.
@@ -445,17 +418,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
                     tmem_load_wait();
-                    float top = -INFINITY;
                     if (masked) {
 #pragma unroll
                         for (int k = 0; k < kTileTokens; ++k)
-                            if (t0 + k < sees) top = fmaxf(top, v[k]);
-                    } else {
-                        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int k = 0; k < kTileTokens / 2; ++k) tops[k % 4] = max3(tops[k % 4], v[2 * k], v[2 * k + 1]);
-                        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                            if (t0 + k >= sees) v[k] = -INFINITY;
                     }
+                    float tops[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) tops[k] = fmaxf(v[2 * k], v[2 * k + 1]);
+#pragma unroll
+                    for (int k = 8; k < kTileTokens / 2; ++k) tops[k % 8] = max3(tops[k % 8], v[2 * k], v[2 * k + 1]);
+                    float top = max3(max3(max3(tops[0], tops[1], tops[2]), tops[3], tops[4]), tops[5], fmaxf(tops[6], tops[7]));
                     top = top == -INFINITY ? top : top * scale;
                     if (__any_sync(~0u, top > m + kGrowth || (m == -INFINITY && top > m))) {
                         const float new_m = fmaxf(m, top), f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
@@ -476,11 +449,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     }
                     const float base = m == -INFINITY ? 0.f : m;
                     if (with_logits) {
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
                             float z[32];
+                            tmem_load(z, s_at + 32 * c);
+                            tmem_load_wait();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) z[k] = t0 + 32 * c + k < sees ? v[32 * c + k] * scale : -INFINITY;
+                            for (int k = 0; k < 32; ++k) z[k] = t0 + 32 * c + k < sees ? z[k] * scale : -INFINITY;
                             by_rows(z, [&](int r4, int col, float4 x) {
                                 const int64_t at = __shfl_sync(~0u, logit_row, r4);
                                 const int tok = t0 + 32 * c + col;
@@ -498,16 +473,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         for (int k = 0; k < 16; ++k) {
                             const int i0 = 32 * c + 2 * k;
                             float2 x = fma2(make_float2(v[i0], v[i0 + 1]), scale2, base2);
-                            if (k % 8 == 2 || k % 8 == 4 || k % 8 == 7) {   // three of eight: both units take about as long
-                                x = pow2_arithmetic(x);
-                            } else {
-                                x.x = pow2(x.x);
-                                x.y = pow2(x.y);
-                            }
-                            if (masked) {
-                                if (t0 + i0 >= sees) x.x = 0.f;
-                                if (t0 + i0 + 1 >= sees) x.y = 0.f;
-                            }
+                            x.x = pow2(x.x);
+                            x.y = pow2(x.y);
                             sums[k % 2] = add2(sums[k % 2], x);
                             packed[k] = pack<T>(x.x, x.y);
                         }

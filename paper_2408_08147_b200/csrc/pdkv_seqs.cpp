@@ -113,9 +113,9 @@ Shape shape_of(int64_t rows, bool tile_ok)
     return {0, rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile, 64};
 }
 
-// What starting and finishing an item costs, in quanta of its kernel.  Measured: about 10000 cycles against
-// 2100 a quantum in the tile kernel, 3 us against 1.5 us (a CTA's share of the memory rate) in the warp kernel.
-constexpr int64_t kItemCost[2] = {2, 5};
+// What starting and finishing an item costs, in quanta of its kernel.  Measured: about 15000 cycles against
+// 3700 a quantum in the tile kernel, 3 us against 1.5 us (a CTA's share of the memory rate) in the warp kernel.
+constexpr int64_t kItemCost[2] = {2, 4};
 
 struct Unit { int32_t seg, head, row0, rows; int64_t quanta; };
 struct Piece { size_t unit; int64_t from, n; int32_t cta; };
@@ -179,8 +179,8 @@ std::vector<Unit> units_of(const pdkv_seqs &s, int kernel, const std::vector<int
 
 // SMs for the tile kernel when both kernels have work: they run at the same time, each on SMs of its own (a CTA of
 // the tile kernel leaves no shared memory for others), and the slower one should be as quick as possible.
-// Measured on B200: 1.1 us a quantum of the tile kernel and 4 us around it; the warp kernel reads at up to 6.3
-// TB/s in all and 75 GB/s per SM, 5 us around it.
+// Measured on B200: 2 us a quantum of the tile kernel and 4 us around it; the warp kernel reads 42 GB/s per SM,
+// whether it has all of them or a few, 5 us around it.
 int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std::vector<Unit> &tile_units)
 {
     if (warp_units.empty()) return s.sm_count;
@@ -191,8 +191,8 @@ int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std:
     int best = 1;
     double best_us = 1e30;
     for (int n = 1; n < s.sm_count; ++n) {
-        const double tile_us = 4 + 1.1 * std::max((tile + kItemCost[1] * (double)n) / n, (double)(1 + kItemCost[1]));
-        const double warp_us = 5 + std::max(bytes / 6.3e6, bytes / (75e3 * (s.sm_count - n)));
+        const double tile_us = 4 + 2.0 * std::max((tile + kItemCost[1] * (double)n) / n, (double)(1 + kItemCost[1]));
+        const double warp_us = 5 + bytes / (42e3 * (s.sm_count - n));
         if (std::max(tile_us, warp_us) < best_us) {
             best_us = std::max(tile_us, warp_us);
             best = n;
@@ -602,6 +602,8 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         }
         p.lse = a->lse;
         p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+        // the kernels hide tokens as logits of -infinity, which a scale of zero would turn into NaN
+        if (std::fabs(p.scale_log2) < 1e-30f) p.scale_log2 = std::signbit(p.scale_log2) ? -1e-30f : 1e-30f;
         p.seq_len = a->seq_len;
         char *w = static_cast<char *>(scratch);
         p.part_o = reinterpret_cast<float *>(w + l.o);
