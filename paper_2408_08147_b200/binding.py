@@ -504,7 +504,9 @@ def pdkv_attend_scratch(seqs: int, with_scores: bool) -> int:
 
 
 def pdkv_attend(seqs: int, layer: int, args: pdkv_attend_args, scratch_ptr: int, scratch_bytes: int, stream: int = 0) -> None:
-    _check(lib().pdkv_attend(seqs, layer, C.byref(args), scratch_ptr, scratch_bytes, stream), "pdkv_attend")
+    rc = (_lib or lib()).pdkv_attend(seqs, layer, C.byref(args), scratch_ptr, scratch_bytes, stream)
+    if rc != PDKV_OK:
+        raise PdkvError(rc, "pdkv_attend")
 
 
 def pdkv_evict(seqs: int, dst: int, layer_begin: int, layer_end: int, args: pdkv_evict_args, stream: int = 0) -> None:

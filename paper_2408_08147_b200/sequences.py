@@ -21,6 +21,10 @@ import torch
 
 from . import binding as B
 
+# the handle of torch's current stream, without the Stream object around it where this torch has that call
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
 _DTYPES = {torch.bfloat16: B.PDKV_DTYPE_BF16, torch.float16: B.PDKV_DTYPE_FP16}
 
 
@@ -89,6 +93,7 @@ class CacheSession:
         if not pool_t.is_contiguous():
             raise ValueError("the pool tensor has to be contiguous")
         self.dtype = dtype
+        self._device, self._index = pool_t.device, pool_t.device.index or 0
         try:
             self.pool = B.pdkv_pool_create(B.desc_of(geom), pool_t.data_ptr(), pool_t.numel() * pool_t.element_size(),
                                            pool_t.device.index or 0)
@@ -104,7 +109,10 @@ class CacheSession:
             self._shape = (seqs.n_seq, q_tokens, num_q_heads, geom.head_dim)
             self._max_len = seqs.max_len
             self._scale = geom.head_dim ** -0.5
-            self._device = pool_t.device
+            n, t, h, d = self._shape
+            dense = [t * h * d, h * d, d]
+            # argument block of the plain call: dense q and out, the default scale
+            self._plain = B.pdkv_attend_args(q_stride=(*dense,), out_stride=(*dense,), scale=self._scale)
         except Exception:
             self.close()
             raise
@@ -114,7 +122,7 @@ class CacheSession:
             return stream
         if self.stream is not None:
             return self.stream
-        return torch.cuda.current_stream(self.pool_t.device).cuda_stream if self.pool_t.is_cuda else 0
+        return _current_stream(self._index) if self.pool_t.is_cuda else 0
 
     def _check(self, name, t, dtype, shape):
         if t.dtype != dtype or t.shape != shape or t.device != self._device:
@@ -148,21 +156,30 @@ class CacheSession:
         stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device)."""
         shape = self._shape
         self._check("q_t", q_t, self.dtype, shape)
+        a = B.pdkv_attend_args.from_buffer_copy(self._plain)
+        dense = q_t.is_contiguous()
+        if not dense:
+            stride = q_t.stride()
+            if shape[3] > 1 and stride[3] != 1:
+                raise ValueError("q_t: the dims of a head have to be adjacent")
+            a.q_stride = stride[:3]
         if out_t is None:
-            out_t = torch.empty(shape, dtype=self.dtype, device=self._device)
+            out_t = torch.empty_like(q_t) if dense else torch.empty(shape, dtype=self.dtype, device=self._device)
         else:
             self._check("out_t", out_t, self.dtype, shape)
+            stride = out_t.stride()
+            if shape[3] > 1 and stride[3] != 1:
+                raise ValueError("out_t: the dims of a head have to be adjacent")
+            a.out_stride = stride[:3]
         if lse_t is None:
             lse_t = torch.empty(shape[:3], dtype=torch.float32, device=self._device)
         else:
             self._check("lse_t", lse_t, torch.float32, shape[:3])
             if not lse_t.is_contiguous():
                 raise ValueError("lse_t has to be contiguous")
-        q_stride, out_stride = q_t.stride(), out_t.stride()
-        if shape[3] > 1 and (q_stride[3] != 1 or out_stride[3] != 1):
-            raise ValueError("q_t, out_t: the dims of a head have to be adjacent")
-        a = B.pdkv_attend_args(q=q_t.data_ptr(), q_stride=q_stride[:3], out=out_t.data_ptr(), out_stride=out_stride[:3],
-                               lse=lse_t.data_ptr(), scale=self._scale if scale is None else scale)
+        a.q, a.out, a.lse = q_t.data_ptr(), out_t.data_ptr(), lse_t.data_ptr()
+        if scale is not None:
+            a.scale = scale
         if seq_len_t is not None:
             a.seq_len = self._lens(seq_len_t)
         if scores_t is not None:
@@ -179,8 +196,10 @@ class CacheSession:
             scratch_t = self._scratch[which]
             if scratch_t is None:
                 scratch_t = self._scratch[which] = torch.empty(max(self._need[which], 16), dtype=torch.uint8, device=self._device)
-        B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), scratch_t.numel() * scratch_t.element_size(),
-                      self._on(stream))
+            size = scratch_t.numel()
+        else:
+            size = scratch_t.numel() * scratch_t.element_size()
+        B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, self._on(stream))
         return out_t, lse_t
 
     def evict(self, dst: "CacheSession", scores_t, budget: int, *, sink: int = 0, recent: int = 0,
