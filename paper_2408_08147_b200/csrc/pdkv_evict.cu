@@ -59,9 +59,16 @@ __device__ __forceinline__ int peer_word(const int *p, uint32_t rank)
     return v;
 }
 
+__device__ __forceinline__ void put_peer_word(const int *p, uint32_t rank, int v)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), far;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(at), "r"(rank));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(far), "r"(v) : "memory");
+}
+
 struct SelectShared {
-    int warp_count[2][kSelectWarps][4];
-    int cta_count[2][4];
+    int count[3][4];              // of the CTA, by round modulo 3
+    int exchange[2][8][4];        // of every CTA of the cluster
     int warp_over[kSelectWarps], warp_tie[kSelectWarps];
     int totals[2];
 };
@@ -81,45 +88,54 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
 #pragma unroll
         for (int i = 0; i < K; ++i) keys[i] = i < per && begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u;
     }
+    if (threadIdx.x < 12) sh.count[threadIdx.x / 4][threadIdx.x % 4] = 0;
+    __syncthreads();
     uint32_t key = 0;   // largest value known to be reached by at least `want` keys
     int reached = hi - lo;
 #pragma unroll 1
     for (int round = 0; round < 16 && reached != want; ++round) {
-        const int shift = 30 - 2 * round, buf = round & 1;
+        const int shift = 30 - 2 * round;
         const uint32_t p1 = key | 1u << shift, p2 = key | 2u << shift, p3 = key | 3u << shift;
         int c1 = 0, c2 = 0, c3 = 0;
-        auto add = [&](uint32_t k) {   // (a missing key is 0 and reaches nothing)
-            c1 += k >= p1;
-            c2 += k >= p2;
-            c3 += k >= p3;
-        };
         if (K > 0) {
+            // (a missing key is 0 and reaches nothing).  At most 512 keys a warp: three counts in one number, one
+            // reduction -- there are few lanes for those
+            uint32_t c = 0;
 #pragma unroll
-            for (int i = 0; i < K; ++i) add(keys[i]);
+            for (int i = 0; i < K; ++i) c += (keys[i] >= p1) + (keys[i] >= p2 ? 1u << 10 : 0u) + (keys[i] >= p3 ? 1u << 20 : 0u);
+            c = __reduce_add_sync(~0u, c);
+            c1 = c & 1023;
+            c2 = c >> 10 & 1023;
+            c3 = c >> 20;
         } else {
-            for (int i = 0; i < per; ++i) add(begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u);
-        }
-        c1 = __reduce_add_sync(~0u, c1);
-        c2 = __reduce_add_sync(~0u, c2);
-        c3 = __reduce_add_sync(~0u, c3);
-        if (lane == 0) *reinterpret_cast<int4 *>(sh.warp_count[buf][warp]) = make_int4(c1, c2, c3, 0);
-        __syncthreads();
-        const int4 v = *reinterpret_cast<const int4 *>(sh.warp_count[buf][lane]);   // kSelectWarps == 32: a lane each
-        c1 = __reduce_add_sync(~0u, v.x);
-        c2 = __reduce_add_sync(~0u, v.y);
-        c3 = __reduce_add_sync(~0u, v.z);
-        if (ranks > 1) {
-            if (threadIdx.x == 0) {
-                sh.cta_count[buf][0] = c1;
-                sh.cta_count[buf][1] = c2;
-                sh.cta_count[buf][2] = c3;
+            for (int i = 0; i < per; ++i) {
+                const uint32_t k = begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u;
+                c1 += k >= p1;
+                c2 += k >= p2;
+                c3 += k >= p3;
             }
+            c1 = __reduce_add_sync(~0u, c1);
+            c2 = __reduce_add_sync(~0u, c2);
+            c3 = __reduce_add_sync(~0u, c3);
+        }
+        int *mine = sh.count[round % 3];
+        if (lane < 3) atomicAdd(&mine[lane], lane == 0 ? c1 : lane == 1 ? c2 : c3);
+        if (threadIdx.x < 4) sh.count[(round + 1) % 3][threadIdx.x] = 0;   // (read last two rounds ago)
+        __syncthreads();
+        c1 = mine[0];
+        c2 = mine[1];
+        c3 = mine[2];
+        if (ranks > 1) {
+            int(*far)[4] = sh.exchange[round % 2];
+            if (threadIdx.x < 4 * ranks) put_peer_word(&far[rank][lane % 4], lane / 4, mine[lane % 4]);
             cluster_barrier();
-            // lane 4 r + i: count i of CTA r
-            const int n = lane % 4 < 3 && lane / 4 < ranks ? peer_word(&sh.cta_count[buf][lane % 4], lane / 4) : 0;
-            c1 = __reduce_add_sync(~0u, lane % 4 == 0 ? n : 0);
-            c2 = __reduce_add_sync(~0u, lane % 4 == 1 ? n : 0);
-            c3 = __reduce_add_sync(~0u, lane % 4 == 2 ? n : 0);
+            c1 = c2 = c3 = 0;
+            for (uint32_t r = 0; r < ranks; ++r) {
+                const int4 v = *reinterpret_cast<const int4 *>(far[r]);
+                c1 += v.x;
+                c2 += v.y;
+                c3 += v.z;
+            }
         }
         if (c3 >= want) {
             key = p3;
@@ -175,15 +191,24 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
             cluster_barrier();   // nobody leaves while its shared memory is being read
         }
         const unsigned below = (1u << lane) - 1;
-        each([&](uint32_t k, int t, bool there) {
-            there = there && t < hi;
-            const bool is_over = there && (all ? k >= key : k > key), is_tie = there && !all && k == key;
-            const unsigned over_mask = __ballot_sync(~0u, is_over), tie_mask = __ballot_sync(~0u, is_tie);
-            const int x = over + __popc(over_mask & below), e = tie + __popc(tie_mask & below);
-            if (is_over || (is_tie && e < left)) kept[x + min(e, left)] = t;
-            over += __popc(over_mask);
-            tie += __popc(tie_mask);
-        });
+        if (all) {
+            each([&](uint32_t k, int t, bool there) {
+                const bool stays = there && t < hi && k >= key;
+                const unsigned mask = __ballot_sync(~0u, stays);
+                if (stays) kept[over + __popc(mask & below)] = t;
+                over += __popc(mask);
+            });
+        } else {
+            each([&](uint32_t k, int t, bool there) {
+                there = there && t < hi;
+                const bool is_over = there && k > key, is_tie = there && k == key;
+                const unsigned over_mask = __ballot_sync(~0u, is_over), tie_mask = __ballot_sync(~0u, is_tie);
+                const int x = over + __popc(over_mask & below), e = tie + __popc(tie_mask & below);
+                if (is_over || (is_tie && e < left)) kept[x + min(e, left)] = t;
+                over += __popc(over_mask);
+                tie += __popc(tie_mask);
+            });
+        }
     }
 }
 
@@ -191,9 +216,9 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
 
 // One cluster per (layer, sequence, head): the lightest key that stays is found two bits a round by
 // counting the keys that reach three values, until exactly the wanted number does or all 32 bits are
-// known; then the indices are written in order.  Counting needs two instructions a key and value and
-// no atomics (a histogram in shared memory was 1.5 times slower: scores crowd into few bins);
-// warps add their counts by integer reductions, CTAs of a cluster over distributed shared memory.
+// known; then the indices are written in order.  Counting needs two instructions a key and value (a
+// histogram in shared memory was 1.5 times slower: scores crowd into few bins); the three counts of a
+// warp go through one integer reduction, CTAs of a cluster exchange theirs over distributed shared memory.
 // Every warp owns a contiguous run of tokens, so the order of the indices follows from counts per
 // warp alone.  Bound by the latency of the rounds.
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p)
