@@ -433,7 +433,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             }
             if (lane == 0) {
                 if (it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (mt + log2f(lt)) * kLn2;
-                if (!it.direct || p.logits) *reinterpret_cast<float2 *>(p.part_ml + 2 * (it.part_row + r)) = make_float2(mt, lt);
+                if (!it.direct || p.with_scores) *reinterpret_cast<float2 *>(p.part_ml + 2 * (it.part_row + r)) = make_float2(mt, lt);
             }
         }
         consumer_sync();
@@ -489,76 +489,26 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
 
 namespace {
 
-// The parts of row `row` of (sequence, head): np0 parts of own tokens, then those of the prefix.
-struct Parts {
-    int64_t first[2], step[2];
-    int n[2];
-};
-
-__device__ __forceinline__ Parts parts_of(const AttnParams &p, const AttnSeq &s, int head, int row)
-{
-    Parts x;
-    x.n[0] = x.n[1] = 0;
-    x.first[0] = x.first[1] = x.step[0] = x.step[1] = 0;
-    if (s.own_unit >= 0) {
-        const AttnUnit u = p.units[s.own_unit + row / s.own_tile * p.H + head];
-        x.first[0] = u.part_row + row % s.own_tile;
-        x.step[0] = u.rows;
-        x.n[0] = u.n_parts;
-    }
-    if (s.prefix_unit >= 0) {
-        const int pr = s.prefix_row0 + row;
-        const AttnUnit u = p.units[s.prefix_unit + pr / s.prefix_tile * p.H + head];
-        x.first[1] = u.part_row + pr % s.prefix_tile;
-        x.step[1] = u.rows;
-        x.n[1] = u.n_parts;
-    }
-    return x;
-}
-
-__device__ __forceinline__ int64_t part_at(const Parts &x, int i)
-{
-    return i < x.n[0] ? x.first[0] + i * x.step[0] : x.first[1] + (i - x.n[0]) * x.step[1];
-}
-
-// Maximum and sum of a row over all of its parts, by W neighbouring lanes; each of them gets both.
-template <int W> __device__ __forceinline__ float2 joined_ml(const AttnParams &p, const Parts &x, int lane)
-{
-    const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml);
-    float m = -INFINITY, l = 0.f;
-    for (int i = lane % W; i < x.n[0] + x.n[1]; i += W) {
-        const float2 v = ml[part_at(x, i)];
-        const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
-        l = l * pow2(m - base) + v.y * pow2(v.x - base);
-        m = top;
-    }
-#pragma unroll
-    for (int o = W / 2; o; o /= 2) {
-        const float m2 = __shfl_xor_sync(~0u, m, o), l2 = __shfl_xor_sync(~0u, l, o);
-        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
-        l = l * pow2(m - base) + l2 * pow2(m2 - base);
-        m = top;
-    }
-    return make_float2(m, l);
-}
-
-constexpr int kScoreChunk = 128;   // tokens of one block of the score part
+// Tokens of one block of the score part: four a thread, and either each warp has tokens of its own, or -- many
+// rows -- all warps have the same and share the rows.
+constexpr int kSharedRows = 12;
+__host__ __device__ constexpr int score_chunk(int rows) { return rows > kSharedRows ? 128 : 512; }
 constexpr int kScoreRows = 64;     // rows whose lse is held at a time
 
 }  // namespace
 
 // The first `row_blocks` blocks of a (sequence, head) join the parts of four rows each, a warp per row:
 // m = max m_p, l = sum l_p 2^(m_p - m), O = sum O_p 2^(m_p - m).  The others turn the logits of a chunk of
-// tokens into weights 2^(z - lse) and add them to the scores, a warp every fourth row; they take the lse from
-// the parts themselves, so no block waits for another.
+// tokens into weights 2^(z - lse) and add them to the scores; they take the lse from the parts themselves, so no
+// block waits for another.
 template <typename T>
 __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, const int row_blocks, const int chunks)
 {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, per = row_blocks + chunks;
     const int x = blockIdx.x % per, head = blockIdx.x / per % p.H, seq = blockIdx.x / per / p.H;
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts are written by the kernel before
     const AttnSeq s = p.seqs[seq];
     const int R = p.G * p.q_tokens;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts are written by the kernels before
     if (x < row_blocks) {
         const int row = 4 * x + warp;
         if (s.direct || row >= R) return;
@@ -598,10 +548,11 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     }
     __shared__ float lse[kScoreRows];
     __shared__ float4 sums[4][32];
-    const int chunk = x - row_blocks, len = own_len(p, seq, s.len), t0 = chunk * kScoreChunk + 4 * lane;
+    const bool shared = R > kSharedRows;
+    const int begin = (x - row_blocks) * score_chunk(R), len = own_len(p, seq, s.len), t0 = begin + (shared ? 0 : 128 * warp) + 4 * lane;
     // past the sequence's end there is no weight: nothing to do in place, else the row is carried over
     const int width = p.scores_in == p.scores_out ? len : p.max_len;
-    if (chunk * kScoreChunk >= width) return;
+    if (begin >= width) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int r0 = 0; r0 < R; r0 += kScoreRows) {
         const int n = min(kScoreRows, R - r0);
@@ -614,9 +565,9 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
         }
         __syncthreads();
         const float *z = p.logits + s.logits + ((int64_t)head * R + r0) * s.logit_stride + t0;
-        if (t0 < len) {   // a warp takes every fourth row
-#pragma unroll 8
-            for (int row = warp; row < n; row += 4) {
+        if (t0 < len) {
+#pragma unroll 4
+            for (int row = shared ? warp : 0; row < n; row += shared ? 4 : 1) {
                 const float4 v = *reinterpret_cast<const float4 *>(z + (int64_t)row * s.logit_stride);
                 const float e = lse[row];
                 sum.x += pow2(v.x - e);
@@ -626,16 +577,23 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
             }
         }
     }
-    sums[warp][lane] = sum;
-    __syncthreads();
-    const int t = chunk * kScoreChunk + threadIdx.x;
-    if (t < width) {
+    auto put = [&](int t, float add) {
+        if (t >= width) return;
         const float in = p.scores_in ? p.scores_in[seq * p.scores_in_stride[0] + head * p.scores_in_stride[1] + t] : 0.f;
+        // (what lies in the scratch behind the last token is no logit)
+        p.scores_out[seq * p.scores_out_stride[0] + head * p.scores_out_stride[1] + t] = t < len ? in + add : in;
+    };
+    sums[warp][lane] = sum;
+    if (shared) {
+        __syncthreads();
         float add = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) add += reinterpret_cast<const float *>(sums[w])[threadIdx.x];
-        // (what lies in the scratch behind the last token is no logit)
-        p.scores_out[seq * p.scores_out_stride[0] + head * p.scores_out_stride[1] + t] = t < len ? in + add : in;
+        put(begin + threadIdx.x, add);
+    } else {   // neighbouring lanes store neighbouring tokens
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) put(begin + 128 * warp + 32 * k + lane, reinterpret_cast<const float *>(sums[warp])[32 * k + lane]);
     }
 }
 
@@ -691,7 +649,7 @@ cudaError_t launch_attend(const AttnParams &p, const void *map, int dtype, cudaS
 cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream)
 {
     const int row_blocks = join ? (p.G * p.q_tokens + 3) / 4 : 0;
-    const int chunks = p.logits ? (p.max_len + kScoreChunk - 1) / kScoreChunk : 0;
+    const int per = score_chunk(p.G * p.q_tokens), chunks = p.logits ? (p.max_len + per - 1) / per : 0;
     const int64_t blocks = (int64_t)p.n_seq * p.H * (row_blocks + chunks);
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
     if (blocks == 0) return cudaSuccess;

@@ -12,7 +12,7 @@
 
 namespace pdkv {
 
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ int own_len(const AttnParams &p, int seq, int cap)
 {
@@ -118,6 +118,59 @@ __device__ __forceinline__ float pow2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// The parts of row `row` of (sequence, head): np0 parts of own tokens, then those of the prefix.
+struct Parts {
+    int64_t first[2], step[2];
+    int n[2];
+};
+
+__device__ __forceinline__ Parts parts_of(const AttnParams &p, const AttnSeq &s, int head, int row)
+{
+    Parts x;
+    x.n[0] = x.n[1] = 0;
+    x.first[0] = x.first[1] = x.step[0] = x.step[1] = 0;
+    if (s.own_unit >= 0) {
+        const AttnUnit u = p.units[s.own_unit + row / s.own_tile * p.H + head];
+        x.first[0] = u.part_row + row % s.own_tile;
+        x.step[0] = u.rows;
+        x.n[0] = u.n_parts;
+    }
+    if (s.prefix_unit >= 0) {
+        const int pr = s.prefix_row0 + row;
+        const AttnUnit u = p.units[s.prefix_unit + pr / s.prefix_tile * p.H + head];
+        x.first[1] = u.part_row + pr % s.prefix_tile;
+        x.step[1] = u.rows;
+        x.n[1] = u.n_parts;
+    }
+    return x;
+}
+
+__device__ __forceinline__ int64_t part_at(const Parts &x, int i)
+{
+    return i < x.n[0] ? x.first[0] + i * x.step[0] : x.first[1] + (i - x.n[0]) * x.step[1];
+}
+
+// Maximum and sum of a row over all of its parts, by W neighbouring lanes; each of them gets both.
+template <int W> __device__ __forceinline__ float2 joined_ml(const AttnParams &p, const Parts &x, int lane)
+{
+    const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml);
+    float m = -INFINITY, l = 0.f;
+    for (int i = lane % W; i < x.n[0] + x.n[1]; i += W) {
+        const float2 v = ml[part_at(x, i)];
+        const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.f : top;
+        l = l * pow2(m - base) + v.y * pow2(v.x - base);
+        m = top;
+    }
+#pragma unroll
+    for (int o = W / 2; o; o /= 2) {
+        const float m2 = __shfl_xor_sync(~0u, m, o), l2 = __shfl_xor_sync(~0u, l, o);
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
+        l = l * pow2(m - base) + l2 * pow2(m2 - base);
+        m = top;
+    }
+    return make_float2(m, l);
 }
 
 // The opt-in to more than 48 KB of shared memory is per kernel and device.

@@ -13,6 +13,7 @@
 // O is rescaled only when a row's maximum grew by more than 2^8 since the last time: the weights stay below
 // 2^8, where 16-bit and 32-bit floating point lose nothing.  Maxima and sums are 32 bits, the sums taken
 // before the weights are rounded.
+#include <algorithm>
 #include <numeric>
 #include <type_traits>
 
@@ -388,12 +389,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 q_there = q_done = false;
                 const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;
                 const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
-                const bool with_logits = p.logits && own;
-                int64_t logit_row = -1;   // where this row's logits go
-                if (with_logits && live) {
-                    const AttnSeq s = p.seqs[w.it.seq];
-                    logit_row = s.logits + ((int64_t)w.it.head * p.G * p.q_tokens + w.it.row0 + row) * s.logit_stride;
-                }
                 for (int j = 0; j < w.tiles; ++j) {
                     const int t0 = w.it.tok0 + j * kTileTokens;
                     const bool masked = t0 + kTileTokens > safe;
@@ -448,21 +443,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         }
                     }
                     const float base = m == -INFINITY ? 0.f : m;
-                    if (with_logits) {
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            float z[32];
-                            tmem_load(z, s_at + 32 * c);
-                            tmem_load_wait();
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) z[k] = t0 + 32 * c + k < sees ? z[k] * scale : -INFINITY;
-                            by_rows(z, [&](int r4, int col, float4 x) {
-                                const int64_t at = __shfl_sync(~0u, logit_row, r4);
-                                const int tok = t0 + 32 * c + col;
-                                if (at >= 0 && tok < w.limit) *reinterpret_cast<float4 *>(p.logits + at + tok) = x;
-                            });
-                        }
-                    }
                     __syncwarp();
                     float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     const float2 scale2 = make_float2(scale, scale), base2 = make_float2(-base, -base);
@@ -539,7 +519,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             }
             if (live && !dead) {
                 if (w.it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (m + log2f(l)) * kLn2;
-                if (!w.it.direct || p.logits) *reinterpret_cast<float2 *>(p.part_ml + 2 * (w.it.part_row + row)) = make_float2(m, l);
+                if (!w.it.direct || p.with_scores) *reinterpret_cast<float2 *>(p.part_ml + 2 * (w.it.part_row + row)) = make_float2(m, l);
             }
         }
     }
@@ -548,6 +528,183 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     if (warp == kMmaWarp) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns));
+    }
+}
+
+namespace {
+
+// Shared memory of the weighing kernel: the rows of Q, up to 256, and two tiles of K.
+__host__ __device__ constexpr uint32_t weigh_q_sub(int rows) { return (uint32_t)((rows < 256 ? rows + 15 : 256) / 16 * 16) * 128; }   // 64 dims
+template <int DP> constexpr uint32_t weigh_bytes(int rows)
+{
+    return TileShape<DP>::kSubs * weigh_q_sub(rows) + 2 * TileShape<DP>::kOperand + 1024;
+}
+
+}  // namespace
+
+// Attention weights of own tokens, summed over the rows of their sequence, for segments that the tile kernel
+// attends to: a second pass over K once every row's sum is known.  Writing the logits and reading them
+// back, as is done for few rows, moves 8 bytes a row and token, against 2 bytes a dim for K: with 64 rows the
+// first took 57 us where this takes 13 (12 sequences of 300 to 4096 tokens, 8 heads of 128 dims).
+//
+// S^T = K Q^T: a thread has one token and its logits of all rows in tensor memory, so the sum over
+// the rows needs no other thread.  The next tile's product runs while this one's weights are computed.
+template <typename T, int DP>
+__global__ void __launch_bounds__(128) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
+{
+    using G = TileShape<DP>;
+    extern __shared__ char raw[];
+    __shared__ uint64_t k_full[2], s_full[2];
+    __shared__ uint32_t tmem_s;
+    __shared__ __align__(16) float lse[256];
+    __shared__ __align__(16) int sees[256];
+    char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
+    const uint32_t q_sub = weigh_q_sub(p.G * p.q_tokens), q_at = smem_u32(smem), k_at = q_at + G::kSubs * q_sub;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int chunk = blockIdx.x % chunks, head = blockIdx.x / chunks % p.H, seq = blockIdx.x / chunks / p.H;
+    const int R = p.G * p.q_tokens, columns = R > 128 ? 256 : R > 64 ? 128 : 64;   // of one S^T
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&k_full[i], 1);
+            mbar_init(&s_full[i], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    const AttnSeq s = p.seqs[seq];
+    const AttnSeg seg = p.segs[seq];
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // sums of the rows, current lengths
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_s;
+    const int len = own_len(p, seq, s.len), begin = chunk * chunk_tiles * kTileTokens;
+    const int limit = min(len, begin + chunk_tiles * kTileTokens);
+    const int tiles = limit > begin ? (limit - begin + kTileTokens - 1) / kTileTokens : 0;
+    const float scale = fabsf(p.scale_log2);
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+    bool dead = false;
+    uint32_t phase[2] = {0, 0}, s_phase[2] = {0, 0};   // of K, of S^T
+    auto load_k = [&](int j) {   // warp 0
+        const int t0 = begin + j * kTileTokens, boxes = (min(kTileTokens, limit - t0) + p.tile_box - 1) / p.tile_box, slot = j & 1;
+        if (lane == 0) mbar_expect(&k_full[slot], (uint32_t)boxes * p.tile_box * 128 * G::kSubs);
+        __syncwarp();
+        if (lane < boxes) {
+            const int t = t0 + lane * p.tile_box, block = p.tbl[seg.tbl + t / p.pool.block_tokens], tt = t % p.pool.block_tokens;
+            for (int i = 0; i < G::kSubs; ++i) {
+                const uint32_t to = k_at + slot * G::kOperand + i * G::kSub + lane * p.tile_box * 128;
+                if (p.map_layer_major)
+                    load_box(to, &map, 64 * i, tt, head, block, 2 * p.layer, &k_full[slot]);
+                else
+                    load_box(to, &map, 64 * i, head, tt, 2 * p.layer, block, &k_full[slot]);
+            }
+        }
+        __syncwarp();
+    };
+    const int64_t out_row = seq * p.scores_out_stride[0] + head * p.scores_out_stride[1];
+    const int64_t in_row = seq * p.scores_in_stride[0] + head * p.scores_in_stride[1];
+    for (int r0 = 0; r0 < R && tiles > 0; r0 += 256) {
+        const int rows = min(256, R - r0), n = (rows + 15) / 16 * 16;
+        if (warp == 0) {
+            load_k(0);
+            if (tiles > 1) load_k(1);
+        }
+        // Q: DP / 8 neighbouring lanes a row, rows up to a multiple of 16 filled with zeros
+        constexpr int kLanes = DP / 8, kRows = 128 / kLanes;
+        const int c = threadIdx.x % kLanes;
+        for (int i = threadIdx.x / kLanes; i < n; i += kRows) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (i < rows && 8 * c < p.D) {
+                const int row = r0 + i;
+                v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + seq * p.q_stride[0] + row / p.G * p.q_stride[1] +
+                                                     (head * p.G + row % p.G) * p.q_stride[2] + 8 * c);
+                v = make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
+            }
+            *reinterpret_cast<uint4 *>(smem + c / 8 * q_sub + i * 128 + ((c % 8) ^ (i % 8)) * 16) = v;
+        }
+        for (int i = threadIdx.x; i < columns; i += 128) {
+            const int row = r0 + min(i, rows - 1);
+            const float x = p.lse[((int64_t)seq * p.q_tokens + row / p.G) * p.G * p.H + head * p.G + row % p.G];
+            lse[i] = i >= rows || x == -INFINITY ? INFINITY : x * kLog2e;   // no weight: 2^(z - inf) = 0
+            sees[i] = len - (p.q_tokens - 1 - row / p.G);
+        }
+        fence_async_smem();
+        __syncthreads();
+        auto product = [&](int j) {   // thread 0: S^T of tile j
+            const uint32_t word = instruction<T>(n, false);
+            const uint32_t k = k_at + (j & 1) * G::kOperand;
+            for (int i = 0; i < DP / 16; ++i)
+                mma_shared(tmem + (j & 1) * columns, operand(k + i / 4 * G::kSub + i % 4 * 32, 16), operand(q_at + i / 4 * q_sub + i % 4 * 32, 16), word, i > 0);
+            commit(&s_full[j & 1]);
+        };
+        if (threadIdx.x == 0) {
+            mbar_wait(&k_full[0], phase[0], dead, p.status);
+            fence_after();
+            if (!dead) product(0);
+        }
+        phase[0] ^= 1;
+        for (int j = 0; j < tiles; ++j) {
+            const int b = j & 1, t0 = begin + j * kTileTokens, t = t0 + threadIdx.x;
+            if (j + 1 < tiles) {
+                if (threadIdx.x == 0) {
+                    mbar_wait(&k_full[b ^ 1], phase[b ^ 1], dead, p.status);
+                    fence_after();
+                    if (!dead) product(j + 1);
+                }
+                phase[b ^ 1] ^= 1;
+            }
+            mbar_wait(&s_full[b], s_phase[b], dead, p.status);
+            s_phase[b] ^= 1;
+            __syncwarp();
+            fence_after();
+            if (warp == 0 && j + 2 < tiles && !__any_sync(~0u, dead)) load_k(j + 2);   // the product has read its K
+            const bool masked = t0 + kTileTokens > len - (p.q_tokens - 1);
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int col = 0; col < n; col += 32) {
+                float v[32];
+                tmem_load(v, tmem + ((uint32_t)(warp * 32) << 16) + b * columns + col);
+                tmem_load_wait();
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 e = *reinterpret_cast<const float4 *>(lse + col + k);
+                    float x[4] = {pow2(fmaf(v[k], scale, -e.x)), pow2(fmaf(v[k + 1], scale, -e.y)), pow2(fmaf(v[k + 2], scale, -e.z)),
+                                  pow2(fmaf(v[k + 3], scale, -e.w))};
+                    if (masked) {
+                        const int4 y = *reinterpret_cast<const int4 *>(sees + col + k);
+                        if (t >= y.x) x[0] = 0.f;
+                        if (t >= y.y) x[1] = 0.f;
+                        if (t >= y.z) x[2] = 0.f;
+                        if (t >= y.w) x[3] = 0.f;
+                    }
+                    // (columns past n hold nothing: their lse is infinite, but what lies there may be NaN)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (col + k + i < n) sum[i] += x[i];
+                }
+            }
+            if (t < limit && !dead) {
+                const float add = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                const float in = r0 > 0 ? p.scores_out[out_row + t] : p.scores_in ? p.scores_in[in_row + t] : 0.f;
+                p.scores_out[out_row + t] = in + add;
+            }
+            fence_before();
+            __syncthreads();   // S^T of this tile may be overwritten, and after the last one Q
+            fence_after();
+        }
+    }
+    // tokens past the sequence's end have no weight: the row is carried over where it is not in place
+    if (p.scores_in != p.scores_out)
+        for (int t = max(begin, len) + threadIdx.x; t < min(begin + chunk_tiles * kTileTokens, p.max_len); t += 128)
+            p.scores_out[out_row + t] = p.scores_in ? p.scores_in[in_row + t] : 0.f;
+    fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * columns));
     }
 }
 
@@ -563,6 +720,30 @@ template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const
     if (e != cudaSuccess) return e;
     attend_tile_kernel<T, DP><<<p.n_tile_ctas, kTileThreads, TileShape<DP>::kBytes, stream>>>(map, p);
     return cudaGetLastError();
+}
+
+template <typename T, int DP> cudaError_t launch_weigh(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+{
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = allow_shared(attend_weigh_kernel<T, DP>, (int)weigh_bytes<DP>(256), ready);
+    if (e != cudaSuccess) return e;
+    // two CTAs an SM hold all tiles at once, each at least two
+    const int chunk_tiles = (int)std::max<int64_t>(2, (p.own_tiles + 2 * p.sm_count - 1) / (2 * p.sm_count));
+    const int chunks = (p.max_len + chunk_tiles * kTileTokens - 1) / (chunk_tiles * kTileTokens);
+    const int64_t blocks = (int64_t)p.n_seq * p.H * chunks;
+    if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
+    if (blocks == 0) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = weigh_bytes<DP>(p.G * p.q_tokens);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attend_weigh_kernel<T, DP>, map, p, chunks, chunk_tiles);
 }
 
 }  // namespace
@@ -600,6 +781,14 @@ bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out)
     return reinterpret_cast<EncodeTiled>(sym)(static_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_UINT16, 5, pool.base, layer_major ? dims_l : dims_b, strides,
                                               layer_major ? box_l : box_b, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_attend_weigh(const AttnParams &p, const void *map, int dtype, cudaStream_t stream)
+{
+    const CUtensorMap &m = *static_cast<const CUtensorMap *>(map);
+    if (dtype == PDKV_DTYPE_BF16)
+        return p.D <= 64 ? launch_weigh<__nv_bfloat16, 64>(p, m, stream) : launch_weigh<__nv_bfloat16, 128>(p, m, stream);
+    return p.D <= 64 ? launch_weigh<__half, 64>(p, m, stream) : launch_weigh<__half, 128>(p, m, stream);
 }
 
 cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream)

@@ -372,6 +372,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             }
             std::vector<Shape> shape;
             for (int32_t n : n_rows) shape.push_back(shape_of(n, tile_ok));
+            s->own_tiles = shape_of(R, tile_ok).kernel == 1;
             // unit of (row tile 0, head 0) of every segment
             std::vector<int32_t> unit0(s->segs.size(), -1);
             const std::vector<Unit> warp_units = units_of(*s, 0, n_rows, shape), tile_units = units_of(*s, 1, n_rows, shape);
@@ -390,7 +391,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                 q.prefix_row0 = row0[(size_t)r];
                 q.logit_stride = (q.len + 3) / 4 * 4;
                 q.logits = s->logit_floats;
-                s->logit_floats += (int64_t)q.logit_stride * R * g.num_kv_heads;
+                if (!s->own_tiles) s->logit_floats += (int64_t)q.logit_stride * R * g.num_kv_heads;
                 q.direct = q.own_unit >= 0 && q.prefix_unit < 0;
                 if (q.direct) {   // every (row tile, head) in one part?
                     const int64_t tiles = (R + q.own_tile - 1) / q.own_tile;
@@ -503,7 +504,7 @@ int pdkv_seqs_items(const pdkv_seqs *s, const pdkv_attend_item **items, int64_t 
 namespace {
 
 struct ScratchLayout {
-    size_t o = 0, ml = 0, logits = 0, bytes = 0;
+    size_t o = 0, ml = 0, logits = 0, lse = 0, bytes = 0;
 };
 
 ScratchLayout scratch_layout(const pdkv_seqs *s, bool with_scores)
@@ -517,6 +518,7 @@ ScratchLayout scratch_layout(const pdkv_seqs *s, bool with_scores)
     l.o = place(s->join ? (size_t)s->part_rows * (size_t)s->pool.d.head_dim * 4 : 0);
     l.ml = place((s->join || with_scores) ? (size_t)s->part_rows * 8 : 0);
     l.logits = place(with_scores ? (size_t)s->logit_floats * 4 : 0);
+    l.lse = place(with_scores && s->own_tiles ? (size_t)s->n_seq * s->q_tokens * s->Hq * 4 : 0);
     return l;
 }
 
@@ -609,7 +611,13 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         p.part_o = reinterpret_cast<float *>(w + l.o);
         p.part_ml = reinterpret_cast<float *>(w + l.ml);
         if (scores) {
-            p.logits = reinterpret_cast<float *>(w + l.logits);
+            p.with_scores = 1;
+            if (s->own_tiles) {
+                if (!p.lse) p.lse = reinterpret_cast<float *>(w + l.lse);
+                for (int32_t n : s->len) p.own_tiles += (int64_t)((n + 127) / 128) * p.H;
+                p.sm_count = s->sm_count;
+            } else
+                p.logits = reinterpret_cast<float *>(w + l.logits);
             p.scores_in = a->scores_in;
             p.scores_out = a->scores_out;
             for (int i = 0; i < 2; ++i) {
@@ -631,9 +639,13 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
             const cudaError_t e = pdkv::launch_attend(p, s->map[0], s->dtype, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention kernel launch");
         }
-        if (s->join || scores) {
+        if (s->join || p.logits) {
             const cudaError_t e = pdkv::launch_attend_join(p, s->dtype, s->join, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "join kernel launch");
+        }
+        if (scores && s->own_tiles) {
+            const cudaError_t e = pdkv::launch_attend_weigh(p, s->map[1], s->dtype, st);
+            if (e != cudaSuccess) return pdkv::report_cuda_error(e, "weighing kernel launch");
         }
         return PDKV_OK;
     } catch (const std::bad_alloc &) {

@@ -82,7 +82,10 @@ struct AttnParams {
     const int32_t *seq_len;     // device, or null
     float *part_o;              // [part row][D], unnormalised, relative to the part's maximum
     float *part_ml;             // [part row][2]: maximum (base 2), sum
-    float *logits;              // null: no scores wanted
+    int32_t with_scores;
+    int64_t own_tiles;          // tiles of 128 own tokens, over all sequences and heads
+    int32_t sm_count;
+    float *logits;              // null: no scores wanted, or the weighing kernel finds them
     const float *scores_in;
     float *scores_out;
     int64_t scores_in_stride[2], scores_out_stride[2];
@@ -101,6 +104,7 @@ bool attend_tile_supported(const pdkv_pool_desc &d);
 int attend_tile_box(const pdkv_pool_desc &d);
 bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out);
 cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
+cudaError_t launch_attend_weigh(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream);
 
 struct EvictParams {
@@ -145,6 +149,7 @@ struct pdkv_seqs {
     int32_t n_ctas[2] = {0, 0};
     alignas(64) char map[2][pdkv::kMapBytes] = {};   // tensor maps of the pool, for the two kernels
     bool use_map = false;        // the warp kernel loads through its map
+    bool own_tiles = false;      // the tile kernel has the own tokens (all sequences have the same number of rows)
     std::vector<pdkv_attend_item> listing;
     int64_t part_rows = 0, logit_floats = 0;
     bool join = false;           // some rows have several parts, or none
