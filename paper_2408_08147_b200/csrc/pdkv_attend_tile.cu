@@ -543,163 +543,178 @@ template <int DP> constexpr uint32_t weigh_bytes(int rows)
 }  // namespace
 
 // Attention weights of own tokens, summed over the rows of their sequence, for segments that the tile kernel
-// attends to: a second pass over K once every row's sum is known.  Writing the logits and reading them
-// back, as is done for few rows, moves 8 bytes a row and token, against 2 bytes a dim for K: with 64 rows the
-// first took 57 us where this takes 13 (12 sequences of 300 to 4096 tokens, 8 heads of 128 dims).
+// attends to: a second pass over K once every row's sum is known.  (Writing the logits and reading them back, as
+// is done for few rows, moves 8 bytes a row and token, against 2 bytes a dim for K.)
 //
-// S^T = K Q^T: a thread has one token and its logits of all rows in tensor memory, so the sum over
-// the rows needs no other thread.  The next tile's product runs while this one's weights are computed.
+// S^T = K Q^T: a thread has one token and its logits of all rows in tensor memory, so the sum over the
+// rows needs no other thread.  Six warps: four compute weights, one issues the products, one the loads of K;
+// two tiles of K and two of S^T are on their way.  Two CTAs on an SM up to 128 rows.
 template <typename T, int DP>
-__global__ void __launch_bounds__(128) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
+__global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
 {
     using G = TileShape<DP>;
     extern __shared__ char raw[];
-    __shared__ uint64_t k_full[2], s_full[2];
+    __shared__ uint64_t k_full[2], k_empty[2], s_full[2], s_empty[2], q_full;
     __shared__ uint32_t tmem_s;
-    __shared__ __align__(16) float lse[256];
+    __shared__ __align__(16) float lse[256];   // negated, base 2
     __shared__ __align__(16) int sees[256];
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
-    const uint32_t q_sub = weigh_q_sub(p.G * p.q_tokens), q_at = smem_u32(smem), k_at = q_at + G::kSubs * q_sub;
+    const int R = p.G * p.q_tokens, columns = R > 128 ? 256 : R > 64 ? 128 : 64;   // of one S^T
+    const uint32_t q_sub = weigh_q_sub(R), q_at = smem_u32(smem), k_at = q_at + G::kSubs * q_sub;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int chunk = blockIdx.x % chunks, head = blockIdx.x / chunks % p.H, seq = blockIdx.x / chunks / p.H;
-    const int R = p.G * p.q_tokens, columns = R > 128 ? 256 : R > 64 ? 128 : 64;   // of one S^T
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&k_full[i], 1);
+            mbar_init(&k_empty[i], 1);
             mbar_init(&s_full[i], 1);
+            mbar_init(&s_empty[i], 4);
         }
+        mbar_init(&q_full, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(2 * columns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
-    const AttnSeq s = p.seqs[seq];
     const AttnSeg seg = p.segs[seq];
     asm volatile("griddepcontrol.wait;" ::: "memory");   // sums of the rows, current lengths
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = tmem_s;
-    const int len = own_len(p, seq, s.len), begin = chunk * chunk_tiles * kTileTokens;
+    const int len = own_len(p, seq, seg.len), begin = chunk * chunk_tiles * kTileTokens;
     const int limit = min(len, begin + chunk_tiles * kTileTokens);
     const int tiles = limit > begin ? (limit - begin + kTileTokens - 1) / kTileTokens : 0;
-    const float scale = fabsf(p.scale_log2);
-    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
     bool dead = false;
-    uint32_t phase[2] = {0, 0}, s_phase[2] = {0, 0};   // of K, of S^T
-    auto load_k = [&](int j) {   // warp 0
-        const int t0 = begin + j * kTileTokens, boxes = (min(kTileTokens, limit - t0) + p.tile_box - 1) / p.tile_box, slot = j & 1;
-        if (lane == 0) mbar_expect(&k_full[slot], (uint32_t)boxes * p.tile_box * 128 * G::kSubs);
-        __syncwarp();
-        if (lane < boxes) {
-            const int t = t0 + lane * p.tile_box, block = p.tbl[seg.tbl + t / p.pool.block_tokens], tt = t % p.pool.block_tokens;
-            for (int i = 0; i < G::kSubs; ++i) {
-                const uint32_t to = k_at + slot * G::kOperand + i * G::kSub + lane * p.tile_box * 128;
-                if (p.map_layer_major)
-                    load_box(to, &map, 64 * i, tt, head, block, 2 * p.layer, &k_full[slot]);
-                else
-                    load_box(to, &map, 64 * i, head, tt, 2 * p.layer, block, &k_full[slot]);
-            }
-        }
-        __syncwarp();
-    };
-    const int64_t out_row = seq * p.scores_out_stride[0] + head * p.scores_out_stride[1];
-    const int64_t in_row = seq * p.scores_in_stride[0] + head * p.scores_in_stride[1];
-    for (int r0 = 0; r0 < R && tiles > 0; r0 += 256) {
-        const int rows = min(256, R - r0), n = (rows + 15) / 16 * 16;
-        if (warp == 0) {
-            load_k(0);
-            if (tiles > 1) load_k(1);
-        }
-        // Q: DP / 8 neighbouring lanes a row, rows up to a multiple of 16 filled with zeros
-        constexpr int kLanes = DP / 8, kRows = 128 / kLanes;
-        const int c = threadIdx.x % kLanes;
-        for (int i = threadIdx.x / kLanes; i < n; i += kRows) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (i < rows && 8 * c < p.D) {
-                const int row = r0 + i;
-                v = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + seq * p.q_stride[0] + row / p.G * p.q_stride[1] +
-                                                     (head * p.G + row % p.G) * p.q_stride[2] + 8 * c);
-                v = make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
-            }
-            *reinterpret_cast<uint4 *>(smem + c / 8 * q_sub + i * 128 + ((c % 8) ^ (i % 8)) * 16) = v;
-        }
-        for (int i = threadIdx.x; i < columns; i += 128) {
-            const int row = r0 + min(i, rows - 1);
-            const float x = p.lse[((int64_t)seq * p.q_tokens + row / p.G) * p.G * p.H + head * p.G + row % p.G];
-            lse[i] = i >= rows || x == -INFINITY ? INFINITY : x * kLog2e;   // no weight: 2^(z - inf) = 0
-            sees[i] = len - (p.q_tokens - 1 - row / p.G);
-        }
-        fence_async_smem();
-        __syncthreads();
-        auto product = [&](int j) {   // thread 0: S^T of tile j
-            const uint32_t word = instruction<T>(n, false);
-            const uint32_t k = k_at + (j & 1) * G::kOperand;
-            for (int i = 0; i < DP / 16; ++i)
-                mma_shared(tmem + (j & 1) * columns, operand(k + i / 4 * G::kSub + i % 4 * 32, 16), operand(q_at + i / 4 * q_sub + i % 4 * 32, 16), word, i > 0);
-            commit(&s_full[j & 1]);
-        };
-        if (threadIdx.x == 0) {
-            mbar_wait(&k_full[0], phase[0], dead, p.status);
-            fence_after();
-            if (!dead) product(0);
-        }
-        phase[0] ^= 1;
-        for (int j = 0; j < tiles; ++j) {
-            const int b = j & 1, t0 = begin + j * kTileTokens, t = t0 + threadIdx.x;
-            if (j + 1 < tiles) {
-                if (threadIdx.x == 0) {
-                    mbar_wait(&k_full[b ^ 1], phase[b ^ 1], dead, p.status);
-                    fence_after();
-                    if (!dead) product(j + 1);
+    uint32_t n = 0;   // tiles so far, over all groups of 256 rows
+    if (warp == 5) {
+        for (int r0 = 0; r0 < R; r0 += 256)
+            for (int j = 0; j < tiles; ++j, ++n) {
+                const int t0 = begin + j * kTileTokens, boxes = (min(kTileTokens, limit - t0) + p.tile_box - 1) / p.tile_box, slot = n & 1;
+                int block = 0, tt = 0;
+                if (lane < boxes) {
+                    const int t = t0 + lane * p.tile_box;
+                    block = p.tbl[seg.tbl + t / p.pool.block_tokens];
+                    tt = t % p.pool.block_tokens;
                 }
-                phase[b ^ 1] ^= 1;
-            }
-            mbar_wait(&s_full[b], s_phase[b], dead, p.status);
-            s_phase[b] ^= 1;
-            __syncwarp();
-            fence_after();
-            if (warp == 0 && j + 2 < tiles && !__any_sync(~0u, dead)) load_k(j + 2);   // the product has read its K
-            const bool masked = t0 + kTileTokens > len - (p.q_tokens - 1);
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-            for (int col = 0; col < n; col += 32) {
-                float v[32];
-                tmem_load(v, tmem + ((uint32_t)(warp * 32) << 16) + b * columns + col);
-                tmem_load_wait();
+                mbar_wait(&k_empty[slot], (n >> 1 & 1) ^ 1, dead, p.status);
+                dead = __any_sync(~0u, dead);
+                if (dead) continue;
+                if (lane == 0) mbar_expect(&k_full[slot], (uint32_t)boxes * p.tile_box * 128 * G::kSubs);
+                __syncwarp();
+                if (lane < boxes) {
 #pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 e = *reinterpret_cast<const float4 *>(lse + col + k);
-                    float x[4] = {pow2(fmaf(v[k], scale, -e.x)), pow2(fmaf(v[k + 1], scale, -e.y)), pow2(fmaf(v[k + 2], scale, -e.z)),
-                                  pow2(fmaf(v[k + 3], scale, -e.w))};
-                    if (masked) {
-                        const int4 y = *reinterpret_cast<const int4 *>(sees + col + k);
-                        if (t >= y.x) x[0] = 0.f;
-                        if (t >= y.y) x[1] = 0.f;
-                        if (t >= y.z) x[2] = 0.f;
-                        if (t >= y.w) x[3] = 0.f;
+                    for (int i = 0; i < G::kSubs; ++i) {
+                        const uint32_t to = k_at + slot * G::kOperand + i * G::kSub + lane * p.tile_box * 128;
+                        if (p.map_layer_major)
+                            load_box(to, &map, 64 * i, tt, head, block, 2 * p.layer, &k_full[slot]);
+                        else
+                            load_box(to, &map, 64 * i, head, tt, 2 * p.layer, block, &k_full[slot]);
                     }
-                    // (columns past n hold nothing: their lse is infinite, but what lies there may be NaN)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (col + k + i < n) sum[i] += x[i];
                 }
             }
-            if (t < limit && !dead) {
-                const float add = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                const float in = r0 > 0 ? p.scores_out[out_row + t] : p.scores_in ? p.scores_in[in_row + t] : 0.f;
-                p.scores_out[out_row + t] = in + add;
+    } else if (warp == 4) {
+        if (lane == 0) {
+            uint32_t q_phase = 0;
+            for (int r0 = 0; r0 < R && tiles > 0; r0 += 256) {
+                const uint32_t word = instruction<T>((min(256, R - r0) + 15) / 16 * 16, false);
+                mbar_wait(&q_full, q_phase, dead, p.status);
+                q_phase ^= 1;
+                for (int j = 0; j < tiles; ++j, ++n) {
+                    const int b = n & 1;
+                    mbar_wait(&k_full[b], n >> 1 & 1, dead, p.status);
+                    mbar_wait(&s_empty[b], (n >> 1 & 1) ^ 1, dead, p.status);
+                    fence_after();
+                    const uint32_t k = k_at + b * G::kOperand;
+                    if (!dead) {
+#pragma unroll
+                        for (int i = 0; i < DP / 16; ++i)
+                            mma_shared(tmem + b * columns, operand(k + i / 4 * G::kSub + i % 4 * 32, 16), operand(q_at + i / 4 * q_sub + i % 4 * 32, 16), word, i > 0);
+                    }
+                    commit(&k_empty[b]);
+                    commit(&s_full[b]);
+                }
             }
-            fence_before();
-            __syncthreads();   // S^T of this tile may be overwritten, and after the last one Q
-            fence_after();
         }
+        __syncwarp();
+    } else {
+        const float scale = fabsf(p.scale_log2);
+        const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+        const int64_t out_row = seq * p.scores_out_stride[0] + head * p.scores_out_stride[1];
+        const int64_t in_row = seq * p.scores_in_stride[0] + head * p.scores_in_stride[1];
+        for (int r0 = 0; r0 < R && tiles > 0; r0 += 256) {
+            const int rows = min(256, R - r0), width = (rows + 15) / 16 * 16;
+            // Q: DP / 8 neighbouring lanes a row, rows up to a multiple of 16 filled with zeros.  (Every product with the
+            // rows before has been waited for.)
+            constexpr int kLanes = DP / 8, kRows = 128 / kLanes;
+            const int c = threadIdx.x % kLanes;
+#pragma unroll 4
+            for (int i = threadIdx.x / kLanes; i < width; i += kRows) {
+                const int row = r0 + i;
+                const bool there = i < rows && 8 * c < p.D;
+                const int64_t from = there ? seq * p.q_stride[0] + row / p.G * p.q_stride[1] + (head * p.G + row % p.G) * p.q_stride[2] + 8 * c : 0;
+                copy_async(q_at + c / 8 * q_sub + i * 128 + ((c % 8) ^ (i % 8)) * 16, static_cast<const T *>(p.q) + from, there);
+            }
+            for (int i = threadIdx.x; i < columns; i += 128) {
+                const int row = r0 + min(i, rows - 1);
+                const float x = p.lse[((int64_t)seq * p.q_tokens + row / p.G) * p.G * p.H + head * p.G + row % p.G];
+                lse[i] = i >= rows || x == -INFINITY ? -INFINITY : -x * kLog2e;   // no weight: 2^(z - inf) = 0
+                sees[i] = len - (p.q_tokens - 1 - row / p.G);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (flip)   // (a thread turns the signs of what it brought itself)
+                for (int i = threadIdx.x / kLanes; i < width; i += kRows) {
+                    uint4 *x = reinterpret_cast<uint4 *>(smem + c / 8 * q_sub + i * 128 + ((c % 8) ^ (i % 8)) * 16);
+                    *x = make_uint4(x->x ^ flip, x->y ^ flip, x->z ^ flip, x->w ^ flip);
+                }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&q_full);
+            asm volatile("bar.sync 1, 128;" ::: "memory");   // lse, sees
+            for (int j = 0; j < tiles; ++j, ++n) {
+                const int b = n & 1, t0 = begin + j * kTileTokens, t = t0 + threadIdx.x;
+                mbar_wait(&s_full[b], n >> 1 & 1, dead, p.status);
+                __syncwarp();
+                fence_after();
+                const bool masked = t0 + kTileTokens > len - (p.q_tokens - 1);
+                float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                const float2 scale2 = make_float2(scale, scale);
+#pragma unroll 1
+                for (int col = 0; col < width; col += 32) {
+                    float v[32];
+                    tmem_load(v, tmem + ((uint32_t)(warp * 32) << 16) + b * columns + col);
+                    tmem_load_wait();
+                    if (masked || col + 32 > width) {   // (columns past the last row hold anything)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (col + k >= width || t >= sees[col + k]) v[k] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        const float4 e = *reinterpret_cast<const float4 *>(lse + col + k);
+                        float2 x = fma2(make_float2(v[k], v[k + 1]), scale2, make_float2(e.x, e.y));
+                        float2 y = fma2(make_float2(v[k + 2], v[k + 3]), scale2, make_float2(e.z, e.w));
+                        sums[0] = add2(sums[0], make_float2(pow2(x.x), pow2(x.y)));
+                        sums[1] = add2(sums[1], make_float2(pow2(y.x), pow2(y.y)));
+                    }
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&s_empty[b]);
+                if (t < limit && !dead) {
+                    const float add = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
+                    const float in = r0 > 0 ? p.scores_out[out_row + t] : p.scores_in ? p.scores_in[in_row + t] : 0.f;
+                    p.scores_out[out_row + t] = in + add;
+                }
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");   // the next rows' lse, sees and Q take the place of these
+        }
+        // tokens past the sequence's end have no weight: the row is carried over where it is not in place
+        if (p.scores_in != p.scores_out)
+            for (int t = max(begin, len) + threadIdx.x; t < min(begin + chunk_tiles * kTileTokens, p.max_len); t += 128)
+                p.scores_out[out_row + t] = p.scores_in ? p.scores_in[in_row + t] : 0.f;
     }
-    // tokens past the sequence's end have no weight: the row is carried over where it is not in place
-    if (p.scores_in != p.scores_out)
-        for (int t = max(begin, len) + threadIdx.x; t < min(begin + chunk_tiles * kTileTokens, p.max_len); t += 128)
-            p.scores_out[out_row + t] = p.scores_in ? p.scores_in[in_row + t] : 0.f;
     fence_before();
     __syncthreads();
     if (warp == 0) {
@@ -735,7 +750,7 @@ template <typename T, int DP> cudaError_t launch_weigh(const AttnParams &p, cons
     if (blocks == 0) return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(128);
+    cfg.blockDim = dim3(192);
     cfg.dynamicSmemBytes = weigh_bytes<DP>(p.G * p.q_tokens);
     cfg.stream = stream;
     cudaLaunchAttribute at[1];
