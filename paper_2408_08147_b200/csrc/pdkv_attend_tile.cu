@@ -6,7 +6,8 @@
 //     P = 2^(S - m)  one thread a row, rounded to 16 bits and written over S
 //     O += P V       tcgen05.mma, P from tensor memory, O stays in tensor memory
 // Two row tiles take turns: while the threads of one turn S into P, the tensor cores work for the
-// other, and both use the same K and V, which halves what is read from L2.  Ten warps: four per row
+// other, and both use the same K and V, which halves what is read from L2.  When there is only one row tile, the
+// two halves of the CTA take every second tile of tokens each, and leave two parts to be joined.  Ten warps: four per row
 // tile for the softmax, one that issues the matrix instructions, one that issues the loads (TMA boxes of one
 // page, 64 dims and the 128-byte swizzle that the matrix instructions expect).
 //
@@ -139,7 +140,17 @@ __device__ __forceinline__ void commit(uint64_t *b)
 // What every role has to know about an item.
 struct Work {
     AttnItem it;
-    int len, limit, tiles, row_tiles;
+    int len, limit, tiles;   // tiles of tokens
+    bool pair;               // two row tiles share the tokens; else the one row tile has every second tile of tokens
+                             // in each half of the CTA, as two parts to be joined
+    // Tiles of tokens of half t, and which they are.
+    __device__ __forceinline__ int count(int t) const { return pair ? tiles : (tiles + 1 - t) / 2; }
+    __device__ __forceinline__ int tile(int t, int j) const { return pair ? j : 2 * j + t; }
+    // Place of K (kv 0) or V (1) of token tile i in the order of the loads: K, V alternating, or K K V V.
+    __device__ __forceinline__ uint32_t order(int kv, int i) const
+    {
+        return pair ? 2 * i + kv : i / 2 * 4 + kv * ((i | 1) < tiles ? 2 : 1) + i % 2;
+    }
 };
 __device__ __forceinline__ Work work_of(const AttnParams &p, const AttnItem &it)
 {
@@ -148,7 +159,7 @@ __device__ __forceinline__ Work work_of(const AttnParams &p, const AttnItem &it)
     w.len = it.seq >= 0 ? own_len(p, it.seq, it.len) : it.len;
     w.limit = min(it.tok1, w.len);
     w.tiles = w.limit > it.tok0 ? (w.limit - it.tok0 + kTileTokens - 1) / kTileTokens : 0;
-    w.row_tiles = it.rows > kTileRows ? 2 : 1;
+    w.pair = it.rows > kTileRows;
     return w;
 }
 
@@ -158,12 +169,12 @@ template <int DP> __device__ __forceinline__ uint32_t q_place(int t, int k)
 {
     constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
     const int lane = threadIdx.x % 32, row = threadIdx.x / 32 % 4 * 32 + k * kRows + lane / kLanes, c = lane % kLanes;
-    return t * TileShape<DP>::kOperand + c / 8 * TileShape<DP>::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16;
+    return (uint32_t)t * TileShape<DP>::kOperand + c / 8 * TileShape<DP>::kSub + row * 128 + ((c % 8) ^ (row % 8)) * 16;
 }
 template <typename T, int DP> __device__ __forceinline__ void fetch_q(const AttnParams &p, const Work &w, int t, uint32_t q_at)
 {
     constexpr int kLanes = DP / 8, kRows = 32 / kLanes;
-    const int lane = threadIdx.x % 32, mine = t * kTileRows + threadIdx.x % kSoftmaxThreads, d = 8 * (lane % kLanes);
+    const int lane = threadIdx.x % 32, mine = (w.pair ? t * kTileRows : 0) + threadIdx.x % kSoftmaxThreads, d = 8 * (lane % kLanes);
     const bool live = mine < w.it.rows;
     const RowId id = row_id(p, w.it, w.it.row0 + (live ? mine : 0));
     const int64_t at = live ? id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (w.it.head * p.G + id.g) * p.q_stride[2] : -1;
@@ -201,23 +212,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kMmaWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(kColumns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
-    // the first item's Q comes while tensor memory is set up
-    bool q_early = false;
-    if (warp < kMmaWarp) {
-        const Work w = work_of(p, first);
-        q_early = w.tiles > 0 && warp / 4 < w.row_tiles;
-        if (q_early) fetch_q<T, DP>(p, w, warp / 4, q_at);
-    }
-    fence_before();
     __syncthreads();
-    fence_after();
     asm volatile("griddepcontrol.launch_dependents;");
-    const uint32_t tmem = bar.tmem;
     bool dead = false;
+    // tensor memory is there for the warps that use it; the loads of K and V do not wait for it
+    auto tensor_memory = [&]() -> uint32_t {
+        fence_before();
+        asm volatile("bar.sync 1, 288;" ::: "memory");
+        fence_after();
+        return bar.tmem;
+    };
 
     // 168 registers a thread at launch: the softmax threads, which hold a row of S, take 216, the others keep 72
     // (256 x 216 + 128 x 72 = 384 x 168).
@@ -233,37 +237,49 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             more = it.next >= 0;
             const Work w = work_of(p, it);
             it = next_it;
-            for (int j = 0; j < w.tiles; ++j) {
-                const int t0 = w.it.tok0 + j * kTileTokens, live = min(kTileTokens, w.limit - t0);
-                const int boxes = (live + page_rows - 1) / page_rows;   // pages past the end are not loaded
-                int block = 0, tt = 0;
-                if (lane < boxes) {
-                    const int t = t0 + lane * page_rows;
-                    block = p.tbl[w.it.tbl + t / p.pool.block_tokens];
-                    tt = t % p.pool.block_tokens;
-                }
-                for (int kv = 0; kv < 2; ++kv, ++n) {
-                    const int slot = n % G::kSlots;
-                    mbar_wait(&bar.empty[slot], (n / G::kSlots & 1) ^ 1, dead, p.status);
-                    dead = __any_sync(~0u, dead);
-                    if (dead) continue;
-                    if (lane == 0) mbar_expect(&bar.full[slot], (uint32_t)boxes * page_rows * 128 * G::kSubs);
-                    __syncwarp();
-                    if (lane < boxes) {
-                        const uint32_t to = ring_at + slot * G::kOperand + lane * page_rows * 128;
-                        const int lc = 2 * p.layer + kv;
+            const int group = w.pair ? 1 : 2;   // tiles of tokens whose K come before their V
+            for (int i0 = 0; i0 < w.tiles; i0 += group) {
+                int block[2] = {0, 0}, tt[2] = {0, 0}, boxes[2] = {0, 0};
 #pragma unroll
-                        for (int s = 0; s < G::kSubs; ++s) {
-                            if (p.map_layer_major)
-                                load_box(to + s * G::kSub, &map, 64 * s, tt, w.it.head, block, lc, &bar.full[slot]);
-                            else
-                                load_box(to + s * G::kSub, &map, 64 * s, w.it.head, tt, lc, block, &bar.full[slot]);
-                        }
+                for (int g = 0; g < 2; ++g) {
+                    const int t0 = w.it.tok0 + (i0 + g) * kTileTokens;
+                    if (g >= group || t0 >= w.limit) continue;
+                    boxes[g] = (min(kTileTokens, w.limit - t0) + page_rows - 1) / page_rows;   // pages past the end are not loaded
+                    if (lane < boxes[g]) {
+                        const int t = t0 + lane * page_rows;
+                        block[g] = p.tbl[w.it.tbl + t / p.pool.block_tokens];
+                        tt[g] = t % p.pool.block_tokens;
                     }
                 }
+                for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        if (boxes[g] == 0) continue;
+                        const int slot = n % G::kSlots;
+                        mbar_wait(&bar.empty[slot], (n / G::kSlots & 1) ^ 1, dead, p.status);
+                        ++n;
+                        dead = __any_sync(~0u, dead);
+                        if (dead) continue;
+                        if (lane == 0) mbar_expect(&bar.full[slot], (uint32_t)boxes[g] * page_rows * 128 * G::kSubs);
+                        __syncwarp();
+                        if (lane < boxes[g]) {
+                            const uint32_t to = ring_at + slot * G::kOperand + lane * page_rows * 128;
+                            const int lc = 2 * p.layer + kv;
+#pragma unroll
+                            for (int s = 0; s < G::kSubs; ++s) {
+                                if (p.map_layer_major)
+                                    load_box(to + s * G::kSub, &map, 64 * s, tt[g], w.it.head, block[g], lc, &bar.full[slot]);
+                                else
+                                    load_box(to + s * G::kSub, &map, 64 * s, w.it.head, tt[g], lc, block[g], &bar.full[slot]);
+                            }
+                        }
+                    }
             }
         }
     } else if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        const uint32_t tmem = tensor_memory();
         if (lane == 0) {
             constexpr uint32_t kWordS = instruction<T>(kTileTokens, false), kWordO = instruction<T>(DP, true);
             uint32_t n = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
@@ -290,49 +306,58 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 const Work w = work_of(p, it);
                 it = next_it;
                 if (w.tiles == 0) continue;
-                uint32_t k_slot = n % G::kSlots;
-                mbar_wait(&bar.full[k_slot], n / G::kSlots & 1, dead, p.status);
-                for (int t = 0; t < w.row_tiles; ++t) {
+                // the operand at place `at` of the load order has arrived, is no longer needed
+                auto arrived = [&](uint32_t at) {
+                    const uint32_t slot = (n + at) % G::kSlots;
+                    mbar_wait(&bar.full[slot], (n + at) / G::kSlots & 1, dead, p.status);
+                    fence_after();
+                    return slot;
+                };
+                for (int t = 0; t < 2; ++t) {
+                    if (w.count(t) == 0) continue;
                     mbar_wait(&bar.q_ready[t], q_phase[t], dead, p.status);
                     q_phase[t] ^= 1;
-                    fence_after();
-                    if (!dead) product_s(t, k_slot);
+                    const uint32_t k = arrived(w.order(0, w.tile(t, 0)));
+                    if (!dead) product_s(t, k);
                     commit(&bar.s_full[t]);
+                    if (!w.pair || t == 1) commit(&bar.empty[k]);
                 }
-                commit(&bar.empty[k_slot]);
-                for (int j = 0; j < w.tiles; ++j, n += 2) {
-                    const uint32_t v_slot = (n + 1) % G::kSlots;
-                    const bool last = j + 1 == w.tiles;
-                    mbar_wait(&bar.full[v_slot], (n + 1) / G::kSlots & 1, dead, p.status);
-                    for (int t = 0; t < w.row_tiles; ++t) {
+                for (int j = 0; j < w.count(0); ++j) {
+                    for (int t = 0; t < 2; ++t) {
+                        if (j >= w.count(t)) continue;
+                        const bool last = j + 1 == w.count(t), release = !w.pair || t == 1;
                         mbar_wait(&bar.p_half[t], p_phase[t], dead, p.status);
-                        fence_after();
-                        if (!dead) product_o(t, v_slot, 0, j > 0);
+                        const uint32_t v = arrived(w.order(1, w.tile(t, j)));
+                        if (!dead) product_o(t, v, 0, j > 0);
                         mbar_wait(&bar.p_ready[t], p_phase[t], dead, p.status);
                         p_phase[t] ^= 1;
                         fence_after();
-                        if (!dead) product_o(t, v_slot, 1, true);
+                        if (!dead) product_o(t, v, 1, true);
+                        if (release) commit(&bar.empty[v]);
                         if (last) {
                             commit(&bar.o_full[t]);
                         } else {
-                            if (t == 0) {
-                                k_slot = (n + 2) % G::kSlots;
-                                mbar_wait(&bar.full[k_slot], (n + 2) / G::kSlots & 1, dead, p.status);
-                                fence_after();
-                            }
-                            if (!dead) product_s(t, k_slot);
+                            const uint32_t k = arrived(w.order(0, w.tile(t, j + 1)));
+                            if (!dead) product_s(t, k);
                             commit(&bar.s_full[t]);
+                            if (release) commit(&bar.empty[k]);
                         }
                     }
-                    commit(&bar.empty[v_slot]);
-                    if (!last) commit(&bar.empty[k_slot]);
                 }
+                n += 2 * w.tiles;
             }
         }
         __syncwarp();
     }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        bool q_early = false;   // the first item's Q comes while tensor memory is set up
+        {
+            const Work w = work_of(p, first);
+            q_early = w.count(warp / 4) > 0;
+            if (q_early) fetch_q<T, DP>(p, w, warp / 4, q_at);
+        }
+        const uint32_t tmem = tensor_memory();
         // softmax of row tile t: one thread a row
         const int t = warp / 4, r = threadIdx.x % kSoftmaxThreads;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
@@ -378,27 +403,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             it = next_it;
             const uint32_t n0 = n;
             n += 2 * w.tiles;
-            if (t >= w.row_tiles) continue;
-            const int row = t * kTileRows + r;
+            const int count = w.count(t), row = (w.pair ? t * kTileRows : 0) + r;
             const bool live = row < w.it.rows, own = w.it.seq >= 0;
             const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             float m = -INFINITY, l = 0.f;
-            if (w.tiles > 0) {
+            if (count > 0) {
                 if (!q_there) fetch_q<T, DP>(p, w, t, q_at);
                 if (!q_there || !q_done) finish_q();
                 q_there = q_done = false;
                 const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;
                 const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
-                for (int j = 0; j < w.tiles; ++j) {
-                    const int t0 = w.it.tok0 + j * kTileTokens;
+                for (int j = 0; j < count; ++j) {
+                    const int t0 = w.it.tok0 + w.tile(t, j) * kTileTokens;
                     const bool masked = t0 + kTileTokens > safe;
                     mbar_wait(&bar.s_full[t], s_phase, dead, p.status);
                     s_phase ^= 1;
                     __syncwarp();
                     fence_after();
-                    if (t == 0 && t0 + kTileTokens > w.limit) {
+                    if ((t == 0 || !w.pair) && t0 + kTileTokens > w.limit) {
                         // rows of V past the end may hold anything, and 0 * NaN is NaN: they become zero
-                        const uint32_t v = n0 + 2 * j + 1;
+                        const uint32_t v = n0 + w.order(1, w.tile(t, j));
                         mbar_wait(&bar.full[v % G::kSlots], v / G::kSlots & 1, dead, p.status);
                         if (t0 + r >= w.limit) {
                             char *zero = smem + 2 * G::kOperand + v % G::kSlots * G::kOperand + r * 128;
@@ -475,7 +499,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 // every product with Q is done: the next item's Q may take its place
                 if (more) {
                     const Work next = work_of(p, next_it);
-                    if (t < next.row_tiles && next.tiles > 0) {
+                    if (next.count(t) > 0) {
                         fetch_q<T, DP>(p, next, t, q_at);
                         finish_q();
                         q_there = q_done = true;
@@ -487,16 +511,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 fence_after();
             }
             const int head = w.it.head * p.G + id.g;
+            const int64_t part_row = w.it.part_row + (!w.pair && t == 1 ? w.it.rows : 0);
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const int64_t to = !live || dead ? -1
                                : w.it.direct ? id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2]
-                                             : (w.it.part_row + row) * p.D;
+                                             : (part_row + row) * p.D;
             // (loops that run once an item stay rolled: fetching their instructions costs more than running them)
 #pragma unroll 1
             for (int c = 0; c < DP / 32; ++c) {
                 float v[32];
                 __syncwarp();
-                if (w.tiles > 0) {
+                if (count > 0) {
                     tmem_load(v, o_at + 32 * c);
                     tmem_load_wait();
                 } else {
@@ -519,7 +544,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             }
             if (live && !dead) {
                 if (w.it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (m + log2f(l)) * kLn2;
-                if (!w.it.direct || p.with_scores) *reinterpret_cast<float2 *>(p.part_ml + 2 * (w.it.part_row + row)) = make_float2(m, l);
+                if (!w.it.direct || p.with_scores) *reinterpret_cast<float2 *>(p.part_ml + 2 * (part_row + row)) = make_float2(m, l);
             }
         }
     }
@@ -527,7 +552,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     __syncthreads();
     if (warp == kMmaWarp) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns));
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(bar.tmem), "r"(kColumns));
     }
 }
 

@@ -117,7 +117,7 @@ Shape shape_of(int64_t rows, bool tile_ok)
 // 3700 a quantum in the tile kernel, 3 us against 1.5 us (a CTA's share of the memory rate) in the warp kernel.
 constexpr int64_t kItemCost[2] = {2, 4};
 
-struct Unit { int32_t seg, head, row0, rows; int64_t quanta; };
+struct Unit { int32_t seg, head, row0, rows; int64_t quantum, quanta; };   // tokens of a quantum, how many
 struct Piece { size_t unit; int64_t from, n; int32_t cta; };
 
 // Deals units to CTAs in order, each CTA up to a load of `most` quanta; units are cut where a CTA is full.
@@ -170,9 +170,11 @@ std::vector<Unit> units_of(const pdkv_seqs &s, int kernel, const std::vector<int
         const AttnSeg &seg = s.segs[g];
         if (shape[g].kernel != kernel || seg.len == 0 || n_rows[g] == 0) continue;
         for (int32_t r0 = 0; r0 < n_rows[g]; r0 += shape[g].row_tile)
-            for (int32_t h = 0; h < s.pool.d.num_kv_heads; ++h)
-                units.push_back({(int32_t)g, h, r0, std::min<int32_t>(shape[g].row_tile, n_rows[g] - r0),
-                                 (seg.len + shape[g].quantum - 1) / shape[g].quantum});
+            for (int32_t h = 0; h < s.pool.d.num_kv_heads; ++h) {
+                const int32_t rows = std::min<int32_t>(shape[g].row_tile, n_rows[g] - r0);
+                const int64_t quantum = kernel == 1 && rows <= 128 ? 256 : shape[g].quantum;   // two tiles of tokens at a time
+                units.push_back({(int32_t)g, h, r0, rows, quantum, (seg.len + quantum - 1) / quantum});
+            }
     }
     return units;
 }
@@ -187,7 +189,7 @@ int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std:
     if (tile_units.empty()) return 0;
     double tile = 0, bytes = 0;
     for (const Unit &u : tile_units) tile += (double)(u.quanta + kItemCost[1]);
-    for (const Unit &u : warp_units) bytes += 64.0 * (double)u.quanta * 4 * s.pool.d.head_dim;
+    for (const Unit &u : warp_units) bytes += (double)(u.quantum * u.quanta) * 4 * s.pool.d.head_dim;
     int best = 1;
     double best_us = 1e30;
     for (int n = 1; n < s.sm_count; ++n) {
@@ -203,8 +205,7 @@ int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std:
 
 // Work list of one kernel.  Whole units when that is as quick as cutting them (nothing is to be joined then,
 // which saves a kernel: about two quanta more); CTAs get at least four quanta, so that joining stays cheap.
-void plan_items(pdkv_seqs &s, int kernel, const std::vector<Unit> &units, const std::vector<Shape> &shape, std::vector<int32_t> &unit0,
-                int n_ctas_max)
+void plan_items(pdkv_seqs &s, int kernel, const std::vector<Unit> &units, std::vector<int32_t> &unit0, int n_ctas_max)
 {
     int64_t quanta = 0;
     for (size_t u = 0; u < units.size(); ++u) {
@@ -223,10 +224,10 @@ void plan_items(pdkv_seqs &s, int kernel, const std::vector<Unit> &units, const 
     for (const Piece &x : pieces) {
         const Unit &w = units[x.unit];
         const AttnSeg &seg = s.segs[(size_t)w.seg];
-        const int64_t quantum = shape[(size_t)w.seg].quantum;
+        const int parts = kernel == 1 && w.rows <= 128 ? 2 : 1;   // the tile kernel leaves one for each half of a CTA
         AttnUnit &unit = s.units[first_unit + x.unit];
         if (x.from == 0) unit = {s.part_rows, 0, w.rows};
-        ++unit.n_parts;
+        unit.n_parts += parts;
         AttnItem it{};
         it.part_row = s.part_rows;
         it.tbl = seg.tbl;
@@ -236,9 +237,9 @@ void plan_items(pdkv_seqs &s, int kernel, const std::vector<Unit> &units, const 
         it.head = w.head;
         it.row0 = w.row0;
         it.rows = w.rows;
-        it.tok0 = (int32_t)(x.from * quantum);
-        it.tok1 = (int32_t)std::min<int64_t>(seg.len, (x.from + x.n) * quantum);
-        s.part_rows += w.rows;
+        it.tok0 = (int32_t)(x.from * w.quantum);
+        it.tok1 = (int32_t)std::min<int64_t>(seg.len, (x.from + x.n) * w.quantum);
+        s.part_rows += parts * w.rows;
         pdkv_attend_item li{};
         li.prefix = w.seg >= s.n_seq ? w.seg - s.n_seq : -1;
         li.seq = w.seg < s.n_seq ? w.seg : -1;
@@ -377,8 +378,8 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             std::vector<int32_t> unit0(s->segs.size(), -1);
             const std::vector<Unit> warp_units = units_of(*s, 0, n_rows, shape), tile_units = units_of(*s, 1, n_rows, shape);
             const int sms = tile_sms(*s, warp_units, tile_units);
-            plan_items(*s, 1, tile_units, shape, unit0, sms);
-            plan_items(*s, 0, warp_units, shape, unit0, pdkv::attend_ctas_per_sm(g.head_dim) * std::max(1, s->sm_count - s->n_ctas[1]));
+            plan_items(*s, 1, tile_units, unit0, sms);
+            plan_items(*s, 0, warp_units, unit0, pdkv::attend_ctas_per_sm(g.head_dim) * std::max(1, s->sm_count - s->n_ctas[1]));
             s->seqs.resize((size_t)s->n_seq);
             for (int32_t r = 0; r < s->n_seq; ++r) {
                 AttnSeq &q = s->seqs[(size_t)r];
