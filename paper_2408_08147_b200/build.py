@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(_HERE, "libpdkv.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-O3", "-std=c++17", "-lineinfo",
+    "-O3", "-std=c++17", "-lineinfo", "--threads", "0",
     "-Xcompiler", "-fPIC,-Wall,-Wextra",
     "-shared",
 ]

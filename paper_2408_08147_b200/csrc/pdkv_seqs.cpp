@@ -181,7 +181,7 @@ std::vector<Unit> units_of(const pdkv_seqs &s, int kernel, const std::vector<int
 
 // SMs for the tile kernel when both kernels have work: they run at the same time, each on SMs of its own (a CTA of
 // the tile kernel leaves no shared memory for others), and the slower one should be as quick as possible.
-// Measured on B200: 2 us a quantum of the tile kernel and 4 us around it; the warp kernel reads 42 GB/s per SM,
+// Measured on B200: 2.3 to 3 us a quantum of the tile kernel beside the other and 4 us around it; the warp kernel reads 42 GB/s per SM,
 // whether it has all of them or a few, 5 us around it.
 int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std::vector<Unit> &tile_units)
 {
@@ -193,7 +193,7 @@ int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std:
     int best = 1;
     double best_us = 1e30;
     for (int n = 1; n < s.sm_count; ++n) {
-        const double tile_us = 4 + 2.0 * std::max((tile + kItemCost[1] * (double)n) / n, (double)(1 + kItemCost[1]));
+        const double tile_us = 4 + 2.6 * std::max((tile + kItemCost[1] * (double)n) / n, (double)(1 + kItemCost[1]));
         const double warp_us = 5 + bytes / (42e3 * (s.sm_count - n));
         if (std::max(tile_us, warp_us) < best_us) {
             best_us = std::max(tile_us, warp_us);

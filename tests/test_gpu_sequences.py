@@ -130,6 +130,10 @@ CASES = [
     dict(lens=[700], H=1, G=4, Q=64, D=64, block=128, layout=LAYER_MAJOR, dtype="fp16"),
     dict(lens=[3000, 2990], H=1, G=8, Q=8, D=128, block=64, prefix_len=[1500], member=[0, 0]),
     dict(lens=[40, 150], H=2, G=50, D=64, block=24),
+    # several items for every CTA
+    dict(lens=[33, 0, 7, 64, 65, 31, 96, 1] * 24, H=8, G=1, D=64, layers=1, layer=0),
+    dict(lens=[70, 300, 5, 129] * 20, H=4, G=4, D=128, block=8, layout=LAYER_MAJOR, layers=1, layer=0, dtype="fp16", prefix_len=[40], member=[0, -1] * 40),
+    dict(lens=[70, 300, 5, 129] * 20, H=4, G=3, Q=4, D=80, block=12, layers=1, layer=0),
 ]
 
 
