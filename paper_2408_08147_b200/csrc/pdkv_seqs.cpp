@@ -181,25 +181,30 @@ std::vector<Unit> units_of(const pdkv_seqs &s, int kernel, const std::vector<int
 
 // SMs for the tile kernel when both kernels have work: they run at the same time, each on SMs of its own (a CTA of
 // the tile kernel leaves no shared memory for others), and the slower one should be as quick as possible.
-// Measured on B200: 2.3 to 3 us a quantum of the tile kernel beside the other and 4 us around it; the warp kernel reads 42 GB/s per SM,
-// whether it has all of them or a few, 5 us around it.
+// Measured on B200: 2.2 us a quantum of the tile kernel -- 3.4 us beside a saturated memory -- and 4 us around it; an SM
+// of the warp kernel reads 76 GB/s and takes 1.8 us to change items, 6.3 TB/s for all of them, 5 us around it.
 int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std::vector<Unit> &tile_units)
 {
     if (warp_units.empty()) return s.sm_count;
     if (tile_units.empty()) return 0;
-    double tile = 0, bytes = 0;
-    for (const Unit &u : tile_units) tile += (double)(u.quanta + kItemCost[1]);
+    double bytes = 0;
     for (const Unit &u : warp_units) bytes += (double)(u.quantum * u.quanta) * 4 * s.pool.d.head_dim;
     int best = 1;
     double best_us = 1e30;
-    for (int n = 1; n < s.sm_count; ++n) {
-        const double tile_us = 4 + 2.6 * std::max((tile + kItemCost[1] * (double)n) / n, (double)(1 + kItemCost[1]));
-        const double warp_us = 5 + bytes / (42e3 * (s.sm_count - n));
-        if (std::max(tile_us, warp_us) < best_us) {
-            best_us = std::max(tile_us, warp_us);
+    auto attempt = [&](int n) {
+        if (n < 1 || n >= s.sm_count) return;
+        const double load = (double)least_load(tile_units, kItemCost[1], n, true);
+        const double warp_us = 5 + std::max(bytes / 6.3e6, (bytes / 76e3 + 1.8 * (double)warp_units.size()) / (s.sm_count - n));
+        const double busy = std::min(1.0, bytes / 6.3e6 / std::max(warp_us, 4 + 2.2 * load));   // share of the time with a saturated memory
+        const double us = std::max(warp_us, 4 + (2.2 + 1.2 * busy) * load);
+        if (us < best_us) {
+            best_us = us;
             best = n;
         }
-    }
+    };
+    for (int n = 4; n < s.sm_count; n += 8) attempt(n);
+    const int about = best;
+    for (int n = about - 7; n <= about + 7; ++n) attempt(n);
     return best;
 }
 
