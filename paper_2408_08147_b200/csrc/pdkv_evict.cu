@@ -28,9 +28,9 @@ __device__ __forceinline__ uint32_t order_key(float x)
 
 namespace {
 
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWarps = kSelectThreads / 32;
-constexpr int kMaxKeys = 16;   // keys a thread holds in registers
+// Threads of a selecting CTA and keys that each holds in registers: small CTAs, several on an SM, for rows that fit
+// one (their rounds are latency, which other CTAs fill); large ones in clusters for longer rows.
+constexpr int kSmallSelect = 256, kSmallKeys = 32, kLargeSelect = 1024, kLargeKeys = 16;
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -59,29 +59,30 @@ __device__ __forceinline__ int peer_word(const int *p, uint32_t rank)
     return v;
 }
 
-__device__ __forceinline__ void put_peer_word(const int *p, uint32_t rank, int v)
+__device__ __forceinline__ void put_peer(const int *p, uint32_t rank, int a, int b, int c)
 {
     uint32_t at = (uint32_t)__cvta_generic_to_shared(p), far;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(at), "r"(rank));
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(far), "r"(v) : "memory");
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(far), "r"(a), "r"(b), "r"(c) : "memory");
 }
 
-struct SelectShared {
+struct alignas(16) SelectShared {
     int count[3][4];              // of the CTA, by round modulo 3
     int exchange[2][8][4];        // of every CTA of the cluster
-    int warp_over[kSelectWarps], warp_tie[kSelectWarps];
+    int warp_over[32], warp_tie[32];
     int totals[2];
 };
 
 // Token t of a row's middle part is one of the `want` heaviest: kept[at ..) receives them in order.
-// K keys a thread live in registers, read once; K = 0 reads them again in every round.
-template <int K>
+// K keys a thread live in registers, read once; K = 0 (rows of more than 8 x 16384 tokens) reads them again in
+// every round.
+template <int THREADS, int K>
 __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, int lo, int hi, int per, int want, int32_t *kept,
                                            uint32_t rank, uint32_t ranks)
 {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     // tokens of this warp: a contiguous run of 32 * per, lane by lane
-    const int64_t first = lo + ((int64_t)rank * kSelectWarps + warp) * 32 * per + lane;
+    const int64_t first = lo + ((int64_t)rank * (THREADS / 32) + warp) * 32 * per + lane;
     const int begin = (int)min(first, (int64_t)hi);
     uint32_t keys[K > 0 ? K : 1];
     if (K > 0) {
@@ -99,14 +100,26 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
         int c1 = 0, c2 = 0, c3 = 0;
         if (K > 0) {
             // (a missing key is 0 and reaches nothing).  At most 512 keys a warp: three counts in one number, one
-            // reduction -- there are few lanes for those
+            // reduction -- there are few lanes for those; 1024 keys: two
             uint32_t c = 0;
+            if (K <= 16) {
 #pragma unroll
-            for (int i = 0; i < K; ++i) c += (keys[i] >= p1) + (keys[i] >= p2 ? 1u << 10 : 0u) + (keys[i] >= p3 ? 1u << 20 : 0u);
-            c = __reduce_add_sync(~0u, c);
-            c1 = c & 1023;
-            c2 = c >> 10 & 1023;
-            c3 = c >> 20;
+                for (int i = 0; i < K; ++i) c += (keys[i] >= p1) + (keys[i] >= p2 ? 1u << 10 : 0u) + (keys[i] >= p3 ? 1u << 20 : 0u);
+                c = __reduce_add_sync(~0u, c);
+                c1 = c & 1023;
+                c2 = c >> 10 & 1023;
+                c3 = c >> 20;
+            } else {
+#pragma unroll
+                for (int i = 0; i < K; ++i) {
+                    c += (keys[i] >= p1) + (keys[i] >= p2 ? 1u << 16 : 0u);
+                    c3 += keys[i] >= p3;
+                }
+                c = __reduce_add_sync(~0u, c);
+                c3 = __reduce_add_sync(~0u, c3);
+                c1 = c & 0xffff;
+                c2 = c >> 16;
+            }
         } else {
             for (int i = 0; i < per; ++i) {
                 const uint32_t k = begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u;
@@ -127,7 +140,7 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
         c3 = mine[2];
         if (ranks > 1) {
             int(*far)[4] = sh.exchange[round % 2];
-            if (threadIdx.x < 4 * ranks) put_peer_word(&far[rank][lane % 4], lane / 4, mine[lane % 4]);
+            if (threadIdx.x < ranks) put_peer(far[rank], lane, c1, c2, c3);
             cluster_barrier();
             c1 = c2 = c3 = 0;
             for (uint32_t r = 0; r < ranks; ++r) {
@@ -173,7 +186,7 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
     }
     __syncthreads();
     {
-        const int o = sh.warp_over[lane], e = sh.warp_tie[lane];
+        const int o = lane < THREADS / 32 ? sh.warp_over[lane] : 0, e = lane < THREADS / 32 ? sh.warp_tie[lane] : 0;
         over = __reduce_add_sync(~0u, lane < warp ? o : 0);   // from here on: counts before this warp
         tie = __reduce_add_sync(~0u, lane < warp ? e : 0);
         const int all_over = __reduce_add_sync(~0u, o), all_tie = __reduce_add_sync(~0u, e);
@@ -221,7 +234,8 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
 // warp go through one integer reduction, CTAs of a cluster exchange theirs over distributed shared memory.
 // Every warp owns a contiguous run of tokens, so the order of the indices follows from counts per
 // warp alone.  Bound by the latency of the rounds.
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kSmallSelect ? 4 : 1) evict_select_kernel(const EvictParams p)
 {
     __shared__ __align__(16) SelectShared sh;
     asm volatile("griddepcontrol.launch_dependents;");
@@ -230,7 +244,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     const int head = row_id % p.H, seq = row_id / p.H % p.n_seq, layer = row_id / p.H / p.n_seq;
     const int len = own_len(p, seq);
     int32_t *kept = p.kept + (int64_t)row_id * p.budget;
-    const int first = rank * kSelectThreads + threadIdx.x, step = ranks * kSelectThreads;
+    const int first = rank * THREADS + threadIdx.x, step = ranks * THREADS;
     const int want = p.budget - p.sink - p.recent;
     for (int j = min(len, p.budget) + first; j < p.budget; j += step) kept[j] = -1;
     if (len <= p.budget || want == 0) {
@@ -245,15 +259,15 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     const int per = (hi - lo + step - 1) / step;
     kept += p.sink;
     if (per <= 2)
-        select_row<2>(sh, row, lo, hi, per, want, kept, rank, ranks);
+        select_row<THREADS, 2>(sh, row, lo, hi, per, want, kept, rank, ranks);
     else if (per <= 4)
-        select_row<4>(sh, row, lo, hi, per, want, kept, rank, ranks);
+        select_row<THREADS, 4>(sh, row, lo, hi, per, want, kept, rank, ranks);
     else if (per <= 8)
-        select_row<8>(sh, row, lo, hi, per, want, kept, rank, ranks);
-    else if (per <= kMaxKeys)
-        select_row<kMaxKeys>(sh, row, lo, hi, per, want, kept, rank, ranks);
+        select_row<THREADS, 8>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else if (per <= 16)
+        select_row<THREADS, 16>(sh, row, lo, hi, per, want, kept, rank, ranks);
     else
-        select_row<0>(sh, row, lo, hi, per, want, kept, rank, ranks);
+        select_row<THREADS, THREADS == kSmallSelect ? kSmallKeys : 0>(sh, row, lo, hi, per, want, kept, rank, ranks);
 }
 
 namespace {
@@ -434,12 +448,18 @@ template <typename V> cudaError_t launch_move(const EvictParams &p, int sm_count
 cudaError_t launch_evict(const EvictParams &p, int sm_count, cudaStream_t stream)
 {
     const int64_t rows = (int64_t)p.n_layers * p.n_seq * p.H;
-    // CTAs per row: one while its keys fit the registers and the rows alone fill the GPU
-    int cluster = 1;
-    while (cluster < 8 && (p.max_len > cluster * kSelectThreads * kMaxKeys || (rows * cluster < 2 * sm_count && p.max_len > cluster * 2048)))
-        cluster *= 2;
-    if (rows * cluster > INT32_MAX) return cudaErrorInvalidConfiguration;
-    const cudaError_t e = launch_clusters(evict_select_kernel, rows, cluster, kSelectThreads, false, stream, p);
+    cudaError_t e;
+    if (p.max_len <= kSmallSelect * kSmallKeys) {
+        if (rows > INT32_MAX) return cudaErrorInvalidConfiguration;
+        e = launch_clusters(evict_select_kernel<kSmallSelect>, rows, 1, kSmallSelect, false, stream, p);
+    } else {
+        // CTAs per row: as many as its keys need registers, or, few rows, as keep every CTA at 2048 keys and more
+        int cluster = 1;
+        while (cluster < 8 && (p.max_len > cluster * kLargeSelect * kLargeKeys || (rows * cluster < 2 * sm_count && p.max_len > cluster * 2048)))
+            cluster *= 2;
+        if (rows * cluster > INT32_MAX) return cudaErrorInvalidConfiguration;
+        e = launch_clusters(evict_select_kernel<kLargeSelect>, rows, cluster, kLargeSelect, false, stream, p);
+    }
     if (e != cudaSuccess) return e;
     switch (p.vec_bytes) {
     case 32: return launch_move<Vec32>(p, sm_count, stream);
