@@ -409,10 +409,15 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                 lt += f[g] * sml[g * WM + w][t * 8 + x % 8][1];
             }
             if (dead) continue;
-            const RowId id = row_id(p, it, it.row0 + r);
-            const int head = it.head * p.G + id.g;
-            const float inv = lt == 0.f ? 0.f : 1.f / lt;
-            T *out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2];
+            T *out = nullptr;
+            float inv = 1.f;
+            if (it.direct) {   // own tokens: whose row it is, is known without a load
+                const RowId id = row_id(p, it, it.row0 + r);
+                const int head = it.head * p.G + id.g;
+                inv = lt == 0.f ? 0.f : 1.f / lt;
+                out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2];
+                if (p.lse && lane == 0) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (mt + log2f(lt)) * kLn2;
+            }
 #pragma unroll
             for (int d0 = 0; d0 < DP; d0 += 128) {
                 const int d = d0 + 4 * lane;
@@ -431,10 +436,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                 else
                     *reinterpret_cast<float4 *>(p.part_o + (it.part_row + r) * p.D + d) = v;
             }
-            if (lane == 0) {
-                if (it.direct && p.lse) p.lse[((int64_t)id.seq * p.q_tokens + id.token) * p.G * p.H + head] = (mt + log2f(lt)) * kLn2;
-                if (!it.direct || p.with_scores) *reinterpret_cast<float2 *>(p.part_ml + 2 * (it.part_row + r)) = make_float2(mt, lt);
-            }
+            if (lane == 0 && (!it.direct || p.with_scores)) *reinterpret_cast<float2 *>(p.part_ml + 2 * (it.part_row + r)) = make_float2(mt, lt);
         }
         consumer_sync();
     }

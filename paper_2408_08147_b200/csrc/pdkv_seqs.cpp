@@ -105,39 +105,60 @@ int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int3
 // 1, the tile kernel: up to 256 rows an item.
 struct Shape {
     int kernel, row_tile;
-    int64_t quantum;      // tokens; work is cut along the tokens in multiples of this
 };
-Shape shape_of(int64_t rows, bool tile_ok)
+
+// Which of the two is quicker for `rows` rows against `len` own tokens of one head.  The tile kernel multiplies faster
+// but takes longer to start and finish an item.  Measured on B200, microseconds of an SM: warp kernel 1.8 an item of
+// 64 rows and 0.95 for each 64 tokens of it; tile kernel 8 an item of up to 256 rows and 2 for each 128 tokens, 256
+// with up to 128 rows.  (64 sequences of 12 to 19 tokens, 49 rows, 5 heads: 31 us against 60.)
+bool tile_is_faster(int64_t rows, int64_t len)
 {
-    if (tile_ok && rows >= kTileMinRows) return {1, 256, 128};
-    return {0, rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile, 64};
+    const double warp = (double)((rows + 63) / 64) * (1.8 + 0.95 * (double)((len + 63) / 64));
+    const int64_t full = rows / 256, rest = rows % 256, n128 = (len + 127) / 128, n256 = (len + 255) / 256;
+    const double tile = (double)full * (8 + 2.0 * (double)n128) + (rest == 0 ? 0 : 8 + 2.0 * (double)(rest > 128 ? n128 : n256));
+    return rows >= kTileMinRows && tile < warp;
+}
+Shape shape_of(int64_t rows, bool tile)
+{
+    if (tile) return {1, 256};
+    return {0, rows <= 16 ? 16 : rows <= 32 ? 32 : kMaxRowTile};
 }
 
-// What starting and finishing an item costs, in quanta of its kernel.  Measured: about 15000 cycles against
-// 3700 a quantum in the tile kernel, 3 us against 1.5 us (a CTA's share of the memory rate) in the warp kernel.
-constexpr int64_t kItemCost[2] = {2, 4};
+// What starting and finishing an item costs, and what a quantum does: 64 tokens for up to 16 rows in the warp kernel,
+// which memory bounds, more rows of long heads by their products; 128 or 256 tokens in the tile kernel.  In halves
+// of such a quantum.  Measured: 3 us against 1.5 us (a CTA's share of the memory rate) in the warp kernel, 15000
+// cycles against 3700 in the tile kernel.
+constexpr int64_t kItemCost[2] = {4, 8};
+int64_t quantum_load(int kernel, int32_t rows, int32_t head_dim)
+{
+    if (kernel == 1 || rows <= 16) return 2;
+    if (rows <= 32) return head_dim <= 128 ? 2 : 3;
+    return head_dim <= 128 ? 3 : 6;
+}
 
-struct Unit { int32_t seg, head, row0, rows; int64_t quantum, quanta; };   // tokens of a quantum, how many
+// Tokens of a quantum, its load, how many there are.
+struct Unit { int32_t seg, head, row0, rows; int64_t quantum, weight, quanta; };
 struct Piece { size_t unit; int64_t from, n; int32_t cta; };
 
-// Deals units to CTAs in order, each CTA up to a load of `most` quanta; units are cut where a CTA is full.
-// Returns false when that takes more than `n_ctas` CTAs.
+// Deals units to CTAs in order, each CTA up to a load of `most`; units are cut where a CTA is full.  Returns
+// false when that takes more than `n_ctas` CTAs.
 bool deal(const std::vector<Unit> &units, int64_t cost, int64_t most, int64_t n_ctas, bool cut, std::vector<Piece> *out)
 {
     int64_t cta = 0, load = 0;
     for (size_t u = 0; u < units.size(); ++u) {
+        const Unit &w = units[u];
         int64_t q = 0;
-        while (q < units[u].quanta) {
-            int64_t room = most - load - cost;
-            if (load > 0 && (room < 1 || (!cut && room < units[u].quanta))) {
+        while (q < w.quanta) {
+            int64_t room = std::max<int64_t>(0, most - load - cost) / w.weight;
+            if (load > 0 && (room < 1 || (!cut && room < w.quanta))) {
                 ++cta;
                 load = 0;
-                room = most - cost;
+                room = std::max<int64_t>(0, most - cost) / w.weight;
             }
-            const int64_t n = std::min(units[u].quanta - q, std::max<int64_t>(room, 1));
-            if (cta >= n_ctas || n > room || (!cut && n < units[u].quanta)) return false;
+            const int64_t n = std::min(w.quanta - q, room);
+            if (cta >= n_ctas || n < 1 || (!cut && n < w.quanta)) return false;
             if (out) out->push_back({u, q, n, (int32_t)cta});
-            load += cost + n;
+            load += cost + n * w.weight;
             q += n;
         }
     }
@@ -147,12 +168,14 @@ bool deal(const std::vector<Unit> &units, int64_t cost, int64_t most, int64_t n_
 // Smallest load per CTA with which the units fit.
 int64_t least_load(const std::vector<Unit> &units, int64_t cost, int64_t n_ctas, bool cut)
 {
-    int64_t total = 0, most = 0;
+    int64_t total = 0, longest = 0, heaviest = 1;
     for (const Unit &u : units) {
-        total += u.quanta + cost;
-        most = std::max(most, u.quanta + cost);
+        total += u.quanta * u.weight + cost;
+        longest = std::max(longest, u.quanta * u.weight + cost);
+        heaviest = std::max(heaviest, u.weight);
     }
-    int64_t lo = std::max((total + n_ctas - 1) / n_ctas, cut ? cost + 1 : most), hi = total;
+    // (cut, every CTA has room for a quantum; a load of everything always fits)
+    int64_t lo = std::max((total + n_ctas - 1) / n_ctas, cut ? cost + heaviest : longest), hi = std::max(lo, total);
     while (lo < hi) {
         const int64_t mid = lo + (hi - lo) / 2;
         if (deal(units, cost, mid, n_ctas, cut, nullptr))
@@ -172,8 +195,8 @@ std::vector<Unit> units_of(const pdkv_seqs &s, int kernel, const std::vector<int
         for (int32_t r0 = 0; r0 < n_rows[g]; r0 += shape[g].row_tile)
             for (int32_t h = 0; h < s.pool.d.num_kv_heads; ++h) {
                 const int32_t rows = std::min<int32_t>(shape[g].row_tile, n_rows[g] - r0);
-                const int64_t quantum = kernel == 1 && rows <= 128 ? 256 : shape[g].quantum;   // two tiles of tokens at a time
-                units.push_back({(int32_t)g, h, r0, rows, quantum, (seg.len + quantum - 1) / quantum});
+                const int64_t quantum = kernel == 0 ? 64 : rows <= 128 ? 256 : 128;   // (one row tile: two tiles of tokens at a time)
+                units.push_back({(int32_t)g, h, r0, rows, quantum, quantum_load(kernel, rows, s.pool.d.head_dim), (seg.len + quantum - 1) / quantum});
             }
     }
     return units;
@@ -193,7 +216,7 @@ int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std:
     double best_us = 1e30;
     auto attempt = [&](int n) {
         if (n < 1 || n >= s.sm_count) return;
-        const double load = (double)least_load(tile_units, kItemCost[1], n, true);
+        const double load = 0.5 * (double)least_load(tile_units, kItemCost[1], n, true);   // quanta
         const double warp_us = 5 + std::max(bytes / 6.3e6, (bytes / 76e3 + 1.8 * (double)warp_units.size()) / (s.sm_count - n));
         const double busy = std::min(1.0, bytes / 6.3e6 / std::max(warp_us, 4 + 2.2 * load));   // share of the time with a saturated memory
         const double us = std::max(warp_us, 4 + (2.2 + 1.2 * busy) * load);
@@ -209,20 +232,22 @@ int tile_sms(const pdkv_seqs &s, const std::vector<Unit> &warp_units, const std:
 }
 
 // Work list of one kernel.  Whole units when that is as quick as cutting them (nothing is to be joined then,
-// which saves a kernel: about two quanta more); CTAs get at least four quanta, so that joining stays cheap.
+// which saves a kernel: about two quanta more); else CTAs get at least two quanta (one of the tile kernel), so that
+// joining stays cheap.
 void plan_items(pdkv_seqs &s, int kernel, const std::vector<Unit> &units, std::vector<int32_t> &unit0, int n_ctas_max)
 {
-    int64_t quanta = 0;
+    int64_t load = 0;
     for (size_t u = 0; u < units.size(); ++u) {
-        quanta += units[u].quanta;
+        load += units[u].quanta * units[u].weight;
         if (unit0[(size_t)units[u].seg] < 0) unit0[(size_t)units[u].seg] = (int32_t)(s.units.size() + u);
     }
     std::vector<AttnItem> &items = s.items[kernel];
     if (units.empty()) return;
-    const int64_t cost = kItemCost[kernel], n_ctas = std::max<int64_t>(1, std::min<int64_t>(n_ctas_max, std::max<int64_t>(units.size(), quanta / 4)));
+    const int64_t cost = kItemCost[kernel], least = kernel == 0 ? 4 : 2;
+    const int64_t n_ctas = std::max<int64_t>(1, std::min<int64_t>(n_ctas_max, std::max<int64_t>(units.size(), load / least)));
     std::vector<Piece> pieces;
     const int64_t cut = least_load(units, cost, n_ctas, true), whole = least_load(units, cost, n_ctas, false);
-    const bool keep_whole = whole <= cut + 2;
+    const bool keep_whole = whole <= cut + 4;
     deal(units, cost, keep_whole ? whole : cut, n_ctas, !keep_whole, &pieces);
     const size_t first_unit = s.units.size();
     s.units.resize(first_unit + units.size());
@@ -377,8 +402,14 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                 s->use_map = pdkv::attend_map_supported(g) && pdkv::make_attend_map(*pool, pdkv::attend_map_box(g), s->map[0]);
             }
             std::vector<Shape> shape;
-            for (int32_t n : n_rows) shape.push_back(shape_of(n, tile_ok));
-            s->own_tiles = shape_of(R, tile_ok).kernel == 1;
+            // one kernel for all own tokens (their scores are found in one way), by their average
+            int64_t own = 0;
+            for (int32_t n : s->len) own += n;
+            s->own_tiles = tile_ok && s->n_seq > 0 && tile_is_faster(R, own / s->n_seq);
+            for (size_t i = 0; i < s->segs.size(); ++i)
+                // (a prefix of many rows always goes to the tile kernel, which runs beside the own tokens: 71 sequences
+                // behind 49 tokens 19 us, 31 with the prefix among the own tokens)
+                shape.push_back(shape_of(n_rows[i], (int32_t)i < s->n_seq ? s->own_tiles : tile_ok && n_rows[i] >= kTileMinRows));
             // unit of (row tile 0, head 0) of every segment
             std::vector<int32_t> unit0(s->segs.size(), -1);
             const std::vector<Unit> warp_units = units_of(*s, 0, n_rows, shape), tile_units = units_of(*s, 1, n_rows, shape);
