@@ -41,7 +41,9 @@ using pdkv::AttnSeq;
 using pdkv::AttnUnit;
 
 constexpr int kMaxRowTile = 64;    // rows of one work item
-constexpr int kTileMinRows = 48;   // rows from which the tile kernel takes a segment
+// Rows from which the tile kernel takes a segment: 40000 tokens of 8 heads of 128 dims, 32 rows 57 us in the warp kernel,
+// 40 rows 82, 64 rows 58 in the tile kernel.
+constexpr int kTileMinRows = 33;
 
 bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
 {
@@ -109,11 +111,11 @@ struct Shape {
 
 // Which of the two is quicker for `rows` rows against `len` own tokens of one head.  The tile kernel multiplies faster
 // but takes longer to start and finish an item.  Measured on B200, microseconds of an SM: warp kernel 1.8 an item of
-// 64 rows and 0.95 for each 64 tokens of it; tile kernel 8 an item of up to 256 rows and 2 for each 128 tokens, 256
+// 64 rows and 2 for each 64 tokens of it; tile kernel 8 an item of up to 256 rows and 2 for each 128 tokens, 256
 // with up to 128 rows.  (64 sequences of 12 to 19 tokens, 49 rows, 5 heads: 31 us against 60.)
 bool tile_is_faster(int64_t rows, int64_t len)
 {
-    const double warp = (double)((rows + 63) / 64) * (1.8 + 0.95 * (double)((len + 63) / 64));
+    const double warp = (double)((rows + 63) / 64) * (1.8 + 2.0 * (double)((len + 63) / 64));
     const int64_t full = rows / 256, rest = rows % 256, n128 = (len + 127) / 128, n256 = (len + 255) / 256;
     const double tile = (double)full * (8 + 2.0 * (double)n128) + (rest == 0 ? 0 : 8 + 2.0 * (double)(rest > 128 ? n128 : n256));
     return rows >= kTileMinRows && tile < warp;
