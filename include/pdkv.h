@@ -422,7 +422,8 @@ typedef struct {
  * size.  Attention takes pools of 2-byte elements whose head_dim is a multiple of 8
  * and at most 256.  Copies of the lists are enqueued on `stream` and waited for.
  * Errors: INVALID_ARG, GEOMETRY (pool or head counts the attention does not take),
- * TABLE (ids out of range, tables too short), BUFFER_TOO_SMALL, CUDA, NOMEM. */
+ * TABLE (ids out of range, tables too short), LIMIT (a sequence or prefix of more than
+ * 2^30 tokens), BUFFER_TOO_SMALL, CUDA, NOMEM. */
 int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *desc, void *workspace, size_t workspace_bytes,
                      size_t *needed_bytes, void *stream, pdkv_seqs **out);
 /* Synchronise `stream` and report the handle's device status word: PDKV_OK,
@@ -463,10 +464,12 @@ typedef struct {
 /* Scratch bytes one pdkv_attend() call needs (device, 32-byte aligned).  The scratch is the caller's; calls that may
  * run at the same time need one each.  Nothing in it outlives the call. */
 int pdkv_attend_scratch(const pdkv_seqs *seqs, int with_scores, size_t *bytes);
-/* Enqueues only (no allocation, copy or synchronisation): it can be recorded into a CUDA
- * graph.  q and out are 16-byte aligned, their strides multiples of 8 elements; rows of out
- * and of scores_out must not overlap; out must not overlap q, the pool or the scratch.
- * Errors: INVALID_ARG, BUFFER_TOO_SMALL (scratch), CUDA. */
+/* Enqueues only (no allocation, copy or synchronisation): after one call outside capture it
+ * can be recorded into a CUDA graph.  q and out are 16-byte aligned, their strides multiples
+ * of 8 elements; rows of out and of scores_out must not overlap; out must not overlap q, the
+ * pool or the scratch.  The same call gives the same bits every time.
+ * Errors: INVALID_ARG, BUFFER_TOO_SMALL (scratch), LIMIT (more blocks than a launch takes),
+ * CUDA. */
 int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, void *scratch, size_t scratch_bytes,
                 void *stream);
 
@@ -495,8 +498,9 @@ typedef struct {
     int32_t *new_len;              /* device [n_seq]: min(len, budget), or NULL.  May equal seq_len */
 } pdkv_evict_args;
 
-/* Enqueues only; no scratch.  Errors: INVALID_ARG, GEOMETRY (the pools disagree), TABLE
- * (dst sequences too short, or a dst block used twice), CUDA. */
+/* Enqueues only (recordable as pdkv_attend()); no scratch.  `kept` must not overlap the scores.
+ * Errors: INVALID_ARG, GEOMETRY (the pools disagree), TABLE (dst sequences too short, or a dst
+ * block used twice), LIMIT, CUDA. */
 int pdkv_evict(const pdkv_seqs *seqs, const pdkv_seqs *dst, int layer_begin, int layer_end, const pdkv_evict_args *args,
                void *stream);
 

@@ -45,6 +45,8 @@ constexpr int kMaxRowTile = 64;    // rows of one work item
 // 40 rows 82, 64 rows 58 in the tile kernel.
 constexpr int kTileMinRows = 33;
 
+constexpr int32_t kMaxTokens = 1 << 30;   // of a sequence or prefix: positions and their next tiles stay below 2^31
+
 bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
 {
     const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
@@ -93,6 +95,7 @@ int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int3
     if (off[0] < 0) return PDKV_ERR_TABLE;
     for (int32_t r = 0; r < n; ++r) {
         if (len[r] < 0) return PDKV_ERR_INVALID_ARG;
+        if (len[r] > kMaxTokens) return PDKV_ERR_LIMIT;
         if (off[r + 1] < off[r]) return PDKV_ERR_TABLE;
         const int64_t need = ((int64_t)len[r] + B - 1) / B;
         if (off[r + 1] - off[r] < need) return PDKV_ERR_TABLE;
@@ -613,6 +616,9 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         if (scratch_bytes < l.bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
         if (!s->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0) return PDKV_OK;
+        // blocks of the joining and weighing kernels: refused before anything is enqueued
+        if ((double)s->n_seq * s->pool.d.num_kv_heads * ((double)s->G * s->q_tokens / 4 + 1 + (scores ? s->max_len / 128.0 + 1 : 0)) > 2e9)
+            return PDKV_ERR_LIMIT;
 
         pdkv::AttnParams p{};
         p.pool = pdkv::pool_view(s->pool);
@@ -715,6 +721,11 @@ int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int laye
             if (!a->scores || !a->kept || !aligned(a->scores, 4) || !aligned(a->kept, 4)) return PDKV_ERR_INVALID_ARG;
             for (int i = 0; i < 3; ++i)
                 if (n[i] > 1 && a->scores_stride[i] < 0) return PDKV_ERR_INVALID_ARG;
+            const size_t kept_bytes = 4 * (size_t)layers * (size_t)s->n_seq * (size_t)x.num_kv_heads * (size_t)a->budget;
+            if (ranges_overlap(a->kept, kept_bytes, a->scores, 4 * (size_t)rows_span(s->max_len, a->scores_stride, n, 3)) ||
+                (a->kept_scores && ranges_overlap(a->kept, kept_bytes, a->kept_scores,
+                                                  4 * (size_t)rows_span(a->kept_scores_len, a->kept_scores_stride, n, 3))))
+                return PDKV_ERR_INVALID_ARG;
             if (a->kept_scores) {
                 if (!aligned(a->kept_scores, 4) || a->kept_scores_len < top) return PDKV_ERR_INVALID_ARG;
                 if (!rows_apart(a->kept_scores_len, a->kept_scores_stride, n, 3)) return PDKV_ERR_INVALID_ARG;
@@ -728,6 +739,7 @@ int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int laye
         }
         if (!s->dev_mem || !t->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0 || layers == 0) return PDKV_OK;
+        if ((double)layers * s->n_seq * x.num_kv_heads * 16 > 2e9) return PDKV_ERR_LIMIT;   // blocks of a kernel
         if (s->max_len > 0 || a->kept || a->new_len) {
             if (!a->kept) return PDKV_ERR_INVALID_ARG;
             pdkv::EvictParams p{};

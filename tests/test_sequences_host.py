@@ -46,6 +46,7 @@ def test_refused_descriptions():
     assert status(create, p, [40], tbl=np.array([0, -1, 3], np.int32)) == B.PDKV_ERR_TABLE
     assert status(create, p, [40], off=np.array([0, 2], np.int64)) == B.PDKV_ERR_TABLE
     assert status(create, p, [40], off=np.array([-1, 3], np.int64)) == B.PDKV_ERR_TABLE
+    assert status(create, p, [(1 << 30) + 1], off=np.array([0, 1 << 27], np.int64)) == B.PDKV_ERR_LIMIT
     assert status(create, p, [4], Hq=6) == B.PDKV_ERR_GEOMETRY          # not a multiple of the KV heads
     assert status(create, p, [4], q_tokens=0) == B.PDKV_ERR_INVALID_ARG
     assert status(create, p, [4], dtype=2) == B.PDKV_ERR_INVALID_ARG
@@ -149,6 +150,8 @@ def test_refused_evictions():
     twice = make([40, 7], tbl=np.array([0, 1, 2, 0], np.int32))
     assert call(twice, twice) == B.PDKV_ERR_TABLE                        # in place with a shared block
     assert call(s, d, kept=0) == bad and call(s, d, scores=0) == bad
+    assert call(s, d, kept=FAKE + (1 << 41) + 64) == bad                  # on the scores
+    assert call(s, d, kept=FAKE + (3 << 41) + 64) == bad                  # on the scores that are kept
     assert call(s, d, kept_scores_len=15) == bad
     assert call(s, d, kept_scores_stride=[400, 200, 15]) == bad
     assert call(s, d, kept_scores=FAKE + (1 << 41), kept_scores_stride=[400, 200, 40]) == bad
