@@ -455,13 +455,17 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
     __shared__ __align__(16) float sml[4][16][2];
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
     AttnItem it = fetch_item(p.items, blockIdx.x);
-    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x < R::kSlots) {
         mbar_init(&bar.full[threadIdx.x], p.use_map ? 1 : 32);
         mbar_init(&bar.empty[threadIdx.x], 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    if (threadIdx.x == kConsumers) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
+    // The first kernel of a call is set up while the work before it ends.  Behind the tile kernel of the same call,
+    // which has waited for that work before it let this one start, there is nothing to wait for.
+    if (p.n_tile_ctas == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x >= kConsumers) {
         load_slices<DP>(p, &map, smem_u32(smem), bar, it);
     } else {
@@ -510,11 +514,14 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     const int x = blockIdx.x % per, head = blockIdx.x / per % p.H, seq = blockIdx.x / per / p.H;
     const AttnSeq s = p.seqs[seq];
     const int R = p.G * p.q_tokens;
+    const int row = 4 * x + warp;
+    const bool mine = x < row_blocks && !s.direct && row < R;
+    Parts parts{};
+    if (mine) parts = parts_of(p, s, head, row);         // where they are is known before they are written
     asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts are written by the kernels before
+    asm volatile("griddepcontrol.launch_dependents;");
     if (x < row_blocks) {
-        const int row = 4 * x + warp;
-        if (s.direct || row >= R) return;
-        const Parts parts = parts_of(p, s, head, row);
+        if (!mine) return;
         const int n = parts.n[0] + parts.n[1];
         const float2 ml = joined_ml<32>(p, parts, lane);
         const float base = ml.x == -INFINITY ? 0.f : ml.x;
@@ -612,10 +619,10 @@ template <typename T, int DP, bool FULL> cudaError_t launch_dims(const AttnParam
     cfg.dynamicSmemBytes = Ring<DP>::kBytes;
     cfg.stream = stream;
     cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // beside the tile kernel, if there is one
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // beside the tile kernel, or early
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = p.n_tile_ctas > 0 ? 1 : 0;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, attend_items_kernel<T, DP, FULL>, map, p);
 }
 
@@ -664,7 +671,7 @@ cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaSt
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = p.n_ctas > 0 || p.n_tile_ctas > 0 ? 1 : 0;
+    cfg.numAttrs = 1;
     if (dtype == PDKV_DTYPE_BF16) return cudaLaunchKernelEx(&cfg, attend_join_kernel<__nv_bfloat16>, p, row_blocks, chunks);
     return cudaLaunchKernelEx(&cfg, attend_join_kernel<__half>, p, row_blocks, chunks);
 }

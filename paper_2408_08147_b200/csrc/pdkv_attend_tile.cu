@@ -213,6 +213,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    if (warp == kLoadWarp && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // set up while the work before this call ends
     asm volatile("griddepcontrol.launch_dependents;");
     bool dead = false;
     // tensor memory is there for the warps that use it; the loads of K and V do not wait for it
@@ -604,6 +606,7 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
     }
     const AttnSeg seg = p.segs[seq];
     asm volatile("griddepcontrol.wait;" ::: "memory");   // sums of the rows, current lengths
+    asm volatile("griddepcontrol.launch_dependents;");
     fence_before();
     __syncthreads();
     fence_after();
@@ -758,8 +761,17 @@ template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_shared(attend_tile_kernel<T, DP>, (int)TileShape<DP>::kBytes, ready);
     if (e != cudaSuccess) return e;
-    attend_tile_kernel<T, DP><<<p.n_tile_ctas, kTileThreads, TileShape<DP>::kBytes, stream>>>(map, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.n_tile_ctas);
+    cfg.blockDim = dim3(kTileThreads);
+    cfg.dynamicSmemBytes = TileShape<DP>::kBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attend_tile_kernel<T, DP>, map, p);
 }
 
 template <typename T, int DP> cudaError_t launch_weigh(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)

@@ -238,6 +238,7 @@ template <int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == kSmallSelect ? 4 : 1) evict_select_kernel(const EvictParams p)
 {
     __shared__ __align__(16) SelectShared sh;
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // set up while the work before this call ends
     asm volatile("griddepcontrol.launch_dependents;");
     const uint32_t rank = cluster_rank(), ranks = cluster_size();
     const int row_id = blockIdx.x / ranks;
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const Evict
 namespace {
 
 template <typename... P, typename... A>
-cudaError_t launch_clusters(void (*kernel)(P...), int64_t rows, int cluster, int threads, bool early, cudaStream_t stream, A... args)
+cudaError_t launch_clusters(void (*kernel)(P...), int64_t rows, int cluster, int threads, cudaStream_t stream, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * cluster));
@@ -421,10 +422,10 @@ cudaError_t launch_clusters(void (*kernel)(P...), int64_t rows, int cluster, int
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = cluster;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // `early`: the kernel waits for the one before it on the device
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits for the one before it on the device
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = early ? 2 : 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -439,8 +440,8 @@ template <typename V> cudaError_t launch_move(const EvictParams &p, int sm_count
     const int64_t most = ordered ? 8 : 1 << 16;
     while (parts * 2 <= most && streams * parts < 4 * sm_count && steps >= 2 * parts) parts *= 2;
     if (streams * parts > INT32_MAX) return cudaErrorInvalidConfiguration;
-    if (ordered) return launch_clusters(evict_move_kernel<V, true>, streams, (int)parts, kMoveThreads, true, stream, p, (int)parts);
-    return launch_clusters(evict_move_kernel<V, false>, streams * parts, 1, kMoveThreads, true, stream, p, (int)parts);
+    if (ordered) return launch_clusters(evict_move_kernel<V, true>, streams, (int)parts, kMoveThreads, stream, p, (int)parts);
+    return launch_clusters(evict_move_kernel<V, false>, streams * parts, 1, kMoveThreads, stream, p, (int)parts);
 }
 
 }  // namespace
@@ -451,14 +452,14 @@ cudaError_t launch_evict(const EvictParams &p, int sm_count, cudaStream_t stream
     cudaError_t e;
     if (p.max_len <= kSmallSelect * kSmallKeys) {
         if (rows > INT32_MAX) return cudaErrorInvalidConfiguration;
-        e = launch_clusters(evict_select_kernel<kSmallSelect>, rows, 1, kSmallSelect, false, stream, p);
+        e = launch_clusters(evict_select_kernel<kSmallSelect>, rows, 1, kSmallSelect, stream, p);
     } else {
         // CTAs per row: as many as its keys need registers, or, few rows, as keep every CTA at 2048 keys and more
         int cluster = 1;
         while (cluster < 8 && (p.max_len > cluster * kLargeSelect * kLargeKeys || (rows * cluster < 2 * sm_count && p.max_len > cluster * 2048)))
             cluster *= 2;
         if (rows * cluster > INT32_MAX) return cudaErrorInvalidConfiguration;
-        e = launch_clusters(evict_select_kernel<kLargeSelect>, rows, cluster, kLargeSelect, false, stream, p);
+        e = launch_clusters(evict_select_kernel<kLargeSelect>, rows, cluster, kLargeSelect, stream, p);
     }
     if (e != cudaSuccess) return e;
     switch (p.vec_bytes) {

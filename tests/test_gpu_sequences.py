@@ -281,6 +281,45 @@ def test_recorded_steps_follow_lengths_and_queries():
             check_scores(s, np.zeros(sc.shape), sc, want, lens)
 
 
+@pytest.mark.parametrize("G", [2, 40])
+def test_calls_follow_the_work_before_them(G):
+    """Queries and lengths written by the operation just before a call, again and again and in a recorded sequence
+    (a copy, a kernel of torch, a call of the library): a call never starts on them too early."""
+    s = Setup([300, 33, 200], G=G, D=64, prefix_len=[70], member=[0, 0, -1])
+    n = len(s.lens)
+    with s.session() as c:
+        qs = [s.q_t * f for f in (1.0, 0.5, 0.25)]
+        want = [c.attend(s.layer, q)[0].clone() for q in qs]
+        short = c.attend(s.layer, qs[1], seq_len_t=torch.tensor([7, 1, 9], dtype=torch.int32, device="cuda"))[0].clone()
+        q, out, lse = torch.empty_like(s.q_t), torch.empty_like(s.q_t), torch.empty(s.q_t.shape[:3], device="cuda")
+        lens, few = torch.empty(n, dtype=torch.int32, device="cuda"), torch.tensor([7, 1, 9], dtype=torch.int32, device="cuda")
+        full = torch.tensor(s.lens, dtype=torch.int32, device="cuda")
+        got = torch.empty(4, *out.shape, dtype=out.dtype, device="cuda")
+
+        def steps():
+            for i, x in enumerate(qs):
+                torch.mul(s.q_t, (1.0, 0.5, 0.25)[i], out=q)
+                lens.copy_(full)
+                c.attend(s.layer, q, out_t=out, lse_t=lse, seq_len_t=lens)
+                got[i].copy_(out)
+            lens.copy_(few)
+            c.attend(s.layer, qs[1], out_t=got[3], lse_t=lse, seq_len_t=lens)
+
+        for _ in range(30):
+            got.zero_()
+            steps()
+            assert all(torch.equal(got[i], want[i]) for i in range(3)) and torch.equal(got[3], short)
+        g = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(g, stream=side):
+            steps()
+        for _ in range(5):
+            got.zero_()
+            g.replay()
+            assert all(torch.equal(got[i], want[i]) for i in range(3)) and torch.equal(got[3], short)
+
+
 def test_offsets_past_32_bits():
     """A pool of 5 GiB whose last blocks hold the tokens (both layouts)."""
     for layout in (BLOCK_MAJOR, LAYER_MAJOR):
