@@ -28,9 +28,9 @@ __device__ __forceinline__ uint32_t order_key(float x)
 
 namespace {
 
-// Threads of a selecting CTA and keys that each holds in registers: small CTAs, several on an SM, for rows that fit
-// one (their rounds are latency, which other CTAs fill); large ones in clusters for longer rows.
-constexpr int kSmallSelect = 256, kSmallKeys = 32, kLargeSelect = 1024, kLargeKeys = 16;
+// Threads of a selecting CTA and keys that each holds in registers: small CTAs, four on an SM, for rows that fit
+// one (their rounds are latency, which other CTAs fill); large ones, two on an SM, in clusters for longer rows.
+constexpr int kSmallSelect = 256, kSmallKeys = 32, kLargeSelect = 512, kLargeKeys = 32;
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -49,16 +49,7 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Word `p` of this CTA's shared memory, as CTA `rank` of the cluster holds it.
-__device__ __forceinline__ int peer_word(const int *p, uint32_t rank)
-{
-    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), far;
-    int v;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(at), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(far) : "memory");
-    return v;
-}
-
+// To shared memory of CTA `rank` of the cluster, at the place that `p` has in this CTA's.
 __device__ __forceinline__ void put_peer(const int *p, uint32_t rank, int a, int b, int c)
 {
     uint32_t at = (uint32_t)__cvta_generic_to_shared(p), far;
@@ -66,67 +57,160 @@ __device__ __forceinline__ void put_peer(const int *p, uint32_t rank, int a, int
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1,%2,%3,%3};" ::"r"(far), "r"(a), "r"(b), "r"(c) : "memory");
 }
 
-struct alignas(16) SelectShared {
-    int count[3][4];              // of the CTA, by round modulo 3
-    int exchange[2][8][4];        // of every CTA of the cluster
+// c + (key >= value), from the carry of key - value (value > 0): two instructions.
+__device__ __forceinline__ void count_reached(uint32_t &c, uint32_t key, uint32_t minus_value)
+{
+    asm("{.reg .u32 t;\n add.cc.u32 t, %1, %2;\n addc.u32 %0, %0, 0;}" : "+r"(c) : "r"(key), "r"(minus_value));
+}
+__device__ __forceinline__ void put_peer(const uint32_t *p, uint32_t rank, uint32_t v)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), far;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(at), "r"(rank));
+    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(far), "r"(v) : "memory");
+}
+
+constexpr int kSample = 128;
+
+template <int THREADS> struct alignas(16) SelectShared {
+    int count[3][4];                       // of the CTA, by round modulo 3
+    alignas(16) int exchange[2][8][4], totals[8][4];   // of every CTA of the cluster, written as vectors of four
+    alignas(16) uint32_t sample[kSample];
+    uint32_t sorted[kSample];
+    uint32_t close[THREADS];               // keys between the bounds, of the CTA
+    uint32_t all_close[THREADS == kSmallSelect ? 1 : 8][THREADS];   // and of every CTA
+    int n_close, n_all_close[8];
+    uint32_t packed[3];
     int warp_over[32], warp_tie[32];
-    int totals[2];
+};
+
+// lo <= the want-th largest key < hi: at least `want` keys reach lo, fewer reach hi.
+struct Bounds {
+    uint32_t lo, hi;
+    int reach_lo, reach_hi;
+    __device__ __forceinline__ bool done(int want) const { return reach_lo == want || hi - lo == 1; }
+    // Three values inside, in order.
+    __device__ __forceinline__ void quarters(uint32_t &p1, uint32_t &p2, uint32_t &p3) const
+    {
+        const uint32_t quarter = max(1u, (hi - lo) / 4);
+        p1 = lo + quarter;
+        p2 = lo + max(1u, (hi - lo) / 2);
+        p3 = hi - quarter;
+    }
+    __device__ __forceinline__ void narrow(uint32_t p1, uint32_t p2, uint32_t p3, int c1, int c2, int c3, int want)
+    {
+        if (c3 >= want) {
+            lo = p3;
+            reach_lo = c3;
+        } else {
+            hi = p3;
+            reach_hi = c3;
+            if (c2 >= want) {
+                lo = p2;
+                reach_lo = c2;
+            } else {
+                hi = p2;
+                reach_hi = c2;
+                if (c1 >= want) {
+                    lo = p1;
+                    reach_lo = c1;
+                } else {
+                    hi = p1;
+                    reach_hi = c1;
+                }
+            }
+        }
+    }
 };
 
 // Token t of a row's middle part is one of the `want` heaviest: kept[at ..) receives them in order.
 // K keys a thread live in registers, read once; K = 0 (rows of more than 8 x 16384 tokens) reads them again in
 // every round.
 template <int THREADS, int K>
-__device__ __forceinline__ void select_row(SelectShared &sh, const float *row, int lo, int hi, int per, int want, int32_t *kept,
+__device__ __forceinline__ void select_row(SelectShared<THREADS> &sh, const float *row, int lo, int hi, int per, int want, int32_t *kept,
                                            uint32_t rank, uint32_t ranks)
 {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     // tokens of this warp: a contiguous run of 32 * per, lane by lane
     const int64_t first = lo + ((int64_t)rank * (THREADS / 32) + warp) * 32 * per + lane;
     const int begin = (int)min(first, (int64_t)hi);
+    const uint32_t drawn = threadIdx.x < kSample ? order_key(row[lo + (int)((int64_t)(hi - lo) * threadIdx.x / kSample)]) : 0u;
     uint32_t keys[K > 0 ? K : 1];
     if (K > 0) {
+        float x[K > 0 ? K : 1];   // all on their way before the first is looked at
 #pragma unroll
-        for (int i = 0; i < K; ++i) keys[i] = i < per && begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u;
+        for (int i = 0; i < K; ++i) x[i] = i < per && begin + 32 * i < hi ? row[begin + 32 * i] : NAN;
+#pragma unroll
+        for (int i = 0; i < K; ++i) keys[i] = order_key(x[i]);
     }
+    auto each = [&](auto &&f) {   // every lane of the warp takes part
+        if (K > 0) {
+#pragma unroll
+            for (int i = 0; i < K; ++i) f(keys[i], begin + 32 * i, i < per);
+        } else {
+            for (int i = 0; i < per; ++i) f(begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u, begin + 32 * i, true);
+        }
+    };
     if (threadIdx.x < 12) sh.count[threadIdx.x / 4][threadIdx.x % 4] = 0;
+    if (threadIdx.x == 0) sh.n_close = 0;
+    if (threadIdx.x < 3) sh.packed[threadIdx.x] = 0;
+    if (threadIdx.x < kSample) sh.sample[threadIdx.x] = drawn;
+    if (ranks > 1)
+        cluster_barrier();   // (from here on the CTAs write to one another: all have to have started)
+    else
+        __syncthreads();
+
+    Bounds at = {0u, ~0u, hi - lo, 0};   // (~0 is no number's key)
+    if (at.reach_lo > THREADS && threadIdx.x < kSample) {
+        int heavier = 0;
+        for (int j = 0; j < kSample; j += 4) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(&sh.sample[j]);
+            const int me = threadIdx.x - j;
+            heavier += (o.x > drawn || (o.x == drawn && 0 < me)) + (o.y > drawn || (o.y == drawn && 1 < me)) +
+                       (o.z > drawn || (o.z == drawn && 2 < me)) + (o.w > drawn || (o.w == drawn && 3 < me));
+        }
+        sh.sorted[heavier] = drawn;
+    }
     __syncthreads();
-    uint32_t key = 0;   // largest value known to be reached by at least `want` keys
-    int reached = hi - lo;
 #pragma unroll 1
-    for (int round = 0; round < 16 && reached != want; ++round) {
-        const int shift = 30 - 2 * round;
-        const uint32_t p1 = key | 1u << shift, p2 = key | 2u << shift, p3 = key | 3u << shift;
+    for (int round = 0; !at.done(want) && at.reach_lo - at.reach_hi > THREADS; ++round) {
+        uint32_t p1, p2, p3;
+        at.quarters(p1, p2, p3);
+        if (round == 0) {
+            // Where a sample of the row expects the key: two standard deviations to either side
+            const float part = (float)want / (float)(hi - lo);
+            const int mid = min((int)(part * kSample), kSample - 1), off = 1 + (int)(2.f * sqrtf(kSample * part * (1.f - part)));
+            p1 = min(max(sh.sorted[min(mid + off, kSample - 1)], 1u), ~0u - 1u);
+            p2 = min(max(sh.sorted[mid], 1u), ~0u - 1u);
+            p3 = min(max(sh.sorted[max(mid - off, 0)], 1u), ~0u - 1u);
+        }
         int c1 = 0, c2 = 0, c3 = 0;
         if (K > 0) {
             // (a missing key is 0 and reaches nothing).  At most 512 keys a warp: three counts in one number, one
             // reduction -- there are few lanes for those; 1024 keys: two
-            uint32_t c = 0;
-            if (K <= 16) {
+            uint32_t n1 = 0, n2 = 0, n3 = 0;
 #pragma unroll
-                for (int i = 0; i < K; ++i) c += (keys[i] >= p1) + (keys[i] >= p2 ? 1u << 10 : 0u) + (keys[i] >= p3 ? 1u << 20 : 0u);
-                c = __reduce_add_sync(~0u, c);
+            for (int i = 0; i < K; ++i) {
+                count_reached(n1, keys[i], 0u - p1);
+                count_reached(n2, keys[i], 0u - p2);
+                count_reached(n3, keys[i], 0u - p3);
+            }
+            if (K <= 16) {
+                const uint32_t c = __reduce_add_sync(~0u, n1 + (n2 << 10) + (n3 << 20));
                 c1 = c & 1023;
                 c2 = c >> 10 & 1023;
                 c3 = c >> 20;
             } else {
-#pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    c += (keys[i] >= p1) + (keys[i] >= p2 ? 1u << 16 : 0u);
-                    c3 += keys[i] >= p3;
-                }
-                c = __reduce_add_sync(~0u, c);
-                c3 = __reduce_add_sync(~0u, c3);
+                const uint32_t c = __reduce_add_sync(~0u, n1 + (n2 << 16));
                 c1 = c & 0xffff;
                 c2 = c >> 16;
+                c3 = __reduce_add_sync(~0u, n3);
             }
         } else {
-            for (int i = 0; i < per; ++i) {
-                const uint32_t k = begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u;
+            each([&](uint32_t k, int, bool) {
                 c1 += k >= p1;
                 c2 += k >= p2;
                 c3 += k >= p3;
-            }
+            });
             c1 = __reduce_add_sync(~0u, c1);
             c2 = __reduce_add_sync(~0u, c2);
             c3 = __reduce_add_sync(~0u, c3);
@@ -150,28 +234,60 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
                 c3 += v.z;
             }
         }
-        if (c3 >= want) {
-            key = p3;
-            reached = c3;
-        } else if (c2 >= want) {
-            key = p2;
-            reached = c2;
-        } else if (c1 >= want) {
-            key = p1;
-            reached = c1;
+        at.narrow(p1, p2, p3, c1, c2, c3, want);
+    }
+    if (!at.done(want)) {
+        // Few keys are left between the bounds: every CTA gets all of them, one a thread (in any order: only their
+        // counts are asked for), and goes on by itself.
+        int n = 0;
+        each([&](uint32_t k, int t, bool there) { n += there && t < hi && k >= at.lo && k < at.hi; });
+        int slot = n;   // of the lane's first, among the warp's
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int x = __shfl_up_sync(~0u, slot, d);
+            if (lane >= d) slot += x;
+        }
+        const int warp_n = __shfl_sync(~0u, slot, 31);
+        slot -= n;
+        if (warp_n > 0) {
+            int to = __shfl_sync(~0u, lane == 0 ? atomicAdd(&sh.n_close, warp_n) : 0, 0) + slot;
+            each([&](uint32_t k, int t, bool there) {
+                if (there && t < hi && k >= at.lo && k < at.hi && to < THREADS) sh.close[to++] = k;
+            });
+        }
+        __syncthreads();
+        uint32_t mine = threadIdx.x < sh.n_close ? sh.close[threadIdx.x] : 0u;
+        if (ranks > 1) {
+            if (threadIdx.x < sh.n_close)
+                for (uint32_t r = 0; r < ranks; ++r) put_peer(&sh.all_close[rank][threadIdx.x], r, mine);
+            if (threadIdx.x < ranks) put_peer(reinterpret_cast<const uint32_t *>(&sh.n_all_close[rank]), lane, sh.n_close);
+            cluster_barrier();
+            int i = threadIdx.x;   // of all
+            mine = 0;
+            for (uint32_t r = 0; r < ranks; ++r) {
+                const int n_r = sh.n_all_close[r];
+                if (i >= 0 && i < n_r) mine = sh.all_close[r][i];
+                i -= n_r;
+            }
+        }
+        const int above = at.reach_hi;
+#pragma unroll 1
+        for (int round = 0; !at.done(want); ++round) {
+            uint32_t p1, p2, p3;
+            at.quarters(p1, p2, p3);
+            // three counts below 1024 in one number
+            const uint32_t c = __reduce_add_sync(~0u, (mine >= p1) + (mine >= p2 ? 1u << 10 : 0u) + (mine >= p3 ? 1u << 20 : 0u));
+            if (lane == 0 && c) atomicAdd(&sh.packed[round % 3], c);
+            if (threadIdx.x == 0) sh.packed[(round + 1) % 3] = 0;   // (read last two rounds ago)
+            __syncthreads();
+            const uint32_t sum = sh.packed[round % 3];
+            at.narrow(p1, p2, p3, above + (sum & 1023), above + (sum >> 10 & 1023), above + (sum >> 20), want);
         }
     }
+    const uint32_t key = at.lo;
     // Either exactly `want` keys reach `key`: all of them stay.  Or `key` is the want-th key itself: of the
     // keys equal to it those of the lowest tokens stay, as many as are left.
-    const bool all = reached == want;
-    auto each = [&](auto &&f) {   // every lane of the warp takes part
-        if (K > 0) {
-#pragma unroll
-            for (int i = 0; i < K; ++i) f(keys[i], begin + 32 * i, i < per);
-        } else {
-            for (int i = 0; i < per; ++i) f(begin + 32 * i < hi ? order_key(row[begin + 32 * i]) : 0u, begin + 32 * i, true);
-        }
-    };
+    const bool all = at.reach_lo == want;
     int over = 0, tie = 0;
     each([&](uint32_t k, int t, bool there) {
         there = there && t < hi;
@@ -192,16 +308,12 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
         const int all_over = __reduce_add_sync(~0u, o), all_tie = __reduce_add_sync(~0u, e);
         int left = want - all_over;   // of the ties
         if (ranks > 1) {
-            if (threadIdx.x == 0) {
-                sh.totals[0] = all_over;
-                sh.totals[1] = all_tie;
-            }
+            if (threadIdx.x < ranks) put_peer(sh.totals[rank], lane, all_over, all_tie, 0);
             cluster_barrier();
-            const int o_r = lane < ranks ? peer_word(&sh.totals[0], lane) : 0, e_r = lane < ranks ? peer_word(&sh.totals[1], lane) : 0;
+            const int o_r = lane < ranks ? sh.totals[lane][0] : 0, e_r = lane < ranks ? sh.totals[lane][1] : 0;
             over += __reduce_add_sync(~0u, lane < rank ? o_r : 0);
             tie += __reduce_add_sync(~0u, lane < rank ? e_r : 0);
             left = want - (int)__reduce_add_sync(~0u, o_r);
-            cluster_barrier();   // nobody leaves while its shared memory is being read
         }
         const unsigned below = (1u << lane) - 1;
         if (all) {
@@ -227,20 +339,21 @@ __device__ __forceinline__ void select_row(SelectShared &sh, const float *row, i
 
 }  // namespace
 
-// One cluster per (layer, sequence, head): the lightest key that stays is found two bits a round by
-// counting the keys that reach three values, until exactly the wanted number does or all 32 bits are
-// known; then the indices are written in order.  Counting needs two instructions a key and value (a
-// histogram in shared memory was 1.5 times slower: scores crowd into few bins); the three counts of a
-// warp go through one integer reduction, CTAs of a cluster exchange theirs over distributed shared memory.
-// Every warp owns a contiguous run of tokens, so the order of the indices follows from counts per
-// warp alone.  Bound by the latency of the rounds.
+// One cluster per (layer, sequence, head).  The lightest key that stays is enclosed by counting the keys that reach
+// three values a round: first three of a sorted sample, then the quarters of the interval.  Once a CTA's threads can hold
+// the keys inside, one each, they are gathered and the rest is counted by barriers; it ends when exactly the
+// wanted number of keys reaches the lower bound, or the interval is one key (17 rounds at most whatever the keys).
+// Then the indices are written in order.  Counting needs two instructions a key and value (a histogram in shared memory
+// was 1.5 times slower: scores crowd into few bins); the three counts of a warp go through one integer reduction, CTAs of
+// a cluster exchange theirs over distributed shared memory.  Every warp owns a contiguous run of tokens, so the order of
+// the indices follows from counts per warp alone.  Bound by the latency of the rounds.
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kSmallSelect ? 4 : 1) evict_select_kernel(const EvictParams p)
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(const EvictParams p)
 {
-    __shared__ __align__(16) SelectShared sh;
+    __shared__ __align__(16) SelectShared<THREADS> sh;
     asm volatile("griddepcontrol.wait;" ::: "memory");   // set up while the work before this call ends
     asm volatile("griddepcontrol.launch_dependents;");
-    const uint32_t rank = cluster_rank(), ranks = cluster_size();
+    const uint32_t rank = THREADS == kSmallSelect ? 0 : cluster_rank(), ranks = THREADS == kSmallSelect ? 1 : cluster_size();
     const int row_id = blockIdx.x / ranks;
     const int head = row_id % p.H, seq = row_id / p.H % p.n_seq, layer = row_id / p.H / p.n_seq;
     const int len = own_len(p, seq);
@@ -257,7 +370,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSmallSelect ? 4 : 1) evic
     for (int j = first; j < p.sink; j += step) kept[j] = j;
     for (int j = first; j < p.recent; j += step) kept[p.budget - p.recent + j] = hi + j;
     const float *row = p.scores + layer * p.scores_stride[0] + seq * p.scores_stride[1] + head * p.scores_stride[2];
-    const int per = (hi - lo + step - 1) / step;
+    const int per = (int)(((int64_t)hi - lo + step - 1) / step);
     kept += p.sink;
     if (per <= 2)
         select_row<THREADS, 2>(sh, row, lo, hi, per, want, kept, rank, ranks);
@@ -267,8 +380,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == kSmallSelect ? 4 : 1) evic
         select_row<THREADS, 8>(sh, row, lo, hi, per, want, kept, rank, ranks);
     else if (per <= 16)
         select_row<THREADS, 16>(sh, row, lo, hi, per, want, kept, rank, ranks);
-    else
-        select_row<THREADS, THREADS == kSmallSelect ? kSmallKeys : 0>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else if (per <= 32)
+        select_row<THREADS, 32>(sh, row, lo, hi, per, want, kept, rank, ranks);
+    else if (THREADS == kLargeSelect)
+        select_row<THREADS, 0>(sh, row, lo, hi, per, want, kept, rank, ranks);
 }
 
 namespace {
@@ -454,10 +569,10 @@ cudaError_t launch_evict(const EvictParams &p, int sm_count, cudaStream_t stream
         if (rows > INT32_MAX) return cudaErrorInvalidConfiguration;
         e = launch_clusters(evict_select_kernel<kSmallSelect>, rows, 1, kSmallSelect, stream, p);
     } else {
-        // CTAs per row: as many as its keys need registers, or, few rows, as keep every CTA at 2048 keys and more
-        int cluster = 1;
-        while (cluster < 8 && (p.max_len > cluster * kLargeSelect * kLargeKeys || (rows * cluster < 2 * sm_count && p.max_len > cluster * 2048)))
-            cluster *= 2;
+        // CTAs per row: as many as its keys need registers, or, few rows, as keep every CTA at 2048 keys and more while
+        // all clusters run at once (a cluster stays within a group of SMs, so an eighth of them can be left over)
+        int cluster = (int)std::min<int64_t>(8, (p.max_len + kLargeSelect * kLargeKeys - 1) / (kLargeSelect * kLargeKeys));
+        while (cluster < 8 && rows * (cluster + 1) <= 2 * (sm_count - sm_count / 8) && p.max_len > cluster * 2048) ++cluster;
         if (rows * cluster > INT32_MAX) return cudaErrorInvalidConfiguration;
         e = launch_clusters(evict_select_kernel<kLargeSelect>, rows, cluster, kLargeSelect, stream, p);
     }
