@@ -534,13 +534,13 @@ cudaError_t launch_clusters(void (*kernel)(P...), int64_t rows, int cluster, int
     cfg.blockDim = dim3(threads);
     cfg.stream = stream;
     cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits for the one before it on the device
-    at[1].val.programmaticStreamSerializationAllowed = 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits for the one before it on the device
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;   // (a CTA is a cluster of one)
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 

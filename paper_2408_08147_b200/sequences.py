@@ -139,10 +139,11 @@ class CacheSession:
 
     def _rows(self, name, t, lead, least):
         """fp32 rows over tokens: shape (*lead, width) with adjacent tokens."""
-        if t.dtype != torch.float32 or t.device != self.pool_t.device or tuple(t.shape[:-1]) != tuple(lead) or t.shape[-1] < least:
-            raise ValueError(f"{name}: expected float32 {tuple(lead)} x at least {least} tokens on {self.pool_t.device}, "
-                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+        shape = t.shape
+        if t.dtype != torch.float32 or t.device != self._device or shape[:-1] != lead or shape[-1] < least:
+            raise ValueError(f"{name}: expected float32 {lead} x at least {least} tokens on {self._device}, "
+                             f"got {t.dtype} {tuple(shape)} on {t.device}")
+        if shape[-1] > 1 and t.stride(-1) != 1:
             raise ValueError(f"{name}: tokens have to be adjacent")
 
     def scratch_bytes(self, with_scores: bool = False) -> int:
@@ -209,21 +210,21 @@ class CacheSession:
         front of the same sequences in ``dst`` (this session itself: in place).  ``scores_t`` is float32
         ``[layers, n_seq, num_kv_heads, >= longest]``.  Returns ``(kept, kept_scores, new_len)``."""
         l0, l1 = (0, self.geom.num_layers) if layers is None else layers
-        lead = (l1 - l0, self.seqs.n_seq, self.geom.num_kv_heads)
-        self._rows("scores_t", scores_t, lead, self.seqs.max_len)
-        dev = self._device
+        n_seq = self._shape[0]
+        lead = (l1 - l0, n_seq, self.geom.num_kv_heads)
+        self._rows("scores_t", scores_t, lead, self._max_len)
         if kept_t is None:
-            kept_t = torch.empty(*lead, budget, dtype=torch.int32, device=dev)
+            kept_t = scores_t.new_empty((*lead, budget), dtype=torch.int32)
         else:
             self._check("kept_t", kept_t, torch.int32, (*lead, budget))
             if not kept_t.is_contiguous():
                 raise ValueError("kept_t has to be contiguous")
         if kept_scores_t is None:
-            kept_scores_t = torch.empty(*lead, budget, dtype=torch.float32, device=dev)
+            kept_scores_t = scores_t.new_empty((*lead, budget))
         else:
-            self._rows("kept_scores_t", kept_scores_t, lead, min(budget, self.seqs.max_len))
+            self._rows("kept_scores_t", kept_scores_t, lead, min(budget, self._max_len))
         if new_len_t is None:
-            new_len_t = torch.empty(self.seqs.n_seq, dtype=torch.int32, device=dev)
+            new_len_t = scores_t.new_empty((n_seq,), dtype=torch.int32)
         a = B.pdkv_evict_args(budget=budget, sink=sink, recent=recent, seq_len=self._lens(seq_len_t), scores=scores_t.data_ptr(),
                               scores_stride=scores_t.stride()[:3], kept=kept_t.data_ptr(), kept_scores=kept_scores_t.data_ptr(),
                               kept_scores_stride=kept_scores_t.stride()[:3], kept_scores_len=kept_scores_t.shape[-1],
