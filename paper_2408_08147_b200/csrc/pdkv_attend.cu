@@ -91,7 +91,6 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
 {
     using R = Ring<DP>;
     const int lane = threadIdx.x % 32;
-    const int cols = (p.D + 15) / 16 * 2;   // 16-byte pieces of a row; one past the row's end is filled with zeros
     bool dead = false;
     uint32_t slot = 0, parity = 1;
     for (bool more = true; more;) {
@@ -155,13 +154,11 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
                     constexpr int kCols = DP / 8;
                     const int x = lane + 32 * k, row = x / kCols, col = x % kCols;
                     const int64_t o = __shfl_sync(~0u, offset, row);
-                    if (col < cols) {
-                        const bool there = o >= 0 && col * 8 < p.D;
-                        const char *from = base + (there ? o + col * 16 : 0);
-                        const uint32_t at = to + col / 8 * R::kSubBytes + row * 128 + (((col % 8) ^ (row % 8)) * 16);
-                        copy_async(at, from, there);
-                        copy_async(at + R::kHalf, from + p.pool.lc_stride, there);
-                    }
+                    const bool there = o >= 0 && col * 8 < p.D;   // else zeros
+                    const char *from = base + (there ? o + col * 16 : 0);
+                    const uint32_t at = to + col / 8 * R::kSubBytes + row * 128 + (((col % 8) ^ (row % 8)) * 16);
+                    copy_async(at, from, there);
+                    copy_async(at + R::kHalf, from + p.pool.lc_stride, there);
                 }
                 copy_arrive(&bar.full[slot]);
             }
@@ -187,8 +184,9 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
 // Maximum and sum of each row are kept in 32 bits; O is rescaled only when a maximum outgrew its base by
 // 2^8 (weights up to 2^8 lose nothing in 16-bit floating point).  The weights are rounded to 16 bits for
 // the product with V (the matrix instruction takes no wider operand beside a 16-bit V); their sum is
-// taken before that.  FULL: the head has exactly DP dims.
-template <typename T, int DP, bool FULL, int NT, int WM>
+// taken before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
+// the loads of the next ones from being issued ahead: 40 rows of 256 dims 338 us, without 164).
+template <typename T, int DP, int KD, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
                                             float (*sml)[16][2], RingBarriers &bar, uint32_t n, bool &dead)
 {
@@ -201,7 +199,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
 
     // operand Q^T: row lane / 4 of each tile of eight, dims 2 (lane % 4) and 8 further of each sixteen
-    uint32_t q[DP / 16][NT][2];
+    uint32_t q[KD][NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int r = (wm * NT + t) * 8 + lane / 4;
@@ -209,11 +207,12 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
         const RowId id = row_id(p, it, it.row0 + (live ? r : 0));
         const T *row = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + (it.head * p.G + id.g) * p.q_stride[2];
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
+        for (int k = 0; k < KD; ++k)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int d = 16 * k + 8 * j + 2 * (lane % 4);
-                q[k][t][j] = live && (FULL || d < p.D) ? *reinterpret_cast<const uint32_t *>(row + d) ^ flip : 0u;
+                const uint32_t x = *reinterpret_cast<const uint32_t *>(row + min(d, p.D - 2));   // (always, so that all are on their way)
+                q[k][t][j] = live && d < p.D ? x ^ flip : 0u;
             }
     }
     // accumulators: rows 2 (lane % 4) and the next of each tile of eight
@@ -238,9 +237,9 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     const int safe = own ? min(limit, len - (p.q_tokens - 1)) : limit;   // tokens before this one are seen by every row
     const bool with_logits = p.logits && own;
 
-    float o[DP / 16][NT][4];
+    float o[KD][NT][4];
 #pragma unroll
-    for (int k = 0; k < DP / 16; ++k)
+    for (int k = 0; k < KD; ++k)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -284,15 +283,13 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
         }
         float z[2][NT][4] = {};   // [16 tokens][8 rows]: tokens lane / 4 and 8 further
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-            if (FULL || 16 * k < p.D) {
+        for (int k = 0; k < KD; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t a[4];
-                    load_matrices(a, slice + k_at + h * 2048 + k / 4 * R::kSubBytes + k_chunk[k % 4]);
+            for (int h = 0; h < 2; ++h) {
+                uint32_t a[4];
+                load_matrices(a, slice + k_at + h * 2048 + k / 4 * R::kSubBytes + k_chunk[k % 4]);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) multiply<T>(z[h][t], a, q[k][t][0], q[k][t][1]);
-                }
+                for (int t = 0; t < NT; ++t) multiply<T>(z[h][t], a, q[k][t][0], q[k][t][1]);
             }
         if (t0 + kSlice > safe)
 #pragma unroll
@@ -334,7 +331,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                     m[t][j] = new_m;
                     l[t][j] *= f;
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
+                    for (int k = 0; k < KD; ++k) {
                         o[k][t][j] *= f;
                         o[k][t][j + 2] *= f;
                     }
@@ -357,15 +354,13 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             }
         }
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-            if (FULL || 16 * k < p.D) {
+        for (int k = 0; k < KD; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t a[4];
-                    load_matrices_trans(a, slice + v_at + h * 2048 + k / 4 * R::kSubBytes + v_chunk[k % 4]);
+            for (int h = 0; h < 2; ++h) {
+                uint32_t a[4];
+                load_matrices_trans(a, slice + v_at + h * 2048 + k / 4 * R::kSubBytes + v_chunk[k % 4]);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) multiply<T>(o[k][t], a, w[h][t][0], w[h][t][1]);
-                }
+                for (int t = 0; t < NT; ++t) multiply<T>(o[k][t], a, w[h][t][0], w[h][t][1]);
             }
         __syncwarp();
         if (lane == 0) mbar_arrive_many(&bar.empty[slot], kGroups);   // a slot is free after four arrivals
@@ -391,7 +386,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     for (int t = 0; t < NT; ++t) {
         float *mine = xch + (warp * 8 + 2 * (lane % 4)) * R::kXchRow + lane / 4;
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
+        for (int k = 0; k < KD; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) mine[(j & 1) * R::kXchRow + 16 * k + 8 * (j >> 1)] = o[k][t][j];
         consumer_sync();
@@ -446,7 +441,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 
 // Every CTA walks its stretch of the work list.  Warps are laid along the rows as far as there are rows,
 // the rest of them along the tokens.
-template <typename T, int DP, bool FULL>
+template <typename T, int DP, int KD>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p)
 {
     using R = Ring<DP>;
@@ -477,13 +472,13 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
             int len, limit;
             const int slices = slices_of(p, it, &len, &limit);
             if (it.rows <= 8)
-                attend_item<T, DP, FULL, 1, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+                attend_item<T, DP, KD, 1, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
             else if (it.rows <= 16)
-                attend_item<T, DP, FULL, 2, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+                attend_item<T, DP, KD, 2, 1>(p, it, slices, len, limit, smem, sml, bar, n, dead);
             else if (it.rows <= 32)
-                attend_item<T, DP, FULL, 2, 2>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+                attend_item<T, DP, KD, 2, 2>(p, it, slices, len, limit, smem, sml, bar, n, dead);
             else
-                attend_item<T, DP, FULL, 2, 4>(p, it, slices, len, limit, smem, sml, bar, n, dead);
+                attend_item<T, DP, KD, 2, 4>(p, it, slices, len, limit, smem, sml, bar, n, dead);
             n += slices;
             it = next_it;
         }
@@ -608,10 +603,10 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
 
 namespace {
 
-template <typename T, int DP, bool FULL> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, int KD> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(attend_items_kernel<T, DP, FULL>, Ring<DP>::kBytes, ready);
+    const cudaError_t e = allow_shared(attend_items_kernel<T, DP, KD>, Ring<DP>::kBytes, ready);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.n_ctas);
@@ -623,18 +618,17 @@ template <typename T, int DP, bool FULL> cudaError_t launch_dims(const AttnParam
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_items_kernel<T, DP, FULL>, map, p);
+    return cudaLaunchKernelEx(&cfg, attend_items_kernel<T, DP, KD>, map, p);
 }
 
 template <typename T> cudaError_t launch_type(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
-    // heads of exactly 64 and 128 dims without the checks for where a head ends
-    if (p.D == 64) return launch_dims<T, 64, true>(p, map, stream);
-    if (p.D == 128) return launch_dims<T, 128, true>(p, map, stream);
-    if (p.D <= 64) return launch_dims<T, 64, false>(p, map, stream);
-    if (p.D <= 128) return launch_dims<T, 128, false>(p, map, stream);
-    if (p.D <= 192) return launch_dims<T, 192, false>(p, map, stream);
-    return launch_dims<T, 256, false>(p, map, stream);
+    // shared memory in pieces of 64 dims, products in steps that cover the head
+    if (p.D <= 64) return launch_dims<T, 64, 4>(p, map, stream);
+    if (p.D <= 96) return launch_dims<T, 128, 6>(p, map, stream);
+    if (p.D <= 128) return launch_dims<T, 128, 8>(p, map, stream);
+    if (p.D <= 192) return launch_dims<T, 192, 12>(p, map, stream);
+    return launch_dims<T, 256, 16>(p, map, stream);
 }
 
 }  // namespace

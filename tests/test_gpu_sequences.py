@@ -454,6 +454,44 @@ def test_equal_zero_infinite_and_nan_scores():
     assert (kept.cpu().numpy() == want[0]).all()
 
 
+def _rows_to_select_from(n, rng):
+    """Scores that a sample, or the halving of an interval, is misled by."""
+    comb = rng.random(n).astype(np.float32)
+    comb[(n * np.arange(128)) // 128] = 5.0                       # evenly spaced: what a sample may see
+    tied = rng.integers(0, 3, n).astype(np.float32)
+    rare = np.full(n, -np.inf, np.float32)
+    rare[rng.integers(0, n, 40)] = rng.standard_normal(40)
+    rare[rng.integers(0, n, 40)] = np.nan
+    tiny = (rng.random(n) * 1e-42).astype(np.float32)             # subnormal
+    return [np.exp(3 * rng.standard_normal(n)).astype(np.float32), np.sort(rng.standard_normal(n)).astype(np.float32)[::-1], comb,
+            tied, rare, tiny, np.where(rng.random(n) < 0.5, np.float32(1), np.float32(1 + 2.0**-23)).astype(np.float32)]
+
+
+@pytest.mark.parametrize("longest", [300, 1500, 8192, 8193, 20000, 131073])
+def test_selection_by_rows_and_budgets(longest):
+    """Rows in registers of one CTA and of clusters, rows that are read again and again, shorter rows beside them."""
+    rng = np.random.default_rng(longest)
+    rows = [_rows_to_select_from(n, rng) for n in (longest, longest - longest // 3, 290)]
+    lens = [len(r[0]) for r in rows]
+    e = Evict(lens, 1, layers=7, H=1, D=8)
+    scores = np.zeros((7, 3, 1, longest), np.float32)
+    for r, kinds in enumerate(rows):
+        for k in range(7):
+            scores[k, r, 0, :lens[r]] = kinds[k]
+    src_t, _ = e.tensors()
+    dev = torch.from_numpy(scores).cuda()
+    for budget, sink, recent in ((1, 0, 0), (64, 4, 16), (289, 0, 1), (longest // 2, 3, 100), (longest - 1, 0, 0)):
+        d = Evict(lens, budget, layers=7, H=1, D=8)
+        _, dst_t = d.tensors()
+        with CacheSession(e.src, src_t, e.src_seqs) as a, CacheSession(d.dst, dst_t, d.dst_seqs) as b:
+            kept, _, n = a.evict(b, dev, budget, sink=sink, recent=recent)
+        kept = kept.cpu().numpy()
+        for k in range(7):
+            for r in range(3):
+                want = O.select(scores[k, r, 0, :lens[r]], budget, sink, recent)
+                assert (kept[k, r, 0, :len(want)] == want).all() and (kept[k, r, 0, len(want):] == -1).all(), (k, r, budget)
+
+
 def test_compaction_in_place_with_its_scores_and_device_lengths():
     """One buffer of scores and one of lengths, both updated in place; a range of layers."""
     e = Evict([100, 12, 0, 64], 30, caps=[160, 40, 20, 64])
