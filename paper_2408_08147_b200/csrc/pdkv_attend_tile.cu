@@ -14,6 +14,12 @@
 // O is rescaled only when a row's maximum grew by more than 2^8 since the last time: the weights stay below
 // 2^8, where 16-bit and 32-bit floating point lose nothing.  Maxima and sums are 32 bits, the sums taken
 // before the weights are rounded.
+//
+// Bound by the tensor core and by the chain S, P, O of a row tile: 256 rows against 128 tokens of 128 dims take it
+// 3024 cycles (125 for 16 dims of Q K^T, whose two operands come from shared memory at 64 bytes a cycle, 64 for 16 tokens
+// of P V), and an iteration takes 3700.  Measured on B200, whole calls: 64 rows of each of 8 heads against 65536 tokens
+// 78 us (3.4 TB/s), 256 rows 99 us (690 TFLOP/s), 512 rows against 200000 tokens 451 us (930 TFLOP/s).  Starting and finishing an
+// item costs about 8 us, which is what short lists pay (256 rows against 4096 tokens: 26 us).
 #include <algorithm>
 #include <numeric>
 #include <type_traits>
@@ -575,7 +581,9 @@ template <int DP> constexpr uint32_t weigh_bytes(int rows)
 //
 // S^T = K Q^T: a thread has one token and its logits of all rows in tensor memory, so the sum over the
 // rows needs no other thread.  Six warps: four compute weights, one issues the products, one the loads of K;
-// two tiles of K and two of S^T are on their way.  Two CTAs on an SM up to 128 rows.
+// two tiles of K and two of S^T are on their way.  Two CTAs on an SM up to 128 rows.  Bound by the exponentials and
+// the loads of S^T from tensor memory: 12 sequences of 300 to 4096 tokens, 64 rows each, 8 heads of 128 dims take 27 us
+// as a kernel alone, of which the bytes of K need 9.
 template <typename T, int DP>
 __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
 {
