@@ -502,19 +502,21 @@ constexpr int kScoreRows = 64;     // rows whose lse is held at a time
 
 }  // namespace
 
-// The first `row_blocks` blocks of a (sequence, head) join the parts of four rows each, a warp per row:
+// The first `row_blocks` blocks of a (sequence, head) join the parts of four rows each, a warp per row, or (WIDE: rows in
+// many parts) of one row, each warp every fourth part:
 // m = max m_p, l = sum l_p 2^(m_p - m), O = sum O_p 2^(m_p - m).  The others turn the logits of a chunk of
 // tokens into weights 2^(z - lse) and add them to the scores; they take the lse from the parts themselves, so no
 // block waits for another.  Bound by the latency of its few dependent loads: 4096 rows of 128 dims in four parts each 10 us
 // alone, about 4 us behind the kernel that left them, since it is set up while that one ends.
-template <typename T>
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, const int row_blocks, const int chunks)
 {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, per = row_blocks + chunks;
     const int x = blockIdx.x % per, head = blockIdx.x / per % p.H, seq = blockIdx.x / per / p.H;
     const AttnSeq s = p.seqs[seq];
     const int R = p.G * p.q_tokens;
-    const int row = 4 * x + warp;
+    constexpr int ways = WIDE ? 4 : 1;
+    const int row = WIDE ? x : 4 * x + warp, way = WIDE ? warp : 0;
     const bool mine = x < row_blocks && !s.direct && row < R;
     Parts parts{};
     if (mine) parts = parts_of(p, s, head, row);         // where they are is known before they are written
@@ -522,17 +524,17 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     asm volatile("griddepcontrol.launch_dependents;");
     if (x < row_blocks) {
         if (!mine) return;
-        const int n = parts.n[0] + parts.n[1];
+        const int n = (parts.n[0] + parts.n[1] - way + ways - 1) / ways;   // of this warp: way, way + ways, ...
         const float2 ml = joined_ml<32>(p, parts, lane);
         const float base = ml.x == -INFINITY ? 0.f : ml.x;
         float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
         for (int i0 = 0; i0 < n; i0 += 32) {
-            const float w = i0 + lane < n ? pow2(p.part_ml[2 * part_at(parts, i0 + lane)] - base) : 0.f;
+            const float w = i0 + lane < n ? pow2(p.part_ml[2 * part_at(parts, (i0 + lane) * ways + way)] - base) : 0.f;
             const int top = min(32, n - i0);
 #pragma unroll 8
             for (int i = 0; i < top; ++i) {
                 const float wi = __shfl_sync(~0u, w, i);
-                const float4 *o = reinterpret_cast<const float4 *>(p.part_o + part_at(parts, i0 + i) * p.D);
+                const float4 *o = reinterpret_cast<const float4 *>(p.part_o + part_at(parts, (i0 + i) * ways + way) * p.D);
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     if (4 * (lane + 32 * k) < p.D) {
@@ -543,6 +545,25 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
                         acc[k].w += wi * v.w;
                     }
             }
+        }
+        if (WIDE) {
+            __shared__ float4 others[3][64];
+            if (warp > 0) {
+                others[warp - 1][lane] = acc[0];
+                others[warp - 1][lane + 32] = acc[1];
+            }
+            __syncthreads();   // (a block has one row: all warps come here)
+            if (warp > 0) return;
+#pragma unroll
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float4 v = others[w][lane + 32 * k];
+                    acc[k].x += v.x;
+                    acc[k].y += v.y;
+                    acc[k].z += v.z;
+                    acc[k].w += v.w;
+                }
         }
         const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
         const int token = row / p.G, h = head * p.G + row % p.G;
@@ -566,7 +587,11 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     for (int r0 = 0; r0 < R; r0 += kScoreRows) {
         const int n = min(kScoreRows, R - r0);
         __syncthreads();
-        for (int r = warp * 8; r < n; r += 32) {
+        for (int r = warp; WIDE && r < n; r += 4) {
+            const float2 ml = joined_ml<32>(p, parts_of(p, s, head, r0 + r), lane);
+            if (lane == 0) lse[r] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+        }
+        for (int r = warp * 8; !WIDE && r < n; r += 32) {
             const int row = r + lane / 4;
             const float2 ml = joined_ml<4>(p, parts_of(p, s, head, r0 + min(row, n - 1)), lane);
             // an empty row gives no weight to anything: 2^(z - inf) = 0
@@ -654,9 +679,11 @@ cudaError_t launch_attend(const AttnParams &p, const void *map, int dtype, cudaS
     return dtype == PDKV_DTYPE_BF16 ? launch_type<__nv_bfloat16>(p, m, stream) : launch_type<__half>(p, m, stream);
 }
 
-cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream)
+cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, int most_parts, cudaStream_t stream)
 {
-    const int row_blocks = join ? (p.G * p.q_tokens + 3) / 4 : 0;
+    // A row in hundreds of parts would keep one warp waiting for them: 12 rows in 290 parts each 51 us a call, 23 with four warps a row
+    const bool wide = most_parts > 16;
+    const int rows = p.G * p.q_tokens, row_blocks = join ? (wide ? rows : (rows + 3) / 4) : 0;
     const int per = score_chunk(p.G * p.q_tokens), chunks = p.logits ? (p.max_len + per - 1) / per : 0;
     const int64_t blocks = (int64_t)p.n_seq * p.H * (row_blocks + chunks);
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
@@ -671,8 +698,9 @@ cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaSt
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (dtype == PDKV_DTYPE_BF16) return cudaLaunchKernelEx(&cfg, attend_join_kernel<__nv_bfloat16>, p, row_blocks, chunks);
-    return cudaLaunchKernelEx(&cfg, attend_join_kernel<__half>, p, row_blocks, chunks);
+    if (dtype == PDKV_DTYPE_BF16)
+        return cudaLaunchKernelEx(&cfg, wide ? attend_join_kernel<__nv_bfloat16, true> : attend_join_kernel<__nv_bfloat16, false>, p, row_blocks, chunks);
+    return cudaLaunchKernelEx(&cfg, wide ? attend_join_kernel<__half, true> : attend_join_kernel<__half, false>, p, row_blocks, chunks);
 }
 
 }  // namespace pdkv

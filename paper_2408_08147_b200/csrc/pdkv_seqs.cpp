@@ -442,6 +442,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
                 }
                 if (!q.direct) s->join = true;
             }
+            for (const AttnUnit &u : s->units) s->most_parts = std::max(s->most_parts, u.n_parts);
             for (std::vector<AttnItem> &list : s->items)
                 for (AttnItem &it : list) it.direct = it.seq >= 0 && s->seqs[(size_t)it.seq].direct;
         }
@@ -617,7 +618,7 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         if (!s->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0) return PDKV_OK;
         // blocks of the joining and weighing kernels: refused before anything is enqueued
-        if ((double)s->n_seq * s->pool.d.num_kv_heads * ((double)s->G * s->q_tokens / 4 + 1 + (scores ? s->max_len / 128.0 + 1 : 0)) > 2e9)
+        if ((double)s->n_seq * s->pool.d.num_kv_heads * ((double)s->G * s->q_tokens + 1 + (scores ? s->max_len / 128.0 + 1 : 0)) > 2e9)
             return PDKV_ERR_LIMIT;
 
         pdkv::AttnParams p{};
@@ -685,7 +686,7 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "attention kernel launch");
         }
         if (s->join || p.logits) {
-            const cudaError_t e = pdkv::launch_attend_join(p, s->dtype, s->join, st);
+            const cudaError_t e = pdkv::launch_attend_join(p, s->dtype, s->join, s->most_parts, st);
             if (e != cudaSuccess) return pdkv::report_cuda_error(e, "join kernel launch");
         }
         if (scores && s->own_tiles) {

@@ -105,7 +105,7 @@ int attend_tile_box(const pdkv_pool_desc &d);
 bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out);
 cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 cudaError_t launch_attend_weigh(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
-cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, cudaStream_t stream);
+cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, int most_parts, cudaStream_t stream);
 
 struct EvictParams {
     PoolView src, dst;
@@ -153,6 +153,7 @@ struct pdkv_seqs {
     std::vector<pdkv_attend_item> listing;
     int64_t part_rows = 0, logit_floats = 0;
     bool join = false;           // some rows have several parts, or none
+    int32_t most_parts = 0;      // of a row behind one segment
     // device arrays
     void *dev_mem = nullptr;
     bool owns_dev_mem = true;
