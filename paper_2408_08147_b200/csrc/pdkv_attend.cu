@@ -442,7 +442,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 // Every CTA walks its stretch of the work list.  Warps are laid along the rows as far as there are rows,
 // the rest of them along the tokens.
 // Bound by memory up to 16 rows: 32 sequences of 2048 tokens, 8 heads of 128 dims, 4 rows each 43.6 us (6.2 TB/s of K and V),
-// 2 sequences of about 110000 tokens, 8 rows each, 6.3 TB/s.  Above, by the products of the four warps, or eight, of an SM
+// 2 sequences of about 110000 tokens, 8 rows each, 6.4 TB/s.  Above, by the products of the four warps, or eight, of an SM
 // (64 rows of 256 dims over 40000 tokens 174 us, 8 rows 63).  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
 // them busy for 9% of the time.
 template <typename T, int DP, int KD>

@@ -161,6 +161,26 @@ def test_scores(kw):
         assert torch.equal(other[..., :-3], scores[..., :-3]) and (other[..., -3:] == 7.0).all()
 
 
+@pytest.mark.parametrize("kw", [
+    dict(lens=[20000], H=1, G=3, D=96),
+    dict(lens=[9000, 700], H=1, G=2, Q=3, D=256, prefix_len=[8000], member=[0, -1]),
+    dict(lens=[12000, 3], H=1, G=40, D=64, prefix_len=[5000], member=[-1, 0]),
+    dict(lens=[15000, 2], H=1, G=20, Q=4, D=128),
+], ids=str)
+def test_rows_in_many_parts(kw):
+    """Few heads and long lists: a row is cut into one part for each of the machine's CTAs."""
+    s = Setup(layers=1, layer=0, **kw)
+    scores = torch.zeros(len(s.lens), s.H, max(s.lens), device="cuda")
+    want = s.expect()
+    with s.session() as c:
+        items = c.items()
+        assert max(np.unique(np.stack([items["seq"], items["prefix"], items["row_begin"]]), axis=1, return_counts=True)[1]) > 16
+        check(s, *c.attend(0, s.q_t), want)
+        check(s, *c.attend(0, s.q_t, scores_t=scores), want)
+        c.status()
+    check_scores(s, np.zeros(scores.shape), scores, want, s.lens)
+
+
 def test_current_lengths_from_the_device():
     """Lengths under the handle's; negative and too large ones are clamped; slots past them hold NaN."""
     s = Setup([3, 0, 90, 33, 200], caps=[40, 50, 128, 33, 200], G=4, Q=2, prefix_len=[50], member=[-1, -1, 0, 0, -1])
