@@ -77,7 +77,9 @@ class CacheSession:
     ``num_q_heads`` the session attends; ``dtype`` (torch.bfloat16 or torch.float16) is the type
     of K, V, q and out and defaults to the pool's own.  Scratch is allocated once and kept: calls
     of one session are meant for one stream at a time (pass ``scratch_t`` for others).
-    ``stream`` None means torch's current stream of the pool's device at each call.
+    ``stream`` None means torch's current stream of the pool's device at each call.  What a call
+    allocates comes from torch's current stream and is recorded on the stream that it runs on, so its
+    memory is not given away before the call has run; that stream has to live as long as the tensors.
     """
 
     def __init__(self, geom, pool_t, seqs: Sequences, *, num_q_heads: int = 0, q_tokens: int = 1, dtype=None,
@@ -86,6 +88,7 @@ class CacheSession:
         self.num_q_heads, self.q_tokens, self.stream = num_q_heads, q_tokens, stream
         self.pool = self.handle = None
         self._scratch = [None, None]   # without and with scores; never replaced, recorded graphs may hold them
+        self._scratch_stream = [0, 0]  # torch's current stream when they were allocated
         if dtype is None:
             dtype = pool_t.dtype if pool_t.dtype in _DTYPES else torch.bfloat16
         if dtype not in _DTYPES:
@@ -122,7 +125,18 @@ class CacheSession:
             return stream
         if self.stream is not None:
             return self.stream
+        return self._on_current()
+
+    def _on_current(self) -> int:
         return _current_stream(self._index) if self.pool_t.is_cuda else 0
+
+    def _record(self, stream: int, home: int, *tensors) -> None:
+        """The caching allocator hands a freed block to the next request on its ``home`` stream: tell it of
+        the other stream that uses these."""
+        if stream != home and self.pool_t.is_cuda:
+            user = torch.cuda.ExternalStream(stream, self._device)
+            for t in tensors:
+                t.record_stream(user)
 
     def _check(self, name, t, dtype, shape):
         if t.dtype != dtype or t.shape != shape or t.device != self._device:
@@ -156,6 +170,7 @@ class CacheSession:
         the attention weights of the own tokens are added to it, or to ``scores_in_t`` and the sums
         stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device)."""
         shape = self._shape
+        made = []
         self._check("q_t", q_t, self.dtype, shape)
         a = B.pdkv_attend_args.from_buffer_copy(self._plain)
         dense = q_t.is_contiguous()
@@ -166,6 +181,7 @@ class CacheSession:
             a.q_stride = stride[:3]
         if out_t is None:
             out_t = torch.empty_like(q_t) if dense else torch.empty(shape, dtype=self.dtype, device=self._device)
+            made.append(out_t)
         else:
             self._check("out_t", out_t, self.dtype, shape)
             stride = out_t.stride()
@@ -174,6 +190,7 @@ class CacheSession:
             a.out_stride = stride[:3]
         if lse_t is None:
             lse_t = torch.empty(shape[:3], dtype=torch.float32, device=self._device)
+            made.append(lse_t)
         else:
             self._check("lse_t", lse_t, torch.float32, shape[:3])
             if not lse_t.is_contiguous():
@@ -192,15 +209,19 @@ class CacheSession:
             a.scores_in_stride, a.scores_out_stride = scores_in_t.stride()[:2], scores_t.stride()[:2]
         elif scores_in_t is not None:
             raise ValueError("scores_in_t needs scores_t to receive the sums")
+        stream, home = self._on(stream), self._on_current()
         if scratch_t is None:
             which = scores_t is not None
             scratch_t = self._scratch[which]
             if scratch_t is None:
                 scratch_t = self._scratch[which] = torch.empty(max(self._need[which], 16), dtype=torch.uint8, device=self._device)
+                self._scratch_stream[which] = home
+            self._record(stream, self._scratch_stream[which], scratch_t)
             size = scratch_t.numel()
         else:
             size = scratch_t.numel() * scratch_t.element_size()
-        B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, self._on(stream))
+        self._record(stream, home, *made)
+        B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, stream)
         return out_t, lse_t
 
     def evict(self, dst: "CacheSession", scores_t, budget: int, *, sink: int = 0, recent: int = 0,
@@ -213,23 +234,29 @@ class CacheSession:
         n_seq = self._shape[0]
         lead = (l1 - l0, n_seq, self.geom.num_kv_heads)
         self._rows("scores_t", scores_t, lead, self._max_len)
+        made = []
         if kept_t is None:
             kept_t = scores_t.new_empty((*lead, budget), dtype=torch.int32)
+            made.append(kept_t)
         else:
             self._check("kept_t", kept_t, torch.int32, (*lead, budget))
             if not kept_t.is_contiguous():
                 raise ValueError("kept_t has to be contiguous")
         if kept_scores_t is None:
             kept_scores_t = scores_t.new_empty((*lead, budget))
+            made.append(kept_scores_t)
         else:
             self._rows("kept_scores_t", kept_scores_t, lead, min(budget, self._max_len))
         if new_len_t is None:
             new_len_t = scores_t.new_empty((n_seq,), dtype=torch.int32)
+            made.append(new_len_t)
         a = B.pdkv_evict_args(budget=budget, sink=sink, recent=recent, seq_len=self._lens(seq_len_t), scores=scores_t.data_ptr(),
                               scores_stride=scores_t.stride()[:3], kept=kept_t.data_ptr(), kept_scores=kept_scores_t.data_ptr(),
                               kept_scores_stride=kept_scores_t.stride()[:3], kept_scores_len=kept_scores_t.shape[-1],
                               new_len=self._lens(new_len_t))
-        B.pdkv_evict(self.handle, dst.handle, l0, l1, a, self._on(stream))
+        stream = self._on(stream)
+        self._record(stream, self._on_current(), *made)
+        B.pdkv_evict(self.handle, dst.handle, l0, l1, a, stream)
         return kept_t, kept_scores_t, new_len_t
 
     def items(self) -> np.ndarray:
