@@ -437,7 +437,8 @@ int pdkv_seqs_destroy(pdkv_seqs *seqs);
  * to the whole prefix and to own tokens t < len_r - (q_tokens - 1 - i) (the token's own
  * key is expected in the cache).  Query head h*G + g reads KV head h, G = num_q_heads /
  * num_kv_heads.  Logits are scale * q.k; sums, maxima and weights are held in 32 bits,
- * the weights are rounded to the pool's type for the product with V.  A row with
+ * the weights are rounded to the pool's type for the product with V (off by half a step each; fp16 weights
+ * under 2^-21 of a row's largest by up to 2^-32 of that).  A row with
  * nothing to attend to (or whose every logit is -infinity) gives zeros and lse =
  * -infinity.  Cached rows past a sequence's length are never read into a result,
  * whatever they hold. */

@@ -181,10 +181,9 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
 // K and V are the 16-row operands, read from shared memory as they lie (V transposed by the matrix load), and
 // eight rows cost half the instructions and registers that they would cost as one side of sixteen.  P^T
 // changes from accumulator to operand layout by transposing its 8 x 8 tiles between lanes.
-// Maximum and sum of each row are kept in 32 bits; O is rescaled only when a maximum outgrew its base by
-// 2^8 (weights up to 2^8 lose nothing in 16-bit floating point).  The weights are rounded to 16 bits for
-// the product with V (the matrix instruction takes no wider operand beside a 16-bit V); their sum is
-// taken before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
+// Base and sum of each row are kept in 32 bits; O is rescaled only when a maximum outgrew its base by
+// 2^8.  The weights are rounded to 16 bits for the product with V (one instruction takes no wider operand beside a
+// 16-bit V; see kLift); their sum is taken before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
 // the loads of the next ones from being issued ahead: 40 rows of 256 dims 338 us, without 164).
 template <typename T, int DP, int KD, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
@@ -319,7 +318,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                 x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
                 x = fmaxf(x, __shfl_xor_sync(~0u, x, 8));
                 x = fmaxf(x, __shfl_xor_sync(~0u, x, 16));
-                top[t][j] = x == -INFINITY ? x : x * scale;
+                top[t][j] = x == -INFINITY ? x : fmaf(x, scale, -kLift<T>);   // the base that this slice asks for
                 grew = grew || top[t][j] > m[t][j] + kGrowth || (m[t][j] == -INFINITY && top[t][j] > m[t][j]);
             }
         if (__any_sync(~0u, grew)) {

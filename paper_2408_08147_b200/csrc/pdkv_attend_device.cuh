@@ -53,6 +53,14 @@ __device__ __forceinline__ RowId row_id(const AttnParams &p, const AttnItem &seg
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 constexpr float kGrowth = 8.f;                    // log2 of how far a maximum may run ahead of its base
+// A row's weights are 2^(z - base), rounded to the pool's type for the product with V (their sum is taken before that).  bf16
+// has the exponents of 32 bits: a weight is off by half a step of 2^-8 at most, however small.  fp16 ends at 2^16, has
+// fewer bits below 2^-14 and none below 2^-25, which a long list of light tokens beside one heavy token can
+// notice (131072 tokens 17 nats below it: 0.0078 instead of 0.0054).  So its base lies kLift below the maximum: the
+// heaviest weight is at most 2^(kLift + kGrowth) = 2^15, and weights keep all bits down to 2^-21 of the base's, and lose at most
+// 2^-32 of it each.
+template <typename T> __device__ constexpr float kLift = 0.f;
+template <> __device__ constexpr float kLift<__half> = 7.f;
 constexpr long long kWaitCycles = 2000000000;   // a wait gives up after a second
 
 __device__ __forceinline__ void mbar_init(uint64_t *b, int count)

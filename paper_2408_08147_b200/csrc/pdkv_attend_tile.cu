@@ -11,9 +11,8 @@
 // tile for the softmax, one that issues the matrix instructions, one that issues the loads (TMA boxes of one
 // page, 64 dims and the 128-byte swizzle that the matrix instructions expect).
 //
-// O is rescaled only when a row's maximum grew by more than 2^8 since the last time: the weights stay below
-// 2^8, where 16-bit and 32-bit floating point lose nothing.  Maxima and sums are 32 bits, the sums taken
-// before the weights are rounded.
+// O is rescaled only when a row's maximum grew by more than 2^8 since the last time.  Bases and sums are 32 bits, the sums
+// taken before the weights are rounded (see kLift).
 //
 // Bound by the tensor core and by the chain S, P, O of a row tile: 256 rows against 128 tokens of 128 dims take it
 // 3024 cycles (125 for 16 dims of Q K^T, whose two operands come from shared memory at 64 bytes a cycle, 64 for 16 tokens
@@ -456,7 +455,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int k = 8; k < kTileTokens / 2; ++k) tops[k % 8] = max3(tops[k % 8], v[2 * k], v[2 * k + 1]);
                     float top = max3(max3(max3(tops[0], tops[1], tops[2]), tops[3], tops[4]), tops[5], fmaxf(tops[6], tops[7]));
-                    top = top == -INFINITY ? top : top * scale;
+                    top = top == -INFINITY ? top : fmaf(top, scale, -kLift<T>);
                     if (__any_sync(~0u, top > m + kGrowth || (m == -INFINITY && top > m))) {
                         const float new_m = fmaxf(m, top), f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
                         l *= f;

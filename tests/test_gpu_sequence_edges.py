@@ -3,7 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2408_08147_b200.sequences import CacheSession
+from paper_2408_08147_b200.sequences import CacheSession, Sequences
+from paper_2408_08147_b200.workloads import LAYER_MAJOR, Geometry
 from test_gpu_sequences import Evict, Setup
 
 pytestmark = pytest.mark.gpu
@@ -76,3 +77,34 @@ def test_outputs_of_eviction_on_another_stream():
         a.evict(b, scores, 30)
         torch.cuda.synchronize()
         not_given_away(lambda side: a.evict(b, scores, 30, stream=side.cuda_stream))
+
+
+@pytest.mark.parametrize("G", [2, 40])                  # warp kernel, tile kernel
+@pytest.mark.parametrize("below", [11.0, 14.0, 17.0, 18.5])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_many_light_tokens_beside_a_heavy_one(dtype, below, G):
+    """A heavy token without a value before 40000 tokens that lie `below` nats under it and have a value of one.  Many
+    sequences share the blocks, so that no list is cut: all tokens meet the heavy one's base."""
+    n, D, n_seq = 40000, 64, 320
+    dt = {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+    geom = Geometry(LAYER_MAJOR, 1, 1, D, 2, 64, n // 64)
+    pool = torch.zeros(geom.shape(), dtype=dt, device="cuda")     # [layer][K/V][block][head][token][dim]
+    pool[0, 0, :, 0, :, 0] = -2 * below                           # q 4, scale 1/8: logits of -below (exact in both types)
+    pool[0, 1] = 1.0
+    pool[0, :, 0, 0, 5] = 0.0
+    q = torch.zeros(n_seq, 1, G, D, dtype=dt, device="cuda")
+    q[..., 0] = 4.0
+    light = (n - 1) * np.exp(-below)
+    want = light / (1 + light)
+    seqs = Sequences([n] * n_seq, n // 64 * np.arange(n_seq + 1), np.tile(np.arange(n // 64), n_seq))
+    with CacheSession(geom, pool, seqs, num_q_heads=G, dtype=dt) as c:
+        items = c.items()
+        assert set(items["kernel"]) == {1 if G == 40 else 0} and items["tok_end"].max() > 20000
+        out, _ = c.attend(0, q)
+    # A light weight is rounded once, by half a step, and fp16 loses 2^-32 of the heaviest weight at most; logits are exact but
+    # for 4 roundings of 18.5 nats (2^-24 each) and the exponential (2^-22); sums of n terms in 32 bits (the tensor cores cut: 2^-23
+    # of the sum each, in steps of 16 tokens); the result is rounded once more.
+    half = torch.finfo(dt).eps / 2
+    tol = 1.01 * want * (2 * half + 4 * 18.5 * 2.0 ** -23 + 2.0 ** -22 + 2 * (n / 16 + 64) * 2.0 ** -23) + n * 2.0 ** -32 + 2.0 ** -25
+    off = (out.double() - want).abs().max().item()
+    assert off <= tol
