@@ -330,7 +330,8 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
         if (d->q_tokens < 1 || (d->dtype != PDKV_DTYPE_BF16 && d->dtype != PDKV_DTYPE_FP16)) return PDKV_ERR_INVALID_ARG;
         if (d->num_q_heads % g.num_kv_heads || g.elem_bytes != 2 || g.head_dim % 8 || g.head_dim > 256) return PDKV_ERR_GEOMETRY;
         // rows of one sequence and head, and rows behind one prefix, are counted in 32 bits
-        if ((int64_t)d->q_tokens * d->num_q_heads * std::max(1, d->n_seq) > (int64_t)1 << 30) return PDKV_ERR_INVALID_ARG;
+        const int64_t rows = (int64_t)d->q_tokens * d->num_q_heads, most = (int64_t)1 << 30;
+        if (rows > most / std::max(1, d->n_seq)) return PDKV_ERR_INVALID_ARG;
     }
     const int64_t B = g.block_tokens;
     try {
