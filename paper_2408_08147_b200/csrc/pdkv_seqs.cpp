@@ -92,11 +92,13 @@ int64_t rows_span(int64_t len, const int64_t *stride, const int64_t *n, int axes
 int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int32_t n, int64_t B, int64_t NB)
 {
     if (!off || !len) return PDKV_ERR_INVALID_ARG;
+    // all offsets before the first id: a caller who knows where the table ends compares it with off[n]
     if (off[0] < 0) return PDKV_ERR_TABLE;
+    for (int32_t r = 0; r < n; ++r)
+        if (off[r + 1] < off[r]) return PDKV_ERR_TABLE;
     for (int32_t r = 0; r < n; ++r) {
         if (len[r] < 0) return PDKV_ERR_INVALID_ARG;
         if (len[r] > kMaxTokens) return PDKV_ERR_LIMIT;
-        if (off[r + 1] < off[r]) return PDKV_ERR_TABLE;
         const int64_t need = ((int64_t)len[r] + B - 1) / B;
         if (off[r + 1] - off[r] < need) return PDKV_ERR_TABLE;
         if (need && !tbl) return PDKV_ERR_INVALID_ARG;
