@@ -467,8 +467,9 @@ typedef struct {
 int pdkv_attend_scratch(const pdkv_seqs *seqs, int with_scores, size_t *bytes);
 /* Enqueues only (no allocation, copy or synchronisation): after one call outside capture it
  * can be recorded into a CUDA graph.  q and out are 16-byte aligned, their strides multiples
- * of 8 elements; rows of out and of scores_out must not overlap; out must not overlap q, the
- * pool or the scratch.  The same call gives the same bits every time.
+ * of 8 elements; rows of out and of scores_out must not overlap.  What the call writes (out, lse,
+ * scores_out, scratch) must not overlap what it reads (q, the pool, seq_len, scores_in unless it is scores_out, the
+ * handle's workspace) nor one another; rows of one buffer that lie between one another are no overlap.  The same call gives the same bits every time.
  * Errors: INVALID_ARG, BUFFER_TOO_SMALL (scratch), LIMIT (more blocks than a launch takes),
  * CUDA. */
 int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, void *scratch, size_t scratch_bytes,

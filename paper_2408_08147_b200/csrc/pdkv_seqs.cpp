@@ -53,6 +53,52 @@ bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
     return a_bytes && b_bytes && a0 < b0 + b_bytes && b0 < a0 + a_bytes;
 }
 
+// Rows of memory of one length at base + sum of i * stride (none where base is null).
+struct Rows {
+    uintptr_t base = 0;
+    int64_t bytes = 0, stride[3] = {0, 0, 0}, n[3] = {1, 1, 1};
+    Rows() = default;
+    Rows(const void *p, int64_t row_bytes) : base(reinterpret_cast<uintptr_t>(p)), bytes(p ? row_bytes : 0) {}
+    Rows(const void *p, int64_t row_len, int64_t elem, const int64_t *s, const int64_t *count, int axes) : Rows(p, row_len * elem)
+    {
+        for (int i = 0; i < axes; ++i) {
+            n[i] = count[i];
+            stride[i] = count[i] > 1 ? s[i] * elem : 0;
+        }
+    }
+    int64_t span() const
+    {
+        if (bytes <= 0 || n[0] <= 0 || n[1] <= 0 || n[2] <= 0) return 0;
+        return bytes + stride[0] * (n[0] - 1) + stride[1] * (n[1] - 1) + stride[2] * (n[2] - 1);
+    }
+    std::vector<uintptr_t> starts() const
+    {
+        std::vector<uintptr_t> at;
+        at.reserve((size_t)(n[0] * n[1] * n[2]));
+        for (int64_t i = 0; i < n[0]; ++i)
+            for (int64_t j = 0; j < n[1]; ++j)
+                for (int64_t k = 0; k < n[2]; ++k) at.push_back(base + i * stride[0] + j * stride[1] + k * stride[2]);
+        std::sort(at.begin(), at.end());
+        return at;
+    }
+};
+
+// Do a row of `a` and one of `b` share a byte?  Row by row only where their spans meet (views of one buffer).
+bool meet(const Rows &a, const Rows &b)
+{
+    const int64_t na = a.span(), nb = b.span();
+    if (na == 0 || nb == 0 || a.base >= b.base + nb || b.base >= a.base + na) return false;
+    const std::vector<uintptr_t> x = a.starts(), y = b.starts();
+    for (size_t i = 0, j = 0; i < x.size() && j < y.size();) {
+        if (x[i] < y[j] + b.bytes && y[j] < x[i] + a.bytes) return true;
+        if (x[i] + a.bytes <= y[j])
+            ++i;
+        else
+            ++j;
+    }
+    return false;
+}
+
 bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 int32_t log2_of(int32_t n)
@@ -476,6 +522,7 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             put(o_segs, s->segs.data(), s->segs.size() * sizeof(AttnSeg));
             put(o_units, s->units.data(), s->units.size() * sizeof(AttnUnit));
             put(o_seqs, s->seqs.data(), s->seqs.size() * sizeof(AttnSeq));
+            s->dev_bytes = bytes;
             pdkv::DeviceGuard guard(s->device);
             if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
             if (workspace) {
@@ -591,11 +638,6 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
             for (int i = 0; i < 3; ++i)
                 if (rows[i] > 1 && (a->q_stride[i] % 8 || a->out_stride[i] % 8 || a->q_stride[i] < 0)) return PDKV_ERR_INVALID_ARG;
             if (!rows_apart(D, a->out_stride, rows, 3)) return PDKV_ERR_INVALID_ARG;
-            const size_t out_span = 2 * (size_t)rows_span(D, a->out_stride, rows, 3);
-            const size_t q_span = 2 * (size_t)rows_span(D, a->q_stride, rows, 3);
-            if (ranges_overlap(a->out, out_span, s->pool.base, pdkv_pool_bytes(&s->pool.d)) || ranges_overlap(a->out, out_span, a->q, q_span) ||
-                ranges_overlap(a->out, out_span, scratch, scratch_bytes))
-                return PDKV_ERR_INVALID_ARG;
         }
         if (a->lse && !aligned(a->lse, 4)) return PDKV_ERR_INVALID_ARG;
         if (a->seq_len && !aligned(a->seq_len, 4)) return PDKV_ERR_INVALID_ARG;
@@ -610,13 +652,25 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
                 for (int i = 0; i < 2; ++i)
                     if (n[i] > 1 && (a->scores_in_stride[i] < 0 || (same && a->scores_in_stride[i] != a->scores_out_stride[i])))
                         return PDKV_ERR_INVALID_ARG;
-                if (!same && ranges_overlap(a->scores_in, 4 * (size_t)rows_span(s->max_len, a->scores_in_stride, n, 2), a->scores_out,
-                                            4 * (size_t)rows_span(s->max_len, a->scores_out_stride, n, 2)))
-                    return PDKV_ERR_INVALID_ARG;
             }
         }
         const ScratchLayout l = scratch_layout(s, scores);
         if (l.bytes && (!scratch || !aligned(scratch, 32))) return PDKV_ERR_INVALID_ARG;
+        if (s->n_seq > 0) {
+            // what the call writes lies apart from what it reads and from one another
+            const int64_t heads[2] = {s->n_seq, s->pool.d.num_kv_heads};
+            const Rows written[4] = {Rows(a->out, D, 2, a->out_stride, rows, 3), Rows(a->lse, 4 * rows[0] * rows[1] * rows[2]),
+                                     Rows(a->scores_out, s->max_len, 4, a->scores_out_stride, heads, 2), Rows(scratch, (int64_t)std::min(scratch_bytes, l.bytes))};
+            const Rows read[5] = {Rows(a->q, D, 2, a->q_stride, rows, 3), Rows(s->pool.base, (int64_t)pdkv_pool_bytes(&s->pool.d)),
+                                  Rows(a->seq_len, 4 * rows[0]), Rows(s->dev_mem, (int64_t)s->dev_bytes),
+                                  Rows(a->scores_in, s->max_len, 4, a->scores_in_stride, heads, 2)};
+            for (int i = 0; i < 4; ++i) {
+                for (int j = 0; j < i; ++j)
+                    if (meet(written[i], written[j])) return PDKV_ERR_INVALID_ARG;
+                for (int j = 0; j < 5; ++j)
+                    if (!(i == 2 && j == 4 && a->scores_in == a->scores_out) && meet(written[i], read[j])) return PDKV_ERR_INVALID_ARG;
+            }
+        }
         if (scratch_bytes < l.bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
         if (!s->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0) return PDKV_OK;

@@ -156,6 +156,7 @@ struct pdkv_seqs {
     int32_t most_parts = 0;      // of a row behind one segment
     // device arrays
     void *dev_mem = nullptr;
+    size_t dev_bytes = 0;
     bool owns_dev_mem = true;
     unsigned long long *d_status = nullptr;
     const int32_t *d_tbl = nullptr, *d_members = nullptr;

@@ -22,3 +22,42 @@ def test_offsets_are_checked_before_ids_are_read():
     off, tbl = csr([40, 7], 16)
     assert status(B.pdkv_seqs_create, pool(), [40, 7], off, tbl, prefix_len=[160, 0], prefix_tbl_off=np.array([0, 10, 5], np.int64), prefix_tbl=None,
                   seq_prefix=[0, 1], num_q_heads=8, q_tokens=1) == B.PDKV_ERR_TABLE
+
+
+def test_what_attention_writes_lies_apart():
+    """out, lse, scores_out and scratch on one another and on q, pool, lengths and scores_in: refused.  The scratch is a byte
+    short, which is noticed after that."""
+    p = pool()
+    s, _ = create(p, [40, 7], q_tokens=2)
+    n = B.pdkv_attend_scratch(s, True) - 1
+    rows, scores = 2 * 2 * 2 * 8 * 64, 4 * (160 + 3 * 40 + 40)
+    at = {k: (FAKE + (i << 40), size) for i, (k, size) in enumerate(
+        dict(pool=B.pdkv_pool_bytes(B.make_desc(0, 2, 4, 64, 2, 16, 400)), q=rows, out=rows, lse=4 * 2 * 2 * 8, scores_out=scores, scores_in=scores,
+             seq_len=8, scratch=n).items())}
+
+    def call(**over):
+        kw = {k: v for k, (v, _) in at.items() if k not in ("pool", "scratch")}
+        kw.update(scores_out_stride=[160, 40], scores_in_stride=[160, 40])
+        kw.update(over)
+        scratch = kw.pop("scratch", at["scratch"][0])
+        return status(B.pdkv_attend, s, 0, args(Q=2, **kw), scratch, n)
+
+    assert call() == B.PDKV_ERR_BUFFER_TOO_SMALL
+    assert call(scores_in=at["scores_out"][0]) == B.PDKV_ERR_BUFFER_TOO_SMALL
+    for w in ("out", "lse", "scores_out", "scratch"):
+        for r in at:
+            if r == w or (w, r) == ("scores_out", "scores_in"):
+                continue
+            for spot in (at[r][0], at[r][0] + at[r][1] - 32 if r != "seq_len" else at[r][0]):   # its first and its last bytes
+                spot -= spot % 32
+                assert call(**{w: spot}) == B.PDKV_ERR_INVALID_ARG, (w, r)
+            assert call(**{w: at[r][0] + (at[r][1] + 31) // 32 * 32}) == B.PDKV_ERR_BUFFER_TOO_SMALL, (w, r)   # right behind it
+    assert call(scores_out=at["scores_in"][0] + 32) == B.PDKV_ERR_INVALID_ARG
+    # views of one buffer that lie between one another: q and out, scores and their input
+    buf = at["q"][0]
+    wide = dict(q_stride=[4 * 512, 2 * 512, 64], out_stride=[4 * 512, 2 * 512, 64])
+    assert call(out=buf + 2 * 512, **wide) == B.PDKV_ERR_BUFFER_TOO_SMALL
+    assert call(out=buf + 2 * 448, **wide) == B.PDKV_ERR_INVALID_ARG
+    both = dict(scores_in_stride=[320, 80], scores_out_stride=[320, 80])
+    assert call(scores_in=at["scores_out"][0] + 160, **both) == B.PDKV_ERR_BUFFER_TOO_SMALL
+    assert call(scores_in=at["scores_out"][0] + 156, **both) == B.PDKV_ERR_INVALID_ARG
