@@ -502,7 +502,7 @@ typedef struct {
 
 /* Enqueues only (recordable as pdkv_attend()); no scratch.  `kept` must not overlap the scores.
  * Errors: INVALID_ARG, GEOMETRY (the pools disagree), TABLE (dst sequences too short, or a dst
- * block used twice), LIMIT, CUDA. */
+ * block used twice), LIMIT (a budget or kept_scores_len above 2^30, more rows than a launch takes), CUDA. */
 int pdkv_evict(const pdkv_seqs *seqs, const pdkv_seqs *dst, int layer_begin, int layer_end, const pdkv_evict_args *args,
                void *stream);
 

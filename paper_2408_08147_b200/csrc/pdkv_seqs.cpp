@@ -795,6 +795,8 @@ int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int laye
                     return PDKV_ERR_INVALID_ARG;
             }
         }
+        // the kernels count tokens and entries of a row in 32 bits
+        if (a->budget > kMaxTokens || (a->kept_scores && a->kept_scores_len > kMaxTokens)) return PDKV_ERR_LIMIT;
         if (!s->dev_mem || !t->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0 || layers == 0) return PDKV_OK;
         if ((double)layers * s->n_seq * x.num_kv_heads * 16 > 2e9) return PDKV_ERR_LIMIT;   // blocks of a kernel

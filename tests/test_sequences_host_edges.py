@@ -61,3 +61,28 @@ def test_what_attention_writes_lies_apart():
     both = dict(scores_in_stride=[320, 80], scores_out_stride=[320, 80])
     assert call(scores_in=at["scores_out"][0] + 160, **both) == B.PDKV_ERR_BUFFER_TOO_SMALL
     assert call(scores_in=at["scores_out"][0] + 156, **both) == B.PDKV_ERR_INVALID_ARG
+
+
+def evict_args(**over):
+    a = B.pdkv_evict_args()
+    a.budget, a.sink, a.recent = 16, 2, 3
+    a.scores, a.kept, a.kept_scores = FAKE + (1 << 41), FAKE + (2 << 41), FAKE + (3 << 41)
+    a.scores_stride[:] = [400, 200, 50]
+    a.kept_scores_stride[:] = [400, 200, 50]
+    a.kept_scores_len = 16
+    for k, v in over.items():
+        if k.endswith("stride"):
+            getattr(a, k)[:] = v
+        else:
+            setattr(a, k, v)
+    return a
+
+
+def test_budgets_that_32_bit_indices_do_not_hold():
+    """A kernel's index runs a block's threads past the last entry of a row of the budget: at 2^31 - 1 it would wrap."""
+    s = create(pool(), [40, 7], Hq=0)[0]
+    for over in (dict(budget=2 ** 31 - 1, kept_scores_len=40), dict(budget=2 ** 30 + 1, kept_scores_len=40),
+                 dict(kept_scores_len=2 ** 31 - 1, kept_scores_stride=[1 << 36, 1 << 34, 1 << 32]),
+                 dict(kept_scores_len=2 ** 30 + 1, kept_scores_stride=[1 << 36, 1 << 34, 1 << 32])):
+        assert status(B.pdkv_evict, s, s, 0, 2, evict_args(kept_scores=FAKE + (1 << 45), **over)) == B.PDKV_ERR_LIMIT
+    assert status(B.pdkv_evict, s, s, 0, 2, evict_args(budget=2 ** 30, kept_scores=0)) == B.PDKV_ERR_INVALID_ARG   # (a host-only handle)
