@@ -500,7 +500,9 @@ typedef struct {
     int32_t *new_len;              /* device [n_seq]: min(len, budget), or NULL.  May equal seq_len */
 } pdkv_evict_args;
 
-/* Enqueues only (recordable as pdkv_attend()); no scratch.  `kept` must not overlap the scores.
+/* Enqueues only (recordable as pdkv_attend()); no scratch.  What the call writes (kept, kept_scores, new_len, the pool of dst)
+ * must not overlap what it reads (scores, seq_len, either pool, the handles' workspaces) nor one another, but for
+ * the three pairs that may be equal: dst, kept_scores, new_len.
  * Errors: INVALID_ARG, GEOMETRY (the pools disagree), TABLE (dst sequences too short, or a dst
  * block used twice), LIMIT (a budget or kept_scores_len above 2^30, more rows than a launch takes), CUDA. */
 int pdkv_evict(const pdkv_seqs *seqs, const pdkv_seqs *dst, int layer_begin, int layer_end, const pdkv_evict_args *args,

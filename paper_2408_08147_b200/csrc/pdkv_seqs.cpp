@@ -126,15 +126,6 @@ bool rows_apart(int64_t len, const int64_t *stride, const int64_t *n, int axes)
     return true;
 }
 
-// Bytes from the first to past the last element of such rows.
-int64_t rows_span(int64_t len, const int64_t *stride, const int64_t *n, int axes)
-{
-    int64_t span = len;
-    for (int i = 0; i < axes; ++i)
-        if (n[i] > 0) span += stride[i] * (n[i] - 1);
-    return span;
-}
-
 int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int32_t n, int64_t B, int64_t NB)
 {
     if (!off || !len) return PDKV_ERR_INVALID_ARG;
@@ -775,25 +766,34 @@ int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int laye
         const int64_t layers = layer_end - layer_begin;
         const int64_t n[3] = {layers, s->n_seq, x.num_kv_heads};
         const int64_t top = std::min(s->max_len, a->budget);
-        if (s->n_seq > 0 && layers > 0 && s->max_len > 0) {
-            if (!a->scores || !a->kept || !aligned(a->scores, 4) || !aligned(a->kept, 4)) return PDKV_ERR_INVALID_ARG;
+        if (s->n_seq > 0 && layers > 0) {
+            if (!a->kept || (!a->scores && s->max_len > 0)) return PDKV_ERR_INVALID_ARG;
+            if (!aligned(a->scores, 4) || !aligned(a->kept, 4) || !aligned(a->kept_scores, 4) || !aligned(a->seq_len, 4) || !aligned(a->new_len, 4))
+                return PDKV_ERR_INVALID_ARG;
             for (int i = 0; i < 3; ++i)
                 if (n[i] > 1 && a->scores_stride[i] < 0) return PDKV_ERR_INVALID_ARG;
-            const size_t kept_bytes = 4 * (size_t)layers * (size_t)s->n_seq * (size_t)x.num_kv_heads * (size_t)a->budget;
-            if (ranges_overlap(a->kept, kept_bytes, a->scores, 4 * (size_t)rows_span(s->max_len, a->scores_stride, n, 3)) ||
-                (a->kept_scores && ranges_overlap(a->kept, kept_bytes, a->kept_scores,
-                                                  4 * (size_t)rows_span(a->kept_scores_len, a->kept_scores_stride, n, 3))))
-                return PDKV_ERR_INVALID_ARG;
+            const bool same = a->kept_scores && a->kept_scores == a->scores;
             if (a->kept_scores) {
-                if (!aligned(a->kept_scores, 4) || a->kept_scores_len < top) return PDKV_ERR_INVALID_ARG;
-                if (!rows_apart(a->kept_scores_len, a->kept_scores_stride, n, 3)) return PDKV_ERR_INVALID_ARG;
-                const bool same = a->kept_scores == a->scores;
+                if (a->kept_scores_len < top || !rows_apart(a->kept_scores_len, a->kept_scores_stride, n, 3)) return PDKV_ERR_INVALID_ARG;
                 for (int i = 0; i < 3; ++i)
                     if (same && n[i] > 1 && a->scores_stride[i] != a->kept_scores_stride[i]) return PDKV_ERR_INVALID_ARG;
-                if (!same && ranges_overlap(a->scores, 4 * (size_t)rows_span(s->max_len, a->scores_stride, n, 3), a->kept_scores,
-                                            4 * (size_t)rows_span(a->kept_scores_len, a->kept_scores_stride, n, 3)))
-                    return PDKV_ERR_INVALID_ARG;
             }
+            // what the call writes lies apart from what it reads and from one another
+            const Rows written[3] = {Rows(a->kept, 4 * layers * s->n_seq * x.num_kv_heads * a->budget), Rows(a->kept_scores, a->kept_scores_len, 4, a->kept_scores_stride, n, 3),
+                                     Rows(a->new_len, 4 * (int64_t)s->n_seq)};
+            const Rows read[6] = {Rows(a->scores, s->max_len, 4, a->scores_stride, n, 3), Rows(a->seq_len, 4 * (int64_t)s->n_seq),
+                                  Rows(s->pool.base, (int64_t)pdkv_pool_bytes(&x)), Rows(t->pool.base, (int64_t)pdkv_pool_bytes(&y)),
+                                  Rows(s->dev_mem, (int64_t)s->dev_bytes), Rows(t->dev_mem, (int64_t)t->dev_bytes)};
+            for (int i = 0; i < 3; ++i) {
+                for (int j = 0; j < i; ++j)
+                    if (meet(written[i], written[j])) return PDKV_ERR_INVALID_ARG;
+                for (int j = 0; j < 6; ++j) {
+                    if ((i == 1 && j == 0 && same) || (i == 2 && j == 1 && a->new_len == a->seq_len)) continue;   // updated where they stand
+                    if (meet(written[i], read[j])) return PDKV_ERR_INVALID_ARG;
+                }
+            }
+            for (int j = 0; j < 2; ++j)   // (the moved rows)
+                if (meet(read[j], read[3])) return PDKV_ERR_INVALID_ARG;
         }
         // the kernels count tokens and entries of a row in 32 bits
         if (a->budget > kMaxTokens || (a->kept_scores && a->kept_scores_len > kMaxTokens)) return PDKV_ERR_LIMIT;

@@ -86,3 +86,55 @@ def test_budgets_that_32_bit_indices_do_not_hold():
                  dict(kept_scores_len=2 ** 30 + 1, kept_scores_stride=[1 << 36, 1 << 34, 1 << 32])):
         assert status(B.pdkv_evict, s, s, 0, 2, evict_args(kept_scores=FAKE + (1 << 45), **over)) == B.PDKV_ERR_LIMIT
     assert status(B.pdkv_evict, s, s, 0, 2, evict_args(budget=2 ** 30, kept_scores=0)) == B.PDKV_ERR_INVALID_ARG   # (a host-only handle)
+
+
+def test_what_eviction_writes_lies_apart():
+    """kept, kept_scores and new_len on one another, on scores, lengths and pools: refused; in place: taken.  The budget is over
+    the limit, which is noticed after that."""
+    def make(base):
+        return create(pool(H=4, base=base), [40, 7], Hq=0)[0]
+
+    far, budget = 1 << 44, 2 ** 30 + 1
+    s, d = make(FAKE), make(FAKE + far)
+    nbytes, scores = B.pdkv_pool_bytes(B.make_desc(0, 2, 4, 64, 2, 16, 400)), 4 * (400 + 200 + 3 * 50 + 40)
+    at = {k: (FAKE + (i << 41), size) for i, (k, size) in enumerate(
+        dict(src=nbytes, scores=scores, kept_scores=scores, new_len=8, seq_len=8, kept=4 * 2 * 2 * 4 * budget).items())}
+    at["dst"] = (FAKE + far, nbytes)
+
+    def call(dst=d, **over):
+        kw = {k: v for k, (v, _) in at.items() if k not in ("src", "dst")}
+        kw.update(budget=budget, kept_scores_len=40)
+        kw.update(over)
+        return status(B.pdkv_evict, s, dst, 0, 2, evict_args(**kw))
+
+    assert call() == B.PDKV_ERR_LIMIT and call(dst=s) == B.PDKV_ERR_LIMIT
+    assert call(kept_scores=at["scores"][0], new_len=at["seq_len"][0]) == B.PDKV_ERR_LIMIT
+    assert call(kept_scores=0, new_len=0, seq_len=0) == B.PDKV_ERR_LIMIT
+    for w in ("kept", "kept_scores", "new_len"):
+        for r in at:
+            if r == w or (w, r) in (("kept_scores", "scores"), ("new_len", "seq_len")):
+                continue
+            assert call(**{w: at[r][0]}) == B.PDKV_ERR_INVALID_ARG, (w, r)
+            assert call(**{w: at[r][0] + at[r][1] - 4}) == B.PDKV_ERR_INVALID_ARG, (w, r)
+            assert call(**{w: at[r][0] + (at[r][1] + 3) // 4 * 4}) == B.PDKV_ERR_LIMIT, (w, r)
+    assert call(kept_scores=at["scores"][0] + 4) == B.PDKV_ERR_INVALID_ARG and call(new_len=at["seq_len"][0] + 4) == B.PDKV_ERR_INVALID_ARG
+    for r in ("scores", "seq_len"):
+        assert call(**{r: at["dst"][0] + 64}) == B.PDKV_ERR_INVALID_ARG, r
+    # rows of one buffer that lie between one another
+    wide = dict(scores_stride=[800, 400, 100], kept_scores_stride=[800, 400, 100])
+    assert call(kept_scores=at["scores"][0] + 4 * 40, **wide) == B.PDKV_ERR_LIMIT
+    assert call(kept_scores=at["scores"][0] + 4 * 39, **wide) == B.PDKV_ERR_INVALID_ARG
+
+
+def test_unaligned_buffers_of_eviction():
+    """Of every buffer, and also where no sequence has a token."""
+    for lens in ([40, 7], [0, 0]):
+        s = create(pool(H=4), lens, Hq=0)[0]
+        for over in (dict(scores=FAKE + (1 << 41) + 2), dict(kept=FAKE + (2 << 41) + 1), dict(kept_scores=FAKE + (3 << 41) + 2),
+                     dict(seq_len=FAKE + (4 << 41) + 2), dict(new_len=FAKE + (5 << 41) + 2), dict(kept=0),
+                     dict(kept_scores_len=-1), dict(kept_scores_stride=[400, 200, 10])):
+            over = {"budget": 2 ** 30 + 1, "kept_scores": 0, **over}     # (over the limit: noticed after that)
+            if "kept_scores_len" in over or "kept_scores_stride" in over:
+                over["kept_scores"] = FAKE + (1 << 45)
+            assert status(B.pdkv_evict, s, s, 0, 2, evict_args(**over)) == B.PDKV_ERR_INVALID_ARG, (lens, over)
+    assert status(B.pdkv_evict, s, s, 0, 2, evict_args(budget=2 ** 30 + 1, scores=0, kept_scores=0)) == B.PDKV_ERR_LIMIT
