@@ -441,7 +441,7 @@ int pdkv_seqs_destroy(pdkv_seqs *seqs);
  * under 2^-21 of a row's largest by up to 2^-32 of that).  A row with
  * nothing to attend to (or whose every logit is -infinity) gives zeros and lse =
  * -infinity.  Cached rows past a sequence's length are never read into a result,
- * whatever they hold. */
+ * whatever they hold, nor are tokens into the results of queries that do not attend to them. */
 typedef struct {
     const void *q;                 /* device [n_seq][q_tokens][num_q_heads][head_dim] */
     int64_t q_stride[3];           /* elements between sequences, query tokens, heads */

@@ -120,6 +120,49 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// Values that are not finite.  A row that does not see a token gives it the weight 0, but 0 * infinity is NaN.  So the
+// 16-byte pieces of V that hold such a value, among the tokens that some of an item's rows do not see, become zero before the product,
+// and what they would have added is added to the rows that see them once their sums are complete.  (Tokens past the end of a sequence, which
+// nobody sees, become zero as well.)
+//
+// Is one of eight 16-bit numbers infinite or NaN: an exponent of ones, which carries into the sign's place?
+template <typename T> __device__ __forceinline__ bool any_not_finite(const uint4 &x);
+template <> __device__ __forceinline__ bool any_not_finite<__nv_bfloat16>(const uint4 &x)
+{
+    auto carry = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };
+    return ((carry(x.x) | carry(x.y) | carry(x.z) | carry(x.w)) & 0x80008000u) != 0;
+}
+template <> __device__ __forceinline__ bool any_not_finite<__half>(const uint4 &x)
+{
+    auto carry = [](uint32_t w) { return (w & 0x7c007c00u) + 0x04000400u; };
+    return ((carry(x.x) | carry(x.y) | carry(x.z) | carry(x.w)) & 0x80008000u) != 0;
+}
+// What such pieces of own tokens [from, to) add to dims [d, d + 4) of a row: sum of 2^(z - base) v.  Rare, and slow: one
+// thread, from the pool.
+template <typename T>
+__device__ __forceinline__ float4 left_out(const AttnParams &p, const T *q, int64_t tbl, int head, int from, int to, float base, int d)
+{
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (base == -INFINITY) return sum;   // a row without weights
+#pragma unroll 1
+    for (int t = from; t < to; ++t) {
+        const int block = t / p.pool.block_tokens;
+        const char *row = p.pool.base + 2 * (int64_t)p.layer * p.pool.lc_stride + head * p.pool.head_stride +
+                          p.tbl[tbl + block] * p.pool.block_stride + (int64_t)(t - block * p.pool.block_tokens) * p.pool.tok_stride;
+        const T *k = reinterpret_cast<const T *>(row), *v = reinterpret_cast<const T *>(row + p.pool.lc_stride);
+        if (!any_not_finite<T>(*reinterpret_cast<const uint4 *>(v + d / 8 * 8))) continue;
+        float z = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < p.D; ++i) z = fmaf(static_cast<float>(q[i]), static_cast<float>(k[i]), z);
+        const float w = exp2f(fmaf(z, p.scale_log2, -base));
+        sum.x = fmaf(w, static_cast<float>(v[d]), sum.x);
+        sum.y = fmaf(w, static_cast<float>(v[d + 1]), sum.y);
+        sum.z = fmaf(w, static_cast<float>(v[d + 2]), sum.z);
+        sum.w = fmaf(w, static_cast<float>(v[d + 3]), sum.w);
+    }
+    return sum;
+}
+
 // 2^x, off by 2 units in the last place at most; 0 for -infinity.
 __device__ __forceinline__ float pow2(float x)
 {

@@ -142,6 +142,20 @@ __device__ __forceinline__ void commit(uint64_t *b)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
+// Barrier of `threads` threads; true for all of them where one has something.
+__device__ __forceinline__ bool any_of(int barrier, int threads, bool mine)
+{
+    uint32_t any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n barrier.cta.red.or.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(any) : "r"(barrier), "r"(threads), "r"((uint32_t)mine) : "memory");
+    return any != 0;
+}
+// (a call: the code is not there eight times)
+template <typename T>
+__device__ __noinline__ float4 left_out_call(const AttnParams &p, const T *q, int64_t tbl, int head, int from, int to, float base, int d)
+{
+    return left_out<T>(p, q, tbl, head, from, to, base, d);
+}
 // What every role has to know about an item.
 struct Work {
     AttnItem it;
@@ -194,7 +208,7 @@ template <typename T, int DP> __device__ __forceinline__ void fetch_q(const Attn
 }  // namespace
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p)
+__global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
     using G = TileShape<DP>;
     extern __shared__ char raw[];
@@ -414,12 +428,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const bool live = row < w.it.rows, own = w.it.seq >= 0;
             const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             float m = -INFINITY, l = 0.f;
+            const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;   // tokens before this one
+            const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;              // the same of every row
+            bool wild = false;   // pieces of V were left out
             if (count > 0) {
                 if (!q_there) fetch_q<T, DP>(p, w, t, q_at);
                 if (!q_there || !q_done) finish_q();
                 q_there = q_done = false;
-                const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;
-                const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;
                 for (int j = 0; j < count; ++j) {
                     const int t0 = w.it.tok0 + w.tile(t, j) * kTileTokens;
                     const bool masked = t0 + kTileTokens > safe;
@@ -427,19 +442,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     s_phase ^= 1;
                     __syncwarp();
                     fence_after();
-                    if ((t == 0 || !w.pair) && t0 + kTileTokens > w.limit) {
-                        // rows of V past the end may hold anything, and 0 * NaN is NaN: they become zero
-                        const uint32_t v = n0 + w.order(1, w.tile(t, j));
-                        mbar_wait(&bar.full[v % G::kSlots], v / G::kSlots & 1, dead, p.status);
-                        if (t0 + r >= w.limit) {
-                            char *zero = smem + 2 * G::kOperand + v % G::kSlots * G::kOperand + r * 128;
-#pragma unroll
-                            for (int s = 0; s < G::kSubs; ++s)
-#pragma unroll
-                                for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4 *>(zero + s * G::kSub + c * 16) = make_uint4(0, 0, 0, 0);
-                        }
-                        fence_async_smem();
-                    }
                     float v[kTileTokens];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
@@ -491,6 +493,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                         }
                         tmem_store16(s_at + 16 * c, packed);
                         if (c == 1) {
+                            if (masked && (t == 0 || !w.pair)) {
+                                // rows of V past the end may hold anything; and see left_out
+                                const uint32_t x = n0 + w.order(1, w.tile(t, j));
+                                mbar_wait(&bar.full[x % G::kSlots], x / G::kSlots & 1, dead, p.status);
+                                if (t0 + r >= safe) {
+                                    const bool past = t0 + r >= w.limit;
+                                    char *row = smem + 2 * G::kOperand + x % G::kSlots * G::kOperand + r * 128;
+#pragma unroll 2
+                                    for (int i = 0; i < 8 * G::kSubs; ++i) {
+                                        uint4 *at = reinterpret_cast<uint4 *>(row + i / 8 * G::kSub + (i + r) % 8 * 16);
+                                        if (past || any_not_finite<T>(*at)) {
+                                            *at = make_uint4(0, 0, 0, 0);
+                                            wild = wild || !past;
+                                        }
+                                    }
+                                }
+                                fence_async_smem();
+                            }
                             tmem_store_wait();
                             fence_before();
                             __syncwarp();
@@ -503,6 +523,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bar.p_ready[t]);
                 }
+                // (one row tile: the halves have tiles of tokens, and barriers, of their own)
+                if (safe < w.limit) wild = any_of(w.pair ? 2 : 3 + t, w.pair ? 2 * kSoftmaxThreads : kSoftmaxThreads, wild);
                 // every product with Q is done: the next item's Q may take its place
                 if (more) {
                     const Work next = work_of(p, next_it);
@@ -534,6 +556,23 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = 0.f;
+                }
+                if (wild && live) {
+                    const T *q = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + head * p.q_stride[2];
+#pragma unroll 1
+                    for (int j = 0; j < count; ++j) {
+                        const int t0 = w.it.tok0 + w.tile(t, j) * kTileTokens, from = max(t0, safe), to = min(t0 + kTileTokens, sees);
+                        if (from < to)
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4)
+                                if (32 * c + k < p.D) {
+                                    const float4 y = left_out_call<T>(p, q, w.it.tbl, w.it.head, from, to, m, 32 * c + k);
+                                    v[k] += y.x;
+                                    v[k + 1] += y.y;
+                                    v[k + 2] += y.z;
+                                    v[k + 3] += y.w;
+                                }
+                    }
                 }
                 const float f = w.it.direct ? inv : 1.f;
 #pragma unroll

@@ -4,8 +4,8 @@ import pytest
 import torch
 
 from paper_2408_08147_b200.sequences import CacheSession, Sequences
-from paper_2408_08147_b200.workloads import LAYER_MAJOR, Geometry
-from test_gpu_sequences import Evict, Setup
+from paper_2408_08147_b200.workloads import BLOCK_MAJOR, LAYER_MAJOR, Geometry
+from test_gpu_sequences import Evict, Setup, logit_error
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +108,71 @@ def test_many_light_tokens_beside_a_heavy_one(dtype, below, G):
     tol = 1.01 * want * (2 * half + 4 * 18.5 * 2.0 ** -23 + 2.0 ** -22 + 2 * (n / 16 + 64) * 2.0 ** -23) + n * 2.0 ** -32 + 2.0 ** -25
     off = (out.double() - want).abs().max().item()
     assert off <= tol
+
+
+def cached_row(s, r, token, kv, head):
+    """A row of K or V in the pool of a Setup."""
+    b, tt = int(s.seqs.tbl[s.seqs.tbl_off[r] + token // s.block]), token % s.block
+    return s.pool_t[b, s.layer, kv, tt, head] if s.layout == BLOCK_MAJOR else s.pool_t[s.layer, kv, b, head, tt]
+
+
+def kernel_of_own_tokens(c):
+    items = c.items()
+    kernels = set(items["kernel"][items["seq"] >= 0].tolist())
+    assert len(kernels) == 1
+    return kernels.pop()
+
+
+def check_where_finite(s, out_t, want):
+    """Infinite and NaN where the definition is, close to it elsewhere (the tolerance of test_attention with one more rounding of the result;
+    magnitudes and the largest value are those of the dims that are finite)."""
+    out, _, _, e = want
+    got = out_t.double().cpu().numpy()
+    fin = np.isfinite(out)
+    assert (np.isfinite(got) == fin).all() and (np.isnan(got) == np.isnan(out)).all()
+    assert (got[np.isinf(out)] == out[np.isinf(out)]).all()
+    half = torch.finfo(s.dtype).eps / 2
+    rel = 2 * logit_error(e, s.D) + half + (e["n"] + 64) * 2.0 ** -23
+    pool = s.pool_t.double()
+    v_max = pool[torch.isfinite(pool)].abs().max().item()
+    with np.errstate(invalid="ignore"):
+        tol = 1.01 * (rel[..., None] * e["mag"] + 2 * half * np.abs(out)) + (e["n"][..., None] * 2.0 ** -32 * v_max + 2.0 ** -25 if s.dtype == torch.float16 else 0)
+    assert (np.abs(got[fin] - out[fin]) <= tol[fin]).all()
+
+
+HIDDEN = [   # kernel, then the shape
+    (0, dict(lens=[90, 33, 2], G=2, Q=4, D=64)),
+    (0, dict(lens=[90, 33], G=2, Q=4, D=80, block=7)),
+    (0, dict(lens=[90, 33], G=4, Q=8, D=128, block=24, dtype="fp16")),
+    (0, dict(lens=[90, 33], G=3, Q=40, D=192, layout=LAYER_MAJOR)),
+    (0, dict(lens=[90, 260], G=16, Q=4, D=256, layout=LAYER_MAJOR)),
+    (0, dict(lens=[3000], H=1, G=2, Q=4, D=128, block=32)),
+    (1, dict(lens=[700, 500], G=12, Q=4, D=64, layout=LAYER_MAJOR)),
+    (1, dict(lens=[700, 500], G=50, Q=4, D=128, dtype="fp16")),
+    (1, dict(lens=[700, 300], H=1, G=1, Q=200, D=96)),
+    (1, dict(lens=[400, 290], H=2, G=2, Q=140, D=72, block=8, prefix_len=[70], member=[0, -1])),
+]
+
+
+@pytest.mark.parametrize("scale", [1, -1])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=str)
+@pytest.mark.parametrize("kernel,kw", HIDDEN, ids=[str(i) for i in range(len(HIDDEN))])
+def test_values_that_a_query_does_not_see(kernel, kw, value, scale):
+    """The newest tokens have infinite and NaN values: queries before them are not touched, queries that see them are."""
+    s = Setup(q_scale=0.5, **kw)
+    for r, n in enumerate(s.lens):
+        for back, d in ((1, 0), (2, 5), (3, 9), (s.Q - 1, 30), (s.Q // 2, 60)):
+            if back <= n:
+                row = cached_row(s, r, n - back, 1, back % s.H)
+                row[d], row[d + 1] = value, -value
+    scores = torch.zeros(len(s.lens), s.H, max(s.lens), device="cuda")
+    scale *= s.D ** -0.5
+    with s.session() as c:
+        assert kernel_of_own_tokens(c) == kernel
+        with np.errstate(invalid="ignore"):
+            want = s.expect(scale=scale)
+        assert not np.isfinite(want[0][:, -1]).all() and np.isfinite(want[0][:, 0]).all()
+        check_where_finite(s, c.attend(s.layer, s.q_t, scale=scale)[0], want)
+        check_where_finite(s, c.attend(s.layer, s.q_t, scale=scale, scores_t=scores)[0], want)
+        c.status()
+    assert torch.isfinite(scores).all()
