@@ -759,10 +759,10 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
                     float v[32];
                     tmem_load(v, tmem + ((uint32_t)(warp * 32) << 16) + b * columns + col);
                     tmem_load_wait();
-                    if (masked || col + 32 > width) {   // (columns past the last row hold anything)
+                    if (masked || col + 32 > rows) {   // (columns past the last row hold anything, or products of zeros, NaN for an infinite K)
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
-                            if (col + k >= width || t >= sees[col + k]) v[k] = -INFINITY;
+                            if (col + k >= rows || t >= sees[col + k]) v[k] = -INFINITY;
                     }
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) {

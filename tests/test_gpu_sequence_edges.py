@@ -5,7 +5,7 @@ import torch
 
 from paper_2408_08147_b200.sequences import CacheSession, Sequences
 from paper_2408_08147_b200.workloads import BLOCK_MAJOR, LAYER_MAJOR, Geometry
-from test_gpu_sequences import Evict, Setup, logit_error
+from test_gpu_sequences import Evict, Setup, check, check_scores, logit_error
 
 pytestmark = pytest.mark.gpu
 
@@ -176,3 +176,21 @@ def test_values_that_a_query_does_not_see(kernel, kw, value, scale):
         check_where_finite(s, c.attend(s.layer, s.q_t, scale=scale, scores_t=scores)[0], want)
         c.status()
     assert torch.isfinite(scores).all()
+
+
+@pytest.mark.parametrize("G,Q", [(2, 2), (12, 3), (33, 1), (50, 6)])
+def test_weights_of_a_key_that_no_row_heeds(G, Q):
+    """A key of infinite length whose logits are all -infinity has no weight, however many rows fill a block of the kernel."""
+    s = Setup([700, 260], H=1, G=G, Q=Q, D=64, block=32)
+    s.q_t[..., 0] = -s.q_t[..., 0].abs() - 0.1
+    cached_row(s, 0, 300, 0, 0)[0] = float("inf")
+    before = np.random.default_rng(2).random((2, 1, 700)).astype(np.float32)
+    scores = torch.from_numpy(before).cuda()
+    with s.session() as c:
+        assert kernel_of_own_tokens(c) == (G * Q > 32)
+        out, lse = c.attend(s.layer, s.q_t, scores_t=scores)
+        c.status()
+    want = s.expect()
+    check(s, out, lse, want)
+    check_scores(s, before.astype(np.float64), scores, want, s.lens)
+    assert scores[0, 0, 300].item() == before[0, 0, 300]
