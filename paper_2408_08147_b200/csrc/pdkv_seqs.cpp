@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <limits>
 #include <new>
 #include <stdexcept>
 
@@ -620,7 +621,8 @@ int pdkv_attend_scratch(const pdkv_seqs *s, int with_scores, size_t *bytes)
 int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *scratch, size_t scratch_bytes, void *stream)
 {
     if (!s || !a || s->Hq == 0 || layer < 0 || layer >= s->pool.d.num_layers) return PDKV_ERR_INVALID_ARG;
-    if (!std::isfinite(a->scale)) return PDKV_ERR_INVALID_ARG;
+    const float scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+    if (!std::isfinite(scale_log2)) return PDKV_ERR_INVALID_ARG;
     try {
         const int64_t rows[3] = {s->n_seq, s->q_tokens, s->Hq};
         const int64_t D = s->pool.d.head_dim;
@@ -697,9 +699,10 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
             p.out_stride[i] = rows[i] > 1 ? a->out_stride[i] : 0;
         }
         p.lse = a->lse;
-        p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
-        // the kernels hide tokens as logits of -infinity, which a scale of zero would turn into NaN
-        if (std::fabs(p.scale_log2) < 1e-30f) p.scale_log2 = std::signbit(p.scale_log2) ? -1e-30f : 1e-30f;
+        p.scale_log2 = scale_log2;
+        // The kernels hide tokens as logits of -infinity, which a scale of zero would turn into NaN: the smallest number
+        // instead, by which no finite logit comes near 1.
+        if (p.scale_log2 == 0.f) p.scale_log2 = std::copysign(std::numeric_limits<float>::denorm_min(), a->scale);
         p.seq_len = a->seq_len;
         char *w = static_cast<char *>(scratch);
         p.part_o = reinterpret_cast<float *>(w + l.o);

@@ -194,3 +194,20 @@ def test_weights_of_a_key_that_no_row_heeds(G, Q):
     check(s, out, lse, want)
     check_scores(s, before.astype(np.float64), scores, want, s.lens)
     assert scores[0, 0, 300].item() == before[0, 0, 300]
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-37])
+@pytest.mark.parametrize("G", [2, 40])                  # warp kernel, tile kernel
+def test_scale_of_zero_and_large_products(G, scale):
+    """Products of 1e36: with a scale of zero all tokens weigh the same; a small scale is not taken for zero."""
+    s = Setup([700], H=1, G=G, D=64)
+    s.q_t[..., 0] = 2.0 ** 60
+    for t in range(700):
+        cached_row(s, 0, t, 0, 0)[0] = 2.0 ** 60 * (-1) ** t * (1 + t % 3)
+    scores = torch.zeros(1, 1, 700, device="cuda")
+    with s.session() as c:
+        assert kernel_of_own_tokens(c) == (G == 40)
+        out, lse = c.attend(s.layer, s.q_t, scale=scale, scores_t=scores)
+    want = s.expect(scale=scale)
+    check(s, out, lse, want)
+    check_scores(s, np.zeros((1, 1, 700)), scores, want, s.lens)

@@ -138,3 +138,10 @@ def test_unaligned_buffers_of_eviction():
                 over["kept_scores"] = FAKE + (1 << 45)
             assert status(B.pdkv_evict, s, s, 0, 2, evict_args(**over)) == B.PDKV_ERR_INVALID_ARG, (lens, over)
     assert status(B.pdkv_evict, s, s, 0, 2, evict_args(budget=2 ** 30 + 1, scores=0, kept_scores=0)) == B.PDKV_ERR_LIMIT
+
+
+def test_scales_that_overflow_in_base_2():
+    """Logits are kept in base 2: a scale that is finite alone, but not times log2(e), is refused."""
+    s, _ = create(pool(), [40, 7])
+    for scale, want in ((2.3e38, B.PDKV_ERR_BUFFER_TOO_SMALL), (2.4e38, B.PDKV_ERR_INVALID_ARG), (-3e38, B.PDKV_ERR_INVALID_ARG)):
+        assert status(B.pdkv_attend, s, 0, args(scale=scale, scores_out=FAKE + (5 << 40), scores_out_stride=[160, 40]), FAKE + (3 << 40), 0) == want
