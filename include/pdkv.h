@@ -427,8 +427,8 @@ typedef struct {
 int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *desc, void *workspace, size_t workspace_bytes,
                      size_t *needed_bytes, void *stream, pdkv_seqs **out);
 /* Synchronise `stream` and report the handle's device status word: PDKV_OK,
- * PDKV_ERR_DEVICE_BOUNDS (a bounded wait inside an attention kernel gave up and the results of
- * that call are not valid) or PDKV_ERR_CUDA. */
+ * PDKV_ERR_DEVICE_BOUNDS (a bounded wait inside an attention kernel gave up, and the results of a
+ * call since the last report are not valid; the word is cleared) or PDKV_ERR_CUDA. */
 int pdkv_seqs_status(const pdkv_seqs *seqs, void *stream);
 /* Call it once the work enqueued with the handle has completed. */
 int pdkv_seqs_destroy(pdkv_seqs *seqs);

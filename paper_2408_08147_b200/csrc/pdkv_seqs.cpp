@@ -573,7 +573,11 @@ int pdkv_seqs_status(const pdkv_seqs *s, void *stream)
     cudaError_t e = cudaMemcpyAsync(&v, s->d_status, sizeof v, cudaMemcpyDeviceToHost, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaMemcpyAsync");
-    return v ? PDKV_ERR_DEVICE_BOUNDS : PDKV_OK;
+    if (v == 0) return PDKV_OK;
+    // reported once: the calls that follow are judged by themselves
+    e = cudaMemsetAsync(s->d_status, 0, sizeof v, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    return e == cudaSuccess ? PDKV_ERR_DEVICE_BOUNDS : pdkv::report_cuda_error(e, "cudaMemsetAsync");
 }
 
 int pdkv_seqs_items(const pdkv_seqs *s, const pdkv_attend_item **items, int64_t *n_items)

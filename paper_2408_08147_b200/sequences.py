@@ -264,7 +264,7 @@ class CacheSession:
         return B.pdkv_seqs_items(self.handle)
 
     def status(self, stream: Optional[int] = None) -> None:
-        """Wait for the session's stream and raise if a kernel reported an error."""
+        """Wait for the session's stream and raise if a kernel reported an error since the last call of this."""
         B.pdkv_seqs_status(self.handle, self._on(stream))
 
     def close(self) -> None:

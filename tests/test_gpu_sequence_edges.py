@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2408_08147_b200 import binding as B
 from paper_2408_08147_b200.sequences import CacheSession, Sequences
 from paper_2408_08147_b200.workloads import BLOCK_MAJOR, LAYER_MAJOR, Geometry
 from test_gpu_sequences import Evict, Setup, check, check_scores, logit_error
@@ -211,3 +212,17 @@ def test_scale_of_zero_and_large_products(G, scale):
     want = s.expect(scale=scale)
     check(s, out, lse, want)
     check_scores(s, np.zeros((1, 1, 700)), scores, want, s.lens)
+
+
+def test_an_error_is_reported_once():
+    """A kernel's report, as a write to the handle's status word (the first of its workspace)."""
+    s = Setup([90, 33], G=2, D=64)
+    workspace = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    with s.session(workspace_t=workspace) as c:
+        c.status()
+        workspace[0] = 1
+        with pytest.raises(B.PdkvError) as e:
+            c.status()
+        assert e.value.status == B.PDKV_ERR_DEVICE_BOUNDS
+        check(s, *c.attend(s.layer, s.q_t), s.expect())
+        c.status()
