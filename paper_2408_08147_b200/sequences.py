@@ -168,10 +168,13 @@ class CacheSession:
         """Attention of one layer; ``q_t`` is ``[n_seq, q_tokens, num_q_heads, head_dim]`` (any strides with
         adjacent dims).  Returns ``(out, lse)``.  With ``scores_t`` (float32 ``[n_seq, num_kv_heads, >= longest]``)
         the attention weights of the own tokens are added to it, or to ``scores_in_t`` and the sums
-        stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device)."""
+        stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device).  There is no backward pass: a
+        ``q_t`` that asks for a gradient is refused."""
         shape = self._shape
         made = []
         self._check("q_t", q_t, self.dtype, shape)
+        if q_t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("q_t: attention over a cache has no gradient; detach it or call under torch.no_grad()")
         a = B.pdkv_attend_args.from_buffer_copy(self._plain)
         dense = q_t.is_contiguous()
         if not dense:

@@ -1,8 +1,11 @@
 """Corners of the handles of cached sequences and of their calls without a GPU."""
 import numpy as np
 import pytest
+import torch
 
 from paper_2408_08147_b200 import binding as B
+from paper_2408_08147_b200 import workloads as W
+from paper_2408_08147_b200.sequences import CacheSession, Sequences
 from test_sequences_host import FAKE, args, built, create, csr, pool, status  # noqa: F401 (`built` is a fixture)
 
 
@@ -145,3 +148,22 @@ def test_scales_that_overflow_in_base_2():
     s, _ = create(pool(), [40, 7])
     for scale, want in ((2.3e38, B.PDKV_ERR_BUFFER_TOO_SMALL), (2.4e38, B.PDKV_ERR_INVALID_ARG), (-3e38, B.PDKV_ERR_INVALID_ARG)):
         assert status(B.pdkv_attend, s, 0, args(scale=scale, scores_out=FAKE + (5 << 40), scores_out_stride=[160, 40]), FAKE + (3 << 40), 0) == want
+
+
+def cpu_session(dtype=torch.bfloat16, **kw):
+    """A session over host memory: its handle can be asked, not launched."""
+    geom = W.Geometry(W.BLOCK_MAJOR, 2, 4, 64, 2, 16, 8)
+    off, tbl = csr([40, 7], 16)
+    kw = {"num_q_heads": 8, **kw}
+    return CacheSession(geom, torch.zeros(geom.shape(), dtype=dtype), Sequences([40, 7], off, tbl), **kw)
+
+
+def test_queries_that_ask_for_a_gradient():
+    with cpu_session() as c:
+        q = torch.zeros(2, 1, 8, 64, dtype=torch.bfloat16, requires_grad=True)
+        with pytest.raises(ValueError, match="gradient"):
+            c.attend(0, q)
+        with torch.no_grad(), pytest.raises(B.PdkvError):      # (a host-only handle)
+            c.attend(0, q)
+        with pytest.raises(B.PdkvError):
+            c.attend(0, q.detach())
