@@ -75,7 +75,7 @@ class CacheSession:
 
     ``pool_t`` is the torch CUDA tensor that holds the pool described by ``geom``.  With
     ``num_q_heads`` the session attends; ``dtype`` (torch.bfloat16 or torch.float16) is the type
-    of K, V, q and out and defaults to the pool's own.  Scratch is allocated once and kept: calls
+    of K, V, q and out and defaults to the pool's own; it is needed for a pool that is held as bytes or words.  Scratch is allocated once and kept: calls
     of one session are meant for one stream at a time (pass ``scratch_t`` for others).
     ``stream`` None means torch's current stream of the pool's device at each call.  What a call
     allocates comes from torch's current stream and is recorded on the stream that it runs on, so its
@@ -93,6 +93,8 @@ class CacheSession:
             dtype = pool_t.dtype if pool_t.dtype in _DTYPES else torch.bfloat16
         if dtype not in _DTYPES:
             raise ValueError("attention takes bfloat16 or float16")
+        if num_q_heads and pool_t.dtype in _DTYPES and dtype != pool_t.dtype:
+            raise ValueError(f"the pool holds {pool_t.dtype}, not {dtype}")
         if not pool_t.is_contiguous():
             raise ValueError("the pool tensor has to be contiguous")
         self.dtype = dtype

@@ -167,3 +167,14 @@ def test_queries_that_ask_for_a_gradient():
             c.attend(0, q)
         with pytest.raises(B.PdkvError):
             c.attend(0, q.detach())
+
+
+def test_type_of_the_pool():
+    """16-bit words can be declared to be either type; a tensor of one type cannot be the other."""
+    for held, named in ((torch.bfloat16, torch.float16), (torch.float16, torch.bfloat16), (torch.bfloat16, torch.float32)):
+        with pytest.raises(ValueError):
+            cpu_session(held, dtype=named)
+    for held, named in ((torch.int16, torch.float16), (torch.float16, None), (torch.float16, torch.float16)):
+        with cpu_session(held, dtype=named) as c:
+            assert c.dtype == torch.float16
+    cpu_session(torch.float16, dtype=torch.bfloat16, num_q_heads=0).close()     # rows are moved as they are
