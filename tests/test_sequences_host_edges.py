@@ -150,12 +150,12 @@ def test_scales_that_overflow_in_base_2():
         assert status(B.pdkv_attend, s, 0, args(scale=scale, scores_out=FAKE + (5 << 40), scores_out_stride=[160, 40]), FAKE + (3 << 40), 0) == want
 
 
-def cpu_session(dtype=torch.bfloat16, **kw):
+def cpu_session(held=torch.bfloat16, **kw):
     """A session over host memory: its handle can be asked, not launched."""
     geom = W.Geometry(W.BLOCK_MAJOR, 2, 4, 64, 2, 16, 8)
     off, tbl = csr([40, 7], 16)
     kw = {"num_q_heads": 8, **kw}
-    return CacheSession(geom, torch.zeros(geom.shape(), dtype=dtype), Sequences([40, 7], off, tbl), **kw)
+    return CacheSession(geom, torch.zeros(geom.shape(), dtype=held), Sequences([40, 7], off, tbl), **kw)
 
 
 def test_queries_that_ask_for_a_gradient():
