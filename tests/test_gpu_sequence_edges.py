@@ -226,3 +226,228 @@ def test_an_error_is_reported_once():
         assert e.value.status == B.PDKV_ERR_DEVICE_BOUNDS
         check(s, *c.attend(s.layer, s.q_t), s.expect())
         c.status()
+
+
+# ---------------------------------------------------------------------------
+# paths that only some shapes take
+# ---------------------------------------------------------------------------
+
+LARGE = [   # own tokens in the tile kernel: one row tile, two, several items of 256 rows, heads of 72 to 128 dims
+    dict(lens=[700, 500], G=12, Q=4, D=64),
+    dict(lens=[700, 333], G=50, Q=4, D=128, layout=LAYER_MAJOR, dtype="fp16"),
+    dict(lens=[700, 130], H=1, G=8, Q=40, D=64),                          # 320 rows: 256 and 64
+    dict(lens=[700, 290], H=1, G=7, Q=43, D=128, block=24),               # 301 rows: the last group is no multiple of 16
+    dict(lens=[600, 400], H=1, G=5, Q=110, D=72, block=8, layout=LAYER_MAJOR),   # 550 rows: three groups
+    dict(lens=[900, 260, 700], H=2, G=20, Q=2, D=96, prefix_len=[300], member=[0, -1, 0]),
+]
+FEW = [     # own tokens in the warp kernel
+    dict(lens=[90, 33], G=4, D=64),
+    dict(lens=[90, 200], G=4, Q=6, D=128, block=24, dtype="fp16"),
+    dict(lens=[300, 190], H=1, G=10, Q=9, D=256),                         # 90 rows: items behind the first row tile
+    dict(lens=[130, 60], H=2, G=7, Q=20, D=80, block=7),                  # 140 rows, a block size without boxes
+    dict(lens=[500, 60], H=1, G=20, Q=10, D=192, layout=LAYER_MAJOR, dtype="fp16", prefix_len=[150], member=[0, 0]),
+]
+ALL = [(1, kw) for kw in LARGE] + [(0, kw) for kw in FEW]
+ids = [f"tile{i}" for i in range(len(LARGE))] + [f"warp{i}" for i in range(len(FEW))]
+
+
+def scores_like(s, width=None, seed=1):
+    host = np.random.default_rng(seed).random((len(s.lens), s.H, width or max(s.caps))).astype(np.float32)
+    return host.astype(np.float64), torch.from_numpy(host).cuda()
+
+
+@pytest.mark.parametrize("scale", [None, -0.2, 0.0])
+@pytest.mark.parametrize("kernel,kw", ALL, ids=ids)
+def test_scores_and_scales(kernel, kw, scale):
+    s = Setup(**kw)
+    before, scores = scores_like(s)
+    want = s.expect(scale=scale)
+    with s.session() as c:
+        assert kernel_of_own_tokens(c) == kernel
+        check(s, *c.attend(s.layer, s.q_t, scale=scale), want)
+        check(s, *c.attend(s.layer, s.q_t, scale=scale, scores_t=scores), want)
+        c.status()
+    check_scores(s, before, scores, want, s.lens)
+
+
+@pytest.mark.parametrize("kernel,kw", ALL, ids=ids)
+def test_current_lengths_of_all_kinds(kernel, kw):
+    """Lengths from the device below the handle's, down to none and to fewer than query tokens; NaN behind them in the pool."""
+    full = kw["lens"]
+    for lens in ([n - 1 - 127 * i for i, n in enumerate(full)], [n // 3 for n in full], [0] + full[1:], [kw.get("Q", 1) - 1] * len(full), [1] * len(full)):
+        lens = [max(0, n) for n in lens]
+        s = Setup(**{**kw, "lens": lens, "caps": full})
+        lens_t = torch.tensor([n if n else -3 for n in lens], dtype=torch.int32, device="cuda")
+        before, scores = scores_like(s)
+        other = torch.full_like(scores, 7.0)
+        want = s.expect()
+        with s.session() as c:
+            assert kernel_of_own_tokens(c) == kernel
+            check(s, *c.attend(s.layer, s.q_t, seq_len_t=lens_t), want)
+            c.attend(s.layer, s.q_t, seq_len_t=lens_t, scores_t=other, scores_in_t=scores)
+            check(s, *c.attend(s.layer, s.q_t, seq_len_t=lens_t, scores_t=scores), want)
+            c.status()
+        check_scores(s, before, scores, want, s.lens)
+        assert torch.equal(other, scores)
+
+
+@pytest.mark.parametrize("kernel,kw", ALL, ids=ids)
+def test_strides_of_all_kinds(kernel, kw):
+    """q, out and scores as views in other orders, of wider buffers."""
+    s = Setup(**kw)
+    n, Q, Hq, D = s.q_t.shape
+    q = torch.zeros(Q, n, Hq + 5, D + 8, dtype=s.dtype, device="cuda").permute(1, 0, 2, 3)[:, :, 2:2 + Hq, :D]
+    q.copy_(s.q_t)
+    out = torch.full((Hq, n, Q, D + 16), 9.0, dtype=s.dtype, device="cuda")
+    view = out.permute(1, 2, 0, 3)[..., 8:8 + D]
+    before, dense = scores_like(s, max(s.caps) + 5)
+    both = torch.full((2, s.H, n, max(s.caps) + 5), 7.0, device="cuda")
+    both[0] = dense.transpose(0, 1)
+    want = s.expect()
+    with s.session() as c:
+        _, lse = c.attend(s.layer, q, out_t=view, scores_in_t=both[0].transpose(0, 1), scores_t=both[1].transpose(0, 1))
+        c.status()
+    check(s, view, lse, want)
+    assert (out[..., :8] == 9).all() and (out[..., 8 + D:] == 9).all()
+    got = both[1].transpose(0, 1)
+    assert (got[..., -5:] == 7).all() and torch.equal(both[0].transpose(0, 1), dense)
+    check_scores(s, before[..., :-5], got[..., :-5], want, s.lens)
+
+
+@pytest.mark.parametrize("one_q", [False, True])
+@pytest.mark.parametrize("kernel,kw", ALL, ids=ids)
+def test_scores_without_an_input(kernel, kw, one_q):
+    """scores_in NULL stands for zeros: tokens past a sequence's end get them, entries behind the longest sequence are left.  And q
+    with strides of zero: one query for all."""
+    s = Setup(**kw)
+    if one_q:
+        s.q_t = s.q_t[:1, :1, :1].expand_as(s.q_t)
+    width = max(s.lens) + 3
+    scores = torch.full((len(s.lens), s.H, width), 7.0, device="cuda")
+    want = s.expect(q_t=s.q_t)
+    with s.session() as c:
+        out, lse = torch.empty(s.q_t.shape, dtype=s.dtype, device="cuda"), torch.empty(s.q_t.shape[:3], device="cuda")
+        scratch = torch.empty(c.scratch_bytes(True), dtype=torch.uint8, device="cuda")
+        a = B.pdkv_attend_args(q=s.q_t.data_ptr(), out=out.data_ptr(), lse=lse.data_ptr(), scale=s.D ** -0.5, scores_out=scores.data_ptr())
+        a.q_stride[:], a.out_stride[:], a.scores_out_stride[:] = s.q_t.stride()[:3], out.stride()[:3], scores.stride()[:2]
+        torch.cuda.synchronize()
+        B.pdkv_attend(c.handle, s.layer, a, scratch.data_ptr(), scratch.numel(), torch.cuda.current_stream().cuda_stream)
+        c.status()
+    check(s, out, lse, want)
+    assert (scores[..., -3:] == 7).all()
+    check_scores(s, np.zeros((len(s.lens), s.H, width - 3)), scores[..., :-3], want, s.lens)
+
+
+def test_lse_is_optional():
+    for kernel, kw in ALL[::3]:
+        s = Setup(**kw)
+        before, scores = scores_like(s)
+        with s.session() as c:
+            want = c.attend(s.layer, s.q_t)[0]
+            out = torch.empty_like(want)
+            scratch = torch.empty(c.scratch_bytes(True), dtype=torch.uint8, device="cuda")
+            a = B.pdkv_attend_args(q=s.q_t.data_ptr(), out=out.data_ptr(), scale=s.D ** -0.5, scores_in=scores.data_ptr(), scores_out=scores.data_ptr())
+            a.q_stride[:], a.out_stride[:] = s.q_t.stride()[:3], out.stride()[:3]
+            a.scores_in_stride[:], a.scores_out_stride[:] = scores.stride()[:2], scores.stride()[:2]
+            torch.cuda.synchronize()
+            B.pdkv_attend(c.handle, s.layer, a, scratch.data_ptr(), scratch.numel(), torch.cuda.current_stream().cuda_stream)
+            c.status()
+        assert torch.equal(out, want)
+        check_scores(s, before, scores, s.expect(), s.lens)
+
+
+@pytest.mark.parametrize("kernel,kw", ALL, ids=ids)
+def test_the_same_bits_from_a_graph_beside_another(kernel, kw):
+    """Two recorded calls with a scratch each, replayed at once on two streams, again and again."""
+    s = Setup(**kw)
+    with s.session() as c:
+        q = [s.q_t, (s.q_t * 0.5)]
+        zero = torch.zeros(len(s.lens), s.H, max(s.caps), device="cuda")
+        sc = [zero.clone() for _ in q]
+        want = [c.attend(s.layer, x, scores_t=y)[0].clone() for x, y in zip(q, sc)]
+        want_sc = [x.clone() for x in sc]
+        out = [torch.empty_like(x) for x in want]
+        lse = [torch.empty(s.q_t.shape[:3], device="cuda") for _ in q]
+        scratch = [torch.empty(c.scratch_bytes(True), dtype=torch.uint8, device="cuda") for _ in q]
+        streams, graphs = [torch.cuda.Stream() for _ in q], []
+        torch.cuda.synchronize()
+        for i in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=streams[i]):
+                for _ in range(5):
+                    c.attend(s.layer, q[i], out_t=out[i], lse_t=lse[i], scores_t=sc[i], scores_in_t=zero, scratch_t=scratch[i])
+            graphs.append(g)
+        for _ in range(5):
+            for x in out + sc:
+                x.zero_()
+            torch.cuda.synchronize()
+            for g, st in zip(graphs, streams):
+                with torch.cuda.stream(st):
+                    g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out + sc, want + want_sc))
+        c.status()
+
+
+def test_on_the_streams_of_an_sm_partition():
+    """Attention and eviction on few SMs and on the others."""
+    part = B.pdkv_sm_partition_create(0, 8)
+    try:
+        for which in (0, 1):
+            stream = torch.cuda.ExternalStream(B.pdkv_sm_partition_stream(part, which))
+            for kernel, kw in ALL[::4]:
+                s = Setup(**kw)
+                before, scores = scores_like(s)
+                out, lse = torch.empty_like(s.q_t), torch.empty(s.q_t.shape[:3], device="cuda")
+                with s.session() as c:
+                    c.attend(s.layer, s.q_t, out_t=out, lse_t=lse)
+                    scratch = torch.empty(c.scratch_bytes(True), dtype=torch.uint8, device="cuda")
+                    torch.cuda.synchronize()
+                    c.attend(s.layer, s.q_t, out_t=out, lse_t=lse, scores_t=scores, scratch_t=scratch, stream=stream.cuda_stream)
+                    c.status(stream.cuda_stream)
+                want = s.expect()
+                check(s, out, lse, want)
+                check_scores(s, before, scores, want, s.lens)
+            for kw in (dict(lens=[300, 50], budget=64), dict(lens=[20000, 9000], budget=2049, H=1, layers=1)):
+                e = Evict(**kw)
+                src_t, dst_t = e.tensors()
+                want_kept, want_sc, want_pool = e.expect(0, 0, (0, e.layers))
+                scores = torch.from_numpy(e.scores).cuda()
+                kept, sc = torch.zeros(want_kept.shape, dtype=torch.int32, device="cuda"), torch.zeros(want_sc.shape, device="cuda")
+                n = torch.zeros(len(e.lens), dtype=torch.int32, device="cuda")
+                with CacheSession(e.src, src_t, e.src_seqs) as a, CacheSession(e.dst, dst_t, e.dst_seqs) as b:
+                    torch.cuda.synchronize()
+                    a.evict(b, scores, e.budget, kept_t=kept, kept_scores_t=sc, new_len_t=n, stream=stream.cuda_stream)
+                    torch.cuda.synchronize()
+                assert (kept.cpu().numpy() == want_kept).all() and (sc.cpu().numpy() == want_sc).all()
+                assert (e.back(dst_t, want_pool) == want_pool).all()
+    finally:
+        B.pdkv_sm_partition_destroy(part)
+
+
+@pytest.mark.parametrize("longest", [300, 9000])
+def test_evictions_of_lengths_from_the_device(longest):
+    """Into another pool and in place; lengths of none, one, the budget and above it, below the handle's."""
+    caps = [longest, 40, 64, 90, 200, 33]
+    for lens in ([longest - 7, 0, 1, 30, 31, 29], [5, 40, 64, 90, 200, 33], [longest, 0, 0, 0, 0, 0]):
+        for in_place in (False, True):
+            e = Evict(lens, 30, caps=caps, H=2, D=8, layers=2)
+            src_t, dst_t = e.tensors()
+            want_kept, want_sc, want_pool = e.expect(1, 2, (0, 2), in_place)
+            lens_t = torch.tensor([n if n else -9 for n in lens], dtype=torch.int32, device="cuda")
+            with CacheSession(e.src, src_t, e.src_seqs) as a, CacheSession(e.dst, dst_t, e.dst_seqs) as b:
+                kept, sc, n = a.evict(a if in_place else b, torch.from_numpy(e.scores).cuda(), 30, sink=1, recent=2, seq_len_t=lens_t)
+            assert (kept.cpu().numpy() == want_kept).all() and (sc.cpu().numpy() == want_sc).all()
+            assert n.tolist() == [min(x, 30) for x in lens]
+            assert (e.back(src_t if in_place else dst_t, want_pool) == want_pool).all()
+
+
+def test_sequences_without_a_token():
+    """Handles whose sequences hold none: zeros, -infinity, -1 and lengths of zero."""
+    s = Setup([0, 0], G=2, D=64, prefix_len=[0], member=[0, -1])
+    with s.session() as c:
+        out, lse = c.attend(s.layer, s.q_t, scores_t=torch.zeros(2, s.H, 4, device="cuda"))
+        assert (out == 0).all() and torch.isneginf(lse).all()
+        kept, sc, n = c.evict(c, torch.zeros(2, 2, s.H, 0, device="cuda"), 5)
+        assert (kept == -1).all() and (sc == 0).all() and n.tolist() == [0, 0]
+        c.status()
