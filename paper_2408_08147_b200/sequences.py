@@ -236,6 +236,8 @@ class CacheSession:
         front of the same sequences in ``dst`` (this session itself: in place).  ``scores_t`` is float32
         ``[layers, n_seq, num_kv_heads, >= longest]``.  Returns ``(kept, kept_scores, new_len)``."""
         l0, l1 = (0, self.geom.num_layers) if layers is None else layers
+        if not 0 <= l0 < l1 <= self.geom.num_layers:
+            raise ValueError(f"layers: expected a range within [0, {self.geom.num_layers}), got {layers}")
         n_seq = self._shape[0]
         lead = (l1 - l0, n_seq, self.geom.num_kv_heads)
         self._rows("scores_t", scores_t, lead, self._max_len)

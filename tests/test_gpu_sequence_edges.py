@@ -451,3 +451,13 @@ def test_sequences_without_a_token():
         kept, sc, n = c.evict(c, torch.zeros(2, 2, s.H, 0, device="cuda"), 5)
         assert (kept == -1).all() and (sc == 0).all() and n.tolist() == [0, 0]
         c.status()
+
+
+def test_the_default_stream_from_another_current_one():
+    s = Setup([90, 33], G=2, D=64)
+    with s.session() as c:
+        torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            out, lse = c.attend(s.layer, s.q_t, stream=0)
+            torch.cuda.default_stream().synchronize()
+        check(s, out, lse, s.expect())

@@ -178,3 +178,11 @@ def test_type_of_the_pool():
         with cpu_session(held, dtype=named) as c:
             assert c.dtype == torch.float16
     cpu_session(torch.float16, dtype=torch.bfloat16, num_q_heads=0).close()     # rows are moved as they are
+
+
+def test_ranges_of_layers_to_evict():
+    """An empty range would return lengths that nobody wrote."""
+    with cpu_session(num_q_heads=0) as c:
+        for layers in ((1, 1), (0, 0), (1, 0), (-1, 1), (0, 3)):
+            with pytest.raises(ValueError, match="layers"):
+                c.evict(c, torch.zeros(max(0, layers[1] - layers[0]), 2, 4, 40), 8, layers=layers)
