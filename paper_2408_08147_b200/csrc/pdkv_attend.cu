@@ -509,19 +509,21 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
         mbar_init(&bar.empty[threadIdx.x], 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (threadIdx.x == kConsumers && p.n_tile_ctas > 0) {   // (see below; for the CTA, by the barrier.  A fence took 3 us of a call of 64)
+        unsigned long long any;
+        asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(any) : "l"(p.status) : "memory");
+    }
     __syncthreads();
     if (threadIdx.x == kConsumers) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
     // The first kernel of a call is set up while the work before it ends.  Behind the tile kernel of the same call it does not
     // wait: it would wait for the whole of that kernel, which it is to run beside.  It starts once every CTA of that kernel has
-    // seen the work before the call complete and has said so (griddepcontrol.launch_dependents behind griddepcontrol.wait).  PTX
-    // promises what was written before only to a grid that waits itself, so this goes beyond it by one step: what
-    // the tile kernel's CTAs saw before a fence is seen behind a fence by a CTA that started after them.
-    if (p.n_tile_ctas == 0) {
+    // seen the work before the call complete (griddepcontrol.wait) and has said so (launch_dependents).  PTX promises what that
+    // work wrote only to a grid that waits itself, so this goes beyond it by one step: a CTA that started after
+    // that completion finds the writes in L2, and the acquiring load above and the fence below keep it from anything older.
+    if (p.n_tile_ctas == 0)
         asm volatile("griddepcontrol.wait;" ::: "memory");
-    } else {
-        __threadfence();
-        asm volatile("fence.proxy.async.global;" ::: "memory");   // the loads of K and V
-    }
+    else if (threadIdx.x == kConsumers)
+        asm volatile("fence.proxy.async.global;" ::: "memory");   // its loads of K and V
     asm volatile("griddepcontrol.launch_dependents;");
     if (threadIdx.x >= kConsumers) {
         load_slices<DP>(p, &map, smem_u32(smem), bar, it);

@@ -234,7 +234,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
     __syncthreads();
     if (warp == kLoadWarp && lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");   // set up while the work before this call ends
-    if (p.n_ctas > 0) __threadfence();                   // the warp kernel, which starts now, does not wait for that work itself
     asm volatile("griddepcontrol.launch_dependents;");
     bool dead = false;
     // tensor memory is there for the warps that use it; the loads of K and V do not wait for it
