@@ -54,23 +54,18 @@ bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
     return a_bytes && b_bytes && a0 < b0 + b_bytes && b0 < a0 + a_bytes;
 }
 
-// Rows of memory of one length at base + sum of i * stride (none where base is null).
+// Rows of memory of one length at base + sum of i * stride, from `base` to before `end` (nothing where base is null).
 struct Rows {
-    uintptr_t base = 0;
+    uintptr_t base = 0, end = 0;
     int64_t bytes = 0, stride[3] = {0, 0, 0}, n[3] = {1, 1, 1};
-    Rows() = default;
-    Rows(const void *p, int64_t row_bytes) : base(reinterpret_cast<uintptr_t>(p)), bytes(p ? row_bytes : 0) {}
+    Rows(const void *p, int64_t row_bytes) : base(reinterpret_cast<uintptr_t>(p)), end(base + (p ? row_bytes : 0)), bytes(row_bytes) {}
     Rows(const void *p, int64_t row_len, int64_t elem, const int64_t *s, const int64_t *count, int axes) : Rows(p, row_len * elem)
     {
         for (int i = 0; i < axes; ++i) {
             n[i] = count[i];
             stride[i] = count[i] > 1 ? s[i] * elem : 0;
+            if (end > base) end = count[i] > 0 ? end + stride[i] * (count[i] - 1) : base;
         }
-    }
-    int64_t span() const
-    {
-        if (bytes <= 0 || n[0] <= 0 || n[1] <= 0 || n[2] <= 0) return 0;
-        return bytes + stride[0] * (n[0] - 1) + stride[1] * (n[1] - 1) + stride[2] * (n[2] - 1);
     }
     std::vector<uintptr_t> starts() const
     {
@@ -87,8 +82,7 @@ struct Rows {
 // Do a row of `a` and one of `b` share a byte?  Row by row only where their spans meet (views of one buffer).
 bool meet(const Rows &a, const Rows &b)
 {
-    const int64_t na = a.span(), nb = b.span();
-    if (na == 0 || nb == 0 || a.base >= b.base + nb || b.base >= a.base + na) return false;
+    if (a.base >= b.end || b.base >= a.end || a.base == a.end || b.base == b.end) return false;
     const std::vector<uintptr_t> x = a.starts(), y = b.starts();
     for (size_t i = 0, j = 0; i < x.size() && j < y.size();) {
         if (x[i] < y[j] + b.bytes && y[j] < x[i] + a.bytes) return true;

@@ -132,10 +132,10 @@ class CacheSession:
     def _on_current(self) -> int:
         return _current_stream(self._index) if self.pool_t.is_cuda else 0
 
-    def _record(self, stream: int, home: int, *tensors) -> None:
-        """The caching allocator hands a freed block to the next request on its ``home`` stream: tell it of
+    def _record(self, stream: int, *tensors) -> None:
+        """The caching allocator hands a freed block to the next request on the stream it was allocated for: tell it of
         the other stream that uses these."""
-        if stream != home and self.pool_t.is_cuda:
+        if self.pool_t.is_cuda:
             user = torch.cuda.ExternalStream(stream, self._device)
             for t in tensors:
                 t.record_stream(user)
@@ -214,18 +214,21 @@ class CacheSession:
             a.scores_in_stride, a.scores_out_stride = scores_in_t.stride()[:2], scores_t.stride()[:2]
         elif scores_in_t is not None:
             raise ValueError("scores_in_t needs scores_t to receive the sums")
-        stream, home = self._on(stream), self._on_current()
+        home = self._on_current()
+        stream = home if stream is None and self.stream is None else self._on(stream)
         if scratch_t is None:
             which = scores_t is not None
             scratch_t = self._scratch[which]
             if scratch_t is None:
                 scratch_t = self._scratch[which] = torch.empty(max(self._need[which], 16), dtype=torch.uint8, device=self._device)
                 self._scratch_stream[which] = home
-            self._record(stream, self._scratch_stream[which], scratch_t)
+            if stream != self._scratch_stream[which]:
+                self._record(stream, scratch_t)
             size = scratch_t.numel()
         else:
             size = scratch_t.numel() * scratch_t.element_size()
-        self._record(stream, home, *made)
+        if stream != home:
+            self._record(stream, *made)
         B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, stream)
         return out_t, lse_t
 
@@ -262,7 +265,8 @@ class CacheSession:
                               kept_scores_stride=kept_scores_t.stride()[:3], kept_scores_len=kept_scores_t.shape[-1],
                               new_len=self._lens(new_len_t))
         stream = self._on(stream)
-        self._record(stream, self._on_current(), *made)
+        if stream != self._on_current():
+            self._record(stream, *made)
         B.pdkv_evict(self.handle, dst.handle, l0, l1, a, stream)
         return kept_t, kept_scores_t, new_len_t
 
