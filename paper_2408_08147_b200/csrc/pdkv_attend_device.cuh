@@ -54,7 +54,7 @@ __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)_
 
 constexpr float kGrowth = 8.f;                    // log2 of how far a maximum may run ahead of its base
 // A row's weights are 2^(z - base), rounded to the pool's type for the product with V (their sum is taken before that).  bf16
-// has the exponents of 32 bits: a weight is off by half a step of 2^-8 at most, however small.  fp16 ends at 2^16, has
+// has the exponents of 32 bits: a weight is off by 2^-8 of itself at most, however small.  fp16 ends at 2^16, has
 // fewer bits below 2^-14 and none below 2^-25, which a long list of light tokens beside one heavy token can
 // notice (131072 tokens 17 nats below it: 0.0078 instead of 0.0054).  So its base lies kLift below the maximum: the
 // heaviest weight is at most 2^(kLift + kGrowth) = 2^15, and weights keep all bits down to 2^-21 of the base's, and lose at most

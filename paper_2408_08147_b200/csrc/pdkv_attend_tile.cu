@@ -7,9 +7,9 @@
 //     O += P V       tcgen05.mma, P from tensor memory, O stays in tensor memory
 // Two row tiles take turns: while the threads of one turn S into P, the tensor cores work for the
 // other, and both use the same K and V, which halves what is read from L2.  When there is only one row tile, the
-// two halves of the CTA take every second tile of tokens each, and leave two parts to be joined.  Ten warps: four per row
+// two halves of the CTA take every second tile of tokens each, and leave two parts to be joined.  Twelve warps: four per row
 // tile for the softmax, one that issues the matrix instructions, one that issues the loads (TMA boxes of one
-// page, 64 dims and the 128-byte swizzle that the matrix instructions expect).
+// page, 64 dims and the 128-byte swizzle that the matrix instructions expect), two that only give up their registers.
 //
 // O is rescaled only when a row's maximum grew by more than 2^8 since the last time.  Bases and sums are 32 bits, the sums
 // taken before the weights are rounded (see kLift).
@@ -17,7 +17,8 @@
 // Bound by the tensor core and by the chain S, P, O of a row tile: 256 rows against 128 tokens of 128 dims take it
 // 3024 cycles (125 for 16 dims of Q K^T, whose two operands come from shared memory at 64 bytes a cycle, 64 for 16 tokens
 // of P V), and an iteration takes 3700.  Measured on B200, whole calls: 64 rows of each of 8 heads against 65536 tokens
-// 78 us (3.4 TB/s), 256 rows 99 us (690 TFLOP/s), 512 rows against 200000 tokens 451 us (930 TFLOP/s).  Starting and finishing an
+// 70 us (3.9 TB/s), 256 rows 101 us (680 TFLOP/s), 512 rows against 200000 tokens 453 us (925 TFLOP/s).  (A row of S does not
+// quite fit: ptxas spills 240 bytes a thread.)  Starting and finishing an
 // item costs about 8 us, which is what short lists pay (256 rows against 4096 tokens: 26 us).
 #include <algorithm>
 #include <numeric>
@@ -619,9 +620,10 @@ template <int DP> constexpr uint32_t weigh_bytes(int rows)
 //
 // S^T = K Q^T: a thread has one token and its logits of all rows in tensor memory, so the sum over the
 // rows needs no other thread.  Six warps: four compute weights, one issues the products, one the loads of K;
-// two tiles of K and two of S^T are on their way.  Two CTAs on an SM up to 128 rows.  Bound by the exponentials and
-// the loads of S^T from tensor memory: 12 sequences of 300 to 4096 tokens, 64 rows each, 8 heads of 128 dims take 27 us
-// as a kernel alone, of which the bytes of K need 9.
+// two tiles of K and two of S^T are on their way.  Two CTAs on an SM up to 128 rows.  12 sequences of 300 to 4096
+// tokens, 64 rows each, 8 heads of 128 dims take 27 us as a kernel alone, of which the bytes of K need 9 and the exponentials 3 (16
+// a cycle and SM); the tensor pipe is active for 8%, DRAM for 24%.  So latency bounds it: a CTA starts (Q, sums of the rows) for a
+// handful of tiles, and ragged lists leave a few CTAs for a second wave.
 template <typename T, int DP>
 __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
 {
@@ -825,7 +827,7 @@ template <typename T, int DP> cudaError_t launch_weigh(const AttnParams &p, cons
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_shared(attend_weigh_kernel<T, DP>, (int)weigh_bytes<DP>(256), ready);
     if (e != cudaSuccess) return e;
-    // two CTAs an SM hold all tiles at once, each at least two
+    // two CTAs an SM would hold the sum of all tiles at once (ragged lists make some CTAs more), each at least two
     const int chunk_tiles = (int)std::max<int64_t>(2, (p.own_tiles + 2 * p.sm_count - 1) / (2 * p.sm_count));
     const int chunks = (p.max_len + chunk_tiles * kTileTokens - 1) / (chunk_tiles * kTileTokens);
     const int64_t blocks = (int64_t)p.n_seq * p.H * chunks;

@@ -342,12 +342,16 @@ __device__ __forceinline__ void select_row(SelectShared<THREADS> &sh, const floa
 // One cluster per (layer, sequence, head).  The lightest key that stays is enclosed by counting the keys that reach
 // three values a round: first three of a sorted sample, then the quarters of the interval.  Once a CTA's threads can hold
 // the keys inside, one each, they are gathered and the rest is counted by barriers; it ends when exactly the
-// wanted number of keys reaches the lower bound, or the interval is one key (17 rounds at most whatever the keys).
+// wanted number of keys reaches the lower bound, or the interval is one key (18 rounds at most whatever the keys: the one of the
+// sample, which may cut off a single key, and 17 quarterings of 2^32).
 // Then the indices are written in order.  Counting needs two instructions a key and value (a histogram in shared memory
 // was 1.5 times slower: scores crowd into few bins); the three counts of a warp go through one integer reduction, CTAs of
 // a cluster exchange theirs over distributed shared memory.  Every warp owns a contiguous run of tokens, so the order of
-// the indices follows from counts per warp alone.  Bound by the latency of the rounds: 16 rows of 100000 tokens 35 us (of a
-// cluster 4000 cycles a round, 5 rounds instead of 13 for two bits of the key at a time), 2048 rows of 16 to 8192 tokens 35 us.
+// the indices follows from counts per warp alone.  Bound by the latency of its steps.  16 rows of 100003 tokens, a cluster of 8
+// each, take 28 to 30 us: 8000 cycles until the keys are there, 3100 to sort the sample, 2 to 7 rounds over the cluster of
+// 3700 to 4900 (the exchange 1500 of them), 8000 to 11000 to gather the keys inside, 4 to 6 rounds within the CTA for 4000, 17000 to
+// write the indices.  2048 rows of 16 to 8192 tokens, a CTA each, 35 us.
+// (ptxas keeps the kernel to the 64 registers that two CTAs of 512 threads leave, at 108 to 136 bytes of spills.)
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(const EvictParams p)
 {

@@ -42,8 +42,8 @@ using pdkv::AttnSeq;
 using pdkv::AttnUnit;
 
 constexpr int kMaxRowTile = 64;    // rows of one work item
-// Rows from which the tile kernel takes a segment: 40000 tokens of 8 heads of 128 dims, 32 rows 57 us in the warp kernel,
-// 40 rows 82, 64 rows 58 in the tile kernel.
+// Rows from which the tile kernel takes a segment: 40000 tokens of 8 heads of 128 dims, 32 rows 54 us in the warp kernel and
+// 40 rows 82, in the tile kernel 33 to 64 rows 48 to 49.
 constexpr int kTileMinRows = 33;
 
 constexpr int32_t kMaxTokens = 1 << 30;   // of a sequence or prefix: positions and their next tiles stay below 2^31
