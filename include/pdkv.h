@@ -437,8 +437,9 @@ int pdkv_seqs_destroy(pdkv_seqs *seqs);
  * to the whole prefix and to own tokens t < len_r - (q_tokens - 1 - i) (the token's own
  * key is expected in the cache).  Query head h*G + g reads KV head h, G = num_q_heads /
  * num_kv_heads.  Logits are scale * q.k; sums, maxima and weights are held in 32 bits,
- * the weights are rounded to the pool's type for the product with V (off by half a step each; fp16 weights
- * under 2^-21 of a row's largest by up to 2^-32 of that).  A row with
+ * for the product with V the weights of more than 8 rows over a list of tokens (q_tokens * G, behind a prefix of all its
+ * sequences) are rounded to the pool's type: off by half a step each, fp16 weights under 2^-21 of a row's largest
+ * by up to 2^-32 of that.  Those of fewer rows are two numbers of that type.  A row with
  * nothing to attend to (or whose every logit is -infinity) gives zeros and lse =
  * -infinity.  Cached rows past a sequence's length are never read into a result,
  * whatever they hold, nor are tokens into the results of queries that do not attend to them. */

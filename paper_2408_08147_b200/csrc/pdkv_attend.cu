@@ -212,8 +212,10 @@ __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it
 // eight rows cost half the instructions and registers that they would cost as one side of sixteen.  P^T
 // changes from accumulator to operand layout by transposing its 8 x 8 tiles between lanes.
 // Base and sum of each row are kept in 32 bits; O is rescaled only when a maximum outgrew its base by
-// 2^8.  The weights are rounded to 16 bits for the product with V (one instruction takes no wider operand beside a
-// 16-bit V; see kLift); their sum is taken before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
+// 2^8.  An instruction takes no wider operand beside a 16-bit V: up to 8 rows the weights go into the product as two 16-bit
+// numbers, the second what the rounding to the first left (the tensor pipe has time: 32 x 2048 tokens 43.5 us either way, 256 small
+// requests 79 -> 82); with more rows, which its registers and products bound, they are rounded (see kLift).  Their sum is taken
+// before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
 // the loads of the next ones from being issued ahead: 40 rows of 256 dims 338 us, without 166).
 template <typename T, int DP, int KD, bool HIDES, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
@@ -379,7 +381,8 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                     }
                 }
         }
-        uint32_t w[2][NT][2];   // operand P^T
+        constexpr bool kTwo = NT == 1;
+        uint32_t w[2][NT][2], rest[2][2];   // operand P^T, and what its rounding left
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const float b0 = m[t][0] == -INFINITY ? 0.f : m[t][0], b1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
@@ -391,8 +394,12 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                     l[t][j & 1] += x;
                     z[h][t][j] = x;
                 }
-                w[h][t][0] = transpose8(pack<T>(z[h][t][0], z[h][t][1]));
-                w[h][t][1] = transpose8(pack<T>(z[h][t][2], z[h][t][3]));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t two = pack<T>(z[h][t][2 * j], z[h][t][2 * j + 1]);
+                    w[h][t][j] = transpose8(two);
+                    if (kTwo) rest[h][j] = transpose8(pack<T>(z[h][t][2 * j] - unpack<T>(two & 0xffffu), z[h][t][2 * j + 1] - unpack<T>(two >> 16)));
+                }
             }
         }
 #pragma unroll
@@ -403,6 +410,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                 load_matrices_trans(a, slice + v_at + h * 2048 + k / 4 * R::kSubBytes + v_chunk[k % 4]);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) multiply<T>(o[k][t], a, w[h][t][0], w[h][t][1]);
+                if (kTwo) multiply<T>(o[k][0], a, rest[h][0], rest[h][1]);
             }
         __syncwarp();
         if (lane == 0) mbar_arrive_many(&bar.empty[slot], kGroups);   // a slot is free after four arrivals

@@ -163,6 +163,12 @@ __device__ __forceinline__ float4 left_out(const AttnParams &p, const T *q, int6
     return sum;
 }
 
+template <typename T> __device__ __forceinline__ float unpack(uint32_t low)
+{
+    const uint16_t bits = (uint16_t)low;
+    return static_cast<float>(*reinterpret_cast<const T *>(&bits));
+}
+
 // 2^x, off by 2 units in the last place at most; 0 for -infinity.
 __device__ __forceinline__ float pow2(float x)
 {

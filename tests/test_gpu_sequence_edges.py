@@ -461,3 +461,26 @@ def test_the_default_stream_from_another_current_one():
             out, lse = c.attend(s.layer, s.q_t, stream=0)
             torch.cuda.default_stream().synchronize()
         check(s, out, lse, s.expect())
+
+
+@pytest.mark.parametrize("kw", [
+    dict(lens=[300, 41], G=8, D=64),
+    dict(lens=[300, 41], G=4, Q=2, D=128, layout=LAYER_MAJOR, block=128),
+    dict(lens=[700, 41], G=1, D=256, dtype="fp16"),
+    dict(lens=[300, 41], G=7, D=80, block=7),
+    dict(lens=[900, 300], G=3, D=128, dtype="fp16", prefix_len=[200], member=[0, -1]),
+    dict(lens=[5000], H=1, G=6, D=96),
+], ids=str)
+def test_weights_of_few_rows_keep_their_bits(kw):
+    """Up to 8 rows of a KV head: the weights go into the product with V as two 16-bit numbers, so that a weight is off by half a step of half
+    a step, and the result by little more than its own rounding (half a step)."""
+    s = Setup(q_scale=0.7, **kw)
+    out, _, _, e = s.expect()
+    with s.session() as c:
+        assert kernel_of_own_tokens(c) == 0 and (c.items()["row_end"] - c.items()["row_begin"]).max() <= 8
+        got = c.attend(s.layer, s.q_t)[0].double().cpu().numpy()
+    half = torch.finfo(s.dtype).eps / 2
+    rel = 2 * logit_error(e, s.D) + half * half + (e["n"] + 64) * 2.0 ** -23
+    tol = 1.01 * (rel[..., None] * e["mag"] + half * np.abs(out)) + (e["n"][..., None] * 2.0 ** -32 * e["v"][..., None] + 2.0 ** -25 if s.dtype == torch.float16 else 0)
+    over = (np.abs(got - out) / tol).max()
+    assert over <= 1
