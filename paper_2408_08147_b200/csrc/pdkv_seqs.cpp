@@ -745,6 +745,8 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         return PDKV_OK;
     } catch (const std::bad_alloc &) {
         return PDKV_ERR_NOMEM;
+    } catch (const std::length_error &) {
+        return PDKV_ERR_NOMEM;
     }
 }
 
@@ -841,6 +843,8 @@ int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int laye
         }
         return PDKV_OK;
     } catch (const std::bad_alloc &) {
+        return PDKV_ERR_NOMEM;
+    } catch (const std::length_error &) {
         return PDKV_ERR_NOMEM;
     }
 }
