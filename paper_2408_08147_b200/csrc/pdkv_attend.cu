@@ -652,6 +652,8 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     const int width = p.scores_in == p.scores_out ? len : p.max_len;
     if (begin >= width) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    // (a token that a row does not see weighs nothing even where the row's sum is NaN)
+    auto weight = [](float z, float e) { return z == -INFINITY ? 0.f : pow2(z - e); };
     for (int r0 = 0; r0 < R; r0 += kScoreRows) {
         const int n = min(kScoreRows, R - r0);
         __syncthreads();
@@ -672,10 +674,10 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
             for (int row = shared ? warp : 0; row < n; row += shared ? 4 : 1) {
                 const float4 v = *reinterpret_cast<const float4 *>(z + (int64_t)row * s.logit_stride);
                 const float e = lse[row];
-                sum.x += pow2(v.x - e);
-                sum.y += pow2(v.y - e);
-                sum.z += pow2(v.z - e);
-                sum.w += pow2(v.w - e);
+                sum.x += weight(v.x, e);
+                sum.y += weight(v.y, e);
+                sum.z += weight(v.z, e);
+                sum.w += weight(v.w, e);
             }
         }
     }

@@ -761,10 +761,18 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
                     float v[32];
                     tmem_load(v, tmem + ((uint32_t)(warp * 32) << 16) + b * columns + col);
                     tmem_load_wait();
-                    if (masked || col + 32 > rows) {   // (columns past the last row hold anything, or products of zeros, NaN for an infinite K)
+                    if (masked || col + 32 > rows) {
+                        // Columns past the last row hold anything, or products of zeros, NaN for an infinite K; a token that a row
+                        // does not see weighs nothing even where the row's sum is NaN.
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (col + k >= rows || t >= sees[col + k]) v[k] = -INFINITY;
+                        for (int k = 0; k < 32; ++k) {
+                            const float x = pow2(fmaf(v[k], scale, lse[col + k]));
+                            if (k % 2)
+                                sums[0].y += col + k >= rows || t >= sees[col + k] ? 0.f : x;
+                            else
+                                sums[0].x += col + k >= rows || t >= sees[col + k] ? 0.f : x;
+                        }
+                        continue;
                     }
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) {

@@ -484,3 +484,30 @@ def test_weights_of_few_rows_keep_their_bits(kw):
     tol = 1.01 * (rel[..., None] * e["mag"] + half * np.abs(out)) + (e["n"][..., None] * 2.0 ** -32 * e["v"][..., None] + 2.0 ** -25 if s.dtype == torch.float16 else 0)
     over = (np.abs(got - out) / tol).max()
     assert over <= 1
+
+
+@pytest.mark.parametrize("kernel,kw", [(0, dict(lens=[90, 33], G=2, Q=4, D=64)), (0, dict(lens=[90, 33], G=7, Q=3, D=80, block=7)),
+                                       (1, dict(lens=[700, 260], G=12, Q=4, D=64)), (1, dict(lens=[700, 260], H=1, G=3, Q=100, D=128, block=32))], ids=str)
+def test_weights_of_queries_that_are_nan(kernel, kw):
+    """A query of NaN gives NaN to the tokens it sees, and nothing to those behind it."""
+    s = Setup(**kw)
+    before, scores = scores_like(s)
+    want = s.expect()
+    for r, i, hq, dims in ((0, 0, 0, slice(None)), (len(s.lens) - 1, 1, s.H * s.G - 1, 3)):
+        s.q_t[r, i, hq, dims] = float("nan")
+        want[0][r, i, hq] = want[1][r, i, hq] = np.nan
+        want[2][r][hq // s.G, i * s.G + hq % s.G, :s.lens[r] - (s.Q - 1 - i)] = np.nan
+    with s.session() as c:
+        assert kernel_of_own_tokens(c) == kernel
+        out, lse = c.attend(s.layer, s.q_t, scores_t=scores)
+        c.status()
+    assert (torch.isnan(out).cpu().numpy() == np.isnan(want[0])).all() and (torch.isnan(lse).cpu().numpy() == np.isnan(want[1])).all()
+    assert torch.isnan(out).any() and not torch.isnan(out).all()
+    got = scores.double().cpu().numpy()
+    for r, n in enumerate(s.lens):
+        add = want[2][r].sum(1)
+        assert (np.isnan(got[r, :, :n]) == np.isnan(add)).all()
+        assert np.isnan(add).any() and not np.isnan(add).all()
+        # (the errors of test_scores are far below this)
+        fin = ~np.isnan(add)
+        assert (np.abs(got[r, :, :n][fin] - before[r, :, :n][fin] - add[fin]) <= 1e-4 * (1 + add[fin])).all()
