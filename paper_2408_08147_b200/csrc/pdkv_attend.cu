@@ -216,7 +216,7 @@ __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it
 // numbers, the second what the rounding to the first left (the tensor pipe has time: 32 x 2048 tokens 43.5 us either way, 256 small
 // requests 79 -> 82); with more rows, which its registers and products bound, they are rounded (see kLift).  Their sum is taken
 // before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
-// the loads of the next ones from being issued ahead: 40 rows of 256 dims 338 us, without 166).
+// the loads of the next ones from being issued ahead: 40 rows of 256 dims 338 us, without 165).
 template <typename T, int DP, int KD, bool HIDES, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
                                             float (*sml)[16][2], volatile uint32_t *wild, RingBarriers &bar, uint32_t n, bool &dead)
@@ -499,8 +499,8 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 // the rest of them along the tokens.
 // Bound by memory up to 16 rows: 32 sequences of 2048 tokens, 8 heads of 128 dims, 4 rows each 43.6 us (6.2 TB/s of K and V),
 // 2 sequences of about 110000 tokens, 8 rows each, 6.4 TB/s.  Above, by the products of the four warps, or eight, of an SM
-// (64 rows of 256 dims over 40000 tokens 170 us, 8 rows 61; ptxas spills 130 to 190 bytes in the variants for 96, 128 and 256 dims).  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
-// them busy for 9% of the time.
+// (64 rows of 256 dims over 40000 tokens 169 us, 8 rows 60; ptxas spills 130 to 190 bytes in the variants for 96, 128 and 256 dims).  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
+// them busy for 13% of the time.
 template <typename T, int DP, int KD, bool HIDES>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {

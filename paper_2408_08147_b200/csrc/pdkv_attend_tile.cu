@@ -17,7 +17,7 @@
 // Bound by the tensor core and by the chain S, P, O of a row tile: 256 rows against 128 tokens of 128 dims take it
 // 3024 cycles (125 for 16 dims of Q K^T, whose two operands come from shared memory at 64 bytes a cycle, 64 for 16 tokens
 // of P V), and an iteration takes 3700.  Measured on B200, whole calls: 64 rows of each of 8 heads against 65536 tokens
-// 70 us (3.9 TB/s), 256 rows 101 us (680 TFLOP/s), 512 rows against 200000 tokens 453 us (925 TFLOP/s).  (A row of S does not
+// 70 us (3.8 TB/s), 256 rows 102 us (670 TFLOP/s), 512 rows against 200000 tokens 438 to 453 us (925 to 958 TFLOP/s).  (A row of S does not
 // quite fit: ptxas spills 240 bytes a thread.)  Starting and finishing an
 // item costs about 8 us, which is what short lists pay (256 rows against 4096 tokens: 26 us).
 #include <algorithm>
@@ -621,8 +621,8 @@ template <int DP> constexpr uint32_t weigh_bytes(int rows)
 // S^T = K Q^T: a thread has one token and its logits of all rows in tensor memory, so the sum over the
 // rows needs no other thread.  Six warps: four compute weights, one issues the products, one the loads of K;
 // two tiles of K and two of S^T are on their way.  Two CTAs on an SM up to 128 rows.  12 sequences of 300 to 4096
-// tokens, 64 rows each, 8 heads of 128 dims take 27 us as a kernel alone, of which the bytes of K need 9 and the exponentials 3 (16
-// a cycle and SM); the tensor pipe is active for 8%, DRAM for 24%.  So latency bounds it: a CTA starts (Q, sums of the rows) for a
+// tokens, 64 rows each, 8 heads of 128 dims take 27 us as a kernel alone (cold), of which the bytes of K need 9 and the exponentials 3 (16
+// a cycle and SM); the tensor pipe is active for 8%, DRAM for 25%.  So latency bounds it: a CTA starts (Q, sums of the rows) for a
 // handful of tiles, and ragged lists leave a few CTAs for a second wave.
 template <typename T, int DP>
 __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)

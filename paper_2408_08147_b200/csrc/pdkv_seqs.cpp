@@ -42,7 +42,7 @@ using pdkv::AttnSeq;
 using pdkv::AttnUnit;
 
 constexpr int kMaxRowTile = 64;    // rows of one work item
-// Rows from which the tile kernel takes a segment: 40000 tokens of 8 heads of 128 dims, 32 rows 54 us in the warp kernel and
+// Rows from which the tile kernel takes a segment: 40000 tokens of 8 heads of 128 dims, 32 rows 52 to 54 us in the warp kernel and
 // 40 rows 82, in the tile kernel 33 to 64 rows 48 to 49.
 constexpr int kTileMinRows = 33;
 
