@@ -568,7 +568,7 @@ int pdkv_seqs_status(const pdkv_seqs *s, void *stream)
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaMemcpyAsync");
     if (v == 0) return PDKV_OK;
-    // reported once: the calls that follow are judged by themselves
+    // reported once: it says nothing about the calls that follow
     e = cudaMemsetAsync(s->d_status, 0, sizeof v, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     return e == cudaSuccess ? PDKV_ERR_DEVICE_BOUNDS : pdkv::report_cuda_error(e, "cudaMemsetAsync");

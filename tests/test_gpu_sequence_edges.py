@@ -16,7 +16,7 @@ def not_given_away(make):
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        torch.cuda._sleep(400_000_000)      # a fifth of a second
+        torch.cuda._sleep(1_000_000_000)    # half a second
     mine = make(side)
     lost = [(t.data_ptr(), t.numel() * t.element_size()) for t in mine]
     assert all(n > 0 for _, n in lost)
