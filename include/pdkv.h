@@ -476,6 +476,63 @@ int pdkv_attend_scratch(const pdkv_seqs *seqs, int with_scores, size_t *bytes);
 int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, void *scratch, size_t scratch_bytes,
                 void *stream);
 
+/* Rotation of query and key heads by position, over one or several axes (text; time, height and width of images and video). */
+typedef struct {
+    int32_t dims;                  /* dims that turn, the first of a head; even, at most head_dim; 0: none */
+    int32_t adjacent;              /* pairs 0: (i, i + dims / 2), 1: (2i, 2i + 1) */
+    int32_t n_axes;                /* rows of positions */
+    const uint64_t *turns;         /* device [dims / 2]: what a pair turns by per position, in 2^-64 turns (pdkv_rotary_turns()) */
+    const uint8_t *axis;           /* device [dims / 2], with n_axes > 1: whose position turns the pair (the last axis for larger entries) */
+    float scale;                   /* factor of the dims that turn */
+} pdkv_rotary;
+/* Host only: angles per position in radians as fractions of a turn.  An angle, position * turns, is off by 2^-32 of a turn at most,
+ * whatever the position, for angles of up to a turn per position (2^-32 for each turn above).  Errors: INVALID_ARG (an angle that is not finite). */
+int pdkv_rotary_turns(const double *radians, int n, uint64_t *turns);
+
+/* Append: the new tokens of a batch enter the cache.  Row i of sequence r's new tokens becomes own token len_r - n_r + i (len_r counts the
+ * new ones, n_r are there), in the pages of its table: its keys and values in `layer`, its queries in q_out.  On the way queries and
+ * keys are normalised head by head, x * w / sqrt(mean x^2 + eps), where a weight is given, then rotated, (a, b) -> (a cos - b sin,
+ * b cos + a sin) * scale; values are copied.  All in 32 bits, rounded once.  Other cached tokens stay as they are, and so do rows of q_out that
+ * are not tokens; a token without a place (len_r < n_r) enters no page.  A block that receives tokens has to belong to one sequence.
+ * 2-byte pools with a head_dim as for attention; the handle's dtype is the type of everything but the norms' weights. */
+typedef struct {
+    int32_t rows;                  /* of q, k and v */
+    const int32_t *row_begin;      /* device [n_seq + 1]: sequence r has rows [row_begin[r], row_begin[r + 1]), ascending.
+                                      NULL: rows / n_seq of each, one sequence after the other */
+    const int32_t *n_new;          /* device [n_seq], with row_begin NULL: only the first n_new[r] rows of a sequence are tokens; NULL: all */
+    const int32_t *seq_len;        /* device [n_seq] own lengths with the new tokens, or NULL: those of the handle; clamped as for attention */
+    const void *q;                 /* device [row][num_q_heads][head_dim], or NULL: keys and values alone */
+    const void *k, *v;             /* device [row][num_kv_heads][head_dim] */
+    void *q_out;                   /* as q; may equal it (same strides) */
+    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3];   /* elements between sequences (not with row_begin), rows of
+                                      one, heads; multiples of 8, dims adjacent, bases 16-byte aligned */
+    const float *q_norm, *k_norm;  /* device [head_dim], 16-byte aligned, or NULL: not normalised */
+    float norm_eps;
+    const int32_t *position;       /* device [n_axes][row], rows in their order; NULL (one axis): that of the token, from the prefix' first */
+    int64_t position_stride;       /* entries between axes */
+    pdkv_rotary rotary;
+} pdkv_append_args;
+/* Enqueues only (recordable as pdkv_attend()); no scratch.  What it writes must not overlap what it reads nor one another, but for q_out
+ * equal to q.  Errors: INVALID_ARG, GEOMETRY, LIMIT (more rows than a launch takes), CUDA. */
+int pdkv_append(const pdkv_seqs *seqs, int layer, const pdkv_append_args *args, void *stream);
+
+/* Accept: of a sequence's n newest tokens (a drafted tree) those on the path stay.  Path entries 0 <= p_0 < p_1 < ... < n; the path ends at its
+ * length or before the first entry that breaks that (-1, say).  Own token len - n + p_j becomes own token len - n + j, bit for bit,
+ * in layers [layer_begin, layer_end); the length becomes len - n + accepted.  Everything else in the pool stays as it is.  Pools of any
+ * elem_bytes; the blocks of the newest tokens have to belong to one sequence. */
+typedef struct {
+    const int32_t *path;           /* device [n_seq][path_len] */
+    int64_t path_stride;           /* entries between sequences */
+    int32_t path_len;
+    int32_t new_tokens;            /* newest tokens of a sequence */
+    const int32_t *n_new;          /* device [n_seq], clamped to [0, new_tokens]; NULL: new_tokens */
+    const int32_t *seq_len;        /* device [n_seq], or NULL (as for pdkv_attend) */
+    int32_t *new_len;              /* device [n_seq], or NULL.  May equal seq_len */
+} pdkv_accept_args;
+/* Enqueues only (recordable as pdkv_attend()); no scratch.  Overlaps are refused as for pdkv_evict().
+ * Errors: INVALID_ARG, LIMIT (longer rows than a launch takes), CUDA. */
+int pdkv_accept(const pdkv_seqs *seqs, int layer_begin, int layer_end, const pdkv_accept_args *args, void *stream);
+
 /* Eviction by accumulated attention weight, per (layer, sequence, KV head), over layers
  * [layer_begin, layer_end).  With len tokens and `budget`: len <= budget keeps all of them;
  * otherwise the first `sink` tokens, the last `recent` ones and the budget - sink - recent

@@ -89,3 +89,54 @@ def move(src, src_layout, src_block, src_tbl, dst, dst_layout, dst_block, dst_tb
                 dst[b, layer, kv, j % dst_block, head] = row
             else:
                 dst[layer, kv, b, head, j % dst_block] = row
+
+
+def turned(x, weight, eps, position, frequencies, dims, adjacent, axes=None, scale=1.0):
+    """One head row of queries or keys, normalised (``weight`` not None) and rotated; ``position``: one number, or one for each axis.  Also the
+    magnitude of what each result is a sum of."""
+    y = np.array(x, np.float64)
+    if weight is not None:
+        y = y * weight / np.sqrt(np.mean(y * y) + eps)
+    out, mag = y.copy(), np.abs(y)
+    for i in range(dims // 2):
+        a, b = (2 * i, 2 * i + 1) if adjacent else (i, i + dims // 2)
+        p = position if axes is None else position[axes[i]]
+        # (the product in whole turns: 64 bits lose the angle of a far position)
+        angle = float(np.longdouble(p) * np.longdouble(frequencies[i]) % (2 * np.longdouble("3.14159265358979323846264338327950288")))
+        c, s = np.cos(angle), np.sin(angle)
+        out[a], out[b] = scale * (y[a] * c - y[b] * s), scale * (y[b] * c + y[a] * s)
+        mag[a] = mag[b] = abs(scale) * (abs(y[a]) + abs(y[b]))
+    return out, mag
+
+
+def place(pool, layout, block, layer, kv, tbl, slot, rows):
+    """Stores ``rows`` [head, dim] as token ``slot`` of the sequence with block ids ``tbl``."""
+    b, tt = int(tbl[slot // block]), slot % block
+    if layout == BLOCK_MAJOR:
+        pool[b, layer, kv, tt] = rows
+    else:
+        pool[layer, kv, b, :, tt] = rows
+
+
+def accept(pool, layout, block, seqs, lens, news, paths, layers):
+    """Moves the accepted tokens of ``pool`` in place; returns the new lengths."""
+    src = pool.copy()
+    out = []
+    for r, (n, m) in enumerate(zip(lens, news)):
+        first, last, count = int(n) - int(m), -1, 0
+        tbl = seqs.tbl[seqs.tbl_off[r]:seqs.tbl_off[r + 1]]
+        for j, x in enumerate(paths[r]):
+            if not last < x < m:
+                break
+            last, count = int(x), j + 1
+            if first + j < 0:
+                continue
+            a, b = first + last, first + j
+            for layer in range(*layers):
+                for kv in (0, 1):
+                    if layout == BLOCK_MAJOR:
+                        pool[int(tbl[b // block]), layer, kv, b % block] = src[int(tbl[a // block]), layer, kv, a % block]
+                    else:
+                        pool[layer, kv, int(tbl[b // block]), :, b % block] = src[layer, kv, int(tbl[a // block]), :, a % block]
+        out.append(max(0, first + count))
+    return out

@@ -47,6 +47,7 @@ EXPORTS = (
     "pdkv_sm_partition_create", "pdkv_sm_partition_info", "pdkv_sm_partition_stream", "pdkv_sm_partition_destroy",
     "pdkv_transfer_copies",
     "pdkv_seqs_create", "pdkv_seqs_destroy", "pdkv_seqs_items", "pdkv_seqs_status", "pdkv_attend_scratch", "pdkv_attend", "pdkv_evict",
+    "pdkv_rotary_turns", "pdkv_append", "pdkv_accept",
 )
 
 
@@ -87,6 +88,24 @@ class pdkv_attend_args(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64 * 3), ("out", C.c_void_p), ("out_stride", C.c_int64 * 3),
                 ("lse", C.c_void_p), ("scale", C.c_float), ("seq_len", C.c_void_p), ("scores_in", C.c_void_p),
                 ("scores_out", C.c_void_p), ("scores_in_stride", C.c_int64 * 2), ("scores_out_stride", C.c_int64 * 2)]
+
+
+class pdkv_rotary(C.Structure):
+    _fields_ = [("dims", C.c_int32), ("adjacent", C.c_int32), ("n_axes", C.c_int32), ("turns", C.c_void_p),
+                ("axis", C.c_void_p), ("scale", C.c_float)]
+
+
+class pdkv_append_args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("row_begin", C.c_void_p), ("n_new", C.c_void_p), ("seq_len", C.c_void_p),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("q_out_stride", C.c_int64 * 3), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("norm_eps", C.c_float),
+                ("position", C.c_void_p), ("position_stride", C.c_int64), ("rotary", pdkv_rotary)]
+
+
+class pdkv_accept_args(C.Structure):
+    _fields_ = [("path", C.c_void_p), ("path_stride", C.c_int64), ("path_len", C.c_int32), ("new_tokens", C.c_int32),
+                ("n_new", C.c_void_p), ("seq_len", C.c_void_p), ("new_len", C.c_void_p)]
 
 
 class pdkv_evict_args(C.Structure):
@@ -166,6 +185,9 @@ def lib() -> C.CDLL:
     L.pdkv_seqs_status.argtypes = [vp, vp]
     L.pdkv_attend_scratch.argtypes = [vp, C.c_int, C.POINTER(C.c_size_t)]
     L.pdkv_attend.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), vp, C.c_size_t, vp]
+    L.pdkv_rotary_turns.argtypes = [vp, C.c_int, vp]
+    L.pdkv_append.argtypes = [vp, C.c_int, C.POINTER(pdkv_append_args), vp]
+    L.pdkv_accept.argtypes = [vp, C.c_int, C.c_int, C.POINTER(pdkv_accept_args), vp]
     L.pdkv_evict.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(pdkv_evict_args), vp]
     for name in EXPORTS:
         if name not in ("pdkv_pool_bytes", "pdkv_strerror"):
@@ -507,6 +529,26 @@ def pdkv_attend(seqs: int, layer: int, args: pdkv_attend_args, scratch_ptr: int,
     rc = (_lib or lib()).pdkv_attend(seqs, layer, C.byref(args), scratch_ptr, scratch_bytes, stream)
     if rc != PDKV_OK:
         raise PdkvError(rc, "pdkv_attend")
+
+
+def pdkv_rotary_turns(radians) -> np.ndarray:
+    """Angles per position in radians as uint64 fractions of a turn."""
+    x = np.ascontiguousarray(radians, np.float64).reshape(-1)
+    out = np.zeros(x.shape, np.uint64)
+    _check(lib().pdkv_rotary_turns(x.ctypes.data, x.shape[0], out.ctypes.data), "pdkv_rotary_turns")
+    return out
+
+
+def pdkv_append(seqs: int, layer: int, args: pdkv_append_args, stream: int = 0) -> None:
+    rc = (_lib or lib()).pdkv_append(seqs, layer, C.byref(args), stream)
+    if rc != PDKV_OK:
+        raise PdkvError(rc, "pdkv_append")
+
+
+def pdkv_accept(seqs: int, layer_begin: int, layer_end: int, args: pdkv_accept_args, stream: int = 0) -> None:
+    rc = (_lib or lib()).pdkv_accept(seqs, layer_begin, layer_end, C.byref(args), stream)
+    if rc != PDKV_OK:
+        raise PdkvError(rc, "pdkv_accept")
 
 
 def pdkv_evict(seqs: int, dst: int, layer_begin: int, layer_end: int, args: pdkv_evict_args, stream: int = 0) -> None:

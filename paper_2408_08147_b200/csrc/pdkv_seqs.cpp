@@ -8,6 +8,7 @@
 #include <new>
 #include <stdexcept>
 
+#include "pdkv_checks.h"
 #include "pdkv_seqs.h"
 
 namespace pdkv {
@@ -40,86 +41,18 @@ using pdkv::AttnItem;
 using pdkv::AttnSeg;
 using pdkv::AttnSeq;
 using pdkv::AttnUnit;
+using pdkv::aligned;
+using pdkv::kMaxTokens;
+using pdkv::log2_of;
+using pdkv::meet;
+using pdkv::ranges_overlap;
+using pdkv::Rows;
+using pdkv::rows_apart;
 
 constexpr int kMaxRowTile = 64;    // rows of one work item
 // Rows from which the tile kernel takes a segment: 40000 tokens of 8 heads of 128 dims, 32 rows 52 to 54 us in the warp kernel and
 // 40 rows 82, in the tile kernel 33 to 64 rows 48 to 49.
 constexpr int kTileMinRows = 33;
-
-constexpr int32_t kMaxTokens = 1 << 30;   // of a sequence or prefix: positions and their next tiles stay below 2^31
-
-bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
-{
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return a_bytes && b_bytes && a0 < b0 + b_bytes && b0 < a0 + a_bytes;
-}
-
-// Rows of memory of one length at base + sum of i * stride, from `base` to before `end` (nothing where base is null).
-struct Rows {
-    uintptr_t base = 0, end = 0;
-    int64_t bytes = 0, stride[3] = {0, 0, 0}, n[3] = {1, 1, 1};
-    Rows(const void *p, int64_t row_bytes) : base(reinterpret_cast<uintptr_t>(p)), end(base + (p ? row_bytes : 0)), bytes(row_bytes) {}
-    Rows(const void *p, int64_t row_len, int64_t elem, const int64_t *s, const int64_t *count, int axes) : Rows(p, row_len * elem)
-    {
-        for (int i = 0; i < axes; ++i) {
-            n[i] = count[i];
-            stride[i] = count[i] > 1 ? s[i] * elem : 0;
-            if (end > base) end = count[i] > 0 ? end + stride[i] * (count[i] - 1) : base;
-        }
-    }
-    std::vector<uintptr_t> starts() const
-    {
-        std::vector<uintptr_t> at;
-        at.reserve((size_t)(n[0] * n[1] * n[2]));
-        for (int64_t i = 0; i < n[0]; ++i)
-            for (int64_t j = 0; j < n[1]; ++j)
-                for (int64_t k = 0; k < n[2]; ++k) at.push_back(base + i * stride[0] + j * stride[1] + k * stride[2]);
-        std::sort(at.begin(), at.end());
-        return at;
-    }
-};
-
-// Do a row of `a` and one of `b` share a byte?  Row by row only where their spans meet (views of one buffer).
-bool meet(const Rows &a, const Rows &b)
-{
-    if (a.base >= b.end || b.base >= a.end || a.base == a.end || b.base == b.end) return false;
-    const std::vector<uintptr_t> x = a.starts(), y = b.starts();
-    for (size_t i = 0, j = 0; i < x.size() && j < y.size();) {
-        if (x[i] < y[j] + b.bytes && y[j] < x[i] + a.bytes) return true;
-        if (x[i] + a.bytes <= y[j])
-            ++i;
-        else
-            ++j;
-    }
-    return false;
-}
-
-bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-
-int32_t log2_of(int32_t n)
-{
-    for (int b = 0; b < 31; ++b)
-        if (n == 1 << b) return b;
-    return -1;
-}
-
-// Do rows of `len` entries at i0*s0 + i1*s1 + i2*s2 lie apart from one another?  Axes of one entry do
-// not count; the others have to nest (each stride spans everything inside it).
-bool rows_apart(int64_t len, const int64_t *stride, const int64_t *n, int axes)
-{
-    std::vector<std::pair<int64_t, int64_t>> ax;
-    for (int i = 0; i < axes; ++i) {
-        if (n[i] > 1) ax.emplace_back(stride[i], n[i]);
-        if (stride[i] < 0) return false;
-    }
-    std::sort(ax.begin(), ax.end());
-    int64_t span = len;
-    for (const auto &a : ax) {
-        if (a.first < span) return false;
-        span += a.first * (a.second - 1);
-    }
-    return true;
-}
 
 int check_lists(const int64_t *off, const int32_t *tbl, const int32_t *len, int32_t n, int64_t B, int64_t NB)
 {
@@ -418,7 +351,10 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *d, void *works
             }
             s->segs.push_back(seg);
         };
-        for (int32_t r = 0; r < d->n_seq; ++r) add(d->tbl_off, d->tbl, r, d->seq_len[r], r);
+        for (int32_t r = 0; r < d->n_seq; ++r) {
+            add(d->tbl_off, d->tbl, r, d->seq_len[r], r);
+            if (d->n_prefix > 0 && d->seq_prefix[r] >= 0) s->segs.back().before = d->prefix_len[d->seq_prefix[r]];
+        }
         for (int32_t p = 0; p < d->n_prefix; ++p) add(d->prefix_tbl_off, d->prefix_tbl, p, d->prefix_len[p], -1);
 
         std::vector<int32_t> members;

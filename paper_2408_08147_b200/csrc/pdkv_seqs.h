@@ -21,7 +21,7 @@ struct AttnSeg {
     int32_t len;
     int32_t seq;            // own tokens: the sequence; prefix: -1
     int32_t member_begin;   // prefix: its sequences are members[member_begin ..)
-    int32_t pad;
+    int32_t before;         // own tokens: tokens of the prefix in front of them
 };
 
 // (segment, row tile, KV head): the rows whose parts are joined.

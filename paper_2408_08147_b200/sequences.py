@@ -70,6 +70,37 @@ class Sequences:
         return int(self.seq_len.max()) if self.n_seq else 0
 
 
+class Rotary:
+    """Rotation of heads by position (see ``pdkv_rotary``), laid out once on the device.
+
+    ``dims`` of a head turn, from the first; ``frequencies`` are radians per position, one for each pair of dims (default:
+    ``base ** (-2 i / dims)``).  ``adjacent``: pairs ``(2i, 2i + 1)`` instead of ``(i, i + dims / 2)``.  ``axes``: the axis whose position
+    turns each pair, for positions in time, height and width (``np.repeat(range(3), (16, 24, 24))``).  ``scale``: factor of the dims that turn.
+    """
+
+    def __init__(self, dims: int, *, base: float = 10000.0, frequencies=None, adjacent: bool = False, axes=None, scale: float = 1.0, device="cuda"):
+        if dims < 2 or dims % 2:
+            raise ValueError(f"dims: expected an even number of at least 2, got {dims}")
+        pairs = dims // 2
+        if frequencies is None:
+            frequencies = float(base) ** (-np.arange(pairs, dtype=np.float64) / pairs)
+        frequencies = np.asarray(frequencies, np.float64)
+        if frequencies.shape != (pairs,):
+            raise ValueError(f"frequencies: expected {pairs}, got the shape {frequencies.shape}")
+        self.dims, self.adjacent, self.scale, self.n_axes = dims, bool(adjacent), float(scale), 1
+        self.turns_t = torch.from_numpy(B.pdkv_rotary_turns(frequencies).view(np.int64)).to(device)
+        self.axis_t = None
+        if axes is not None:
+            axes = np.asarray(axes, np.int64)
+            if axes.shape != (pairs,) or axes.min() < 0 or axes.max() > 255:
+                raise ValueError(f"axes: expected {pairs} axes from 0 to 255")
+            self.n_axes = int(axes.max()) + 1
+            self.axis_t = torch.from_numpy(axes.astype(np.uint8)).to(device)
+        self.desc = B.pdkv_rotary(dims=dims, adjacent=int(self.adjacent), n_axes=self.n_axes, turns=self.turns_t.data_ptr(),
+                                  axis=self.axis_t.data_ptr() if self.n_axes > 1 else None, scale=self.scale)
+        self.device = self.turns_t.device
+
+
 class CacheSession:
     """Pool handle + sequence handle of one batch.
 
@@ -231,6 +262,114 @@ class CacheSession:
             self._record(stream, *made)
         B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, stream)
         return out_t, lse_t
+
+    def _heads(self, name, t, lead, heads, out):
+        """Strides between sequences, rows and heads of a tensor [*lead, heads, head_dim]."""
+        D = self._shape[3]
+        if t.dtype != self.dtype or t.shape != (*lead, heads, D) or t.device != self._device:
+            raise ValueError(f"{name}: expected {self.dtype} {(*lead, heads, D)} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if not out and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name}: entering a cache has no gradient; detach it or call under torch.no_grad()")
+        stride = t.stride()
+        if D > 1 and stride[-1] != 1:
+            raise ValueError(f"{name}: the dims of a head have to be adjacent")
+        return stride[:3] if len(lead) == 2 else (0, *stride[:2])
+
+    def _ints(self, name, t, shape):
+        """Device address of a dense int32 tensor."""
+        if t is None:
+            return None
+        self._check(name, t, torch.int32, shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} has to be contiguous")
+        return t.data_ptr()
+
+    def append(self, layer: int, k_t, v_t, q_t=None, *, q_out_t=None, rotary: Optional[Rotary] = None, position_t=None, q_norm_t=None,
+               k_norm_t=None, eps: float = 1e-6, seq_len_t=None, n_new_t=None, row_begin_t=None, stream: Optional[int] = None):
+        """New tokens enter the cache of one layer.  ``k_t`` and ``v_t`` are ``[n_seq, new, num_kv_heads, head_dim]`` (of which the first
+        ``n_new_t[r]`` count), or ``[rows, num_kv_heads, head_dim]`` with the sequences' rows one after the other at ``row_begin_t``
+        (int32 ``[n_seq + 1]``); any strides with adjacent dims.  The lengths (the session's, or ``seq_len_t``) count the new tokens, which become
+        the last ones.  ``q_t`` (as ``k_t``, with the query heads) is returned normalised and rotated, in ``q_out_t`` (which may be ``q_t``).
+        Keys and queries are divided by their root mean square and multiplied by ``k_norm_t`` / ``q_norm_t`` (float32 ``[head_dim]``) where
+        given, then turned by ``rotary`` at ``position_t`` (int32, one for each row, ``[axes, rows]`` for several axes; default: where the token
+        stands behind its prefix).  There is no backward pass."""
+        lead = tuple(k_t.shape[:-2])
+        packed = row_begin_t is not None
+        if len(lead) != (1 if packed else 2) or (not packed and lead[0] != self._shape[0]):
+            raise ValueError(f"k_t: expected {'[rows, ' if packed else f'[{self._shape[0]}, new, '}heads, dims], got {tuple(k_t.shape)}")
+        rows = lead[0] if packed else lead[0] * lead[1]
+        heads = self.geom.num_kv_heads
+        a = B.pdkv_append_args(rows=rows, k=k_t.data_ptr(), v=v_t.data_ptr(), k_stride=self._heads("k_t", k_t, lead, heads, False),
+                               v_stride=self._heads("v_t", v_t, lead, heads, False))
+        made = None
+        if q_t is not None:
+            if not self.num_q_heads:
+                raise ValueError("q_t: the session has no query heads")
+            a.q, a.q_stride = q_t.data_ptr(), self._heads("q_t", q_t, lead, self.num_q_heads, False)
+            if q_out_t is None:
+                q_out_t = made = torch.empty(q_t.shape, dtype=self.dtype, device=self._device)
+            a.q_out, a.q_out_stride = q_out_t.data_ptr(), self._heads("q_out_t", q_out_t, lead, self.num_q_heads, True)
+        elif q_out_t is not None:
+            raise ValueError("q_out_t needs q_t")
+        n_seq, D = self._shape[0], self._shape[3]
+        if packed:
+            a.row_begin = self._ints("row_begin_t", row_begin_t, (n_seq + 1,))
+            if n_new_t is not None:
+                raise ValueError("n_new_t does not go with row_begin_t")
+        if n_new_t is not None:
+            a.n_new = self._ints("n_new_t", n_new_t, (n_seq,))
+        if seq_len_t is not None:
+            a.seq_len = self._lens(seq_len_t)
+        if q_norm_t is not None or k_norm_t is not None:
+            for name, t in (("q_norm_t", q_norm_t), ("k_norm_t", k_norm_t)):
+                if t is not None:
+                    self._check(name, t, torch.float32, (D,))
+                    if D > 1 and t.stride(0) != 1:
+                        raise ValueError(f"{name} has to be contiguous")
+            a.q_norm = None if q_norm_t is None else q_norm_t.data_ptr()
+            a.k_norm = None if k_norm_t is None else k_norm_t.data_ptr()
+            a.norm_eps = eps
+        if rotary is not None:
+            if rotary.device != self._device:
+                raise ValueError(f"rotary: laid out on {rotary.device}, the pool is on {self._device}")
+            a.rotary = rotary.desc
+            if position_t is not None:
+                a.position = self._ints("position_t", position_t, (rotary.n_axes, rows) if rotary.n_axes > 1 else (rows,))
+                a.position_stride = rows
+            elif rotary.n_axes > 1:
+                raise ValueError("rotary: several axes need position_t")
+        elif position_t is not None:
+            raise ValueError("position_t needs rotary")
+        stream = self._on(stream)
+        if made is not None and stream != self._on_current():
+            self._record(stream, made)
+        B.pdkv_append(self.handle, layer, a, stream)
+        return q_out_t
+
+    def accept(self, path_t, *, n_new_t=None, new_tokens: Optional[int] = None, seq_len_t=None, new_len_t=None,
+               layers: Optional[Tuple[int, int]] = None, stream: Optional[int] = None):
+        """Of the newest tokens of each sequence (``new_tokens``, default: the session's ``q_tokens``; ``n_new_t[r]`` of them are there) those named by
+        ``path_t`` (int32 ``[n_seq, path]``, ascending, -1 behind the last) stay: their keys and values move to the place behind the tokens
+        before the newest, in all layers.  Returns the new lengths (``new_len_t`` may be ``seq_len_t``)."""
+        l0, l1 = (0, self.geom.num_layers) if layers is None else layers
+        if not 0 <= l0 < l1 <= self.geom.num_layers:
+            raise ValueError(f"layers: expected a range within [0, {self.geom.num_layers}), got {layers}")
+        n_seq = self._shape[0]
+        if path_t.dtype != torch.int32 or path_t.dim() != 2 or path_t.shape[0] != n_seq or path_t.device != self._device:
+            raise ValueError(f"path_t: expected int32 [{n_seq}, path] on {self._device}, got {path_t.dtype} {tuple(path_t.shape)} on {path_t.device}")
+        if path_t.shape[1] > 1 and path_t.stride(1) != 1:
+            raise ValueError("path_t: the entries of a path have to be adjacent")
+        made = None
+        if new_len_t is None:
+            new_len_t = made = path_t.new_empty((n_seq,))
+        a = B.pdkv_accept_args(path=path_t.data_ptr(), path_stride=path_t.stride(0), path_len=path_t.shape[1],
+                               new_tokens=self.q_tokens if new_tokens is None else new_tokens, n_new=self._ints("n_new_t", n_new_t, (n_seq,)),
+                               seq_len=self._ints("seq_len_t", seq_len_t, (n_seq,)), new_len=self._ints("new_len_t", new_len_t, (n_seq,)))
+        stream = self._on(stream)
+        if made is not None and stream != self._on_current():
+            self._record(stream, made)
+        B.pdkv_accept(self.handle, l0, l1, a, stream)
+        return new_len_t
 
     def evict(self, dst: "CacheSession", scores_t, budget: int, *, sink: int = 0, recent: int = 0,
               layers: Optional[Tuple[int, int]] = None, kept_t=None, kept_scores_t=None, new_len_t=None, seq_len_t=None,
