@@ -476,6 +476,26 @@ int pdkv_attend_scratch(const pdkv_seqs *seqs, int with_scores, size_t *bytes);
 int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, void *scratch, size_t scratch_bytes,
                 void *stream);
 
+/* Attention in another form than plain causal: any mask among the newest tokens, capped scores, a bias by
+ * distance; everything else is as for pdkv_attend() (plan, strides, scratch, scores, errors).  With `n` newest tokens of sequence r, query
+ * token i < n sees every token before them and, of the newest, those that its mask names (a drafted tree: its ancestors and
+ * itself; documents packed into a chunk; a prefix seen both ways).  Query tokens i >= n are not there: zeros, lse
+ * = -infinity, no weight in scores.  A logit is
+ *     z = scale * q.k,   cap * tanh(z / cap) where cap > 0,   + slopes[head] * (position of the key - of the query)
+ * Positions count from the first token of the prefix; the newest tokens' are len_r - n + offset. */
+typedef struct {
+    float cap;                     /* 0: none */
+    const float *slopes;           /* device [num_q_heads], finite; NULL: none */
+    const uint32_t *mask;          /* device: bit j % 32 of word j / 32 of (sequence, query token i): i sees newest token j; words of a query
+                                      token are adjacent, (q_tokens + 31) / 32 of them are read.  NULL: i sees j <= i */
+    int64_t mask_stride[2];        /* words between sequences (0: one mask for all), query tokens */
+    const int32_t *n_new;          /* device [n_seq] newest tokens, clamped to [0, q_tokens]; NULL: q_tokens of every sequence */
+    const int32_t *offset;         /* device: position of newest token j minus the first one's (a tree: its depth), for slopes; NULL: j */
+    int64_t offset_stride;         /* entries between sequences (0: the same for all); tokens are adjacent */
+} pdkv_attend_form;
+int pdkv_attend_formed(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, const pdkv_attend_form *form, void *scratch,
+                       size_t scratch_bytes, void *stream);
+
 /* Rotation of query and key heads by position, over one or several axes (text; time, height and width of images and video). */
 typedef struct {
     int32_t dims;                  /* dims that turn, the first of a head; even, at most head_dim; 0: none */

@@ -140,3 +140,64 @@ def accept(pool, layout, block, seqs, lens, news, paths, layers):
                         pool[layer, kv, int(tbl[b // block]), :, b % block] = src[layer, kv, int(tbl[a // block]), :, a % block]
         out.append(max(0, first + count))
     return out
+
+
+def attend_formed(pool, layout, block, layer, seqs, lens, q, num_kv_heads, scale, cap=0.0, slopes=None, see=None, news=None, offset=None):
+    """Attention in another form than plain causal: as :func:`attend`, with the terms by which cap and bias add to a logit's error scale.
+    ``see``: bool [n, Q, Q] (None: causal); ``news``: newest tokens of each sequence (None: Q); ``offset``: int [n, Q] (None: 0, 1, 2 ...)."""
+    n, Q, Hq, D = q.shape
+    G = Hq // num_kv_heads
+    out, lse = np.zeros(q.shape), np.full((n, Q, Hq), -np.inf)
+    mag = np.zeros(q.shape)
+    dot_mag, z_mag, seen_n, v_mag, form_mag = (np.zeros((n, Q, Hq)) for _ in range(5))
+    weights = []
+    for r in range(n):
+        own, m = int(lens[r]), Q if news is None else min(max(int(news[r]), 0), Q)
+        weights.append(np.zeros((num_kv_heads, Q * G, own)))
+        tbl = seqs.tbl[seqs.tbl_off[r]:seqs.tbl_off[r + 1]]
+        p = int(seqs.seq_prefix[r]) if seqs.seq_prefix is not None and seqs.prefix_len is not None else -1
+        first = int(seqs.prefix_len[p]) if p >= 0 else 0
+        place = np.arange(first + own)                                     # positions of the keys
+        for j in range(m):
+            if own - m + j >= 0:
+                place[first + own - m + j] = first + own - m + (j if offset is None else int(offset[r, j]))
+        for h in range(num_kv_heads):
+            k = token_rows(pool, layout, block, layer, 0, h, tbl, own)
+            v = token_rows(pool, layout, block, layer, 1, h, tbl, own)
+            if p >= 0:
+                ptbl = seqs.prefix_tbl[seqs.prefix_tbl_off[p]:seqs.prefix_tbl_off[p + 1]]
+                k = np.concatenate([token_rows(pool, layout, block, layer, 0, h, ptbl, first), k])
+                v = np.concatenate([token_rows(pool, layout, block, layer, 1, h, ptbl, first), v])
+            for i in range(m):
+                t = np.arange(first + own)
+                j = t - (first + own - m)
+                visible = np.array([jj < 0 or (jj <= i if see is None else bool(see[r, i, jj])) for jj in j], bool)
+                if not visible.any():
+                    continue
+                here = first + own - m + (i if offset is None else int(offset[r, i]))
+                for g in range(G):
+                    x = q[r, i, h * G + g]
+                    with np.errstate(invalid="ignore", over="ignore"):
+                        z0 = scale * (k[visible] @ x)
+                        z = cap * np.tanh(z0 / cap) if cap else z0
+                    bias = slopes[h * G + g] * (place[visible] - here) if slopes is not None else np.zeros(len(z))
+                    z = z + bias
+                    top = z.max()
+                    if top == -np.inf:
+                        continue
+                    w = np.exp(z - top)
+                    total = w.sum()
+                    w /= total
+                    out[r, i, h * G + g] = w @ v[visible]
+                    lse[r, i, h * G + g] = top + np.log(total)
+                    mag[r, i, h * G + g] = w @ np.abs(v[visible])
+                    fin = np.isfinite(z0)
+                    dot_mag[r, i, h * G + g] = abs(scale) * (np.abs(k[visible][fin]) @ np.abs(x)).max() if fin.any() else 0
+                    z_mag[r, i, h * G + g] = np.abs(z0[fin]).max() if fin.any() else 0
+                    form_mag[r, i, h * G + g] = np.abs(bias).max()
+                    v_mag[r, i, h * G + g] = np.abs(v[visible]).max()
+                    seen_n[r, i, h * G + g] = visible.sum()
+                    all_w = np.zeros(first + own)
+                    all_w[visible] = w
+                    weights[r][h, i * G + g] = all_w[first:]
+    return out, lse, weights, dict(mag=mag, dot=dot_mag, z=z_mag, n=seen_n, v=v_mag, bias=form_mag)

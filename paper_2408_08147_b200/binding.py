@@ -47,7 +47,7 @@ EXPORTS = (
     "pdkv_sm_partition_create", "pdkv_sm_partition_info", "pdkv_sm_partition_stream", "pdkv_sm_partition_destroy",
     "pdkv_transfer_copies",
     "pdkv_seqs_create", "pdkv_seqs_destroy", "pdkv_seqs_items", "pdkv_seqs_status", "pdkv_attend_scratch", "pdkv_attend", "pdkv_evict",
-    "pdkv_rotary_turns", "pdkv_append", "pdkv_accept",
+    "pdkv_attend_formed", "pdkv_rotary_turns", "pdkv_append", "pdkv_accept",
 )
 
 
@@ -88,6 +88,11 @@ class pdkv_attend_args(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64 * 3), ("out", C.c_void_p), ("out_stride", C.c_int64 * 3),
                 ("lse", C.c_void_p), ("scale", C.c_float), ("seq_len", C.c_void_p), ("scores_in", C.c_void_p),
                 ("scores_out", C.c_void_p), ("scores_in_stride", C.c_int64 * 2), ("scores_out_stride", C.c_int64 * 2)]
+
+
+class pdkv_attend_form(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("mask", C.c_void_p), ("mask_stride", C.c_int64 * 2),
+                ("n_new", C.c_void_p), ("offset", C.c_void_p), ("offset_stride", C.c_int64)]
 
 
 class pdkv_rotary(C.Structure):
@@ -185,6 +190,7 @@ def lib() -> C.CDLL:
     L.pdkv_seqs_status.argtypes = [vp, vp]
     L.pdkv_attend_scratch.argtypes = [vp, C.c_int, C.POINTER(C.c_size_t)]
     L.pdkv_attend.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), vp, C.c_size_t, vp]
+    L.pdkv_attend_formed.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), C.POINTER(pdkv_attend_form), vp, C.c_size_t, vp]
     L.pdkv_rotary_turns.argtypes = [vp, C.c_int, vp]
     L.pdkv_append.argtypes = [vp, C.c_int, C.POINTER(pdkv_append_args), vp]
     L.pdkv_accept.argtypes = [vp, C.c_int, C.c_int, C.POINTER(pdkv_accept_args), vp]
@@ -529,6 +535,13 @@ def pdkv_attend(seqs: int, layer: int, args: pdkv_attend_args, scratch_ptr: int,
     rc = (_lib or lib()).pdkv_attend(seqs, layer, C.byref(args), scratch_ptr, scratch_bytes, stream)
     if rc != PDKV_OK:
         raise PdkvError(rc, "pdkv_attend")
+
+
+def pdkv_attend_formed(seqs: int, layer: int, args: pdkv_attend_args, form: pdkv_attend_form, scratch_ptr: int, scratch_bytes: int,
+                       stream: int = 0) -> None:
+    rc = (_lib or lib()).pdkv_attend_formed(seqs, layer, C.byref(args), C.byref(form), scratch_ptr, scratch_bytes, stream)
+    if rc != PDKV_OK:
+        raise PdkvError(rc, "pdkv_attend_formed")
 
 
 def pdkv_rotary_turns(radians) -> np.ndarray:

@@ -174,10 +174,10 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
 
 // Adds what was left out of the products of an item (see left_out) to its results: a warp a row, the rows and dims that the
 // same thread has written.  A direct result has been rounded already, and such pieces of it are rounded twice.
-template <typename T>
+template <typename T, bool FORM>
 __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it, int len, int limit, const float (*sml)[16][2], int nt, int wm)
 {
-    const int lane = threadIdx.x % 32, safe = min(limit, len - (p.q_tokens - 1));
+    const int lane = threadIdx.x % 32, safe = min(limit, FORM ? len - newest_of(p, it.seq) : len - (p.q_tokens - 1));
     for (int r = threadIdx.x / 32; r < it.rows; r += 4) {
         const int w = r / (8 * nt), at = r % (8 * nt);
         float base = -INFINITY, sum = 0.f;
@@ -188,7 +188,11 @@ __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it
         const int h = it.head * p.G + id.g, to = min(limit, len - (p.q_tokens - 1 - id.token));
         const T *q = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + h * p.q_stride[2];
         for (int d = 4 * lane; d < p.D; d += 128) {
-            const float4 y = left_out<T>(p, q, it.tbl, it.head, max(safe, it.tok0), to, base, d);
+            float4 y;
+            if constexpr (FORM)
+                y = left_out_formed<T>(p, q, it, id, len, max(safe, it.tok0), limit, base, d);
+            else
+                y = left_out<T>(p, q, it.tbl, it.head, max(safe, it.tok0), to, base, d);
             if (it.direct) {
                 T *out = static_cast<T *>(p.out) + id.seq * p.out_stride[0] + id.token * p.out_stride[1] + h * p.out_stride[2] + d;
                 const float inv = 1.f / sum;
@@ -217,7 +221,10 @@ __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it
 // requests 79 -> 82); with more rows, which its registers and products bound, they are rounded (see kLift).  Their sum is taken
 // before that.  KD: steps of 16 dims; behind the last dim Q, K and V are zero (a step that is skipped at run time keeps
 // the loads of the next ones from being issued ahead: 40 rows of 256 dims 338 us, without 165).
-template <typename T, int DP, int KD, bool HIDES, int NT, int WM>
+//
+// FORM: another form than plain causal.  The logits, once they are there, become what the form says (capped, biased, hidden by the
+// rows' masks); from then on they are in base 2 and nothing else differs, but that a row may see nothing of what it is multiplied with.
+template <typename T, int DP, int KD, bool HIDES, bool FORM, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
                                             float (*sml)[16][2], volatile uint32_t *wild, RingBarriers &bar, uint32_t n, bool &dead)
 {
@@ -226,7 +233,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, wm = warp % WM, group = warp / WM;
     const bool own = it.seq >= 0;
     const uint32_t ring = smem_u32(smem);
-    const float scale = fabsf(p.scale_log2);
+    const float scale = FORM ? 1.f : fabsf(p.scale_log2);
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
 
     // operand Q^T: row lane / 4 of each tile of eight, dims 2 (lane % 4) and 8 further of each sixteen
@@ -249,6 +256,10 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     // accumulators: rows 2 (lane % 4) and the next of each tile of eight
     int sees[NT][2];
     float *logits[NT][2];
+    int n_new = 0;           // FORM, own tokens: the newest of the sequence
+    bool there[NT][2];       // FORM: the query token is one of them
+    Bias bias[NT][2];
+    if (FORM && own) n_new = newest_of(p, it.seq);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -257,15 +268,20 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             const bool live = r < it.rows;
             sees[t][j] = limit;
             logits[t][j] = nullptr;
+            if (FORM) {
+                const RowId id = row_id(p, it, it.row0 + (live ? r : 0));
+                there[t][j] = id.token < (own ? n_new : newest_of(p, id.seq));
+                bias[t][j] = bias_of(p, it, id, own ? len : own_len(p, id.seq, p.segs[id.seq].len));
+            }
             if (own) {
-                sees[t][j] = min(limit, len - (p.q_tokens - 1 - (it.row0 + (live ? r : 0)) / p.G));
+                if (!FORM) sees[t][j] = min(limit, len - (p.q_tokens - 1 - (it.row0 + (live ? r : 0)) / p.G));
                 if (p.logits && live) {
                     const AttnSeq s = p.seqs[it.seq];
                     logits[t][j] = p.logits + s.logits + ((int64_t)it.head * p.G * p.q_tokens + it.row0 + r) * s.logit_stride;
                 }
             }
         }
-    const int safe = own ? min(limit, len - (p.q_tokens - 1)) : limit;   // tokens before this one are seen by every row
+    const int safe = own ? min(limit, FORM ? len - n_new : len - (p.q_tokens - 1)) : limit;   // tokens before this one are seen by every row
     const bool with_logits = p.logits && own;
 
     float o[KD][NT][4];
@@ -335,7 +351,40 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 #pragma unroll
                 for (int t = 0; t < NT; ++t) multiply<T>(z[h][t], a, q[k][t][0], q[k][t][1]);
             }
-        if (t0 + kSlice > safe)
+        if constexpr (FORM) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const Bias b = bias[t][j & 1];
+                    const int first = t0 + lane / 4 + 8 * (j >> 1) - b.query;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float x = p.cap_out != 0.f ? capped(z[h][t][j], fabsf(p.cap_in), p.cap_out) : z[h][t][j] * fabsf(p.scale_log2);
+                        x = fmaf(b.slope, (float)(first + 16 * h), x);
+                        z[h][t][j] = there[t][j & 1] ? x : -INFINITY;
+                    }
+                }
+            if (own && t0 + kSlice > safe) {
+                const int from = t0 - (len - n_new);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int r = (wm * NT + t) * 8 + 2 * (lane % 4) + j, token = (it.row0 + min(r, it.rows - 1)) / p.G;
+                        const uint32_t seen = newest_seen(p, it.seq, token, n_new, from) >> (lane / 4);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {   // tokens lane / 4 + 8 x
+                            float &y = z[x / 2][t][x % 2 * 2 + j];
+                            if (!(seen >> (8 * x) & 1))
+                                y = -INFINITY;
+                            else if (p.offset && p.slopes && from + lane / 4 + 8 * x >= 0)   // its place is not its slot
+                                y = fmaf(bias[t][j].slope, (float)(offset_of(p, it.seq, from + lane / 4 + 8 * x) - (from + lane / 4 + 8 * x)), y);
+                        }
+                    }
+            }
+        }
+        if ((FORM ? limit : safe) < t0 + kSlice)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -472,6 +521,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
+                    if (FORM && lt == 0.f) break;   // a row that saw nothing: its products may be 0 * infinity
                     const float4 y = *reinterpret_cast<const float4 *>(xch + ((g * WM + w) * 8 + x % 8) * R::kXchRow + d);
                     v.x += f[g] * y.x;
                     v.y += f[g] * y.y;
@@ -488,7 +538,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
         consumer_sync();
     }
     if (HIDES && pieces_left_out) {
-        if (!dead) add_left_out<T>(p, it, len, limit, sml, NT, WM);
+        if (!dead) add_left_out<T, FORM>(p, it, len, limit, sml, NT, WM);
         consumer_sync();
     }
 }
@@ -501,7 +551,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 // 2 sequences of about 110000 tokens, 8 rows each, 6.4 TB/s.  Above, by the products of the four warps, or eight, of an SM
 // (64 rows of 256 dims over 40000 tokens 169 us, 8 rows 60; ptxas spills 130 to 190 bytes in the variants for 96, 128 and 256 dims).  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
 // them busy for 13% of the time.
-template <typename T, int DP, int KD, bool HIDES>
+template <typename T, int DP, int KD, bool HIDES, bool FORM>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
     using R = Ring<DP>;
@@ -544,13 +594,13 @@ __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel
             int len, limit;
             const int slices = slices_of(p, it, &len, &limit);
             if (it.rows <= 8)
-                attend_item<T, DP, KD, HIDES, 1, 1>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
+                attend_item<T, DP, KD, HIDES, FORM, 1, 1>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
             else if (it.rows <= 16)
-                attend_item<T, DP, KD, HIDES, 2, 1>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
+                attend_item<T, DP, KD, HIDES, FORM, 2, 1>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
             else if (it.rows <= 32)
-                attend_item<T, DP, KD, HIDES, 2, 2>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
+                attend_item<T, DP, KD, HIDES, FORM, 2, 2>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
             else
-                attend_item<T, DP, KD, HIDES, 2, 4>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
+                attend_item<T, DP, KD, HIDES, FORM, 2, 4>(p, it, slices, len, limit, smem, sml, &wild, bar, n, dead);
             n += slices;
             it = next_it;
         }
@@ -703,10 +753,10 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
 
 namespace {
 
-template <typename T, int DP, int KD, bool HIDES> cudaError_t launch_hides(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, int KD, bool HIDES, bool FORM> cudaError_t launch_hides(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(attend_items_kernel<T, DP, KD, HIDES>, Ring<DP>::kBytes, ready);
+    const cudaError_t e = allow_shared(attend_items_kernel<T, DP, KD, HIDES, FORM>, Ring<DP>::kBytes, ready);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.n_ctas);
@@ -718,14 +768,15 @@ template <typename T, int DP, int KD, bool HIDES> cudaError_t launch_hides(const
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_items_kernel<T, DP, KD, HIDES>, map, p);
+    return cudaLaunchKernelEx(&cfg, attend_items_kernel<T, DP, KD, HIDES, FORM>, map, p);
 }
 
 // With one query token every row sees every token: without the code for tokens that some rows do not see, 256 small requests behind
 // a prefix take 79 us instead of 83.
 template <typename T, int DP, int KD> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
-    return p.q_tokens > 1 ? launch_hides<T, DP, KD, true>(p, map, stream) : launch_hides<T, DP, KD, false>(p, map, stream);
+    if (p.formed) return launch_hides<T, DP, KD, true, true>(p, map, stream);
+    return p.q_tokens > 1 ? launch_hides<T, DP, KD, true, false>(p, map, stream) : launch_hides<T, DP, KD, false, false>(p, map, stream);
 }
 
 template <typename T> cudaError_t launch_type(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)

@@ -177,6 +177,83 @@ __device__ __forceinline__ float pow2(float x)
     return y;
 }
 
+// ---- attention in another form than plain causal ----
+//
+// Own tokens before the newest are seen by every row, the newest by the bits of the row's mask.
+__device__ __forceinline__ int newest_of(const AttnParams &p, int seq)
+{
+    return p.n_new ? max(0, min(p.n_new[seq], p.q_tokens)) : p.q_tokens;
+}
+// Which of the n newest tokens from, from + 1 ... from + 31 query token `token` of `seq` sees; older ones (from + i < 0) are seen.
+__device__ __forceinline__ uint32_t newest_seen(const AttnParams &p, int seq, int token, int n, int from)
+{
+    if (from <= -32) return ~0u;
+    const uint32_t *mask = p.mask ? p.mask + seq * p.mask_stride[0] + token * p.mask_stride[1] : nullptr;
+    auto word = [&](int k) -> uint32_t {
+        if (k < 0) return ~0u;
+        if (32 * k >= n) return 0u;
+        if (mask) return __ldg(mask + k);
+        const int last = token - 32 * k;   // newest token j <= token
+        return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1;
+    };
+    const int k = from >> 5;
+    uint32_t bits = __funnelshift_r(word(k), word(k + 1), from & 31);
+    if (from + 32 > n) bits &= from >= n ? 0u : (1u << (n - from)) - 1;
+    return bits;
+}
+// What a row adds to its logits by distance: slope * (position of the key - of the query).  A key's position among
+// the newest tokens is its slot but for the correction below.
+struct Bias {
+    float slope;   // base 2
+    int query;     // position of the query, counted as the item's tokens are
+};
+__device__ __forceinline__ int offset_of(const AttnParams &p, int seq, int j) { return p.offset ? p.offset[seq * p.offset_stride + j] : j; }
+__device__ __forceinline__ Bias bias_of(const AttnParams &p, const AttnItem &it, const RowId &id, int own)   // own: the sequence's own tokens
+{
+    Bias b;
+    b.slope = p.slopes ? p.slopes[it.head * p.G + id.g] * kLog2e : 0.f;
+    b.query = own - newest_of(p, id.seq) + offset_of(p, id.seq, id.token) + (it.seq >= 0 ? 0 : it.len);
+    return b;
+}
+// Capped logit in base 2.  tanh x = 1 - 2 / (1 + e^2x) is right at both ends, infinities too; its error, 2^-22 of the cap at most, is that
+// of the two approximate functions (ex2, rcp).
+__device__ __forceinline__ float capped(float z, float in, float out)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + pow2(z * in)));
+    return fmaf(-2.f * out, r, out);
+}
+
+// As left_out(): what the pieces of V with infinities or NaN among own tokens [from, to) add to dims [d, d + 4) of a row.
+template <typename T>
+__device__ __noinline__ float4 left_out_formed(const AttnParams &p, const T *q, const AttnItem &it, const RowId id, int len, int from, int to, float base, int d)
+{
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (base == -INFINITY) return sum;
+    const int n = newest_of(p, id.seq), old = len - n;
+    const Bias bias = bias_of(p, it, id, len);
+#pragma unroll 1
+    for (int t = from; t < to; ++t) {
+        if (!(newest_seen(p, id.seq, id.token, n, t - old) & 1)) continue;
+        const int block = t / p.pool.block_tokens;
+        const char *row = p.pool.base + 2 * (int64_t)p.layer * p.pool.lc_stride + it.head * p.pool.head_stride +
+                          p.tbl[it.tbl + block] * p.pool.block_stride + (int64_t)(t - block * p.pool.block_tokens) * p.pool.tok_stride;
+        const T *k = reinterpret_cast<const T *>(row), *v = reinterpret_cast<const T *>(row + p.pool.lc_stride);
+        if (!any_not_finite<T>(*reinterpret_cast<const uint4 *>(v + d / 8 * 8))) continue;
+        float z = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < p.D; ++i) z = fmaf(static_cast<float>(q[i]), static_cast<float>(k[i]), z);
+        z = p.cap_out != 0.f ? capped(z, p.cap_in, p.cap_out) : z * p.scale_log2;
+        if (p.slopes) z += bias.slope * (float)((t < old ? t : old + offset_of(p, id.seq, t - old)) - bias.query);
+        const float w = exp2f(z - base);
+        sum.x = fmaf(w, static_cast<float>(v[d]), sum.x);
+        sum.y = fmaf(w, static_cast<float>(v[d + 1]), sum.y);
+        sum.z = fmaf(w, static_cast<float>(v[d + 2]), sum.z);
+        sum.w = fmaf(w, static_cast<float>(v[d + 3]), sum.w);
+    }
+    return sum;
+}
+
 // The parts of row `row` of (sequence, head): np0 parts of own tokens, then those of the prefix.
 struct Parts {
     int64_t first[2], step[2];

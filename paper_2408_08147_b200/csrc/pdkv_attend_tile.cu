@@ -208,7 +208,9 @@ template <typename T, int DP> __device__ __forceinline__ void fetch_q(const Attn
 
 }  // namespace
 
-template <typename T, int DP>
+// FORM: another form than plain causal.  A thread turns the logits of its row into what the form says (capped, biased, hidden by the
+// row's mask) while they are in registers; from then on they are in base 2.
+template <typename T, int DP, bool FORM>
 __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
     using G = TileShape<DP>;
@@ -384,7 +386,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         const int t = warp / 4, r = threadIdx.x % kSoftmaxThreads;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + kColS + t * kColTile, o_at = tmem + lanes + kColO + t * kColTile;
-        const float scale = fabsf(p.scale_log2);
+        const float scale = FORM ? 1.f : fabsf(p.scale_log2);
         const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
         uint32_t s_phase = 0, o_phase = 0, n = 0;
         bool q_there = q_early, q_done = false;   // the item's Q is on its way, has been handed over
@@ -429,8 +431,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const bool live = row < w.it.rows, own = w.it.seq >= 0;
             const RowId id = row_id(p, w.it, w.it.row0 + (live ? row : 0));
             float m = -INFINITY, l = 0.f;
-            const int sees = own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;   // tokens before this one
-            const int safe = own ? min(w.limit, w.len - (p.q_tokens - 1)) : w.limit;              // the same of every row
+            const int n_new = FORM ? newest_of(p, id.seq) : 0;
+            const int sees = FORM ? w.limit : own ? min(w.limit, w.len - (p.q_tokens - 1 - id.token)) : w.limit;   // tokens before this one
+            const int safe = own ? min(w.limit, FORM ? w.len - n_new : w.len - (p.q_tokens - 1)) : w.limit;        // the same of every row
+            const bool there = id.token < n_new;   // FORM: one of the newest
+            Bias bias{0.f, 0};
+            if (FORM) bias = bias_of(p, w.it, id, own ? w.len : own_len(p, id.seq, p.segs[id.seq].len));
             bool wild = false;   // pieces of V were left out
             if (count > 0) {
                 if (!q_there) fetch_q<T, DP>(p, w, t, q_at);
@@ -447,7 +453,45 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
                     tmem_load_wait();
-                    if (masked) {
+                    if constexpr (FORM) {
+                        const float far = bias.slope * (float)(t0 - bias.query);
+                        if (p.cap_out != 0.f) {
+                            const float in = fabsf(p.cap_in), out = p.cap_out;
+#pragma unroll
+                            for (int k = 0; k < kTileTokens; ++k) v[k] = capped(v[k], in, out);
+                            if (p.slopes) {
+#pragma unroll
+                                for (int k = 0; k < kTileTokens; ++k) v[k] += fmaf(bias.slope, (float)k, far);
+                            }
+                        } else {
+                            const float in = fabsf(p.scale_log2);
+#pragma unroll
+                            for (int k = 0; k < kTileTokens; ++k) v[k] = fmaf(v[k], in, fmaf(bias.slope, (float)k, far));
+                        }
+                        if (!there) {
+#pragma unroll
+                            for (int k = 0; k < kTileTokens; ++k) v[k] = -INFINITY;
+                        }
+                    }
+                    if (FORM && masked) {
+                        const int from = t0 - (w.len - n_new);   // number of tile's first token among the newest
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t seen = own ? newest_seen(p, id.seq, id.token, n_new, from + 32 * c) : ~0u;
+                            const int left = w.limit - (t0 + 32 * c);
+                            if (left < 32) seen &= left <= 0 ? 0u : (1u << left) - 1;
+                            if (own && p.offset && p.slopes && seen != 0) {   // the place of a newest token is not its slot
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) {
+                                    const int j = from + 32 * c + k;
+                                    if (j >= 0 && (seen >> k & 1)) v[32 * c + k] = fmaf(bias.slope, (float)(offset_of(p, id.seq, j) - j), v[32 * c + k]);
+                                }
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (!(seen >> k & 1)) v[32 * c + k] = -INFINITY;
+                        }
+                    } else if (masked) {
 #pragma unroll
                         for (int k = 0; k < kTileTokens; ++k)
                             if (t0 + k >= sees) v[k] = -INFINITY;
@@ -558,6 +602,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = 0.f;
                 }
+                if (FORM && l == 0.f) {   // a row that saw nothing: its products may be 0 * infinity
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] = 0.f;
+                }
                 if (wild && live) {
                     const T *q = static_cast<const T *>(p.q) + id.seq * p.q_stride[0] + id.token * p.q_stride[1] + head * p.q_stride[2];
 #pragma unroll 1
@@ -567,7 +615,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                             for (int k = 0; k < 32; k += 4)
                                 if (32 * c + k < p.D) {
-                                    const float4 y = left_out_call<T>(p, q, w.it.tbl, w.it.head, from, to, m, 32 * c + k);
+                                    float4 y;
+                                    if constexpr (FORM)
+                                        y = left_out_formed<T>(p, q, w.it, id, w.len, from, to, m, 32 * c + k);
+                                    else
+                                        y = left_out_call<T>(p, q, w.it.tbl, w.it.head, from, to, m, 32 * c + k);
                                     v[k] += y.x;
                                     v[k + 1] += y.y;
                                     v[k + 2] += y.z;
@@ -624,7 +676,7 @@ template <int DP> constexpr uint32_t weigh_bytes(int rows)
 // tokens, 64 rows each, 8 heads of 128 dims take 27 us as a kernel alone (cold), of which the bytes of K need 9 and the exponentials 3 (16
 // a cycle and SM); the tensor pipe is active for 8%, DRAM for 25%.  So latency bounds it: a CTA starts (Q, sums of the rows) for a
 // handful of tiles, and ragged lists leave a few CTAs for a second wave.
-template <typename T, int DP>
+template <typename T, int DP, bool FORM>
 __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
 {
     using G = TileShape<DP>;
@@ -633,6 +685,7 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
     __shared__ uint32_t tmem_s;
     __shared__ __align__(16) float lse[256];   // negated, base 2
     __shared__ __align__(16) int sees[256];
+    __shared__ Bias bias[FORM ? 256 : 1];
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) / 1024 * 1024);
     const int R = p.G * p.q_tokens, columns = R > 128 ? 256 : R > 64 ? 128 : 64;   // of one S^T
     const uint32_t q_sub = weigh_q_sub(R), q_at = smem_u32(smem), k_at = q_at + G::kSubs * q_sub;
@@ -737,6 +790,12 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
                 const float x = p.lse[((int64_t)seq * p.q_tokens + row / p.G) * p.G * p.H + head * p.G + row % p.G];
                 lse[i] = i >= rows || x == -INFINITY ? -INFINITY : -x * kLog2e;   // no weight: 2^(z - inf) = 0
                 sees[i] = len - (p.q_tokens - 1 - row / p.G);
+                if constexpr (FORM) {
+                    AttnItem it{};
+                    it.seq = seq;
+                    it.head = head;
+                    bias[i] = bias_of(p, it, {seq, row / p.G, row % p.G}, len);
+                }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (flip)   // (a thread turns the signs of what it brought itself)
@@ -761,6 +820,21 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
                     float v[32];
                     tmem_load(v, tmem + ((uint32_t)(warp * 32) << 16) + b * columns + col);
                     tmem_load_wait();
+                    if constexpr (FORM) {
+                        const int n_new = newest_of(p, seq), j = t - (len - n_new);
+#pragma unroll 4
+                        for (int k = 0; k < 32; ++k) {
+                            if (col + k >= rows) break;
+                            const int token = (r0 + col + k) / p.G;
+                            const Bias b = bias[col + k];
+                            // (tokens before the newest: seen by every query token that is there)
+                            const bool seen = token < n_new && (j < 0 || (newest_seen(p, seq, token, n_new, j) & 1)) && lse[col + k] != -INFINITY;
+                            float x = p.cap_out != 0.f ? capped(v[k], fabsf(p.cap_in), p.cap_out) : v[k] * fabsf(p.scale_log2);
+                            if (p.slopes) x = fmaf(b.slope, (float)((j >= 0 && j < n_new ? len - n_new + offset_of(p, seq, j) : t) - b.query), x);
+                            if (seen) sums[0].x += pow2(x + lse[col + k]);
+                        }
+                        continue;
+                    }
                     if (masked || col + 32 > rows) {
                         // Columns past the last row hold anything, or products of zeros, NaN for an infinite K; a token that a row
                         // does not see weighs nothing even where the row's sum is NaN.
@@ -812,10 +886,10 @@ namespace {
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, bool FORM> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(attend_tile_kernel<T, DP>, (int)TileShape<DP>::kBytes, ready);
+    const cudaError_t e = allow_shared(attend_tile_kernel<T, DP, FORM>, (int)TileShape<DP>::kBytes, ready);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.n_tile_ctas);
@@ -827,13 +901,13 @@ template <typename T, int DP> cudaError_t launch_dims(const AttnParams &p, const
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_tile_kernel<T, DP>, map, p);
+    return cudaLaunchKernelEx(&cfg, attend_tile_kernel<T, DP, FORM>, map, p);
 }
 
-template <typename T, int DP> cudaError_t launch_weigh(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, bool FORM> cudaError_t launch_weigh(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
-    const cudaError_t e = allow_shared(attend_weigh_kernel<T, DP>, (int)weigh_bytes<DP>(256), ready);
+    const cudaError_t e = allow_shared(attend_weigh_kernel<T, DP, FORM>, (int)weigh_bytes<DP>(256), ready);
     if (e != cudaSuccess) return e;
     // two CTAs an SM would hold the sum of all tiles at once (ragged lists make some CTAs more), each at least two
     const int chunk_tiles = (int)std::max<int64_t>(2, (p.own_tiles + 2 * p.sm_count - 1) / (2 * p.sm_count));
@@ -851,7 +925,7 @@ template <typename T, int DP> cudaError_t launch_weigh(const AttnParams &p, cons
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_weigh_kernel<T, DP>, map, p, chunks, chunk_tiles);
+    return cudaLaunchKernelEx(&cfg, attend_weigh_kernel<T, DP, FORM>, map, p, chunks, chunk_tiles);
 }
 
 }  // namespace
@@ -891,20 +965,31 @@ bool make_attend_map(const pdkv_pool &pool, int box_tokens, void *out)
                                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+namespace {
+
+template <typename T> cudaError_t launch_weigh_type(const AttnParams &p, const CUtensorMap &m, cudaStream_t stream)
+{
+    if (p.formed) return p.D <= 64 ? launch_weigh<T, 64, true>(p, m, stream) : launch_weigh<T, 128, true>(p, m, stream);
+    return p.D <= 64 ? launch_weigh<T, 64, false>(p, m, stream) : launch_weigh<T, 128, false>(p, m, stream);
+}
+template <typename T> cudaError_t launch_tile_type(const AttnParams &p, const CUtensorMap &m, cudaStream_t stream)
+{
+    if (p.formed) return p.D <= 64 ? launch_dims<T, 64, true>(p, m, stream) : launch_dims<T, 128, true>(p, m, stream);
+    return p.D <= 64 ? launch_dims<T, 64, false>(p, m, stream) : launch_dims<T, 128, false>(p, m, stream);
+}
+
+}  // namespace
+
 cudaError_t launch_attend_weigh(const AttnParams &p, const void *map, int dtype, cudaStream_t stream)
 {
     const CUtensorMap &m = *static_cast<const CUtensorMap *>(map);
-    if (dtype == PDKV_DTYPE_BF16)
-        return p.D <= 64 ? launch_weigh<__nv_bfloat16, 64>(p, m, stream) : launch_weigh<__nv_bfloat16, 128>(p, m, stream);
-    return p.D <= 64 ? launch_weigh<__half, 64>(p, m, stream) : launch_weigh<__half, 128>(p, m, stream);
+    return dtype == PDKV_DTYPE_BF16 ? launch_weigh_type<__nv_bfloat16>(p, m, stream) : launch_weigh_type<__half>(p, m, stream);
 }
 
 cudaError_t launch_attend_tile(const AttnParams &p, const void *map, int dtype, cudaStream_t stream)
 {
     const CUtensorMap &m = *static_cast<const CUtensorMap *>(map);
-    if (dtype == PDKV_DTYPE_BF16)
-        return p.D <= 64 ? launch_dims<__nv_bfloat16, 64>(p, m, stream) : launch_dims<__nv_bfloat16, 128>(p, m, stream);
-    return p.D <= 64 ? launch_dims<__half, 64>(p, m, stream) : launch_dims<__half, 128>(p, m, stream);
+    return dtype == PDKV_DTYPE_BF16 ? launch_tile_type<__nv_bfloat16>(p, m, stream) : launch_tile_type<__half>(p, m, stream);
 }
 
 }  // namespace pdkv

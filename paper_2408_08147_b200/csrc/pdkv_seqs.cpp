@@ -552,11 +552,26 @@ int pdkv_attend_scratch(const pdkv_seqs *s, int with_scores, size_t *bytes)
     return PDKV_OK;
 }
 
-int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *scratch, size_t scratch_bytes, void *stream)
+}  // extern "C"
+
+namespace {
+
+// `f`: another form than plain causal, or null.
+int attend_call(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, const pdkv_attend_form *f, void *scratch, size_t scratch_bytes, void *stream)
 {
     if (!s || !a || s->Hq == 0 || layer < 0 || layer >= s->pool.d.num_layers) return PDKV_ERR_INVALID_ARG;
     const float scale_log2 = (float)((double)a->scale * 1.4426950408889634);
     if (!std::isfinite(scale_log2)) return PDKV_ERR_INVALID_ARG;
+    double cap_in = 0, cap_out = 0;
+    if (f) {
+        if (!(f->cap >= 0.f) || !std::isfinite(f->cap)) return PDKV_ERR_INVALID_ARG;
+        cap_out = f->cap * 1.4426950408889634;
+        if (f->cap > 0.f) cap_in = 2 * 1.4426950408889634 * a->scale / f->cap;
+        if (!std::isfinite((float)cap_in) || !std::isfinite((float)(2 * cap_out)) || (f->cap > 0.f && (float)cap_out == 0.f)) return PDKV_ERR_INVALID_ARG;
+        if (!aligned(f->slopes, 4) || !aligned(f->mask, 4) || !aligned(f->n_new, 4) || !aligned(f->offset, 4)) return PDKV_ERR_INVALID_ARG;
+        if (f->mask && (f->mask_stride[0] < 0 || f->mask_stride[1] < 0)) return PDKV_ERR_INVALID_ARG;
+        if (f->offset && f->offset_stride < 0) return PDKV_ERR_INVALID_ARG;
+    }
     try {
         const int64_t rows[3] = {s->n_seq, s->q_tokens, s->Hq};
         const int64_t D = s->pool.d.head_dim;
@@ -596,6 +611,14 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
                     if (meet(written[i], written[j])) return PDKV_ERR_INVALID_ARG;
                 for (int j = 0; j < 5; ++j)
                     if (!(i == 2 && j == 4 && a->scores_in == a->scores_out) && meet(written[i], read[j])) return PDKV_ERR_INVALID_ARG;
+            }
+            if (f) {
+                const int64_t words = ((int64_t)s->q_tokens + 31) / 32;
+                const Rows more[4] = {Rows(f->slopes, 4 * rows[2]), Rows(f->mask, words, 4, f->mask_stride, rows, 2), Rows(f->n_new, 4 * rows[0]),
+                                      Rows(f->offset, s->q_tokens, 4, &f->offset_stride, rows, 1)};
+                for (const Rows &w : written)
+                    for (const Rows &r : more)
+                        if (meet(w, r)) return PDKV_ERR_INVALID_ARG;
             }
         }
         if (scratch_bytes < l.bytes) return PDKV_ERR_BUFFER_TOO_SMALL;
@@ -638,6 +661,19 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
         // instead, by which no finite logit comes near 1.
         if (p.scale_log2 == 0.f) p.scale_log2 = std::copysign(std::numeric_limits<float>::denorm_min(), a->scale);
         p.seq_len = a->seq_len;
+        if (f) {
+            p.formed = 1;
+            // (a scale of zero as above: the logits' infinities stay what they are)
+            p.cap_in = cap_in == 0 && f->cap > 0.f ? std::copysign(std::numeric_limits<float>::denorm_min(), a->scale) : (float)cap_in;
+            p.cap_out = (float)cap_out;
+            p.slopes = f->slopes;
+            p.mask = f->mask;
+            p.n_new = f->n_new;
+            p.offset = f->offset;
+            if (f->mask)
+                for (int i = 0; i < 2; ++i) p.mask_stride[i] = rows[i] > 1 ? f->mask_stride[i] : 0;
+            p.offset_stride = f->offset && rows[0] > 1 ? f->offset_stride : 0;
+        }
         char *w = static_cast<char *>(scratch);
         p.part_o = reinterpret_cast<float *>(w + l.o);
         p.part_ml = reinterpret_cast<float *>(w + l.ml);
@@ -684,6 +720,22 @@ int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *
     } catch (const std::length_error &) {
         return PDKV_ERR_NOMEM;
     }
+}
+
+}  // namespace
+
+extern "C" {
+
+int pdkv_attend(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, void *scratch, size_t scratch_bytes, void *stream)
+{
+    return attend_call(s, layer, a, nullptr, scratch, scratch_bytes, stream);
+}
+
+int pdkv_attend_formed(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, const pdkv_attend_form *f, void *scratch, size_t scratch_bytes,
+                       void *stream)
+{
+    if (!f) return PDKV_ERR_INVALID_ARG;
+    return attend_call(s, layer, a, f, scratch, scratch_bytes, stream);
 }
 
 int pdkv_evict(const pdkv_seqs *s, const pdkv_seqs *t, int layer_begin, int layer_end, const pdkv_evict_args *a, void *stream)

@@ -92,6 +92,14 @@ struct AttnParams {
     int32_t max_len;
     int32_t layer;
     int32_t block_shift;        // log2 of block_tokens, -1: not a power of two
+    // another form than plain causal (pdkv_attend_form): a variant of each kernel
+    int32_t formed;
+    float cap_in, cap_out;      // logits (base 2): cap_out tanh(z cap_in / (2 log2 e)); cap_out 0: z scale_log2
+    const float *slopes;
+    const uint32_t *mask;
+    int64_t mask_stride[2];
+    const int32_t *n_new, *offset;
+    int64_t offset_stride;
 };
 
 int attend_ctas_per_sm(int head_dim);

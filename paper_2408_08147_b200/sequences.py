@@ -70,6 +70,16 @@ class Sequences:
         return int(self.seq_len.max()) if self.n_seq else 0
 
 
+def pack_mask(see_t):
+    """Words for ``mask_t`` of :meth:`CacheSession.attend` from truth values ``[..., query, newest token]``: bit ``j % 32`` of int32 word ``j // 32``."""
+    *lead, n = see_t.shape
+    words = (n + 31) // 32
+    bits = torch.zeros((*lead, words * 32), dtype=torch.int64, device=see_t.device)
+    bits[..., :n] = see_t
+    weights = torch.ones(32, dtype=torch.int64, device=see_t.device) << torch.arange(32, device=see_t.device)
+    return (bits.unflatten(-1, (words, 32)) * weights).sum(-1).to(torch.int32)
+
+
 class Rotary:
     """Rotation of heads by position (see ``pdkv_rotary``), laid out once on the device.
 
@@ -197,12 +207,19 @@ class CacheSession:
         return self._need[bool(with_scores)]
 
     def attend(self, layer: int, q_t, *, scale: Optional[float] = None, out_t=None, lse_t=None, scores_t=None,
-               scores_in_t=None, seq_len_t=None, scratch_t=None, stream: Optional[int] = None):
+               scores_in_t=None, seq_len_t=None, scratch_t=None, stream: Optional[int] = None, cap: Optional[float] = None, slopes_t=None,
+               mask_t=None, n_new_t=None, offset_t=None):
         """Attention of one layer; ``q_t`` is ``[n_seq, q_tokens, num_q_heads, head_dim]`` (any strides with
         adjacent dims).  Returns ``(out, lse)``.  With ``scores_t`` (float32 ``[n_seq, num_kv_heads, >= longest]``)
         the attention weights of the own tokens are added to it, or to ``scores_in_t`` and the sums
         stored in ``scores_t``.  ``seq_len_t``: current own lengths (int32, device).  There is no backward pass: a
-        ``q_t`` that asks for a gradient is refused."""
+        ``q_t`` that asks for a gradient is refused.
+
+        Other forms than plain causal (``pdkv_attend_form``): ``cap`` turns logits into ``cap * tanh(logit / cap)``; ``slopes_t`` (float32
+        ``[num_q_heads]``) adds slope times the position of the key minus that of the query; ``mask_t`` (int32 ``[n_seq, q_tokens, words]``, see
+        :func:`pack_mask`; expanded along the batch where all share it) says which of the newest tokens a query token sees: a drafted tree,
+        documents in a chunk, a prefix seen both ways; only ``n_new_t[r]`` (int32 ``[n_seq]``) of the ``q_tokens`` are there; ``offset_t`` (int32
+        ``[n_seq, q_tokens]``): positions of the newest tokens counted from their first, where they are not 0, 1, 2 ... (with ``slopes_t``)."""
         shape = self._shape
         made = []
         self._check("q_t", q_t, self.dtype, shape)
@@ -260,8 +277,40 @@ class CacheSession:
             size = scratch_t.numel() * scratch_t.element_size()
         if stream != home:
             self._record(stream, *made)
-        B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, stream)
+        if cap is None and slopes_t is None and mask_t is None and n_new_t is None and offset_t is None:
+            B.pdkv_attend(self.handle, layer, a, scratch_t.data_ptr(), size, stream)
+        else:
+            B.pdkv_attend_formed(self.handle, layer, a, self._form(cap, slopes_t, mask_t, n_new_t, offset_t), scratch_t.data_ptr(), size, stream)
         return out_t, lse_t
+
+    def _form(self, cap, slopes_t, mask_t, n_new_t, offset_t):
+        n, T, Hq, _ = self._shape
+        f = B.pdkv_attend_form()
+        if cap is not None:
+            if not cap > 0:
+                raise ValueError(f"cap: expected a positive number, got {cap}")
+            f.cap = cap
+        if slopes_t is not None:
+            self._check("slopes_t", slopes_t, torch.float32, (Hq,))
+            if Hq > 1 and slopes_t.stride(0) != 1:
+                raise ValueError("slopes_t has to be contiguous")
+            f.slopes = slopes_t.data_ptr()
+        if mask_t is not None:
+            self._check("mask_t", mask_t, torch.int32, (n, T, (T + 31) // 32))
+            stride = mask_t.stride()
+            if T > 32 and stride[2] != 1:
+                raise ValueError("mask_t: the words of a query token have to be adjacent")
+            f.mask, f.mask_stride = mask_t.data_ptr(), stride[:2]
+        if n_new_t is not None:
+            f.n_new = self._ints("n_new_t", n_new_t, (n,))
+        if offset_t is not None:
+            if slopes_t is None:
+                raise ValueError("offset_t needs slopes_t")
+            self._check("offset_t", offset_t, torch.int32, (n, T))
+            if T > 1 and offset_t.stride(1) != 1:
+                raise ValueError("offset_t: the tokens of a sequence have to be adjacent")
+            f.offset, f.offset_stride = offset_t.data_ptr(), offset_t.stride(0)
+        return f
 
     def _heads(self, name, t, lead, heads, out):
         """Strides between sequences, rows and heads of a tensor [*lead, heads, head_dim]."""
