@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -111,6 +112,19 @@ class pdkv_append_args(C.Structure):
 class pdkv_accept_args(C.Structure):
     _fields_ = [("path", C.c_void_p), ("path_stride", C.c_int64), ("path_len", C.c_int32), ("new_tokens", C.c_int32),
                 ("n_new", C.c_void_p), ("seq_len", C.c_void_p), ("new_len", C.c_void_p)]
+
+
+_APPEND, _ACCEPT = struct.Struct("@i4x7Q12q2Qf4xQq3i4x2Qf4x"), struct.Struct("@Qq2i3Q")
+assert _APPEND.size == C.sizeof(pdkv_append_args) and _ACCEPT.size == C.sizeof(pdkv_accept_args)
+
+
+def append_args(*fields) -> pdkv_append_args:
+    """pdkv_append_args from its fields in order, those of the arrays and of the rotary one by one (a third of the time of naming them)."""
+    return pdkv_append_args.from_buffer_copy(_APPEND.pack(*fields))
+
+
+def accept_args(*fields) -> pdkv_accept_args:
+    return pdkv_accept_args.from_buffer_copy(_ACCEPT.pack(*fields))
 
 
 class pdkv_evict_args(C.Structure):

@@ -12,7 +12,8 @@ namespace pdkv {
 namespace {
 
 constexpr int kAppendThreads = 128;
-constexpr int kBatch = 4;          // steps whose loads are on their way together
+// Steps of a warp in its ring, one of them at work.  Measured on 13262 rows of 48 heads of 128 dims: 3 59.3 us, 4 57.2, 6 57.8.
+constexpr int kRing = 4;
 
 __device__ __forceinline__ int own_tokens(const int32_t *seq_len, int seq, int most)
 {
@@ -41,6 +42,21 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// Two 32-bit numbers at a time.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)),
+        "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return d;
 }
 
 // Eight 16-bit numbers of which the first n are there, as four words.  PIECES: their address is a multiple of 2 only.
@@ -84,19 +100,22 @@ __device__ __forceinline__ int sequence_of(const int32_t *row_begin, int n_seq, 
 
 }  // namespace
 
-// A warp has one row (token) and, a step at a time, 32 / W of its heads: queries, then keys, then values.  W lanes have a head, each
-// two runs of eight dims, chosen so that both members of a rotated pair lie in one lane, which then has eight pairs:
+// A warp has one row (token) and, a step at a time, 32 / W heads of its queries, then of its keys, then of its values.  W lanes have a
+// head, each two runs of eight dims, chosen so that both members of a rotated pair lie in one lane, which then has eight pairs:
 //     y = x w / sqrt(mean x^2 + eps)      (a, b) -> (a cos - b sin, b cos + a sin), the angle position * frequency
-// The sines serve all heads of the row; the lanes of one step share the work of finding them.  The angle is kept in turns as a 64-bit
-// fraction, position * frequency wraps at whole turns by itself, and its upper 32 bits are exact to 2^-32 of a turn at any position
-// (position * frequency in 32-bit floating point is off by 0.004 at 100000).  Everything between load and store is 32 bits, rounded once.
+// The sines serve all heads of the row, each found by one lane.  The angle is kept in turns as a 64-bit fraction: position * frequency
+// wraps at whole turns by itself, and its upper 32 bits are right to 2^-32 of a turn at any position (position * frequency in 32-bit
+// floating point is off by 0.004 at 100000).  Everything between load and store is 32 bits, two numbers at a time, rounded once; the
+// weights are multiplied into the cosines and sines, so a result is two products and one by 1 / sqrt.
 //
 // ODD: half of the rotated dims is no multiple of eight.  Pairs (i, i + half) then lie in runs that are not aligned: a lane takes up
 // to eight pairs, or up to sixteen of the dims behind them, in 16-bit pieces.
-template <typename T, int W, bool ODD>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendParams p)
+template <typename T, int W, bool ODD, bool ADJACENT>
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendParams p)
 {
     constexpr int kHeads = 32 / W;   // of a step
+    __shared__ __align__(16) float sines[kAppendThreads / 32][2][8 * W];
+    __shared__ uint4 ring[kAppendThreads / 32][ODD ? 1 : kRing][2][32];
     const int lane = threadIdx.x % 32, sub = lane / W, i = lane % W;
     const int64_t item = (int64_t)blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
     const int row = (int)(item / p.parts), part = (int)(item - (int64_t)row * p.parts);
@@ -107,7 +126,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
     // which dims are this lane's: na from a, nb from b
     const int half = p.rotated / 2;
     int a, b, na, nb;
-    if (p.adjacent) {
+    if (ADJACENT) {
         a = 16 * i;
         b = a + 8;
         na = p.D - a;
@@ -127,169 +146,239 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
     }
     na = max(0, min(8, na));
     nb = max(0, min(8, nb));
+    a = na > 0 ? a : 0;
+    b = nb > 0 ? b : 0;
 
-    const int first = part * p.steps * kHeads, slots = p.Hq + 2 * p.H;
-    const int last = min(slots, first + p.steps * kHeads);   // heads [first, last) of the row
-
-    // whose row is it, and which of its tokens
-    int seq, at, count;
-    if (p.row_begin) {
-        seq = sequence_of(p.row_begin, p.n_seq, row);
-        if (seq < 0) return;
-        at = row - p.row_begin[seq];
-        count = p.row_begin[seq + 1] - p.row_begin[seq];
-    } else {
-        seq = row / p.per;
-        at = row - seq * p.per;
-        count = p.n_new ? max(0, min(p.n_new[seq], p.per)) : p.per;
-    }
-    if (at >= count) return;   // not a token
-    const int64_t lead = p.row_begin ? row : at, outer = p.row_begin ? 0 : seq;
-    const uint16_t *q = static_cast<const uint16_t *>(p.q) + outer * p.q_stride[0] + lead * p.q_stride[1];
-    const uint16_t *k = static_cast<const uint16_t *>(p.k) + outer * p.k_stride[0] + lead * p.k_stride[1];
-    const uint16_t *v = static_cast<const uint16_t *>(p.v) + outer * p.v_stride[0] + lead * p.v_stride[1];
+    const int first = part * p.steps, last = min(first + p.steps, p.q_steps + 2 * p.k_steps);   // the warp's steps
+    const int outer = p.row_begin ? 0 : row / p.per, lead = row - outer * p.per;   // where the row lies in q, k and v
     uint16_t *q_out = static_cast<uint16_t *>(p.q_out) + outer * p.q_out_stride[0] + lead * p.q_out_stride[1];
-    // values of step s: head `first + s * kHeads + sub` of queries, keys, values
-    auto source = [&](int h) {
-        return h < p.Hq ? q + h * p.q_stride[2] : h < p.Hq + p.H ? k + (h - p.Hq) * p.k_stride[2] : v + (h - p.Hq - p.H) * p.v_stride[2];
+    // Walks the values of the warp's steps: queries (kind 0), then keys (1), then values (2).
+    struct Walk {
+        const uint16_t *src;
+        int64_t stride;      // elements between steps
+        int h, heads, left;  // the lane's head, heads of the kind, steps of the kind that are left
+        int kind;
     };
-    uint4 xa[kBatch], xb[kBatch];
-    auto fetch = [&](int h0) {
-#pragma unroll
-        for (int s = 0; s < kBatch; ++s) {
-            const int h = h0 + s * kHeads + sub;
-            const bool there = h < last;
-            const uint16_t *from = source(there ? h : first);
-            xa[s] = load8<ODD>(from + (na > 0 ? a : 0), there ? na : 0);
-            xb[s] = load8<ODD>(from + (nb > 0 ? b : 0), there ? nb : 0);
+    const auto enter = [&](Walk &w, int kind, int skip) {   // `skip` steps of the kind are not the warp's
+        const int64_t *stride = kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride;
+        w.kind = kind;
+        w.heads = kind == 0 ? p.Hq : p.H;
+        w.h = skip * kHeads + sub;
+        w.left = (kind == 0 ? p.q_steps : p.k_steps) - skip;
+        w.stride = stride[2] * kHeads;
+        w.src = static_cast<const uint16_t *>(kind == 0 ? p.q : kind == 1 ? p.k : p.v) + outer * stride[0] + lead * stride[1] + w.h * stride[2];
+    };
+    Walk load;
+    if (first < p.q_steps)
+        enter(load, 0, first);
+    else if (first < p.q_steps + p.k_steps)
+        enter(load, 1, first - p.q_steps);
+    else
+        enter(load, 2, first - p.q_steps - p.k_steps);
+    const int first_kind = load.kind, first_skip = first - (load.kind == 0 ? 0 : load.kind == 1 ? p.q_steps : p.q_steps + p.k_steps);
+    // The next kRing - 1 steps are on their way into shared memory (a lane copies and reads its own runs: no barrier), the first of them
+    // before it is known where the row goes.  (ODD: the runs are not aligned, a step is loaded when its turn comes.)
+    const bool has_a = na > 0, has_b = nb > 0;
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&ring[threadIdx.x / 32][0][0][lane]);
+    uint32_t load_at = 0, read_at = 0;   // places in the ring
+    int to_load = last - first;
+    auto issue = [&]() {
+        if constexpr (!ODD) {
+            if (to_load > 0) {
+                --to_load;
+                if (load.left == 0) enter(load, load.kind + 1, 0);
+                const bool there = load.h < load.heads;
+                if (there && has_a) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine + load_at), "l"(load.src + a) : "memory");
+                if (there && has_b) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine + load_at + 512), "l"(load.src + b) : "memory");
+                load.src += load.stride;
+                load.h += kHeads;
+                --load.left;
+                load_at = (load_at + 1024) % (kRing * 1024);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
     };
-    fetch(first);
+#pragma unroll 1
+    for (int k = 0; k < kRing - 1; ++k) issue();
 
+    // whose row is it, and which of its tokens
+    int seq = outer, at = lead, count;
+    if (p.row_begin) {
+        seq = sequence_of(p.row_begin, p.n_seq, row);
+        at = seq < 0 ? 0 : row - p.row_begin[seq];
+        count = seq < 0 ? 0 : p.row_begin[seq + 1] - p.row_begin[seq];
+    } else
+        count = p.n_new ? max(0, min(p.n_new[seq], p.per)) : p.per;
+    if (at >= count) {   // not a token
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+    }
     const AttnSeg seg = p.segs[seq];
     const int64_t slot = (int64_t)own_tokens(p.seq_len, seq, seg.len) - count + at;
     const bool cached = slot >= 0 && slot < seg.len;   // (a sequence shorter than its new tokens has no place for the first of them)
     char *place = nullptr;
-    if (cached && last > p.Hq)
+    if (cached && last > p.q_steps)
         place = p.pool.base + 2 * (int64_t)p.layer * p.pool.lc_stride + slot_offset(p.pool, p.tbl, seg.tbl, (int)slot, p.block_shift);
 
-    // cos and sin of the lane's pairs 8i..8i+7; the kHeads lanes with the same dims find 8 / kHeads each
-    float cosine[8], sine[8];
-    const bool turns = p.rotated > 0 && first < p.Hq + p.H;
-    if (turns) {
-        constexpr int kMine = 8 / kHeads;
-        float c[kMine], s[kMine];
+    // cos and sin of the row's pairs, lane, lane + 32 ... by each lane
+    float (&sc)[2][8 * W] = sines[threadIdx.x / 32];
+    if (half > 0 && first < p.q_steps + p.k_steps) {
 #pragma unroll
-        for (int e = 0; e < kMine; ++e) {
-            const int pair = 8 * i + sub * kMine + e;
-            c[e] = 1.f;
-            s[e] = 0.f;
+        for (int e = 0; e < W / 4; ++e) {
+            const int pair = lane + 32 * e;
             if (pair < half) {
                 const int axis = p.axis ? min((int)p.axis[pair], p.axes - 1) : 0;
                 const int64_t pos = p.position ? p.position[axis * p.position_stride + row] : seg.before + slot;
                 const int32_t turn = (int32_t)(((uint64_t)pos * p.turns[pair]) >> 32);
-                sincospif((float)turn * 0x1p-31f, &s[e], &c[e]);   // half turns
-                c[e] *= p.rotary_scale;
-                s[e] *= p.rotary_scale;
+                float s, c;
+                sincospif((float)turn * 0x1p-31f, &s, &c);   // half turns
+                sc[0][pair] = c * p.rotary_scale;
+                sc[1][pair] = s * p.rotary_scale;
             }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            cosine[e] = __shfl_sync(~0u, c[e % kMine], e / kMine * W + i);
-            sine[e] = __shfl_sync(~0u, s[e % kMine], e / kMine * W + i);
-        }
+        __syncwarp();
     }
-    float w[16];
-    const float *have = nullptr;   // whose weights w are
-    for (int h0 = first; h0 < last; h0 += kBatch * kHeads) {
-        if (h0 > first) fetch(h0);
+
+    int steps = last - first;
+#pragma unroll 1
+    for (int kind = first_kind, skip = first_skip; steps > 0; ++kind, skip = 0) {
+        const int count = min(steps, (kind == 0 ? p.q_steps : p.k_steps) - skip);
+        steps -= count;
+        if (count == 0) continue;
+        const int heads = kind == 0 ? p.Hq : p.H;
+        int h = skip * kHeads + sub;
+        const int64_t out_stride = kind == 0 ? p.q_out_stride[2] : p.pool.head_stride / 2;   // elements between heads
+        uint16_t *dst = (kind == 0 ? q_out : reinterpret_cast<uint16_t *>(place + (kind - 1) * p.pool.lc_stride)) + h * out_stride;
+        const bool store = kind == 0 || cached, store_a = store && has_a, store_b = store && has_b;
+        Walk odd;
+        if constexpr (ODD) enter(odd, kind, skip);
+        // y = x A + z B, z the other member of each pair
+        float2 A[8], B[8];
+        const float *norm = kind == 0 ? p.q_norm : kind == 1 ? p.k_norm : nullptr;
+        if (kind < 2) {
+            float w[16];
 #pragma unroll
-        for (int s = 0; s < kBatch; ++s) {
-            const int h = h0 + s * kHeads + sub;
-            if (h0 + s * kHeads >= last) break;   // (the whole warp)
-            const bool value = h >= p.Hq + p.H, query = h < p.Hq;
-            uint4 ya = xa[s], yb = xb[s];
-            if (h0 + s * kHeads < p.Hq + p.H) {   // (the whole warp: some lanes have queries or keys)
-                float x[16];   // a in the first eight, b in the others
-                const uint32_t words[8] = {ya.x, ya.y, ya.z, ya.w, yb.x, yb.y, yb.z, yb.w};
+            for (int e = 0; e < 16; ++e) w[e] = 1.f;
+            if (norm) {
+                if constexpr (ODD) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float2 f = unpack2<T>(words[e]);
-                    x[2 * e] = f.x;
-                    x[2 * e + 1] = f.y;
+                    for (int e = 0; e < 8; ++e) {
+                        w[e] = e < na ? norm[a + e] : 0.f;
+                        w[8 + e] = e < nb ? norm[b + e] : 0.f;
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(w + e) = *reinterpret_cast<const float4 *>(norm + (e < 8 ? a + e : b + e - 8));
                 }
-                const float *norm = query ? p.q_norm : value ? nullptr : p.k_norm;
-                if (__any_sync(~0u, norm != nullptr)) {
-                    float sum = 0.f;
+            }
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum = fmaf(x[e], x[e], sum);
+            for (int e = 0; e < 8; ++e) {
+                A[e] = make_float2(w[2 * e], w[2 * e + 1]);
+                B[e] = make_float2(0.f, 0.f);
+            }
+            if (8 * i < half) {
+                float c[8], s[8];
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    *reinterpret_cast<float4 *>(c + e) = *reinterpret_cast<const float4 *>(&sc[0][8 * i + e]);
+                    *reinterpret_cast<float4 *>(s + e) = *reinterpret_cast<const float4 *>(&sc[1][8 * i + e]);
+                }
+                if (ADJACENT) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!ODD || 8 * i + e < half) {
+                            A[e] = make_float2(c[e] * w[2 * e], c[e] * w[2 * e + 1]);
+                            B[e] = make_float2(-s[e] * w[2 * e + 1], s[e] * w[2 * e]);
+                        }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        A[e] = make_float2(c[2 * e] * w[2 * e], c[2 * e + 1] * w[2 * e + 1]);
+                        B[e] = make_float2(-s[2 * e] * w[8 + 2 * e], -s[2 * e + 1] * w[9 + 2 * e]);
+                        A[4 + e] = make_float2(c[2 * e] * w[8 + 2 * e], c[2 * e + 1] * w[9 + 2 * e]);
+                        B[4 + e] = make_float2(s[2 * e] * w[2 * e], s[2 * e + 1] * w[2 * e + 1]);
+                    }
+                }
+            }
+        }
+#pragma unroll 1
+        for (int n = count; n > 0; --n) {
+            uint4 xa, xb;
+            const bool there = h < heads;
+            if constexpr (ODD) {
+                xa = load8<true>(odd.src + a, there ? na : 0);
+                xb = load8<true>(odd.src + b, there ? nb : 0);
+                odd.src += odd.stride;
+            } else {
+                issue();
+                asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+                // (what is not there holds anything, and stays in its lane but for the sum of squares)
+                const char *at_ring = reinterpret_cast<const char *>(&ring[threadIdx.x / 32][0][0][lane]) + read_at;
+                xa = *reinterpret_cast<const uint4 *>(at_ring);
+                xb = *reinterpret_cast<const uint4 *>(at_ring + 512);
+                read_at = (read_at + 1024) % (kRing * 1024);
+            }
+            if (kind < 2) {
+                const uint32_t words[8] = {xa.x, xa.y, xa.z, xa.w, xb.x, xb.y, xb.z, xb.w};
+                float2 x[8], y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = unpack2<T>(words[e]);
+                float r = 1.f;
+                if (norm) {
+                    float2 sum_a = make_float2(0.f, 0.f), sum_b = sum_a;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sum_a = fma2(x[e], x[e], sum_a);
+                        sum_b = fma2(x[4 + e], x[4 + e], sum_b);
+                    }
+                    float sum = (has_a ? sum_a.x + sum_a.y : 0.f) + (has_b ? sum_b.x + sum_b.y : 0.f);
 #pragma unroll
                     for (int o = W / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-                    if (norm) {
-                        if (norm != have) {
-                            have = norm;
-                            if (ODD) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    w[e] = e < na ? norm[a + e] : 0.f;
-                                    w[8 + e] = e < nb ? norm[b + e] : 0.f;
-                                }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 16; e += 4)
-                                    *reinterpret_cast<float4 *>(w + e) = (e < 8 ? na : nb) > 0 ? *reinterpret_cast<const float4 *>(norm + (e < 8 ? a + e : b + e - 8))
-                                                                                              : make_float4(0.f, 0.f, 0.f, 0.f);
-                            }
-                        }
-                        const float r = 1.f / sqrtf(sum / p.D + p.eps);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] *= r * w[e];
-                    }
+                    r = rsqrtf(fmaf(sum, p.inv_D, p.eps));
                 }
-                if (turns && 8 * i < half) {
-                    if (p.adjacent) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (!ODD || 8 * i + e < half) {
-                                const float u = x[2 * e], t = x[2 * e + 1];
-                                x[2 * e] = u * cosine[e] - t * sine[e];
-                                x[2 * e + 1] = t * cosine[e] + u * sine[e];
-                            }
-                    } else {
+                if (8 * i < half) {
+                    if (ADJACENT) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const float u = x[e], t = x[8 + e];
-                            x[e] = u * cosine[e] - t * sine[e];
-                            x[8 + e] = t * cosine[e] + u * sine[e];
+                            y[e] = mul2(x[e], A[e]);
+                            if (!ODD || 8 * i + e < half) y[e] = fma2(make_float2(x[e].y, x[e].x), B[e], y[e]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            y[e] = fma2(x[4 + e], B[e], mul2(x[e], A[e]));
+                            y[4 + e] = fma2(x[e], B[4 + e], mul2(x[4 + e], A[4 + e]));
                         }
                     }
+                } else {   // dims that do not turn are not mixed: 0 * infinity
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = mul2(x[e], A[e]);
                 }
-                if (!value) {
-                    ya = make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
-                    yb = make_uint4(pack2<T>(x[8], x[9]), pack2<T>(x[10], x[11]), pack2<T>(x[12], x[13]), pack2<T>(x[14], x[15]));
+                if (norm) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = mul2(y[e], make_float2(r, r));
                 }
+                xa = make_uint4(pack2<T>(y[0].x, y[0].y), pack2<T>(y[1].x, y[1].y), pack2<T>(y[2].x, y[2].y), pack2<T>(y[3].x, y[3].y));
+                xb = make_uint4(pack2<T>(y[4].x, y[4].y), pack2<T>(y[5].x, y[5].y), pack2<T>(y[6].x, y[6].y), pack2<T>(y[7].x, y[7].y));
             }
-            if (h < last) {
-                uint16_t *to = nullptr;
-                if (query)
-                    to = q_out + h * p.q_out_stride[2];
-                else if (cached)
-                    to = reinterpret_cast<uint16_t *>(place + (value ? p.pool.lc_stride : 0) + (h - p.Hq - (value ? p.H : 0)) * p.pool.head_stride);
-                if (to) {
-                    store8<ODD>(to + (na > 0 ? a : 0), na, ya);
-                    store8<ODD>(to + (nb > 0 ? b : 0), nb, yb);
-                }
-            }
+            store8<ODD>(dst + a, there && store_a ? na : 0, xa);
+            store8<ODD>(dst + b, there && store_b ? nb : 0, xb);
+            dst += kHeads * out_stride;
+            h += kHeads;
         }
     }
 }
 
 namespace {
 
-template <typename T, int W, bool ODD> cudaError_t launch_append_as(AppendParams p, int sm_count, cudaStream_t stream)
+template <typename T, int W, bool ODD, bool ADJACENT> cudaError_t launch_append_as(AppendParams p, int sm_count, cudaStream_t stream)
 {
     // A warp takes all heads of a row, which finds the row's sines once, where that gives each SM 16 warps; else it takes fewer.
-    const int heads = 32 / W, steps = (p.Hq + 2 * p.H + heads - 1) / heads;
+    constexpr int heads = 32 / W;
+    p.q_steps = (p.Hq + heads - 1) / heads;
+    p.k_steps = (p.H + heads - 1) / heads;
+    p.inv_D = 1.f / (float)p.D;
+    const int steps = p.q_steps + 2 * p.k_steps;
     const int64_t most = (int64_t)p.rows * steps / (16 * sm_count);
     p.steps = (int)std::max<int64_t>(1, std::min<int64_t>(steps, most));
     p.parts = (steps + p.steps - 1) / p.steps;
@@ -304,15 +393,19 @@ template <typename T, int W, bool ODD> cudaError_t launch_append_as(AppendParams
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, append_kernel<T, W, ODD>, p);
+    return cudaLaunchKernelEx(&cfg, append_kernel<T, W, ODD, ADJACENT>, p);
 }
 
+template <typename T, bool ADJACENT> cudaError_t launch_append_dims(const AppendParams &p, int sm_count, cudaStream_t stream)
+{
+    if (p.rotated / 2 % 8) return launch_append_as<T, 32, true, ADJACENT>(p, sm_count, stream);
+    if (p.D <= 64) return launch_append_as<T, 4, false, ADJACENT>(p, sm_count, stream);
+    if (p.D <= 128) return launch_append_as<T, 8, false, ADJACENT>(p, sm_count, stream);
+    return launch_append_as<T, 16, false, ADJACENT>(p, sm_count, stream);
+}
 template <typename T> cudaError_t launch_append_type(const AppendParams &p, int sm_count, cudaStream_t stream)
 {
-    if (p.rotated / 2 % 8) return launch_append_as<T, 32, true>(p, sm_count, stream);
-    if (p.D <= 64) return launch_append_as<T, 4, false>(p, sm_count, stream);
-    if (p.D <= 128) return launch_append_as<T, 8, false>(p, sm_count, stream);
-    return launch_append_as<T, 16, false>(p, sm_count, stream);
+    return p.adjacent ? launch_append_dims<T, true>(p, sm_count, stream) : launch_append_dims<T, false>(p, sm_count, stream);
 }
 
 }  // namespace

@@ -25,8 +25,9 @@ struct AppendParams {
     const uint8_t *axis;
     float rotary_scale;
     int32_t block_shift;          // log2 of block_tokens, -1: not a power of two
-    // set by the launcher: a row is `parts` pieces of work of `steps` steps each
-    int32_t parts, steps;
+    // set by the launcher: a row is `parts` pieces of work of `steps` steps each; steps of its queries, of its keys
+    int32_t parts, steps, q_steps, k_steps;
+    float inv_D;
 };
 cudaError_t launch_append(AppendParams p, int dtype, int sm_count, cudaStream_t stream);
 

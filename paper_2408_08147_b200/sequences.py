@@ -25,6 +25,7 @@ from . import binding as B
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
+_NO_STRIDE, _NO_ROTARY = (0, 0, 0), (0, 0, 1, 0, 0, 1.0)
 _DTYPES = {torch.bfloat16: B.PDKV_DTYPE_BF16, torch.float16: B.PDKV_DTYPE_FP16}
 
 
@@ -106,8 +107,8 @@ class Rotary:
                 raise ValueError(f"axes: expected {pairs} axes from 0 to 255")
             self.n_axes = int(axes.max()) + 1
             self.axis_t = torch.from_numpy(axes.astype(np.uint8)).to(device)
-        self.desc = B.pdkv_rotary(dims=dims, adjacent=int(self.adjacent), n_axes=self.n_axes, turns=self.turns_t.data_ptr(),
-                                  axis=self.axis_t.data_ptr() if self.n_axes > 1 else None, scale=self.scale)
+        # of pdkv_rotary, in order
+        self.fields = (dims, int(self.adjacent), self.n_axes, self.turns_t.data_ptr(), self.axis_t.data_ptr() if self.n_axes > 1 else 0, self.scale)
         self.device = self.turns_t.device
 
 
@@ -291,10 +292,7 @@ class CacheSession:
                 raise ValueError(f"cap: expected a positive number, got {cap}")
             f.cap = cap
         if slopes_t is not None:
-            self._check("slopes_t", slopes_t, torch.float32, (Hq,))
-            if Hq > 1 and slopes_t.stride(0) != 1:
-                raise ValueError("slopes_t has to be contiguous")
-            f.slopes = slopes_t.data_ptr()
+            f.slopes = self._weights("slopes_t", slopes_t, Hq)
         if mask_t is not None:
             self._check("mask_t", mask_t, torch.int32, (n, T, (T + 31) // 32))
             stride = mask_t.stride()
@@ -312,22 +310,24 @@ class CacheSession:
             f.offset, f.offset_stride = offset_t.data_ptr(), offset_t.stride(0)
         return f
 
-    def _heads(self, name, t, lead, heads, out):
-        """Strides between sequences, rows and heads of a tensor [*lead, heads, head_dim]."""
-        D = self._shape[3]
-        if t.dtype != self.dtype or t.shape != (*lead, heads, D) or t.device != self._device:
-            raise ValueError(f"{name}: expected {self.dtype} {(*lead, heads, D)} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        if not out and t.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{name}: entering a cache has no gradient; detach it or call under torch.no_grad()")
+    def _heads(self, name, t, shape):
+        """Strides between sequences, rows and heads of a tensor [sequences, rows, heads, head_dim] or [rows, heads, head_dim]."""
+        if t.dtype != self.dtype or t.shape != shape or t.device != self._device:
+            raise ValueError(f"{name}: expected {self.dtype} {shape} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         stride = t.stride()
-        if D > 1 and stride[-1] != 1:
+        if stride[-1] != 1 and shape[-1] > 1:
             raise ValueError(f"{name}: the dims of a head have to be adjacent")
-        return stride[:3] if len(lead) == 2 else (0, *stride[:2])
+        return stride[:3] if len(shape) == 4 else (0, stride[0], stride[1])
+
+    def _weights(self, name, t, n):
+        """Device address of n float32 numbers."""
+        self._check(name, t, torch.float32, (n,))
+        if n > 1 and t.stride(0) != 1:
+            raise ValueError(f"{name} has to be contiguous")
+        return t.data_ptr()
 
     def _ints(self, name, t, shape):
         """Device address of a dense int32 tensor."""
-        if t is None:
-            return None
         self._check(name, t, torch.int32, shape)
         if not t.is_contiguous():
             raise ValueError(f"{name} has to be contiguous")
@@ -342,56 +342,57 @@ class CacheSession:
         Keys and queries are divided by their root mean square and multiplied by ``k_norm_t`` / ``q_norm_t`` (float32 ``[head_dim]``) where
         given, then turned by ``rotary`` at ``position_t`` (int32, one for each row, ``[axes, rows]`` for several axes; default: where the token
         stands behind its prefix).  There is no backward pass."""
-        lead = tuple(k_t.shape[:-2])
+        n_seq, _, _, D = self._shape
+        lead = tuple(k_t.shape)[:-2]
         packed = row_begin_t is not None
-        if len(lead) != (1 if packed else 2) or (not packed and lead[0] != self._shape[0]):
-            raise ValueError(f"k_t: expected {'[rows, ' if packed else f'[{self._shape[0]}, new, '}heads, dims], got {tuple(k_t.shape)}")
-        rows = lead[0] if packed else lead[0] * lead[1]
-        heads = self.geom.num_kv_heads
-        a = B.pdkv_append_args(rows=rows, k=k_t.data_ptr(), v=v_t.data_ptr(), k_stride=self._heads("k_t", k_t, lead, heads, False),
-                               v_stride=self._heads("v_t", v_t, lead, heads, False))
-        made = None
+        if len(lead) != (1 if packed else 2) or (not packed and lead[0] != n_seq):
+            raise ValueError(f"k_t: expected {'[rows, ' if packed else f'[{n_seq}, new, '}heads, dims], got {tuple(k_t.shape)}")
+        rows = lead[0] if packed else n_seq * lead[1]
+        shape = (*lead, self.geom.num_kv_heads, D)
+        k_stride, v_stride = self._heads("k_t", k_t, shape), self._heads("v_t", v_t, shape)
+        if (k_t.requires_grad or v_t.requires_grad or (q_t is not None and q_t.requires_grad)) and torch.is_grad_enabled():
+            raise ValueError("entering a cache has no gradient; detach the tensors or call under torch.no_grad()")
+        stream = self._on(stream)
+        q = q_out = 0
+        q_stride = q_out_stride = _NO_STRIDE
         if q_t is not None:
             if not self.num_q_heads:
                 raise ValueError("q_t: the session has no query heads")
-            a.q, a.q_stride = q_t.data_ptr(), self._heads("q_t", q_t, lead, self.num_q_heads, False)
+            shape = (*lead, self.num_q_heads, D)
+            q_stride = self._heads("q_t", q_t, shape)
             if q_out_t is None:
-                q_out_t = made = torch.empty(q_t.shape, dtype=self.dtype, device=self._device)
-            a.q_out, a.q_out_stride = q_out_t.data_ptr(), self._heads("q_out_t", q_out_t, lead, self.num_q_heads, True)
+                q_out_t = q_t.new_empty(shape)
+                if stream != self._on_current():
+                    self._record(stream, q_out_t)
+            q, q_out, q_out_stride = q_t.data_ptr(), q_out_t.data_ptr(), self._heads("q_out_t", q_out_t, shape)
         elif q_out_t is not None:
             raise ValueError("q_out_t needs q_t")
-        n_seq, D = self._shape[0], self._shape[3]
+        row_begin = n_new = seq_len = position = q_norm = k_norm = 0
         if packed:
-            a.row_begin = self._ints("row_begin_t", row_begin_t, (n_seq + 1,))
+            row_begin = self._ints("row_begin_t", row_begin_t, (n_seq + 1,))
             if n_new_t is not None:
                 raise ValueError("n_new_t does not go with row_begin_t")
-        if n_new_t is not None:
-            a.n_new = self._ints("n_new_t", n_new_t, (n_seq,))
+        elif n_new_t is not None:
+            n_new = self._ints("n_new_t", n_new_t, (n_seq,))
         if seq_len_t is not None:
-            a.seq_len = self._lens(seq_len_t)
-        if q_norm_t is not None or k_norm_t is not None:
-            for name, t in (("q_norm_t", q_norm_t), ("k_norm_t", k_norm_t)):
-                if t is not None:
-                    self._check(name, t, torch.float32, (D,))
-                    if D > 1 and t.stride(0) != 1:
-                        raise ValueError(f"{name} has to be contiguous")
-            a.q_norm = None if q_norm_t is None else q_norm_t.data_ptr()
-            a.k_norm = None if k_norm_t is None else k_norm_t.data_ptr()
-            a.norm_eps = eps
+            seq_len = self._ints("seq_len_t", seq_len_t, (n_seq,))
+        if q_norm_t is not None:
+            q_norm = self._weights("q_norm_t", q_norm_t, D)
+        if k_norm_t is not None:
+            k_norm = self._weights("k_norm_t", k_norm_t, D)
+        turn = _NO_ROTARY
         if rotary is not None:
             if rotary.device != self._device:
                 raise ValueError(f"rotary: laid out on {rotary.device}, the pool is on {self._device}")
-            a.rotary = rotary.desc
+            turn = rotary.fields
             if position_t is not None:
-                a.position = self._ints("position_t", position_t, (rotary.n_axes, rows) if rotary.n_axes > 1 else (rows,))
-                a.position_stride = rows
+                position = self._ints("position_t", position_t, (rotary.n_axes, rows) if rotary.n_axes > 1 else (rows,))
             elif rotary.n_axes > 1:
                 raise ValueError("rotary: several axes need position_t")
         elif position_t is not None:
             raise ValueError("position_t needs rotary")
-        stream = self._on(stream)
-        if made is not None and stream != self._on_current():
-            self._record(stream, made)
+        a = B.append_args(rows, row_begin, n_new, seq_len, q, k_t.data_ptr(), v_t.data_ptr(), q_out, *q_stride, *k_stride, *v_stride, *q_out_stride, q_norm, k_norm, eps,
+                          position, rows, *turn)
         B.pdkv_append(self.handle, layer, a, stream)
         return q_out_t
 
@@ -404,19 +405,22 @@ class CacheSession:
         if not 0 <= l0 < l1 <= self.geom.num_layers:
             raise ValueError(f"layers: expected a range within [0, {self.geom.num_layers}), got {layers}")
         n_seq = self._shape[0]
-        if path_t.dtype != torch.int32 or path_t.dim() != 2 or path_t.shape[0] != n_seq or path_t.device != self._device:
-            raise ValueError(f"path_t: expected int32 [{n_seq}, path] on {self._device}, got {path_t.dtype} {tuple(path_t.shape)} on {path_t.device}")
-        if path_t.shape[1] > 1 and path_t.stride(1) != 1:
+        shape, stride = path_t.shape, path_t.stride()
+        if path_t.dtype != torch.int32 or len(shape) != 2 or shape[0] != n_seq or path_t.device != self._device:
+            raise ValueError(f"path_t: expected int32 [{n_seq}, path] on {self._device}, got {path_t.dtype} {tuple(shape)} on {path_t.device}")
+        if shape[1] > 1 and stride[1] != 1:
             raise ValueError("path_t: the entries of a path have to be adjacent")
-        made = None
-        if new_len_t is None:
-            new_len_t = made = path_t.new_empty((n_seq,))
-        a = B.pdkv_accept_args(path=path_t.data_ptr(), path_stride=path_t.stride(0), path_len=path_t.shape[1],
-                               new_tokens=self.q_tokens if new_tokens is None else new_tokens, n_new=self._ints("n_new_t", n_new_t, (n_seq,)),
-                               seq_len=self._ints("seq_len_t", seq_len_t, (n_seq,)), new_len=self._ints("new_len_t", new_len_t, (n_seq,)))
         stream = self._on(stream)
-        if made is not None and stream != self._on_current():
-            self._record(stream, made)
+        lens = (n_seq,)
+        if new_len_t is None:
+            new_len_t = path_t.new_empty(lens)
+            new_len = new_len_t.data_ptr()
+            if stream != self._on_current():
+                self._record(stream, new_len_t)
+        else:
+            new_len = self._ints("new_len_t", new_len_t, lens)
+        a = B.accept_args(path_t.data_ptr(), stride[0], shape[1], self.q_tokens if new_tokens is None else new_tokens,
+                          0 if n_new_t is None else self._ints("n_new_t", n_new_t, lens), 0 if seq_len_t is None else self._ints("seq_len_t", seq_len_t, lens), new_len)
         B.pdkv_accept(self.handle, l0, l1, a, stream)
         return new_len_t
 
