@@ -174,7 +174,7 @@ __device__ __forceinline__ void load_slices(const AttnParams &p, const CUtensorM
 
 // Adds what was left out of the products of an item (see left_out) to its results: a warp a row, the rows and dims that the
 // same thread has written.  A direct result has been rounded already, and such pieces of it are rounded twice.
-template <typename T, bool FORM>
+template <typename T, int FORM>
 __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it, int len, int limit, const float (*sml)[16][2], int nt, int wm)
 {
     const int lane = threadIdx.x % 32, safe = min(limit, FORM ? len - newest_of(p, it.seq) : len - (p.q_tokens - 1));
@@ -224,7 +224,7 @@ __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it
 //
 // FORM: another form than plain causal.  The logits, once they are there, become what the form says (capped, biased, hidden by the
 // rows' masks); from then on they are in base 2 and nothing else differs, but that a row may see nothing of what it is multiplied with.
-template <typename T, int DP, int KD, bool HIDES, bool FORM, int NT, int WM>
+template <typename T, int DP, int KD, bool HIDES, int FORM, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
                                             float (*sml)[16][2], volatile uint32_t *wild, RingBarriers &bar, uint32_t n, bool &dead)
 {
@@ -233,7 +233,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, wm = warp % WM, group = warp / WM;
     const bool own = it.seq >= 0;
     const uint32_t ring = smem_u32(smem);
-    const float scale = FORM ? 1.f : fabsf(p.scale_log2);
+    const float scale = FORM >= kCapped ? 1.f : fabsf(p.scale_log2);
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
 
     // operand Q^T: row lane / 4 of each tile of eight, dims 2 (lane % 4) and 8 further of each sixteen
@@ -257,7 +257,6 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
     int sees[NT][2];
     float *logits[NT][2];
     int n_new = 0;           // FORM, own tokens: the newest of the sequence
-    bool there[NT][2];       // FORM: the query token is one of them
     Bias bias[NT][2];
     if (FORM && own) n_new = newest_of(p, it.seq);
 #pragma unroll
@@ -270,12 +269,12 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             logits[t][j] = nullptr;
             if (FORM) {
                 const RowId id = row_id(p, it, it.row0 + (live ? r : 0));
-                there[t][j] = id.token < (own ? n_new : newest_of(p, id.seq));
-                bias[t][j] = bias_of(p, it, id, own ? len : own_len(p, id.seq, p.segs[id.seq].len));
+                if (id.token >= (own ? n_new : newest_of(p, id.seq))) sees[t][j] = 0;   // the query token is not there
+                if (FORM == kSloped) bias[t][j] = bias_of(p, it, id, own ? len : own_len(p, id.seq, p.segs[id.seq].len));
             }
             if (own) {
                 if (!FORM) sees[t][j] = min(limit, len - (p.q_tokens - 1 - (it.row0 + (live ? r : 0)) / p.G));
-                if (p.logits && live) {
+                if (!FORM && p.logits && live) {
                     const AttnSeq s = p.seqs[it.seq];
                     logits[t][j] = p.logits + s.logits + ((int64_t)it.head * p.G * p.q_tokens + it.row0 + r) * s.logit_stride;
                 }
@@ -351,7 +350,19 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 #pragma unroll
                 for (int t = 0; t < NT; ++t) multiply<T>(z[h][t], a, q[k][t][0], q[k][t][1]);
             }
-        if constexpr (FORM) {
+        if constexpr (FORM >= kCapped) {
+            if (FORM == kCapped || p.cap_out != 0.f) {
+                const float in = fabsf(p.cap_in);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) z[h][t][j] = capped(z[h][t][j], in, p.cap_out);
+            }
+        }
+        if constexpr (FORM == kSloped) {
+            const float in = p.cap_out != 0.f ? 1.f : fabsf(p.scale_log2);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -359,12 +370,15 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                     const Bias b = bias[t][j & 1];
                     const int first = t0 + lane / 4 + 8 * (j >> 1) - b.query;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float x = p.cap_out != 0.f ? capped(z[h][t][j], fabsf(p.cap_in), p.cap_out) : z[h][t][j] * fabsf(p.scale_log2);
-                        x = fmaf(b.slope, (float)(first + 16 * h), x);
-                        z[h][t][j] = there[t][j & 1] ? x : -INFINITY;
-                    }
+                    for (int h = 0; h < 2; ++h) z[h][t][j] = fmaf(b.slope, (float)(first + 16 * h), z[h][t][j] * in);
                 }
+        }
+        if constexpr (FORM != kPlain) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (sees[t][j & 1] == 0) z[0][t][j] = z[1][t][j] = -INFINITY;
             if (own && t0 + kSlice > safe) {
                 const int from = t0 - (len - n_new);
 #pragma unroll
@@ -378,7 +392,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
                             float &y = z[x / 2][t][x % 2 * 2 + j];
                             if (!(seen >> (8 * x) & 1))
                                 y = -INFINITY;
-                            else if (p.offset && p.slopes && from + lane / 4 + 8 * x >= 0)   // its place is not its slot
+                            else if (FORM == kSloped && p.offset && from + lane / 4 + 8 * x >= 0)   // its place is not its slot
                                 y = fmaf(bias[t][j].slope, (float)(offset_of(p, it.seq, from + lane / 4 + 8 * x) - (from + lane / 4 + 8 * x)), y);
                         }
                     }
@@ -400,7 +414,15 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int tok = t0 + 16 * h + lane / 4 + 8 * (j >> 1);
-                        if (logits[t][j & 1] && tok < limit) logits[t][j & 1][tok] = z[h][t][j] == -INFINITY ? -INFINITY : z[h][t][j] * scale;
+                        if constexpr (FORM != kPlain) {   // (where its row lies is found when it is wanted: that takes no registers)
+                            const int r = (wm * NT + t) * 8 + 2 * (lane % 4) + (j & 1);
+                            if (r < it.rows && tok < limit) {
+                                const AttnSeq s = p.seqs[it.seq];
+                                p.logits[s.logits + ((int64_t)it.head * p.G * p.q_tokens + it.row0 + r) * s.logit_stride + tok] =
+                                    z[h][t][j] == -INFINITY ? -INFINITY : z[h][t][j] * scale;
+                            }
+                        } else if (logits[t][j & 1] && tok < limit)
+                            logits[t][j & 1][tok] = z[h][t][j] == -INFINITY ? -INFINITY : z[h][t][j] * scale;
                     }
         float top[NT][2];
         bool grew = false;
@@ -551,7 +573,7 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 // 2 sequences of about 110000 tokens, 8 rows each, 6.4 TB/s.  Above, by the products of the four warps, or eight, of an SM
 // (64 rows of 256 dims over 40000 tokens 169 us, 8 rows 60; ptxas spills 130 to 190 bytes in the variants for 96, 128 and 256 dims).  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
 // them busy for 13% of the time.
-template <typename T, int DP, int KD, bool HIDES, bool FORM>
+template <typename T, int DP, int KD, bool HIDES, int FORM>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
     using R = Ring<DP>;
@@ -753,7 +775,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
 
 namespace {
 
-template <typename T, int DP, int KD, bool HIDES, bool FORM> cudaError_t launch_hides(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, int KD, bool HIDES, int FORM> cudaError_t launch_hides(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_shared(attend_items_kernel<T, DP, KD, HIDES, FORM>, Ring<DP>::kBytes, ready);
@@ -775,8 +797,10 @@ template <typename T, int DP, int KD, bool HIDES, bool FORM> cudaError_t launch_
 // a prefix take 79 us instead of 83.
 template <typename T, int DP, int KD> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
-    if (p.formed) return launch_hides<T, DP, KD, true, true>(p, map, stream);
-    return p.q_tokens > 1 ? launch_hides<T, DP, KD, true, false>(p, map, stream) : launch_hides<T, DP, KD, false, false>(p, map, stream);
+    if (p.formed == kSloped) return launch_hides<T, DP, KD, true, kSloped>(p, map, stream);
+    if (p.formed == kCapped) return launch_hides<T, DP, KD, true, kCapped>(p, map, stream);
+    if (p.formed == kMasked) return launch_hides<T, DP, KD, true, kMasked>(p, map, stream);
+    return p.q_tokens > 1 ? launch_hides<T, DP, KD, true, kPlain>(p, map, stream) : launch_hides<T, DP, KD, false, kPlain>(p, map, stream);
 }
 
 template <typename T> cudaError_t launch_type(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)

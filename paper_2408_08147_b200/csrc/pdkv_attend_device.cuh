@@ -215,6 +215,9 @@ __device__ __forceinline__ Bias bias_of(const AttnParams &p, const AttnItem &it,
     b.query = own - newest_of(p, id.seq) + offset_of(p, id.seq, id.token) + (it.seq >= 0 ? 0 : it.len);
     return b;
 }
+// What a kernel's variant knows of a form: nothing; who sees which of the newest tokens; caps too; biases too (and caps, where there are).
+enum : int { kPlain = 0, kMasked = 1, kCapped = 2, kSloped = 3 };
+
 // Capped logit in base 2.  tanh x = 1 - 2 / (1 + e^2x) is right at both ends, infinities too; its error, 2^-22 of the cap at most, is that
 // of the two approximate functions (ex2, rcp).
 __device__ __forceinline__ float capped(float z, float in, float out)

@@ -105,6 +105,35 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
     return d;
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return d;
+}
+// tanh(a z) for |a z| <= 0.7, two at a time on the pipe that has time (two special functions a logit more take 2048 cycles a tile of 128 rows,
+// half of the other work): z p(z^2), p the polynomial of degree 4 with the least largest error (a weighted fit of tanh x / x, reweighted
+// until the extremes are level), off by 2^-22.5 at most.  The powers of a are in its terms; returns up to which |z| it holds, nothing
+// where they or z^2 would leave the range of 32 bits.
+__device__ __forceinline__ float tanh_terms(float a, float (&c)[5])
+{
+    const float a2 = a * a;
+    c[0] = 0.9999985f * a;
+    c[1] = -0.33326975f * a * a2;
+    c[2] = 0.13257454f * a * a2 * a2;
+    c[3] = -0.05019526f * a * a2 * (a2 * a2);
+    c[4] = 0.013194186f * a * (a2 * a2) * (a2 * a2);
+    return a > 1e-4f && a < 1e3f ? 0.7f / a : -1.f;
+}
+__device__ __forceinline__ float2 tanh2(float2 z, const float (&c)[5])
+{
+    const float2 u = mul2(z, z);
+    float2 y = fma2(make_float2(c[4], c[4]), u, make_float2(c[3], c[3]));
+    y = fma2(y, u, make_float2(c[2], c[2]));
+    y = fma2(y, u, make_float2(c[1], c[1]));
+    y = fma2(y, u, make_float2(c[0], c[0]));
+    return mul2(z, y);
+}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
@@ -210,7 +239,7 @@ template <typename T, int DP> __device__ __forceinline__ void fetch_q(const Attn
 
 // FORM: another form than plain causal.  A thread turns the logits of its row into what the form says (capped, biased, hidden by the
 // row's mask) while they are in registers; from then on they are in base 2.
-template <typename T, int DP, bool FORM>
+template <typename T, int DP, int FORM>
 __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
     using G = TileShape<DP>;
@@ -386,7 +415,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         const int t = warp / 4, r = threadIdx.x % kSoftmaxThreads;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + kColS + t * kColTile, o_at = tmem + lanes + kColO + t * kColTile;
-        const float scale = FORM ? 1.f : fabsf(p.scale_log2);
+        // what a row's numbers are multiplied by on their way into the exponential (biased ones are in base 2 already)
+        const float scale = FORM == kSloped ? 1.f : FORM == kCapped ? p.cap_out : fabsf(p.scale_log2);
+        float tanh_c[5], tanh_most = 0.f;
+        if (FORM >= kCapped) tanh_most = tanh_terms(0.5f * kLn2 * fabsf(p.cap_in), tanh_c);
         const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
         uint32_t s_phase = 0, o_phase = 0, n = 0;
         bool q_there = q_early, q_done = false;   // the item's Q is on its way, has been handed over
@@ -436,7 +468,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const int safe = own ? min(w.limit, FORM ? w.len - n_new : w.len - (p.q_tokens - 1)) : w.limit;        // the same of every row
             const bool there = id.token < n_new;   // FORM: one of the newest
             Bias bias{0.f, 0};
-            if (FORM) bias = bias_of(p, w.it, id, own ? w.len : own_len(p, id.seq, p.segs[id.seq].len));
+            if (FORM == kSloped) bias = bias_of(p, w.it, id, own ? w.len : own_len(p, id.seq, p.segs[id.seq].len));
             bool wild = false;   // pieces of V were left out
             if (count > 0) {
                 if (!q_there) fetch_q<T, DP>(p, w, t, q_at);
@@ -453,25 +485,46 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
                     tmem_load_wait();
-                    if constexpr (FORM) {
-                        const float far = bias.slope * (float)(t0 - bias.query);
-                        if (p.cap_out != 0.f) {
-                            const float in = fabsf(p.cap_in), out = p.cap_out;
+                    if constexpr (FORM >= kCapped) {
+                        if (FORM == kCapped || p.cap_out != 0.f) {   // in units of the cap
+                            float most = 0.f;
 #pragma unroll
-                            for (int k = 0; k < kTileTokens; ++k) v[k] = capped(v[k], in, out);
-                            if (p.slopes) {
+                            for (int k = 0; k < kTileTokens; k += 2) most = max3(most, fabsf(v[k]), fabsf(v[k + 1]));
+                            if (__all_sync(~0u, most <= tanh_most)) {   // (false where one is infinite)
 #pragma unroll
-                                for (int k = 0; k < kTileTokens; ++k) v[k] += fmaf(bias.slope, (float)k, far);
+                                for (int k = 0; k < kTileTokens; k += 2) {
+                                    const float2 x = tanh2(make_float2(v[k], v[k + 1]), tanh_c);
+                                    v[k] = x.x;
+                                    v[k + 1] = x.y;
+                                }
+                            } else {
+                                const float in = fabsf(p.cap_in);
+#pragma unroll
+                                for (int k = 0; k < kTileTokens; ++k) v[k] = capped(v[k], in, 1.f);
                             }
-                        } else {
-                            const float in = fabsf(p.scale_log2);
-#pragma unroll
-                            for (int k = 0; k < kTileTokens; ++k) v[k] = fmaf(v[k], in, fmaf(bias.slope, (float)k, far));
                         }
-                        if (!there) {
+                    }
+                    if constexpr (FORM == kSloped) {
+                        // slope * (t0 + k - query): steps of sixteen tokens, and within them
+                        const float in = p.cap_out != 0.f ? p.cap_out : fabsf(p.scale_log2), far = bias.slope * (float)(t0 - bias.query);
+                        const float2 in2 = make_float2(in, in);
+                        float2 step[8];
 #pragma unroll
-                            for (int k = 0; k < kTileTokens; ++k) v[k] = -INFINITY;
+                        for (int k = 0; k < 8; ++k) step[k] = make_float2(bias.slope * (2 * k), bias.slope * (2 * k + 1));
+#pragma unroll
+                        for (int c = 0; c < kTileTokens; c += 16) {
+                            const float at = fmaf(bias.slope, (float)c, far);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const float2 x = fma2(make_float2(v[c + 2 * k], v[c + 2 * k + 1]), in2, add2(step[k], make_float2(at, at)));
+                                v[c + 2 * k] = x.x;
+                                v[c + 2 * k + 1] = x.y;
+                            }
                         }
+                    }
+                    if (FORM && !there) {
+#pragma unroll
+                        for (int k = 0; k < kTileTokens; ++k) v[k] = -INFINITY;
                     }
                     if (FORM && masked) {
                         const int from = t0 - (w.len - n_new);   // number of tile's first token among the newest
@@ -480,7 +533,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                             uint32_t seen = own ? newest_seen(p, id.seq, id.token, n_new, from + 32 * c) : ~0u;
                             const int left = w.limit - (t0 + 32 * c);
                             if (left < 32) seen &= left <= 0 ? 0u : (1u << left) - 1;
-                            if (own && p.offset && p.slopes && seen != 0) {   // the place of a newest token is not its slot
+                            if (FORM == kSloped && own && p.offset && seen != 0) {   // the place of a newest token is not its slot
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) {
                                     const int j = from + 32 * c + k;
@@ -886,7 +939,7 @@ namespace {
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-template <typename T, int DP, bool FORM> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
+template <typename T, int DP, int FORM> cudaError_t launch_dims(const AttnParams &p, const CUtensorMap &map, cudaStream_t stream)
 {
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = allow_shared(attend_tile_kernel<T, DP, FORM>, (int)TileShape<DP>::kBytes, ready);
@@ -974,8 +1027,10 @@ template <typename T> cudaError_t launch_weigh_type(const AttnParams &p, const C
 }
 template <typename T> cudaError_t launch_tile_type(const AttnParams &p, const CUtensorMap &m, cudaStream_t stream)
 {
-    if (p.formed) return p.D <= 64 ? launch_dims<T, 64, true>(p, m, stream) : launch_dims<T, 128, true>(p, m, stream);
-    return p.D <= 64 ? launch_dims<T, 64, false>(p, m, stream) : launch_dims<T, 128, false>(p, m, stream);
+    if (p.formed == kSloped) return p.D <= 64 ? launch_dims<T, 64, kSloped>(p, m, stream) : launch_dims<T, 128, kSloped>(p, m, stream);
+    if (p.formed == kCapped) return p.D <= 64 ? launch_dims<T, 64, kCapped>(p, m, stream) : launch_dims<T, 128, kCapped>(p, m, stream);
+    if (p.formed == kMasked) return p.D <= 64 ? launch_dims<T, 64, kMasked>(p, m, stream) : launch_dims<T, 128, kMasked>(p, m, stream);
+    return p.D <= 64 ? launch_dims<T, 64, kPlain>(p, m, stream) : launch_dims<T, 128, kPlain>(p, m, stream);
 }
 
 }  // namespace

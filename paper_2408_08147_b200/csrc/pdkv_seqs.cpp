@@ -662,7 +662,7 @@ int attend_call(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, const 
         if (p.scale_log2 == 0.f) p.scale_log2 = std::copysign(std::numeric_limits<float>::denorm_min(), a->scale);
         p.seq_len = a->seq_len;
         if (f) {
-            p.formed = 1;
+            p.formed = f->slopes ? 3 : f->cap > 0.f ? 2 : 1;
             // (a scale of zero as above: the logits' infinities stay what they are)
             p.cap_in = cap_in == 0 && f->cap > 0.f ? std::copysign(std::numeric_limits<float>::denorm_min(), a->scale) : (float)cap_in;
             p.cap_out = (float)cap_out;

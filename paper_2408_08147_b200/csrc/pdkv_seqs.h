@@ -93,7 +93,7 @@ struct AttnParams {
     int32_t layer;
     int32_t block_shift;        // log2 of block_tokens, -1: not a power of two
     // another form than plain causal (pdkv_attend_form): a variant of each kernel
-    int32_t formed;
+    int32_t formed;             // 1: masks alone, 2: caps too, 3: biases too (and caps, where there are)
     float cap_in, cap_out;      // logits (base 2): cap_out tanh(z cap_in / (2 log2 e)); cap_out 0: z scale_log2
     const float *slopes;
     const uint32_t *mask;
