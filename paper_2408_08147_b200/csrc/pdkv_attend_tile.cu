@@ -201,12 +201,13 @@ struct Work {
         return pair ? 2 * i + kv : i / 2 * 4 + kv * ((i | 1) < tiles ? 2 : 1) + i % 2;
     }
 };
-__device__ __forceinline__ Work work_of(const AttnParams &p, const AttnItem &it)
+template <int FORM> __device__ __forceinline__ Work work_of(const AttnParams &p, const AttnItem &it)
 {
     Work w;
     w.it = it;
     w.len = it.seq >= 0 ? own_len(p, it.seq, it.len) : it.len;
     w.limit = min(it.tok1, w.len);
+    if (FORM && nobody_there(p, it)) w.limit = min(w.limit, it.tok0);
     w.tiles = w.limit > it.tok0 ? (w.limit - it.tok0 + kTileTokens - 1) / kTileTokens : 0;
     w.pair = it.rows > kTileRows;
     return w;
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         for (bool more = true; more;) {
             const AttnItem next_it = fetch_item(p.tile_items, max(it.next, 0));
             more = it.next >= 0;
-            const Work w = work_of(p, it);
+            const Work w = work_of<FORM>(p, it);
             it = next_it;
             const int group = w.pair ? 1 : 2;   // tiles of tokens whose K come before their V
             for (int i0 = 0; i0 < w.tiles; i0 += group) {
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             for (bool more = true; more;) {
                 const AttnItem next_it = fetch_item(p.tile_items, max(it.next, 0));
                 more = it.next >= 0;
-                const Work w = work_of(p, it);
+                const Work w = work_of<FORM>(p, it);
                 it = next_it;
                 if (w.tiles == 0) continue;
                 // the operand at place `at` of the load order has arrived, is no longer needed
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         bool q_early = false;   // the first item's Q comes while tensor memory is set up
         {
-            const Work w = work_of(p, first);
+            const Work w = work_of<FORM>(p, first);
             q_early = w.count(warp / 4) > 0;
             if (q_early) fetch_q<T, DP>(p, w, warp / 4, q_at);
         }
@@ -455,7 +456,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         for (bool more = true; more;) {
             const AttnItem next_it = fetch_item(p.tile_items, max(it.next, 0));
             more = it.next >= 0;
-            const Work w = work_of(p, it);
+            const Work w = work_of<FORM>(p, it);
             it = next_it;
             const uint32_t n0 = n;
             n += 2 * w.tiles;
@@ -625,7 +626,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                 if (safe < w.limit) wild = any_of(w.pair ? 2 : 3 + t, w.pair ? 2 * kSoftmaxThreads : kSoftmaxThreads, wild);
                 // every product with Q is done: the next item's Q may take its place
                 if (more) {
-                    const Work next = work_of(p, next_it);
+                    const Work next = work_of<FORM>(p, next_it);
                     if (next.count(t) > 0) {
                         fetch_q<T, DP>(p, next, t, q_at);
                         finish_q();

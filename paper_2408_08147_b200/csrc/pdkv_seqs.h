@@ -106,6 +106,10 @@ int attend_ctas_per_sm(int head_dim);
 bool attend_map_supported(const pdkv_pool_desc &d);
 int attend_map_box(const pdkv_pool_desc &d);
 cudaError_t launch_attend(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
+// (its variants for other forms than plain causal)
+cudaError_t launch_attend_masked(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
+cudaError_t launch_attend_capped(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
+cudaError_t launch_attend_sloped(const AttnParams &p, const void *map, int dtype, cudaStream_t stream);
 // The tile kernel (tcgen05): segments with many rows.  `map` is a CUtensorMap of the pool.
 constexpr int kMapBytes = 128;
 bool attend_tile_supported(const pdkv_pool_desc &d);
