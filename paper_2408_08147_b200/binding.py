@@ -114,17 +114,27 @@ class pdkv_accept_args(C.Structure):
                 ("n_new", C.c_void_p), ("seq_len", C.c_void_p), ("new_len", C.c_void_p)]
 
 
-_APPEND, _ACCEPT = struct.Struct("@i4x7Q12q2Qf4xQq3i4x2Qf4x"), struct.Struct("@Qq2i3Q")
-assert _APPEND.size == C.sizeof(pdkv_append_args) and _ACCEPT.size == C.sizeof(pdkv_accept_args)
+_APPEND, _ACCEPT, _FORM = struct.Struct("@i4x7Q12q2Qf4xQq3i4x2Qf4x"), struct.Struct("@Qq2i3Q"), struct.Struct("@f4x2Q2q2Qq")
+assert _APPEND.size == C.sizeof(pdkv_append_args) and _ACCEPT.size == C.sizeof(pdkv_accept_args) and _FORM.size == C.sizeof(pdkv_attend_form)
 
 
 def append_args(*fields) -> pdkv_append_args:
-    """pdkv_append_args from its fields in order, those of the arrays and of the rotary one by one (a third of the time of naming them)."""
+    """pdkv_append_args from its fields in order, those of the arrays and of the rotary one by one (a third of the time of naming them).
+    Numbers for its floats have to fit 32 bits (:func:`float32`)."""
     return pdkv_append_args.from_buffer_copy(_APPEND.pack(*fields))
+
+
+def float32(x: float) -> float:
+    """The nearest number of 32 bits, an infinity beyond them."""
+    return C.c_float(x).value
 
 
 def accept_args(*fields) -> pdkv_accept_args:
     return pdkv_accept_args.from_buffer_copy(_ACCEPT.pack(*fields))
+
+
+def attend_form(*fields) -> pdkv_attend_form:
+    return pdkv_attend_form.from_buffer_copy(_FORM.pack(*fields))
 
 
 class pdkv_evict_args(C.Structure):

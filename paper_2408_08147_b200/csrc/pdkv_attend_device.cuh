@@ -201,7 +201,7 @@ __device__ __forceinline__ uint32_t newest_seen(const AttnParams &p, int seq, in
     auto word = [&](int k) -> uint32_t {
         if (k < 0) return ~0u;
         if (32 * k >= n) return 0u;
-        if (mask) return __ldg(mask + k);
+        if (mask) return mask[k];
         const int last = token - 32 * k;   // newest token j <= token
         return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1;
     };

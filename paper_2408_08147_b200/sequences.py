@@ -108,7 +108,7 @@ class Rotary:
             self.n_axes = int(axes.max()) + 1
             self.axis_t = torch.from_numpy(axes.astype(np.uint8)).to(device)
         # of pdkv_rotary, in order
-        self.fields = (dims, int(self.adjacent), self.n_axes, self.turns_t.data_ptr(), self.axis_t.data_ptr() if self.n_axes > 1 else 0, self.scale)
+        self.fields = (dims, int(self.adjacent), self.n_axes, self.turns_t.data_ptr(), self.axis_t.data_ptr() if self.n_axes > 1 else 0, B.float32(self.scale))
         self.device = self.turns_t.device
 
 
@@ -135,7 +135,8 @@ class CacheSession:
             dtype = pool_t.dtype if pool_t.dtype in _DTYPES else torch.bfloat16
         if dtype not in _DTYPES:
             raise ValueError("attention takes bfloat16 or float16")
-        if num_q_heads and pool_t.dtype in _DTYPES and dtype != pool_t.dtype:
+        self._other_type = pool_t.dtype in _DTYPES and dtype != pool_t.dtype
+        if num_q_heads and self._other_type:
             raise ValueError(f"the pool holds {pool_t.dtype}, not {dtype}")
         if not pool_t.is_contiguous():
             raise ValueError("the pool tensor has to be contiguous")
@@ -286,29 +287,32 @@ class CacheSession:
 
     def _form(self, cap, slopes_t, mask_t, n_new_t, offset_t):
         n, T, Hq, _ = self._shape
-        f = B.pdkv_attend_form()
-        if cap is not None:
-            if not cap > 0:
-                raise ValueError(f"cap: expected a positive number, got {cap}")
-            f.cap = cap
+        slopes = mask = n_new = offset = row = 0
+        stride = (0, 0)
+        if cap is None:
+            cap = 0.0
+        elif not cap > 0:
+            raise ValueError(f"cap: expected a positive number, got {cap}")
+        else:
+            cap = B.float32(cap)
         if slopes_t is not None:
-            f.slopes = self._weights("slopes_t", slopes_t, Hq)
+            slopes = self._weights("slopes_t", slopes_t, Hq)
         if mask_t is not None:
             self._check("mask_t", mask_t, torch.int32, (n, T, (T + 31) // 32))
             stride = mask_t.stride()
             if T > 32 and stride[2] != 1:
                 raise ValueError("mask_t: the words of a query token have to be adjacent")
-            f.mask, f.mask_stride = mask_t.data_ptr(), stride[:2]
+            mask = mask_t.data_ptr()
         if n_new_t is not None:
-            f.n_new = self._ints("n_new_t", n_new_t, (n,))
+            n_new = self._ints("n_new_t", n_new_t, (n,))
         if offset_t is not None:
             if slopes_t is None:
                 raise ValueError("offset_t needs slopes_t")
             self._check("offset_t", offset_t, torch.int32, (n, T))
             if T > 1 and offset_t.stride(1) != 1:
                 raise ValueError("offset_t: the tokens of a sequence have to be adjacent")
-            f.offset, f.offset_stride = offset_t.data_ptr(), offset_t.stride(0)
-        return f
+            offset, row = offset_t.data_ptr(), offset_t.stride(0)
+        return B.attend_form(cap, slopes, mask, stride[0], stride[1], n_new, offset, row)
 
     def _heads(self, name, t, shape):
         """Strides between sequences, rows and heads of a tensor [sequences, rows, heads, head_dim] or [rows, heads, head_dim]."""
@@ -343,6 +347,8 @@ class CacheSession:
         given, then turned by ``rotary`` at ``position_t`` (int32, one for each row, ``[axes, rows]`` for several axes; default: where the token
         stands behind its prefix).  There is no backward pass."""
         n_seq, _, _, D = self._shape
+        if self._other_type:
+            raise ValueError(f"the pool holds {self.pool_t.dtype}, not {self.dtype}")
         lead = tuple(k_t.shape)[:-2]
         packed = row_begin_t is not None
         if len(lead) != (1 if packed else 2) or (not packed and lead[0] != n_seq):
@@ -391,7 +397,7 @@ class CacheSession:
                 raise ValueError("rotary: several axes need position_t")
         elif position_t is not None:
             raise ValueError("position_t needs rotary")
-        a = B.append_args(rows, row_begin, n_new, seq_len, q, k_t.data_ptr(), v_t.data_ptr(), q_out, *q_stride, *k_stride, *v_stride, *q_out_stride, q_norm, k_norm, eps,
+        a = B.append_args(rows, row_begin, n_new, seq_len, q, k_t.data_ptr(), v_t.data_ptr(), q_out, *q_stride, *k_stride, *v_stride, *q_out_stride, q_norm, k_norm, B.float32(eps),
                           position, rows, *turn)
         B.pdkv_append(self.handle, layer, a, stream)
         return q_out_t

@@ -43,10 +43,11 @@ class Pool:
 
 
 def tolerance(y, mag, dtype):
-    """The sum of squares is 16 products a lane and 5 sums between lanes, 2^-24 each; half of that enters the root; the mean, root, reciprocal,
-    weight and product round five times: below 16 * 2^-24 of the normalised value.  An angle is off by pi * 2^-25 by its conversion and
-    2^-32 of a turn, its sine and cosine by 2 units in the last place: 2^-22 together; the scale, the products and the sum round three
-    times.  (16 + 4 + 3) 2^-24 < 2^-19 of what is summed.  The result is rounded once, fp16 below 2^-14 to 2^-25."""
+    """The sum of squares is 4 products and 3 sums in a lane and 5 sums between lanes, 2^-24 each; half of that enters the root; the reciprocal of the
+    root is off by 2 units in the last place, mean, factor and product round four times: below 16 * 2^-24 of the normalised value.  An angle
+    is off by pi * 2^-25 by its conversion and 2^-32 of a turn, its sine and cosine by 2 units in the last place: 2^-22 together; the
+    scale, the weight, the products and the sum round five times.  (16 + 4 + 5) 2^-24 < 2^-19 of what is summed.  The result is rounded once,
+    fp16 below 2^-14 to 2^-25."""
     half = torch.finfo(dtype).eps / 2
     return 1.01 * (half * np.abs(y) + 2.0 ** -19 * mag) + (2.0 ** -25 if dtype == torch.float16 else 0)
 
@@ -315,6 +316,13 @@ def test_append_and_accept_on_other_streams_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert lens_t.tolist() == lens and (p.bits.cpu().numpy() == want).all()
+
+
+def test_a_session_of_the_other_type_takes_no_tokens():
+    p = Pool([20], G=2, D=64)
+    with p.session(num_q_heads=0, q_tokens=1, dtype=torch.float16) as s, pytest.raises(ValueError):      # (it may evict: elements are moved bit for bit)
+        s.append(0, p.values(1, 1, 2, 64).half(), p.values(1, 1, 2, 64).half())
+    assert (p.bits.cpu().numpy() == p.before).all()
 
 
 def test_refused_tensors():

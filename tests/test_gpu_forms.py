@@ -130,6 +130,8 @@ def test_weights_of_forms(c):
 
 
 KERNELS = [dict(lens=[150, 90], G=2, D=64, Q=5), dict(lens=[700, 600], H=1, G=4, D=128, Q=40, block=64)]
+# the prefix in the tile kernel, own tokens in the other one beside it
+BOTH = dict(lens=[150, 90, 33], G=4, D=128, Q=5, prefix_len=[700], member=[0, 0, 0], layout=LAYER_MAJOR)
 
 
 @pytest.mark.parametrize("c", KERNELS, ids=["warp", "tile"])
@@ -262,7 +264,7 @@ def test_a_step_of_speculative_decoding():
         assert torch.equal(turned3[:, 0], turned2[:, 0]) and torch.equal(out3, out2)
 
 
-@pytest.mark.parametrize("c", KERNELS, ids=["warp", "tile"])
+@pytest.mark.parametrize("c", KERNELS + [BOTH], ids=["warp", "tile", "both"])
 def test_recorded_and_replayed_beside_another_graph(c):
     s = Setup(**c)
     forms = [Form(s, kind="tree", ragged=True, cap=9.0, seed=1), Form(s, kind="any", ragged=True, slopes=True, seed=2)]
@@ -282,7 +284,7 @@ def test_recorded_and_replayed_beside_another_graph(c):
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-@pytest.mark.parametrize("c", KERNELS, ids=["warp", "tile"])
+@pytest.mark.parametrize("c", KERNELS + [BOTH], ids=["warp", "tile", "both"])
 def test_work_before_the_call_is_waited_for(c):
     s = Setup(**c)
     f = Form(s, kind="tree", ragged=True, cap=9.0, slopes=True, offset=True)
@@ -313,10 +315,32 @@ def test_refused_forms():
                    dict(n_new_t=ints(2 * n)[::2]), dict(offset_t=ints(n, T)), dict(offset_t=ints(n, T + 1), slopes_t=torch.zeros(Hq, device="cuda"))):
             with pytest.raises(ValueError):
                 x.attend(s.layer, s.q_t, **kw)
-        for kw in (dict(cap=float("inf")), dict(cap=1e-44), dict(cap=3e38)):
+        for kw in (dict(cap=float("inf")), dict(cap=1e-44), dict(cap=3e38), dict(cap=1e300)):
             with pytest.raises(B.PdkvError) as e:
                 x.attend(s.layer, s.q_t, **kw)
             assert e.value.status == B.PDKV_ERR_INVALID_ARG
         out = torch.empty_like(s.q_t)
         with pytest.raises(B.PdkvError):                        # written on what is read
             x.attend(s.layer, s.q_t, out_t=out, n_new_t=out.view(torch.int32).flatten()[:2])
+
+
+@pytest.mark.parametrize("c", [
+    dict(lens=[900, 700, 650], H=2, G=4, D=128, Q=160, block=64, form=dict(kind="documents", cap=20.0)),            # whole items of absent tokens
+    dict(lens=[900, 700, 650], H=1, G=2, D=64, Q=200, block=64, prefix_len=[300], member=[0, 0, -1], form=dict(kind="tree")),
+    dict(lens=[90, 70, 65], H=2, G=3, D=256, Q=40, block=64, prefix_len=[100], member=[0, -1, 0], form=dict(kind="any", slopes=True)),
+], ids=["tile", "prefix", "warp"])
+@pytest.mark.parametrize("news", [[1, 0, 64], [0, 0, 0], [65, 3, 1000]], ids=str)
+def test_few_of_many_query_tokens_are_there(c, news):
+    s, f, _ = setup(c)
+    news = [min(x, s.Q) for x in news]
+    f.news[:] = news
+    f.kw["n_new_t"] = torch.tensor(news, dtype=torch.int32, device="cuda")
+    scores = torch.rand(3, s.H, max(s.lens), device="cuda")
+    before = scores.double().cpu().numpy()
+    with s.session() as x:
+        got = x.attend(s.layer, s.q_t, **f.kw)
+        x.attend(s.layer, s.q_t, scores_t=scores, **f.kw)
+        x.status()
+    want = f.expect()
+    check(s, *got, want)
+    check_scores(s, before, scores, want, s.lens)
