@@ -118,23 +118,14 @@ _APPEND, _ACCEPT, _FORM = struct.Struct("@i4x7Q12q2Qf4xQq3i4x2Qf4x"), struct.Str
 assert _APPEND.size == C.sizeof(pdkv_append_args) and _ACCEPT.size == C.sizeof(pdkv_accept_args) and _FORM.size == C.sizeof(pdkv_attend_form)
 
 
-def append_args(*fields) -> pdkv_append_args:
-    """pdkv_append_args from its fields in order, those of the arrays and of the rotary one by one (a third of the time of naming them).
-    Numbers for its floats have to fit 32 bits (:func:`float32`)."""
-    return pdkv_append_args.from_buffer_copy(_APPEND.pack(*fields))
+# The bytes of pdkv_append_args, pdkv_accept_args and pdkv_attend_form from their fields in order, those of arrays and of the rotary one by one (a
+# quarter of the time of naming them).  Numbers for floats have to fit 32 bits (float32()).
+append_args, accept_args, attend_form = _APPEND.pack, _ACCEPT.pack, _FORM.pack
 
 
 def float32(x: float) -> float:
     """The nearest number of 32 bits, an infinity beyond them."""
     return C.c_float(x).value
-
-
-def accept_args(*fields) -> pdkv_accept_args:
-    return pdkv_accept_args.from_buffer_copy(_ACCEPT.pack(*fields))
-
-
-def attend_form(*fields) -> pdkv_attend_form:
-    return pdkv_attend_form.from_buffer_copy(_FORM.pack(*fields))
 
 
 class pdkv_evict_args(C.Structure):
@@ -214,10 +205,10 @@ def lib() -> C.CDLL:
     L.pdkv_seqs_status.argtypes = [vp, vp]
     L.pdkv_attend_scratch.argtypes = [vp, C.c_int, C.POINTER(C.c_size_t)]
     L.pdkv_attend.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), vp, C.c_size_t, vp]
-    L.pdkv_attend_formed.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), C.POINTER(pdkv_attend_form), vp, C.c_size_t, vp]
+    L.pdkv_attend_formed.argtypes = [vp, C.c_int, C.POINTER(pdkv_attend_args), vp, vp, C.c_size_t, vp]
     L.pdkv_rotary_turns.argtypes = [vp, C.c_int, vp]
-    L.pdkv_append.argtypes = [vp, C.c_int, C.POINTER(pdkv_append_args), vp]
-    L.pdkv_accept.argtypes = [vp, C.c_int, C.c_int, C.POINTER(pdkv_accept_args), vp]
+    L.pdkv_append.argtypes = [vp, C.c_int, vp, vp]
+    L.pdkv_accept.argtypes = [vp, C.c_int, C.c_int, vp, vp]
     L.pdkv_evict.argtypes = [vp, vp, C.c_int, C.c_int, C.POINTER(pdkv_evict_args), vp]
     for name in EXPORTS:
         if name not in ("pdkv_pool_bytes", "pdkv_strerror"):
@@ -561,9 +552,9 @@ def pdkv_attend(seqs: int, layer: int, args: pdkv_attend_args, scratch_ptr: int,
         raise PdkvError(rc, "pdkv_attend")
 
 
-def pdkv_attend_formed(seqs: int, layer: int, args: pdkv_attend_args, form: pdkv_attend_form, scratch_ptr: int, scratch_bytes: int,
-                       stream: int = 0) -> None:
-    rc = (_lib or lib()).pdkv_attend_formed(seqs, layer, C.byref(args), C.byref(form), scratch_ptr, scratch_bytes, stream)
+def pdkv_attend_formed(seqs: int, layer: int, args: pdkv_attend_args, form, scratch_ptr: int, scratch_bytes: int, stream: int = 0) -> None:
+    """``form``: a pdkv_attend_form or its bytes."""
+    rc = (_lib or lib()).pdkv_attend_formed(seqs, layer, C.byref(args), form if type(form) is bytes else C.byref(form), scratch_ptr, scratch_bytes, stream)
     if rc != PDKV_OK:
         raise PdkvError(rc, "pdkv_attend_formed")
 
@@ -576,14 +567,16 @@ def pdkv_rotary_turns(radians) -> np.ndarray:
     return out
 
 
-def pdkv_append(seqs: int, layer: int, args: pdkv_append_args, stream: int = 0) -> None:
-    rc = (_lib or lib()).pdkv_append(seqs, layer, C.byref(args), stream)
+def pdkv_append(seqs: int, layer: int, args, stream: int = 0) -> None:
+    """``args``: a pdkv_append_args or its bytes."""
+    rc = (_lib or lib()).pdkv_append(seqs, layer, args if type(args) is bytes else C.byref(args), stream)
     if rc != PDKV_OK:
         raise PdkvError(rc, "pdkv_append")
 
 
-def pdkv_accept(seqs: int, layer_begin: int, layer_end: int, args: pdkv_accept_args, stream: int = 0) -> None:
-    rc = (_lib or lib()).pdkv_accept(seqs, layer_begin, layer_end, C.byref(args), stream)
+def pdkv_accept(seqs: int, layer_begin: int, layer_end: int, args, stream: int = 0) -> None:
+    """``args``: a pdkv_accept_args or its bytes."""
+    rc = (_lib or lib()).pdkv_accept(seqs, layer_begin, layer_end, args if type(args) is bytes else C.byref(args), stream)
     if rc != PDKV_OK:
         raise PdkvError(rc, "pdkv_accept")
 

@@ -159,6 +159,7 @@ class CacheSession:
             self._scale = geom.head_dim ** -0.5
             n, t, h, d = self._shape
             dense = [t * h * d, h * d, d]
+            self._lse_stride = (t * h, h, 1)
             # argument block of the plain call: dense q and out, the default scale
             self._plain = B.pdkv_attend_args(q_stride=(*dense,), out_stride=(*dense,), scale=self._scale)
         except Exception:
@@ -244,7 +245,7 @@ class CacheSession:
                 raise ValueError("out_t: the dims of a head have to be adjacent")
             a.out_stride = stride[:3]
         if lse_t is None:
-            lse_t = torch.empty(shape[:3], dtype=torch.float32, device=self._device)
+            lse_t = torch.empty_strided(shape[:3], self._lse_stride, dtype=torch.float32, device=self._device)   # (quicker than empty)
             made.append(lse_t)
         else:
             self._check("lse_t", lse_t, torch.float32, shape[:3])
@@ -316,7 +317,7 @@ class CacheSession:
 
     def _heads(self, name, t, shape):
         """Strides between sequences, rows and heads of a tensor [sequences, rows, heads, head_dim] or [rows, heads, head_dim]."""
-        if t.dtype != self.dtype or t.shape != shape or t.device != self._device:
+        if t.dtype is not self.dtype or t.shape != shape or t.device != self._device:
             raise ValueError(f"{name}: expected {self.dtype} {shape} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         stride = t.stride()
         if stride[-1] != 1 and shape[-1] > 1:
@@ -332,9 +333,8 @@ class CacheSession:
 
     def _ints(self, name, t, shape):
         """Device address of a dense int32 tensor."""
-        self._check(name, t, torch.int32, shape)
-        if not t.is_contiguous():
-            raise ValueError(f"{name} has to be contiguous")
+        if t.dtype is not torch.int32 or t.shape != shape or t.device != self._device or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous int32 {shape} on {self._device}, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
         return t.data_ptr()
 
     def append(self, layer: int, k_t, v_t, q_t=None, *, q_out_t=None, rotary: Optional[Rotary] = None, position_t=None, q_norm_t=None,
@@ -358,7 +358,8 @@ class CacheSession:
         k_stride, v_stride = self._heads("k_t", k_t, shape), self._heads("v_t", v_t, shape)
         if (k_t.requires_grad or v_t.requires_grad or (q_t is not None and q_t.requires_grad)) and torch.is_grad_enabled():
             raise ValueError("entering a cache has no gradient; detach the tensors or call under torch.no_grad()")
-        stream = self._on(stream)
+        home = self._on_current()
+        stream = home if stream is None and self.stream is None else self._on(stream)
         q = q_out = 0
         q_stride = q_out_stride = _NO_STRIDE
         if q_t is not None:
@@ -367,8 +368,8 @@ class CacheSession:
             shape = (*lead, self.num_q_heads, D)
             q_stride = self._heads("q_t", q_t, shape)
             if q_out_t is None:
-                q_out_t = q_t.new_empty(shape)
-                if stream != self._on_current():
+                q_out_t = torch.empty_like(q_t)
+                if stream != home:
                     self._record(stream, q_out_t)
             q, q_out, q_out_stride = q_t.data_ptr(), q_out_t.data_ptr(), self._heads("q_out_t", q_out_t, shape)
         elif q_out_t is not None:
@@ -412,21 +413,23 @@ class CacheSession:
             raise ValueError(f"layers: expected a range within [0, {self.geom.num_layers}), got {layers}")
         n_seq = self._shape[0]
         shape, stride = path_t.shape, path_t.stride()
-        if path_t.dtype != torch.int32 or len(shape) != 2 or shape[0] != n_seq or path_t.device != self._device:
+        if path_t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n_seq or path_t.device != self._device:
             raise ValueError(f"path_t: expected int32 [{n_seq}, path] on {self._device}, got {path_t.dtype} {tuple(shape)} on {path_t.device}")
         if shape[1] > 1 and stride[1] != 1:
             raise ValueError("path_t: the entries of a path have to be adjacent")
-        stream = self._on(stream)
+        home = self._on_current()
+        stream = home if stream is None and self.stream is None else self._on(stream)
         lens = (n_seq,)
+        n_new = 0 if n_new_t is None else self._ints("n_new_t", n_new_t, lens)
+        seq_len = 0 if seq_len_t is None else self._ints("seq_len_t", seq_len_t, lens)
         if new_len_t is None:
-            new_len_t = path_t.new_empty(lens)
+            new_len_t = torch.empty_like(n_new_t) if n_new_t is not None else path_t.new_empty(lens)
             new_len = new_len_t.data_ptr()
-            if stream != self._on_current():
+            if stream != home:
                 self._record(stream, new_len_t)
         else:
             new_len = self._ints("new_len_t", new_len_t, lens)
-        a = B.accept_args(path_t.data_ptr(), stride[0], shape[1], self.q_tokens if new_tokens is None else new_tokens,
-                          0 if n_new_t is None else self._ints("n_new_t", n_new_t, lens), 0 if seq_len_t is None else self._ints("seq_len_t", seq_len_t, lens), new_len)
+        a = B.accept_args(path_t.data_ptr(), stride[0], shape[1], self.q_tokens if new_tokens is None else new_tokens, n_new, seq_len, new_len)
         B.pdkv_accept(self.handle, l0, l1, a, stream)
         return new_len_t
 
