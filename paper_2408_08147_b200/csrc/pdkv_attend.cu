@@ -37,8 +37,9 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     asm volatile("griddepcontrol.launch_dependents;");
     if (x < row_blocks) {
         if (!mine) return;
-        const int n = (parts.n[0] + parts.n[1] - way + ways - 1) / ways;   // of this warp: way, way + ways, ...
-        const float2 ml = joined_ml<32>(p, parts, lane);
+        const bool absent = p.formed && row / p.G >= newest_of(p, seq);   // a query token that is not there: nothing, and its parts may hold anything
+        const int n = absent ? 0 : (parts.n[0] + parts.n[1] - way + ways - 1) / ways;   // of this warp: way, way + ways, ...
+        const float2 ml = absent ? make_float2(-INFINITY, 0.f) : joined_ml<32>(p, parts, lane);
         const float base = ml.x == -INFINITY ? 0.f : ml.x;
         float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
         for (int i0 = 0; i0 < n; i0 += 32) {

@@ -641,7 +641,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
             const int head = w.it.head * p.G + id.g;
             const int64_t part_row = w.it.part_row + (!w.pair && t == 1 ? w.it.rows : 0);
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            const int64_t to = !live || dead ? -1
+            // (parts of query tokens that are not there are not read)
+            const int64_t to = !live || dead || (FORM && !there && !w.it.direct) ? -1
                                : w.it.direct ? id.seq * p.out_stride[0] + id.token * p.out_stride[1] + head * p.out_stride[2]
                                              : (part_row + row) * p.D;
             // (loops that run once an item stay rolled: fetching their instructions costs more than running them)
