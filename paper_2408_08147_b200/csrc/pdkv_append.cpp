@@ -82,7 +82,7 @@ int pdkv_append(const pdkv_seqs *s, int layer, const pdkv_append_args *a, void *
             for (const Rows &x : small)
                 if (touches(pool, x) || touches(x, q_out)) return PDKV_ERR_INVALID_ARG;
         }
-        // (steps of a head each at worst, four of them a block)
+        // (well inside what a launch takes)
         if ((double)a->rows * ((double)Hq + 2.0 * (double)H) / 4 > 2e9) return PDKV_ERR_LIMIT;
         if (!s->dev_mem) return PDKV_ERR_INVALID_ARG;   // host-only handle
         if (s->n_seq == 0 || a->rows == 0) return PDKV_OK;

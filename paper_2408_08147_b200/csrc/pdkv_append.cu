@@ -11,8 +11,8 @@ namespace pdkv {
 
 namespace {
 
-constexpr int kAppendThreads = 128;
-// Steps of a warp in its ring, one of them at work.  Measured on 13262 rows of 48 heads of 128 dims: 3 59.3 us, 4 57.2, 6 57.8.
+constexpr int kAppendThreads = 64;   // (128: 57.4 us instead of 56.8 for 13262 rows of 48 heads, 3.1 instead of 2.8 for 64)
+// Steps of a warp in its ring, one of them at work.  Measured on 13262 rows of 48 heads of 128 dims: 3 59.3 us, 4 57.2, 6 57.8 (with 128 threads a block).
 constexpr int kRing = 4;
 
 __device__ __forceinline__ int own_tokens(const int32_t *seq_len, int seq, int most)
@@ -109,14 +109,14 @@ __device__ __forceinline__ int sequence_of(const int32_t *row_begin, int n_seq, 
 // weights are multiplied into the cosines and sines, so a result is two products and one by 1 / sqrt.
 //
 // Bound by the issue of instructions and memory in about equal parts: 13262 rows of 48 heads of 128 dims, normalised, into blocks of 16 tokens
-// 56 to 57 us (5.8 TB/s; 207 instructions a step, four warps a scheduler busy for 55% of the time).  With the values' way through
+// 57 us (5.7 TB/s; 207 instructions a step, four warps a scheduler busy for 55% of the time).  With the values' way through
 // registers instead of shared memory 68 us (they crowd the tables out), with weights and sines multiplied one after the other 78.
-// 64 rows: 3.0 us in a recorded graph, the latency of the lookups.
+// 64 rows: 2.8 us in a recorded graph, the latency of the lookups.
 //
 // ODD: half of the rotated dims is no multiple of eight.  Pairs (i, i + half) then lie in runs that are not aligned: a lane takes up
 // to eight pairs, or up to sixteen of the dims behind them, in 16-bit pieces.
 template <typename T, int W, bool ODD, bool ADJACENT>
-__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendParams p)
+__global__ void __launch_bounds__(kAppendThreads, 8) append_kernel(const __grid_constant__ AppendParams p)
 {
     constexpr int kHeads = 32 / W;   // of a step
     __shared__ __align__(16) float sines[kAppendThreads / 32][2][8 * W];
@@ -379,7 +379,7 @@ namespace {
 template <typename T, int W, bool ODD, bool ADJACENT> cudaError_t launch_append_as(AppendParams p, int sm_count, cudaStream_t stream)
 {
     // A warp takes all heads of a row, which finds the row's sines once, where that gives each SM 16 warps; else it takes fewer (64 rows of
-    // 48 heads: a step a warp 3.0 us, all 12 steps a warp would be 64 warps for 148 SMs).
+    // 48 heads: a step a warp 2.8 us, all 12 steps a warp would be 64 warps for 148 SMs; 4547 rows of 36 heads: all 9 steps 19.6 us, three 23.7).
     constexpr int heads = 32 / W;
     p.q_steps = (p.Hq + heads - 1) / heads;
     p.k_steps = (p.H + heads - 1) / heads;

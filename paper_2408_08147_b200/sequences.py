@@ -1,4 +1,4 @@
-"""Operators on a filled pool: attention over cached sequences, and eviction.
+"""Operators on a filled pool: new tokens, attention over cached sequences, accepted drafts, and eviction.
 
 :class:`CacheSession` keeps the C handles of one batch of cached sequences together, as
 :class:`~paper_2408_08147_b200.session.TransferSession` does for a transfer.  It marshals
@@ -10,6 +10,12 @@ library's kernels.
         out, lse = s.attend(layer, q, scores_t=scores)            # scores accumulate in place
         kept, _, new_len = s.evict(s, scores_all, budget=1024, sink=4, recent=256,
                                    kept_scores_t=scores_all)      # compacts the pool in place
+
+A step that drafts a tree of tokens (``lens_t`` counts them):
+
+        q = s.append(layer, k, v, q, rotary=Rotary(128), position_t=positions, seq_len_t=lens_t)
+        out, lse = s.attend(layer, q, mask_t=pack_mask(sees), seq_len_t=lens_t)
+        lens_t = s.accept(path, seq_len_t=lens_t)                 # behind the last layer
 """
 from __future__ import annotations
 
