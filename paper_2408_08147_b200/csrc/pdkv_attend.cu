@@ -98,10 +98,12 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     const int width = p.scores_in == p.scores_out ? len : p.max_len;
     if (begin >= width) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    // Rows of query tokens that are not there, the last ones, weigh nothing, and their logits may never have been written.
+    const int rows = p.formed ? min(R, newest_of(p, seq) * p.G) : R;
     // (a token that a row does not see weighs nothing even where the row's sum is NaN)
     auto weight = [](float z, float e) { return z == -INFINITY ? 0.f : pow2(z - e); };
-    for (int r0 = 0; r0 < R; r0 += kScoreRows) {
-        const int n = min(kScoreRows, R - r0);
+    for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
+        const int n = min(kScoreRows, rows - r0);
         __syncthreads();
         for (int r = warp; WIDE && r < n; r += 4) {
             const float2 ml = joined_ml<32>(p, parts_of(p, s, head, r0 + r), lane);

@@ -305,6 +305,35 @@ def test_work_before_the_call_is_waited_for(c):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("c", [
+    dict(lens=[300, 230], G=2, D=64, Q=9, block=16, form=dict(kind="any", cap=20.0)),
+    dict(lens=[900, 770], H=1, G=4, D=128, Q=100, block=32, form=dict(kind="any", cap=20.0)),
+    dict(lens=[900, 770], H=1, G=2, D=128, Q=140, block=32, form=dict(kind="any", cap=20.0, slopes=True)),
+], ids=["warp", "tile", "tile-sloped"])
+def test_bits_do_not_depend_on_what_is_not_seen(c):
+    """Keys behind a sequence's end, of a token that nobody sees, and queries that are not there: whatever they hold."""
+    s, f, _ = setup(c)
+    f.news[:] = [s.Q - 3, s.Q]
+    f.kw["n_new_t"] = torch.tensor(f.news, dtype=torch.int32, device="cuda")
+    nobody = s.Q // 3
+    with s.session() as x:
+        want = None
+        for value in (float("nan"), 0.0, 1000.0, -3.0, float("inf")):
+            s.q_t[0, s.Q - 3:] = value
+            for r, n in enumerate(s.lens):
+                first = n - f.news[r]
+                f.see[r, :, nobody] = False
+                for kv in (0, 1):
+                    cached_row(s, r, first + nobody, kv, 0)[:] = value
+                    for t in range(n, -(-n // s.block) * s.block):
+                        cached_row(s, r, t, kv, 0)[:] = value
+            got = x.attend(s.layer, s.q_t, **f.kw)
+            if want is None:
+                want = got
+            assert torch.equal(got[0][:, :, :s.G], want[0][:, :, :s.G]) and torch.equal(got[1][:, :, :s.G], want[1][:, :, :s.G]), value
+            assert torch.isfinite(got[0]).all()
+
+
 def test_refused_forms():
     s = Setup([50, 20], G=2, D=64, Q=4)
     n, T, Hq = 2, 4, 4
@@ -339,7 +368,10 @@ def test_few_of_many_query_tokens_are_there(c, news):
     before = scores.double().cpu().numpy()
     with s.session() as x:
         got = x.attend(s.layer, s.q_t, **f.kw)
-        x.attend(s.layer, s.q_t, scores_t=scores, **f.kw)
+        # scratch that holds NaN: what no kernel of this call has written is not read
+        x.attend(s.layer, s.q_t, scores_t=scores, scratch_t=torch.full((max(16, x.scratch_bytes(True)),), 255, dtype=torch.uint8, device="cuda"), **f.kw)
+        again = x.attend(s.layer, s.q_t, scratch_t=torch.full((max(16, x.scratch_bytes()),), 255, dtype=torch.uint8, device="cuda"), **f.kw)
+        assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
         x.status()
     want = f.expect()
     check(s, *got, want)
