@@ -492,7 +492,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                             float most = 0.f;
 #pragma unroll
                             for (int k = 0; k < kTileTokens; k += 2) most = max3(most, fabsf(v[k]), fabsf(v[k + 1]));
-                            if (__all_sync(~0u, most <= tanh_most)) {   // (false where one is infinite)
+                            // (Not by tokens that a row does not see, nor by rows that are not there: bits must not depend on them.  To look at
+                            // the seen ones alone costs all tiles more than it gives these: 148 -> 152 us of the steady case.)
+                            if (!masked && __all_sync(~0u, !there || most <= tanh_most)) {
 #pragma unroll
                                 for (int k = 0; k < kTileTokens; k += 2) {
                                     const float2 x = tanh2(make_float2(v[k], v[k + 1]), tanh_c);
