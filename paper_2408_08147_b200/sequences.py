@@ -141,6 +141,7 @@ class CacheSession:
             dtype = pool_t.dtype if pool_t.dtype in _DTYPES else torch.bfloat16
         if dtype not in _DTYPES:
             raise ValueError("attention takes bfloat16 or float16")
+        self._kv_heads = geom.num_kv_heads
         self._other_type = pool_t.dtype in _DTYPES and dtype != pool_t.dtype
         if num_q_heads and self._other_type:
             raise ValueError(f"the pool holds {pool_t.dtype}, not {dtype}")
@@ -323,7 +324,7 @@ class CacheSession:
 
     def _heads(self, name, t, shape):
         """Strides between sequences, rows and heads of a tensor [sequences, rows, heads, head_dim] or [rows, heads, head_dim]."""
-        if t.dtype is not self.dtype or t.shape != shape or t.device != self._device:
+        if t.shape != shape or t.dtype is not self.dtype or t.device != self._device:
             raise ValueError(f"{name}: expected {self.dtype} {shape} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         stride = t.stride()
         if stride[-1] != 1 and shape[-1] > 1:
@@ -355,12 +356,14 @@ class CacheSession:
         n_seq, _, _, D = self._shape
         if self._other_type:
             raise ValueError(f"the pool holds {self.pool_t.dtype}, not {self.dtype}")
-        lead = tuple(k_t.shape)[:-2]
         packed = row_begin_t is not None
-        if len(lead) != (1 if packed else 2) or (not packed and lead[0] != n_seq):
-            raise ValueError(f"k_t: expected {'[rows, ' if packed else f'[{n_seq}, new, '}heads, dims], got {tuple(k_t.shape)}")
-        rows = lead[0] if packed else n_seq * lead[1]
-        shape = (*lead, self.geom.num_kv_heads, D)
+        if packed:
+            rows = k_t.shape[0]
+            lead = (rows,)
+        else:
+            lead = (n_seq, k_t.shape[1] if len(k_t.shape) == 4 else 0)
+            rows = n_seq * lead[1]
+        shape = (*lead, self._kv_heads, D)
         k_stride, v_stride = self._heads("k_t", k_t, shape), self._heads("v_t", v_t, shape)
         if (k_t.requires_grad or v_t.requires_grad or (q_t is not None and q_t.requires_grad)) and torch.is_grad_enabled():
             raise ValueError("entering a cache has no gradient; detach the tensors or call under torch.no_grad()")
@@ -375,9 +378,13 @@ class CacheSession:
             q_stride = self._heads("q_t", q_t, shape)
             if q_out_t is None:
                 q_out_t = torch.empty_like(q_t)
+                q_out_stride = q_out_t.stride()
+                q_out_stride = (0, q_out_stride[0], q_out_stride[1]) if packed else q_out_stride[:3]
                 if stream != home:
                     self._record(stream, q_out_t)
-            q, q_out, q_out_stride = q_t.data_ptr(), q_out_t.data_ptr(), self._heads("q_out_t", q_out_t, shape)
+            else:
+                q_out_stride = self._heads("q_out_t", q_out_t, shape)
+            q, q_out = q_t.data_ptr(), q_out_t.data_ptr()
         elif q_out_t is not None:
             raise ValueError("q_out_t needs q_t")
         row_begin = n_new = seq_len = position = q_norm = k_norm = 0
