@@ -478,7 +478,7 @@ int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, 
 
 /* Attention in another form than plain causal: any mask among the newest tokens, capped scores, a bias by
  * distance; everything else is as for pdkv_attend() (plan, strides, scratch, scores, errors).  With `n` newest tokens of sequence r, query
- * token i < n sees every token before them and, of the newest, those that its mask names (a drafted tree: its ancestors and
+ * token i < n sees every token before them (the prefix always) and, of the newest, those that its mask names (a drafted tree: its ancestors and
  * itself; documents packed into a chunk; a prefix seen both ways).  Query tokens i >= n are not there: zeros, lse
  * = -infinity, no weight in scores.  A logit is
  *     z = scale * q.k,   cap * tanh(z / cap) where cap > 0,   + slopes[head] * (position of the key - of the query)

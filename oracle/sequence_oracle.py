@@ -171,7 +171,7 @@ def attend_formed(pool, layout, block, layer, seqs, lens, q, num_kv_heads, scale
             for i in range(m):
                 t = np.arange(first + own)
                 j = t - (first + own - m)
-                visible = np.array([jj < 0 or (jj <= i if see is None else bool(see[r, i, jj])) for jj in j], bool)
+                visible = np.array([jj < 0 or tt < first or (jj <= i if see is None else bool(see[r, i, jj])) for tt, jj in zip(t, j)], bool)
                 if not visible.any():
                     continue
                 here = first + own - m + (i if offset is None else int(offset[r, i]))

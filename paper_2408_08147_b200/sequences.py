@@ -327,7 +327,7 @@ class CacheSession:
         if t.shape != shape or t.dtype is not self.dtype or t.device != self._device:
             raise ValueError(f"{name}: expected {self.dtype} {shape} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         stride = t.stride()
-        if stride[-1] != 1 and shape[-1] > 1:
+        if stride[-1] != 1 and shape[-1] > 1 and t.numel():
             raise ValueError(f"{name}: the dims of a head have to be adjacent")
         return stride[:3] if len(shape) == 4 else (0, stride[0], stride[1])
 

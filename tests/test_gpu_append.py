@@ -356,3 +356,55 @@ def test_refused_tensors():
         with pytest.raises(ValueError):
             s.accept(torch.zeros(2, 3, dtype=torch.int32, device="cuda"), layers=(1, 1))
     assert (p.bits.cpu().numpy() == p.before).all()
+
+
+def test_offsets_past_32_bits():
+    """A pool of 6 GB whose used blocks lie at its end: both layouts."""
+    for layout in (BLOCK_MAJOR, LAYER_MAJOR):
+        L, H, D, block, blocks = 2, 8, 128, 128, 6000
+        geom = Geometry(layout, L, H, D, 2, block, blocks)
+        pool_t = torch.zeros(geom.shape(), dtype=torch.bfloat16, device="cuda")
+        tbl = np.array([blocks - 1, blocks - 3], np.int32)
+        with CacheSession(geom, pool_t, Sequences([200], np.array([0, 2]), tbl), num_q_heads=8) as s:
+            k, v = (torch.randn(1, 4, H, D, device="cuda").bfloat16() for _ in range(2))
+            s.append(1, k, v)
+            s.accept(torch.tensor([[1, 3]], dtype=torch.int32, device="cuda"), new_tokens=4)
+            torch.cuda.synchronize()
+
+        def row(kv, slot):
+            b, tt = int(tbl[slot // block]), slot % block
+            return pool_t[b, 1, kv, tt] if layout == BLOCK_MAJOR else pool_t[1, kv, b, :, tt]
+
+        for kv, x in ((0, k), (1, v)):
+            for slot, i in ((196, 1), (197, 3), (198, 2), (199, 3)):
+                assert torch.equal(row(kv, slot), x[0, i]), (layout, kv, slot)
+                row(kv, slot).zero_()
+        assert not pool_t.view(torch.int16).any()
+        del pool_t
+
+
+def test_queries_in_place_in_a_fused_buffer():
+    p = Pool([40, 23], G=2, D=64)
+    freq = 10000.0 ** (-np.arange(32) / 32)
+    fused = p.values(2, 3, 8 * 64)
+    before = fused.clone()
+    cut = lambda x: [y.unflatten(-1, (-1, 64)) for y in x.split([256, 128, 128], -1)]  # noqa: E731
+    q, k, v = cut(fused)
+    with p.session() as s:
+        assert s.append(1, k, v, q, q_out_t=q, rotary=Rotary(64)) is q
+        torch.cuda.synchronize()
+    check(p, 1, every_token(p, *cut(before), 3), q.flatten(0, 1), rotary=Rotary(64), frequencies=freq)
+    assert torch.equal(fused[..., 256:], before[..., 256:])
+
+
+def test_nothing_to_append_and_empty_paths():
+    p = Pool([20, 9], G=2, D=64, q_tokens=4)
+    with p.session() as s:
+        assert s.append(0, p.values(2, 0, 2, 64), p.values(2, 0, 2, 64), p.values(2, 0, 4, 64)).shape == (2, 0, 4, 64)
+        none = torch.zeros(2, dtype=torch.int32, device="cuda")
+        s.append(0, p.values(2, 4, 2, 64), p.values(2, 4, 2, 64), n_new_t=none)
+        s.append(0, p.values(0, 2, 64), p.values(0, 2, 64), row_begin_t=torch.zeros(3, dtype=torch.int32, device="cuda"))
+        assert s.accept(torch.zeros(2, 0, dtype=torch.int32, device="cuda")).tolist() == [16, 5]
+        assert s.accept(torch.tensor([[0], [0]], dtype=torch.int32, device="cuda"), n_new_t=none).tolist() == [20, 9]
+        torch.cuda.synchronize()
+    assert (p.bits.cpu().numpy() == p.before).all()

@@ -85,6 +85,8 @@ CASES = [
     dict(lens=[40, 13, 70], G=2, D=64, Q=4, prefix_len=[70, 33], member=[0, 1, 0], form=dict(kind="tree", ragged=True, slopes=True, offset=True)),
     dict(lens=[40, 13, 70], G=4, D=128, Q=16, prefix_len=[300], member=[0, -1, 0], form=dict(kind="any", ragged=True, cap=10.0, slopes=True)),
     dict(lens=[5, 6, 7, 8], G=8, D=128, Q=6, prefix_len=[200], member=[0] * 4, dtype="fp16", form=dict(kind="tree", ragged=True)),
+    dict(lens=[3, 0, 40], G=3, D=40, Q=6, prefix_len=[50], member=[0, 0, 0], form=dict(kind="any", slopes=True, cap=9.0)),            # the same behind a prefix
+    dict(lens=[70, 33], G=2, D=8, Q=3, form=dict(kind="tree", cap=4.0)),
     # the tile kernel: one and two row tiles, masks that cross its tiles of 128 tokens
     dict(lens=[1200], H=1, G=4, D=128, Q=16, block=16, form=dict(kind="tree"), kernel=1),
     dict(lens=[1200, 700], H=1, G=4, D=128, Q=64, block=128, layout=LAYER_MAJOR, form=dict(kind="tree", ragged=True, slopes=True, offset=True), kernel=1),
