@@ -1,5 +1,6 @@
 // Attention of a batch's newest tokens over a paged pool, and the join of its parts.
 #include <numeric>
+#include <type_traits>
 
 #include "pdkv_attend_warp.cuh"
 
@@ -21,7 +22,7 @@ constexpr int kScoreRows = 64;     // rows whose lse is held at a time
 // tokens into weights 2^(z - lse) and add them to the scores; they take the lse from the parts themselves, so no
 // block waits for another.  Bound by the latency of its few dependent loads: 4096 rows of 128 dims in four parts each 10 us
 // alone, about 4 us behind the kernel that left them, since it is set up while that one ends.
-template <typename T, bool WIDE>
+template <typename T, bool WIDE, bool FORM>
 __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, const int row_blocks, const int chunks)
 {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, per = row_blocks + chunks;
@@ -37,7 +38,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     asm volatile("griddepcontrol.launch_dependents;");
     if (x < row_blocks) {
         if (!mine) return;
-        const bool absent = p.formed && row / p.G >= newest_of(p, seq);   // a query token that is not there: nothing, and its parts may hold anything
+        const bool absent = FORM && row / p.G >= newest_of(p, seq);   // a query token that is not there: nothing, and its parts may hold anything
         const int n = absent ? 0 : (parts.n[0] + parts.n[1] - way + ways - 1) / ways;   // of this warp: way, way + ways, ...
         const float2 ml = absent ? make_float2(-INFINITY, 0.f) : joined_ml<32>(p, parts, lane);
         const float base = ml.x == -INFINITY ? 0.f : ml.x;
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttnParams p, co
     if (begin >= width) return;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     // Rows of query tokens that are not there, the last ones, weigh nothing, and their logits may never have been written.
-    const int rows = p.formed ? min(R, newest_of(p, seq) * p.G) : R;
+    const int rows = FORM ? min(R, newest_of(p, seq) * p.G) : R;
     // (a token that a row does not see weighs nothing even where the row's sum is NaN)
     auto weight = [](float z, float e) { return z == -INFINITY ? 0.f : pow2(z - e); };
     for (int r0 = 0; r0 < rows; r0 += kScoreRows) {
@@ -188,9 +189,13 @@ cudaError_t launch_attend_join(const AttnParams &p, int dtype, bool join, int mo
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (dtype == PDKV_DTYPE_BF16)
-        return cudaLaunchKernelEx(&cfg, wide ? attend_join_kernel<__nv_bfloat16, true> : attend_join_kernel<__nv_bfloat16, false>, p, row_blocks, chunks);
-    return cudaLaunchKernelEx(&cfg, wide ? attend_join_kernel<__half, true> : attend_join_kernel<__half, false>, p, row_blocks, chunks);
+    auto launch = [&](auto type, auto formed) {
+        using T = decltype(type);
+        constexpr bool FORM = decltype(formed)::value;
+        return cudaLaunchKernelEx(&cfg, wide ? attend_join_kernel<T, true, FORM> : attend_join_kernel<T, false, FORM>, p, row_blocks, chunks);
+    };
+    if (dtype == PDKV_DTYPE_BF16) return p.formed ? launch(__nv_bfloat16(), std::true_type()) : launch(__nv_bfloat16(), std::false_type());
+    return p.formed ? launch(__half(), std::true_type()) : launch(__half(), std::false_type());
 }
 
 }  // namespace pdkv
