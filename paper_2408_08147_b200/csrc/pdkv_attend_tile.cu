@@ -240,7 +240,7 @@ template <typename T, int DP> __device__ __forceinline__ void fetch_q(const Attn
 
 // FORM: another form than plain causal.  A thread turns the logits of its row into what the form says (capped, biased, hidden by the
 // row's mask) while they are in registers.  What that takes is added to the chain S, P, O, which bounds an iteration: 8 sequences of 8192 tokens,
-// 256 rows of each of 8 heads take 98 us plain, 102 with masks, 141 capped (tanh by two special functions more 167), 127 biased, 159 both.
+// 256 rows of each of 8 heads take 98 us plain, 102 to 104 with masks, 146 capped (tanh by two special functions more 173), 129 biased, 163 both.
 template <typename T, int DP, int FORM>
 __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
