@@ -91,49 +91,6 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Two 32-bit numbers at a time.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)),
-        "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
-    return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
-    return d;
-}
-// tanh(a z) for |a z| <= 0.7, two at a time on the pipe that has time (two special functions a logit more take 2048 cycles a tile of 128 rows,
-// half of the other work): z p(z^2), p the polynomial of degree 4 with the least largest error (a weighted fit of tanh x / x, reweighted
-// until the extremes are level), off by 2^-22.5 at most.  The powers of a are in its terms; returns up to which |z| it holds, nothing
-// where they or z^2 would leave the range of 32 bits.
-__device__ __forceinline__ float tanh_terms(float a, float (&c)[5])
-{
-    const float a2 = a * a;
-    c[0] = 0.9999985f * a;
-    c[1] = -0.33326975f * a * a2;
-    c[2] = 0.13257454f * a * a2 * a2;
-    c[3] = -0.05019526f * a * a2 * (a2 * a2);
-    c[4] = 0.013194186f * a * (a2 * a2) * (a2 * a2);
-    return a > 1e-4f && a < 1e3f ? 0.7f / a : -1.f;
-}
-__device__ __forceinline__ float2 tanh2(float2 z, const float (&c)[5])
-{
-    const float2 u = mul2(z, z);
-    float2 y = fma2(make_float2(c[4], c[4]), u, make_float2(c[3], c[3]));
-    y = fma2(y, u, make_float2(c[2], c[2]));
-    y = fma2(y, u, make_float2(c[1], c[1]));
-    y = fma2(y, u, make_float2(c[0], c[0]));
-    return mul2(z, y);
-}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
@@ -240,7 +197,8 @@ template <typename T, int DP> __device__ __forceinline__ void fetch_q(const Attn
 
 // FORM: another form than plain causal.  A thread turns the logits of its row into what the form says (capped, biased, hidden by the
 // row's mask) while they are in registers.  What that takes is added to the chain S, P, O, which bounds an iteration: 8 sequences of 8192 tokens,
-// 256 rows of each of 8 heads take 98 us plain, 102 to 104 with masks, 146 capped (tanh by two special functions more 173), 129 biased, 163 both.
+// 256 rows of each of 8 heads take 98 us plain, 104 with masks, 158 capped by 30 (few tiles have a far logit; by 2, where all have, 202), 128 biased, 177
+// capped by 30 and biased.
 template <typename T, int DP, int FORM>
 __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
 {
@@ -417,10 +375,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
         const int t = warp / 4, r = threadIdx.x % kSoftmaxThreads;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + kColS + t * kColTile, o_at = tmem + lanes + kColO + t * kColTile;
-        // what a row's numbers are multiplied by on their way into the exponential (biased ones are in base 2 already)
-        const float scale = FORM == kSloped ? 1.f : FORM == kCapped ? p.cap_out : fabsf(p.scale_log2);
-        float tanh_c[5], tanh_most = 0.f;
-        if (FORM >= kCapped) tanh_most = tanh_terms(0.5f * kLn2 * fabsf(p.cap_in), tanh_c);
+        // what a row's numbers are multiplied by on their way into the exponential (capped and biased ones are in base 2 already)
+        const float scale = FORM >= kCapped ? 1.f : fabsf(p.scale_log2);
         const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale: the signs of Q are turned
         uint32_t s_phase = 0, o_phase = 0, n = 0;
         bool q_there = q_early, q_done = false;   // the item's Q is on its way, has been handed over
@@ -488,29 +444,32 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     for (int c = 0; c < 4; ++c) tmem_load(*reinterpret_cast<float(*)[32]>(v + 32 * c), s_at + 32 * c);
                     tmem_load_wait();
                     if constexpr (FORM >= kCapped) {
-                        if (FORM == kCapped || p.cap_out != 0.f) {   // in units of the cap
+                        if (FORM == kCapped || p.cap_out != 0.f) {
                             float most = 0.f;
 #pragma unroll
                             for (int k = 0; k < kTileTokens; k += 2) most = max3(most, fabsf(v[k]), fabsf(v[k + 1]));
-                            // (Not by tokens that a row does not see, nor by rows that are not there: bits must not depend on them.  To look at
-                            // the seen ones alone costs all tiles more than it gives these: 148 -> 152 us of the steady case.)
-                            if (!masked && __all_sync(~0u, !there || most <= tanh_most)) {
+                            // All near: a shorter way to the same bits, so it may be chosen by whatever lies in the tile.  (Two special functions a logit take 2048
+                            // cycles a tile of 128 rows, half of the other work.)
+                            if (p.cap_unit == 1.f && __all_sync(~0u, !there || __fmul_rn(most, p.cap_in) <= kCapNear)) {
 #pragma unroll
                                 for (int k = 0; k < kTileTokens; k += 2) {
-                                    const float2 x = tanh2(make_float2(v[k], v[k + 1]), tanh_c);
+                                    const float2 z = make_float2(v[k], v[k + 1]), x = capped_near(p, z, mul2(z, z));
                                     v[k] = x.x;
                                     v[k + 1] = x.y;
                                 }
                             } else {
-                                const float in = fabsf(p.cap_in);
 #pragma unroll
-                                for (int k = 0; k < kTileTokens; ++k) v[k] = capped(v[k], in, 1.f);
+                                for (int k = 0; k < kTileTokens; k += 2) {
+                                    const float2 x = capped(p, make_float2(v[k], v[k + 1]));
+                                    v[k] = x.x;
+                                    v[k + 1] = x.y;
+                                }
                             }
                         }
                     }
                     if constexpr (FORM == kSloped) {
                         // slope * (t0 + k - query): steps of sixteen tokens, and within them
-                        const float in = p.cap_out != 0.f ? p.cap_out : fabsf(p.scale_log2), far = bias.slope * (float)(t0 - bias.query);
+                        const float in = p.cap_out != 0.f ? 1.f : fabsf(p.scale_log2), far = bias.slope * (float)(t0 - bias.query);
                         const float2 in2 = make_float2(in, in);
                         float2 step[8];
 #pragma unroll
@@ -887,7 +846,7 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
                             const Bias b = bias[col + k];
                             // (tokens before the newest: seen by every query token that is there)
                             const bool seen = token < n_new && (j < 0 || (newest_seen(p, seq, token, n_new, j) & 1)) && lse[col + k] != -INFINITY;
-                            float x = p.cap_out != 0.f ? capped(v[k], fabsf(p.cap_in), p.cap_out) : v[k] * fabsf(p.scale_log2);
+                            float x = p.cap_out != 0.f ? capped(p, v[k]) : v[k] * fabsf(p.scale_log2);
                             if (p.slopes) x = fmaf(b.slope, (float)((j >= 0 && j < n_new ? len - n_new + offset_of(p, seq, j) : t) - b.query), x);
                             if (seen) sums[0].x += pow2(x + lse[col + k]);
                         }

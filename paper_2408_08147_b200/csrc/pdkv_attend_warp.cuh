@@ -354,13 +354,16 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             }
         if constexpr (FORM >= kCapped) {
             if (FORM == kCapped || p.cap_out != 0.f) {
-                const float in = fabsf(p.cap_in);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) z[h][t][j] = capped(z[h][t][j], in, p.cap_out);
+                        for (int j = 0; j < 4; j += 2) {
+                            const float2 x = capped(p, make_float2(z[h][t][j], z[h][t][j + 1]));
+                            z[h][t][j] = x.x;
+                            z[h][t][j + 1] = x.y;
+                        }
             }
         }
         if constexpr (FORM == kSloped) {

@@ -566,7 +566,7 @@ int attend_call(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, const 
     if (f) {
         if (!(f->cap >= 0.f) || !std::isfinite(f->cap)) return PDKV_ERR_INVALID_ARG;
         cap_out = f->cap * 1.4426950408889634;
-        if (f->cap > 0.f) cap_in = 2 * 1.4426950408889634 * a->scale / f->cap;
+        if (f->cap > 0.f) cap_in = 2 * 1.4426950408889634 * std::fabs(a->scale) / f->cap;
         if (!std::isfinite((float)cap_in) || !std::isfinite((float)(2 * cap_out)) || (f->cap > 0.f && (float)cap_out == 0.f)) return PDKV_ERR_INVALID_ARG;
         if (!aligned(f->slopes, 4) || !aligned(f->mask, 4) || !aligned(f->n_new, 4) || !aligned(f->offset, 4)) return PDKV_ERR_INVALID_ARG;
         if (f->mask && (f->mask_stride[0] < 0 || f->mask_stride[1] < 0)) return PDKV_ERR_INVALID_ARG;
@@ -663,9 +663,13 @@ int attend_call(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, const 
         p.seq_len = a->seq_len;
         if (f) {
             p.formed = f->slopes ? 3 : f->cap > 0.f ? 2 : 1;
-            // (a scale of zero as above: the logits' infinities stay what they are)
-            p.cap_in = cap_in == 0 && f->cap > 0.f ? std::copysign(std::numeric_limits<float>::denorm_min(), a->scale) : (float)cap_in;
+            // (a factor of zero as above: the logits' infinities stay what they are)
+            p.cap_in = (float)cap_in == 0.f && f->cap > 0.f ? std::numeric_limits<float>::denorm_min() : (float)cap_in;
             p.cap_out = (float)cap_out;
+            // the powers of cap_in are in the terms, a product a logit less, where neither they nor z^2 leave the range of 32 bits
+            p.cap_unit = cap_in > 1.0 / (1 << 14) && cap_in < 1 << 14 ? 1.f : p.cap_in;
+            double unit = std::fabs(p.scale_log2);
+            for (int i = 0; i < 5; ++i, unit *= p.cap_unit == 1.f ? (double)p.cap_in * p.cap_in : 1.0) p.cap_terms[i] = (float)(pdkv::kCapTerms[i] * unit);
             p.slopes = f->slopes;
             p.mask = f->mask;
             p.n_new = f->n_new;

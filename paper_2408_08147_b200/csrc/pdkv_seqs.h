@@ -58,6 +58,11 @@ struct AttnSeq {
     int32_t direct;          // 1: nothing to join
 };
 
+// tanh(x) / x for |x| <= 0.65 as a polynomial in (2 x log2 e)^2, that of degree 4 with the least largest relative error (a weighted fit, reweighted
+// until the extremes are level): off by 2^-22.6 at most.
+constexpr double kCapTerms[5] = {0.99999985, -0.04003555, 1.918510e-3, -8.927525e-5, 3.044123e-6};
+constexpr float kCapNear = 1.8755036f;   // 2 * 0.65 log2 e
+
 struct AttnParams {
     PoolView pool;
     const int32_t *tbl;
@@ -94,7 +99,9 @@ struct AttnParams {
     int32_t block_shift;        // log2 of block_tokens, -1: not a power of two
     // another form than plain causal (pdkv_attend_form): a variant of each kernel
     int32_t formed;             // 1: masks alone, 2: caps too, 3: biases too (and caps, where there are)
-    float cap_in, cap_out;      // logits (base 2): cap_out tanh(z cap_in / (2 log2 e)); cap_out 0: z scale_log2
+    // logits (base 2) of products z of the scale's sign: cap_out tanh(z cap_in / (2 log2 e)), which up to |z cap_in| = kCapNear is
+    // z (cap_terms[0] + cap_terms[1] (z cap_unit)^2 + ...); cap_out 0: z scale_log2
+    float cap_in, cap_out, cap_unit, cap_terms[5];
     const float *slopes;
     const uint32_t *mask;
     int64_t mask_stride[2];
