@@ -482,7 +482,7 @@ int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, 
  * itself; documents packed into a chunk; a prefix seen both ways).  Query tokens i >= n are not there: zeros, lse
  * = -infinity, no weight in scores.  A logit is
  *     z = scale * q.k,   cap * tanh(z / cap) where cap > 0,   + slopes[head] * (position of the key - of the query)
- * and the tanh adds an error of 2^-20 of the capped logit at most, whatever the cap.
+ * and the tanh adds an error of 2^-20 of the capped logit at most, whatever the cap.  What the queries of other sequences hold changes no bit of a result.
  * Positions count from the first token of the prefix, below 2^31; the newest tokens' are len_r - n + offset. */
 typedef struct {
     float cap;                     /* 0: none */

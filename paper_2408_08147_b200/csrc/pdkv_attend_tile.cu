@@ -519,8 +519,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) attend_tile_kernel(const __gr
                     for (int k = 8; k < kTileTokens / 2; ++k) tops[k % 8] = max3(tops[k % 8], v[2 * k], v[2 * k + 1]);
                     float top = max3(max3(max3(tops[0], tops[1], tops[2]), tops[3], tops[4]), tops[5], fmaxf(tops[6], tops[7]));
                     top = top == -INFINITY ? top : fmaf(top, scale, -kLift<T>);
-                    if (__any_sync(~0u, top > m + kGrowth || (m == -INFINITY && top > m))) {
-                        const float new_m = fmaxf(m, top), f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
+                    const bool grew = top > m + kGrowth || (m == -INFINITY && top > m);
+                    if (__any_sync(~0u, grew)) {
+                        // (FORM: the row's own maximum alone decides on its base, so that its neighbours change no bit of it)
+                        const float new_m = !FORM || grew ? fmaxf(m, top) : m, f = new_m == -INFINITY ? 1.f : pow2(m - new_m);
                         l *= f;
                         m = new_m;
                         if (j > 0) {

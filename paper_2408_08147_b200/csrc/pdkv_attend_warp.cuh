@@ -447,7 +447,9 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float new_m = fmaxf(m[t][j], top[t][j]), f = new_m == -INFINITY ? 1.f : pow2(m[t][j] - new_m);
+                    // (FORM: the row's own maximum alone decides on its base, so that its neighbours change no bit of it)
+                    const bool mine = top[t][j] > m[t][j] + kGrowth || (m[t][j] == -INFINITY && top[t][j] > m[t][j]);
+                    const float new_m = !FORM || mine ? fmaxf(m[t][j], top[t][j]) : m[t][j], f = new_m == -INFINITY ? 1.f : pow2(m[t][j] - new_m);
                     m[t][j] = new_m;
                     l[t][j] *= f;
 #pragma unroll

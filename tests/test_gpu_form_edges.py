@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import sequence_oracle as O
+from paper_2408_08147_b200.workloads import LAYER_MAJOR
 from test_gpu_forms import KERNELS, Form
 from test_gpu_sequence_edges import cached_row
 from test_gpu_sequences import Setup, check, check_scores
@@ -64,3 +65,22 @@ def test_large_caps_beside_infinite_values(c, scale):
     y, want_lse, w, e = expect(s, f, scale)
     e["mag"] = (e["mag"] + np.abs(y))[..., 1:]                # (a direct result is rounded once more)
     check(s, out[..., 1:], lse, (y[..., 1:], want_lse, w, e))
+
+
+@pytest.mark.parametrize("form", [dict(kind="tree"), dict(kind="tree", cap=2.0), dict(kind="tree", cap=30.0), dict(kind="tree", slopes=True), dict(kind="any", cap=30.0, slopes=True)],
+                         ids=["masked", "small cap", "capped", "biased", "both"])
+@pytest.mark.parametrize("c", [dict(lens=[40, 13, 70], G=2, Q=2), dict(lens=[40, 13, 70], G=2, Q=8, D=256), dict(lens=[150, 90, 33], G=4, D=128, Q=5, layout=LAYER_MAJOR)],
+                         ids=["warp", "warp, many rows", "tile"])
+def test_bits_do_not_depend_on_other_sequences(c, form):
+    """Rows of several sequences behind one prefix share the work of a warp, not what is computed: what one sequence asks changes no bit of another's."""
+    s = Setup(**c, prefix_len=[900], member=[0, 0, 0])
+    f = Form(s, **form)
+    asked = s.q_t[0].clone()
+    with s.session() as x:
+        assert (x.items()["seq"] < 0).any()
+        got = []
+        for factor in (1.0, 0.0, 0.03, 30.0, -1000.0):
+            s.q_t[0] = asked * factor
+            got.append(x.attend(s.layer, s.q_t, **f.kw))
+        for out, lse in got[1:]:
+            assert torch.equal(out[1:], got[0][0][1:]) and torch.equal(lse[1:], got[0][1][1:])
