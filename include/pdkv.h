@@ -428,7 +428,8 @@ int pdkv_seqs_create(const pdkv_pool *pool, const pdkv_seqs_desc *desc, void *wo
                      size_t *needed_bytes, void *stream, pdkv_seqs **out);
 /* Synchronise `stream` and report the handle's device status word: PDKV_OK,
  * PDKV_ERR_DEVICE_BOUNDS (a bounded wait inside an attention kernel gave up, and the results of a
- * call since the last report are not valid; the word is cleared) or PDKV_ERR_CUDA. */
+ * call since the last report are not valid), PDKV_ERR_TABLE (a length that an append or accept read from the device was above the
+ * handle's; see there) or PDKV_ERR_CUDA.  What is reported is cleared. */
 int pdkv_seqs_status(const pdkv_seqs *seqs, void *stream);
 /* Call it once the work enqueued with the handle has completed. */
 int pdkv_seqs_destroy(pdkv_seqs *seqs);
@@ -521,7 +522,10 @@ typedef struct {
     const int32_t *row_begin;      /* device [n_seq + 1]: sequence r has rows [row_begin[r], row_begin[r + 1]), ascending.
                                       NULL: rows / n_seq of each, one sequence after the other */
     const int32_t *n_new;          /* device [n_seq], with row_begin NULL: only the first n_new[r] rows of a sequence are tokens; NULL: all */
-    const int32_t *seq_len;        /* device [n_seq] own lengths with the new tokens, or NULL: those of the handle; clamped as for attention */
+    const int32_t *seq_len;        /* device [n_seq] own lengths with the new tokens, or NULL: those of the handle; clamped as for attention.
+                                      One above the handle's length leaves no place for tokens behind it: it counts as that length, the
+                                      new tokens take the places (and positions) of the last ones that it covers, which are lost, and
+                                      pdkv_seqs_status() reports TABLE.  Make the handle with room for all tokens to come. */
     const void *q;                 /* device [row][num_q_heads][head_dim], or NULL: keys and values alone */
     const void *k, *v;             /* device [row][num_kv_heads][head_dim] */
     void *q_out;                   /* as q; may equal it (same strides) */
@@ -547,7 +551,7 @@ typedef struct {
     int32_t path_len;
     int32_t new_tokens;            /* newest tokens of a sequence */
     const int32_t *n_new;          /* device [n_seq], clamped to [0, new_tokens]; NULL: new_tokens */
-    const int32_t *seq_len;        /* device [n_seq], or NULL (as for pdkv_attend) */
+    const int32_t *seq_len;        /* device [n_seq], or NULL (as for pdkv_attend; one above the handle's length is reported as for pdkv_append) */
     int32_t *new_len;              /* device [n_seq], or NULL.  May equal seq_len */
 } pdkv_accept_args;
 /* Enqueues only (recordable as pdkv_attend()); no scratch.  Overlaps are refused as for pdkv_evict().

@@ -122,6 +122,7 @@ int pdkv_append(const pdkv_seqs *s, int layer, const pdkv_append_args *a, void *
         p.position = a->position;
         p.position_stride = a->position_stride;
         p.block_shift = log2_of(g.block_tokens);
+        p.status = s->d_status;
         pdkv::DeviceGuard guard(s->device);
         if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
         const cudaError_t e = pdkv::launch_append(p, s->dtype, s->sm_count, static_cast<cudaStream_t>(stream));
@@ -173,6 +174,7 @@ int pdkv_accept(const pdkv_seqs *s, int layer_begin, int layer_end, const pdkv_a
         p.new_len = a->new_len;
         p.vec_bytes = vec;
         p.block_shift = log2_of(g.block_tokens);
+        p.status = s->d_status;
         pdkv::DeviceGuard guard(s->device);
         if (guard.err != cudaSuccess) return pdkv::report_cuda_error(guard.err, "cudaSetDevice");
         const cudaError_t e = pdkv::launch_accept(p, static_cast<cudaStream_t>(stream));

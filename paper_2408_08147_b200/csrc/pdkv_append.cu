@@ -22,6 +22,12 @@ __device__ __forceinline__ int own_tokens(const int32_t *seq_len, int seq, int m
     return n < 0 ? 0 : (n < most ? n : most);
 }
 
+// A length above the handle's is taken as the handle's, and the tokens of the call take the places of cached ones: reported.
+__device__ __forceinline__ void report_length(const int32_t *seq_len, int seq, int most, unsigned long long *status)
+{
+    if (seq_len && seq_len[seq] > most) atomicCAS(status, 0ull, kStatusLength);
+}
+
 // Bytes from the pool's base to (layer 0, K, head 0) of token `slot` of a list.
 __device__ __forceinline__ int64_t slot_offset(const PoolView &pool, const int32_t *tbl, int64_t list, int slot, int block_shift)
 {
@@ -220,6 +226,7 @@ __global__ void __launch_bounds__(kAppendThreads, 8) append_kernel(const __grid_
     }
     const AttnSeg seg = p.segs[seq];
     const int64_t slot = (int64_t)own_tokens(p.seq_len, seq, seg.len) - count + at;
+    if (at == 0 && part == 0 && lane == 0) report_length(p.seq_len, seq, seg.len, p.status);
     const bool cached = slot >= 0 && slot < seg.len;   // (a sequence shorter than its new tokens has no place for the first of them)
     char *place = nullptr;
     if (cached && last > p.q_steps)
@@ -503,7 +510,10 @@ template <typename V> __global__ void __launch_bounds__(kAcceptThreads) accept_k
         if (!more) break;
         __syncthreads();
     }
-    if (p.new_len && blockIdx.y == 0 && threadIdx.x == 0) p.new_len[seq] = max(0, first + accepted);
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        report_length(p.seq_len, seq, seg.len, p.status);
+        if (p.new_len) p.new_len[seq] = max(0, first + accepted);
+    }
 }
 
 // The new lengths alone, a warp a sequence: where they replace the lengths that the moves go by.

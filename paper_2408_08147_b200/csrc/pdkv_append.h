@@ -25,6 +25,7 @@ struct AppendParams {
     const uint8_t *axis;
     float rotary_scale;
     int32_t block_shift;          // log2 of block_tokens, -1: not a power of two
+    unsigned long long *status;
     // set by the launcher: a row is `parts` pieces of work of `steps` steps each; steps of its queries, of its keys
     int32_t parts, steps, q_steps, k_steps;
     float inv_D;
@@ -44,6 +45,7 @@ struct AcceptParams {
     int32_t *new_len;
     int32_t vec_bytes;            // alignment every row of the pool has, 16 at most
     int32_t block_shift;
+    unsigned long long *status;
 };
 cudaError_t launch_accept(const AcceptParams &p, cudaStream_t stream);
 

@@ -507,7 +507,8 @@ int pdkv_seqs_status(const pdkv_seqs *s, void *stream)
     // reported once: it says nothing about the calls that follow
     e = cudaMemsetAsync(s->d_status, 0, sizeof v, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    return e == cudaSuccess ? PDKV_ERR_DEVICE_BOUNDS : pdkv::report_cuda_error(e, "cudaMemsetAsync");
+    if (e != cudaSuccess) return pdkv::report_cuda_error(e, "cudaMemsetAsync");
+    return v == pdkv::kStatusLength ? PDKV_ERR_TABLE : PDKV_ERR_DEVICE_BOUNDS;
 }
 
 int pdkv_seqs_items(const pdkv_seqs *s, const pdkv_attend_item **items, int64_t *n_items)

@@ -58,6 +58,9 @@ struct AttnSeq {
     int32_t direct;          // 1: nothing to join
 };
 
+// The status word of a handle on which an append or accept was given a length above the handle's.
+constexpr unsigned long long kStatusLength = 2;
+
 // tanh(x) / x for |x| <= 0.65 as a polynomial in (2 x log2 e)^2, that of degree 4 with the least largest relative error (a weighted fit, reweighted
 // until the extremes are level): off by 2^-22.6 at most.
 constexpr double kCapTerms[5] = {0.99999985, -0.04003555, 1.918510e-3, -8.927525e-5, 3.044123e-6};
@@ -77,7 +80,7 @@ struct AttnParams {
     int32_t use_map;                 // the warp kernel loads through the tensor map
     int32_t map_box, tile_box;       // tokens of a box of the two maps
     int32_t map_layer_major;         // order of the coordinates of the pool's tensor map
-    unsigned long long *status;      // [0] != 0: a bounded wait gave up
+    unsigned long long *status;      // [0] != 0: a bounded wait gave up, or kStatusLength
     int32_t n_seq, H, G, D, q_tokens;
     const void *q;
     void *out;

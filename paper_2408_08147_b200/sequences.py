@@ -349,7 +349,8 @@ class CacheSession:
         """New tokens enter the cache of one layer.  ``k_t`` and ``v_t`` are ``[n_seq, new, num_kv_heads, head_dim]`` (of which the first
         ``n_new_t[r]`` count), or ``[rows, num_kv_heads, head_dim]`` with the sequences' rows one after the other at ``row_begin_t``
         (int32 ``[n_seq + 1]``); any strides with adjacent dims.  The lengths (the session's, or ``seq_len_t``) count the new tokens, which become
-        the last ones.  ``q_t`` (as ``k_t``, with the query heads) is returned normalised and rotated, in ``q_out_t`` (which may be ``q_t``).
+        the last ones; behind the session's lengths there is no place: where ``seq_len_t`` is above them, the new tokens replace the last cached
+        ones, and :meth:`status` raises.  ``q_t`` (as ``k_t``, with the query heads) is returned normalised and rotated, in ``q_out_t`` (which may be ``q_t``).
         Keys and queries are divided by their root mean square and multiplied by ``k_norm_t`` / ``q_norm_t`` (float32 ``[head_dim]``) where
         given, then turned by ``rotary`` at ``position_t`` (int32, one for each row, ``[axes, rows]`` for several axes; default: where the token
         stands behind its prefix).  There is no backward pass."""
@@ -489,7 +490,8 @@ class CacheSession:
         return B.pdkv_seqs_items(self.handle)
 
     def status(self, stream: Optional[int] = None) -> None:
-        """Wait for the session's stream and raise if a kernel reported an error since the last call of this."""
+        """Wait for the session's stream and raise if a kernel reported an error since the last call of this: a wait that gave up, or lengths above
+        the session's in an append or accept."""
         B.pdkv_seqs_status(self.handle, self._on(stream))
 
     def close(self) -> None:
