@@ -484,7 +484,7 @@ int pdkv_attend(const pdkv_seqs *seqs, int layer, const pdkv_attend_args *args, 
  * = -infinity, no weight in scores.  A logit is
  *     z = scale * q.k,   cap * tanh(z / cap) where cap > 0,   + slopes[head] * (position of the key - of the query)
  * and the tanh adds an error of 2^-20 of the capped logit at most, whatever the cap.  What the queries of other sequences hold changes no bit of a result.
- * Positions count from the first token of the prefix, below 2^31; the newest tokens' are len_r - n + offset. */
+ * Positions are places in the cache, from the first token of the prefix, below 2^31; the newest tokens' are len_r - n + offset. */
 typedef struct {
     float cap;                     /* 0: none */
     const float *slopes;           /* device [num_q_heads], finite; NULL: none */
@@ -533,7 +533,8 @@ typedef struct {
                                       one, heads; multiples of 8, dims adjacent, bases 16-byte aligned */
     const float *q_norm, *k_norm;  /* device [head_dim], 16-byte aligned, or NULL: not normalised */
     float norm_eps;
-    const int32_t *position;       /* device [n_axes][row], rows in their order; NULL (one axis): that of the token, from the prefix' first */
+    const int32_t *position;       /* device [n_axes][row], rows in their order; NULL (one axis): the token's place in the cache, from the prefix' first
+                                      (behind an eviction no longer its place in the text) */
     int64_t position_stride;       /* entries between axes */
     pdkv_rotary rotary;
 } pdkv_append_args;
@@ -544,7 +545,9 @@ int pdkv_append(const pdkv_seqs *seqs, int layer, const pdkv_append_args *args, 
 /* Accept: of a sequence's n newest tokens (a drafted tree) those on the path stay.  Path entries 0 <= p_0 < p_1 < ... < n; the path ends at its
  * length or before the first entry that breaks that (-1, say).  Own token len - n + p_j becomes own token len - n + j, bit for bit,
  * in layers [layer_begin, layer_end); the length becomes len - n + accepted.  Everything else in the pool stays as it is.  Pools of any
- * elem_bytes; the blocks of the newest tokens have to belong to one sequence. */
+ * elem_bytes; the blocks of the newest tokens have to belong to one sequence.
+ * Accumulated weights are the caller's and stay where they are: before an eviction goes by them, entry len - n + p_j of each row moves
+ * to len - n + j and those behind the new length become zero.  (What rejected query tokens gave to older ones stays in them.) */
 typedef struct {
     const int32_t *path;           /* device [n_seq][path_len] */
     int64_t path_stride;           /* entries between sequences */

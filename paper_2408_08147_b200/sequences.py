@@ -353,7 +353,8 @@ class CacheSession:
         ones, and :meth:`status` raises.  ``q_t`` (as ``k_t``, with the query heads) is returned normalised and rotated, in ``q_out_t`` (which may be ``q_t``).
         Keys and queries are divided by their root mean square and multiplied by ``k_norm_t`` / ``q_norm_t`` (float32 ``[head_dim]``) where
         given, then turned by ``rotary`` at ``position_t`` (int32, one for each row, ``[axes, rows]`` for several axes; default: where the token
-        stands behind its prefix).  There is no backward pass."""
+        stands in the cache behind its prefix, which an eviction changes).  There is no backward pass.  (:meth:`attend` takes ``[n_seq, q_tokens, ...]``: rows
+        that came one after the other are spread out by the caller.)"""
         n_seq, _, _, D = self._shape
         if self._other_type:
             raise ValueError(f"the pool holds {self.pool_t.dtype}, not {self.dtype}")
@@ -421,7 +422,9 @@ class CacheSession:
                layers: Optional[Tuple[int, int]] = None, stream: Optional[int] = None):
         """Of the newest tokens of each sequence (``new_tokens``, default: the session's ``q_tokens``; ``n_new_t[r]`` of them are there) those named by
         ``path_t`` (int32 ``[n_seq, path]``, ascending, -1 behind the last) stay: their keys and values move to the place behind the tokens
-        before the newest, in all layers.  Returns the new lengths (``new_len_t`` may be ``seq_len_t``)."""
+        before the newest, in all layers.  Returns the new lengths (``new_len_t`` may be ``seq_len_t``).  Accumulated weights do not move: of the
+        ``scores_t`` of :meth:`attend`, entry ``len - new + path[j]`` of each row has to go to ``len - new + j``, and zeros behind, before an eviction
+        goes by them."""
         l0, l1 = (0, self.geom.num_layers) if layers is None else layers
         if not 0 <= l0 < l1 <= self.geom.num_layers:
             raise ValueError(f"layers: expected a range within [0, {self.geom.num_layers}), got {layers}")
