@@ -667,10 +667,13 @@ int attend_call(const pdkv_seqs *s, int layer, const pdkv_attend_args *a, const 
             // (a factor of zero as above: the logits' infinities stay what they are)
             p.cap_in = (float)cap_in == 0.f && f->cap > 0.f ? std::numeric_limits<float>::denorm_min() : (float)cap_in;
             p.cap_out = (float)cap_out;
-            // the powers of cap_in are in the terms, a product a logit less, where neither they nor z^2 leave the range of 32 bits
-            p.cap_unit = cap_in > 1.0 / (1 << 14) && cap_in < 1 << 14 ? 1.f : p.cap_in;
+            // The powers of cap_in are in the terms, a product a logit less, where neither they nor z^2 leave the range of 32 bits (the last
+            // term, of which a few bits are enough, is the first to do so).
+            const double square = (double)p.cap_in * p.cap_in, last = pdkv::kCapTerms[4] * std::fabs(p.scale_log2) * square * square * square * square;
+            const bool folded = cap_in > 1.0 / (1 << 14) && cap_in < 1 << 14 && last > 1e-40 && last < 1e36;
+            p.cap_unit = folded ? 1.f : p.cap_in;
             double unit = std::fabs(p.scale_log2);
-            for (int i = 0; i < 5; ++i, unit *= p.cap_unit == 1.f ? (double)p.cap_in * p.cap_in : 1.0) p.cap_terms[i] = (float)(pdkv::kCapTerms[i] * unit);
+            for (int i = 0; i < 5; ++i, unit *= folded ? square : 1.0) p.cap_terms[i] = (float)(pdkv::kCapTerms[i] * unit);
             p.slopes = f->slopes;
             p.mask = f->mask;
             p.n_new = f->n_new;

@@ -84,3 +84,16 @@ def test_bits_do_not_depend_on_other_sequences(c, form):
             got.append(x.attend(s.layer, s.q_t, **f.kw))
         for out, lse in got[1:]:
             assert torch.equal(out[1:], got[0][0][1:]) and torch.equal(lse[1:], got[0][1][1:])
+
+
+@pytest.mark.parametrize("c", KERNELS, ids=["warp", "tile"])
+@pytest.mark.parametrize("scale, cap, q_scale", [(1e30, 3e26, 1e-30), (1e30, 5.0, 1e-30), (-1e25, 1e26, 1e-25), (1e-30, 2.3e-26, 1e4), (1e-20, 30.0, 1e21)])
+def test_scales_and_caps_far_from_one(c, scale, cap, q_scale):
+    """The terms of a capped logit stay in range, for products of zero too."""
+    s = Setup(**c, q_scale=q_scale)
+    s.q_t[0, 0] = 0
+    f = Form(s, kind="tree", cap=cap)
+    with s.session() as x:
+        got = x.attend(s.layer, s.q_t, scale=scale, **f.kw)
+        x.status()
+    check(s, *got, expect(s, f, scale))
