@@ -272,7 +272,20 @@ __device__ __forceinline__ float2 capped(const AttnParams &p, float2 z)
     const float2 far = fma2(make_float2(-2.f * p.cap_out, -2.f * p.cap_out), r, make_float2(p.cap_out, p.cap_out));
     return make_float2(fabsf(e.x) <= kCapNear ? near.x : far.x, fabsf(e.y) <= kCapNear ? near.y : far.y);
 }
-__device__ __forceinline__ float capped(const AttnParams &p, float z) { return capped(p, make_float2(z, z)).x; }
+// (One at a time: the same operations.)
+__device__ __forceinline__ float capped(const AttnParams &p, float z)
+{
+    const float w = __fmul_rn(z, p.cap_unit), u = __fmul_rn(w, w), e = __fmul_rn(z, p.cap_in);
+    if (fabsf(e) <= kCapNear) {
+        float y = __fmaf_rn(p.cap_terms[4], u, p.cap_terms[3]);
+        y = __fmaf_rn(y, u, p.cap_terms[2]);
+        y = __fmaf_rn(y, u, p.cap_terms[1]);
+        return __fmul_rn(z, __fmaf_rn(y, u, p.cap_terms[0]));
+    }
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(__fadd_rn(pow2(e), 1.f)));
+    return __fmaf_rn(-2.f * p.cap_out, r, p.cap_out);
+}
 
 // As left_out(): what the pieces of V with infinities or NaN among own tokens [from, to) add to dims [d, d + 4) of a row.
 template <typename T>

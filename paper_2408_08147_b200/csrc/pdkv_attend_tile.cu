@@ -848,7 +848,8 @@ __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant
                             const Bias b = bias[col + k];
                             // (tokens before the newest: seen by every query token that is there)
                             const bool seen = token < n_new && (j < 0 || (newest_seen(p, seq, token, n_new, j) & 1)) && lse[col + k] != -INFINITY;
-                            float x = p.cap_out != 0.f ? capped(p, v[k]) : v[k] * fabsf(p.scale_log2);
+                            float x = v[k] * fabsf(p.scale_log2);
+                            if (seen && p.cap_out != 0.f) x = capped(p, v[k]);
                             if (p.slopes) x = fmaf(b.slope, (float)((j >= 0 && j < n_new ? len - n_new + offset_of(p, seq, j) : t) - b.query), x);
                             if (seen) sums[0].x += pow2(x + lse[col + k]);
                         }
