@@ -115,12 +115,17 @@ __device__ __forceinline__ int sequence_of(const int32_t *row_begin, int n_seq, 
 // weights are multiplied into the cosines and sines, so a result is two products and one by 1 / sqrt.
 //
 // Bound by the issue of instructions and memory in about equal parts: 13262 rows of 48 heads of 128 dims, normalised, into blocks of 16 tokens
-// 57 us (5.7 TB/s; 207 instructions a step, four warps a scheduler busy for 55% of the time).  With the values' way through
+// 55.5 us (5.9 TB/s; 207 instructions a step, four warps a scheduler busy for 55% of the time).  With the values' way through
 // registers instead of shared memory 68 us (they crowd the tables out), with weights and sines multiplied one after the other 78.
 // 64 rows: 2.8 us in a recorded graph, the latency of the lookups.
 //
+// Where all dims turn in split pairs, the lanes of a head load 16 bytes side by side.  Where pairs are adjacent, or dims do not turn, a lane's two
+// runs are neighbours and the lanes load every other 16 bytes: the same prompts 86 us with adjacent pairs, 69 with 64 of 128 dims turning, 81 with none.
+// Between its widths lanes idle: 96 dims 56 us, 80 dims 55 (for 0.75 and 0.63 of the bytes).
+//
 // ODD: half of the rotated dims is no multiple of eight.  Pairs (i, i + half) then lie in runs that are not aligned: a lane takes up
-// to eight pairs, or up to sixteen of the dims behind them, in 16-bit pieces.
+// to eight pairs, or up to sixteen of the dims behind them, in 16-bit pieces; a warp has one head a step, and nothing is loaded ahead.
+// Slow: the same prompts with 24 of 96 dims turning 300 us, with 20 of 80 298.
 template <typename T, int W, bool ODD, bool ADJACENT>
 __global__ void __launch_bounds__(kAppendThreads, 8) append_kernel(const __grid_constant__ AppendParams p)
 {

@@ -695,6 +695,10 @@ template <int DP> constexpr uint32_t weigh_bytes(int rows)
 // tokens, 64 rows each, 8 heads of 128 dims take 27 us as a kernel alone (cold), of which the bytes of K need 9 and the exponentials 3 (16
 // a cycle and SM); the tensor pipe is active for 8%, DRAM for 25%.  So latency bounds it: a CTA starts (Q, sums of the rows) for a
 // handful of tiles, and ragged lists leave a few CTAs for a second wave.
+//
+// FORM: logits one by one; a token's bit in the mask, and its place, are looked up for each row, and the row of logits lies in local memory
+// (indexed at run time).  Slow: attention with weights of 16 sequences of 2048 tokens, 256 rows of 8 heads, takes 884 us with a tree's mask and
+// 121 plain causal, of which 52 and 51 are the attention.
 template <typename T, int DP, bool FORM>
 __global__ void __launch_bounds__(192) attend_weigh_kernel(const __grid_constant__ CUtensorMap map, const AttnParams p, const int chunks, const int chunk_tiles)
 {

@@ -225,7 +225,8 @@ __device__ __noinline__ void add_left_out(const AttnParams &p, const AttnItem it
 //
 // FORM: another form than plain causal.  The logits, once they are there, become what the form says (capped, biased, hidden by the
 // rows' masks); from then on nothing else differs, but that a row may see nothing of what it is multiplied with.  A variant each for masks,
-// caps and biases: with all in one, registers spilled in the loop (32 sequences of 2048 tokens, 4 rows, capped 49.6 us, 46 so; 32 rows 92, 73).
+// caps and biases: with all in one (tanh from the exponential alone) 32 sequences of 2048 tokens, 4 rows, capped took 49.6 us instead of 46, 32 rows 92
+// instead of 76.  Now, plain, with masks, capped, biased: 43.7, 46.8, 46.9, 47.0 and, 32 rows, 63, 72, 83, 82.  Every form spills registers (below).
 template <typename T, int DP, int KD, bool HIDES, int FORM, int NT, int WM>
 __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem &it, int n_slices, int len, int limit, char *smem,
                                             float (*sml)[16][2], volatile uint32_t *wild, RingBarriers &bar, uint32_t n, bool &dead)
@@ -578,7 +579,8 @@ __device__ __forceinline__ void attend_item(const AttnParams &p, const AttnItem 
 // the rest of them along the tokens.
 // Bound by memory up to 16 rows: 32 sequences of 2048 tokens, 8 heads of 128 dims, 4 rows each 43.6 us (6.2 TB/s of K and V),
 // 2 sequences of about 110000 tokens, 8 rows each, 6.4 TB/s.  Above, by the products of the four warps, or eight, of an SM
-// (64 rows of 256 dims over 40000 tokens 169 us, 8 rows 60; ptxas spills 130 to 190 bytes in the variants for 96, 128 and 256 dims).  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
+// (64 rows of 256 dims over 40000 tokens 169 us, 8 rows 60).  Bytes of registers that ptxas spills (bf16; stored), plain, with masks, capped, biased: 64
+// dims 0, 112, 120, 220; 96 dims 64, 204, 176, 228; 128 dims 160, 320, 388, 556; 192 dims 24, 68, 76, 52; 256 dims 188, 396, 576, 672.  The matrix instructions of this kind are enough here: 8 rows at full memory rate keep
 // them busy for 13% of the time.
 template <typename T, int DP, int KD, bool HIDES, int FORM>
 __global__ void __launch_bounds__(kThreads, Ring<DP>::kCtas) attend_items_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnParams p)
