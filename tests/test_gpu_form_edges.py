@@ -79,7 +79,7 @@ def test_bits_do_not_depend_on_other_sequences(c, form):
     with s.session() as x:
         assert (x.items()["seq"] < 0).any()
         got = []
-        for factor in (1.0, 0.0, 0.03, 30.0, -1000.0):
+        for factor in (1.0, 0.0, 0.03, 30.0, -1000.0, float("inf"), float("nan")):
             s.q_t[0] = asked * factor
             got.append(x.attend(s.layer, s.q_t, **f.kw))
         for out, lse in got[1:]:
